@@ -32,7 +32,7 @@
  *     first HIP call, so they behave the same on a host without a GPU.  No exception crosses
  *     the boundary.
  *   - Element types: RL_F32, RL_F16, RL_BF16 for every tensor of a call (one type per call).
- *     RL_INT4_G64 is allowed for W only (see rl_tensor_t), with RL_F16 / RL_BF16 activations: W is
+ *     RL_INT4_G64 and RL_FP8_B128 are allowed for W only (see rl_tensor_t), with RL_F16 / RL_BF16 activations.  An int4 W is
  *     dequantised (q * scale, rounded to the activation type) inside the GEMMs that read it, or, where
  *     that is faster, in panels in the workspace, at most 64 MiB of W at a time.
  *     A workspace that holds only what the direct route needs gets the direct route.  The graphs that need W + AB as a matrix (RL_FWD2, RL_BWD4,
@@ -56,7 +56,8 @@ typedef enum {
   RL_F32 = 0,
   RL_F16 = 1,
   RL_BF16 = 2,
-  RL_INT4_G64 = 3 /* frozen W only: symmetric int4, one fp16 scale per 64 rows (d_in) per column */
+  RL_INT4_G64 = 3, /* frozen W only: symmetric int4, one fp16 scale per 64 rows (d_in) per column */
+  RL_FP8_B128 = 4  /* frozen W only: e4m3 values, one power-of-two scale per 128 x 128 block */
 } rl_dtype_t;
 
 typedef enum {
@@ -117,8 +118,11 @@ typedef enum {
  *          (ld a multiple of 8, data and scales 16-byte aligned)
  *   rows, cols, ld   in elements; ld = distance between consecutive rows
  *   dtype  rl_dtype_t
- *   scales RL_INT4_G64 only: device pointer to fp16 scales [ceil(rows/64), cols], row-major, dense
- *   group  RL_INT4_G64 only: must be 64
+ *          For RL_FP8_B128: e4m3 bytes (the type with 448 as its largest value and no infinities), ld in bytes and a multiple of 16
+ *   scales RL_INT4_G64: device pointer to fp16 scales [ceil(rows/64), cols], row-major, dense
+ *          RL_FP8_B128: device pointer to scale bytes [ceil(rows/128), ceil(cols/128)], row-major, dense; byte b stands for 2^(b - 127)
+ *          (255: NaN); value (k,j) = e4m3 (k,j) * scale (k/128, j/128)
+ *   group  RL_INT4_G64: must be 64; RL_FP8_B128: must be 128
  */
 typedef struct {
   void* data;
@@ -291,11 +295,63 @@ int runlora_dora_backward(int variant, const rl_tensor_t* dY, const rl_saved_t* 
 size_t runlora_dora_workspace_bytes(int fwd, int bwd, int64_t n, int64_t i, int64_t o, int64_t r, int dtype);
 
 /*
+ * A frozen weight in 8-bit floating point (W with dtype RL_FP8_B128 in runlora_forward / runlora_backward).  Both large products run on
+ * 8-bit operands: the other operand's rows are rounded to e4m3 on the way, in blocks of 128 columns,
+ *     Y = Q(X) W + 1 b^T + s (X A) B,     dX = Q(dY) W^T + s (dY B^T) A^T,     dA, dB as ever (from X and dY themselves),
+ * Q(x) = e4m3(x / 2^e) 2^e with e the smallest integer >= -127 for which the block's largest magnitude is at most 448 * 2^e (rounding to
+ * nearest, ties to even; a block holding an infinity or a NaN becomes NaN).  RL_F16 / RL_BF16 activations, i and o multiples of 16; graphs
+ * RL_FWD1 (also asked for as RL_FWD3) and RL_BWD1, no LoRA dropout; everything else returns RL_ERR_UNSUPPORTED.  Workspace:
+ * runlora_workspace_bytes_w with w_dtype = RL_FP8_B128.  runlora_select takes RL_FP8_B128 as its dtype.
+ *
+ * runlora_fp8_quantize rounds a dense matrix (RL_F32 / RL_F16 / RL_BF16, [rows, cols]) to the same values in blocks of 128 x 128:
+ * dst->data and dst->scales (RL_FP8_B128, same rows and cols, cols a multiple of 16) are written.
+ */
+int runlora_fp8_quantize(const rl_tensor_t* src, rl_tensor_t* dst, const rl_opts_t* opts);
+
+/*
+ * Layers over a stack of expert weights: the rows of X are sorted by expert, and
+ *     Y_t  = X_t W_e + bias_e + s (X_t A_e) B_e                    for every row t of expert e,
+ *     dX_t = dY_t W_e^T + s (dY_t B_e^T) A_e^T,   dA_e = s X_e^T (dY_e B_e^T),   dB_e = s (X_e A_e)^T dY_e
+ * (sums over the expert's rows; zeros for an expert without any).  The forward is RL_FWD1's graph and the backward RL_BWD1's.
+ *   ends     device pointer to `experts` int32: expert e owns the rows [ends[e-1], ends[e]) (from 0 for e = 0).  Read on the device
+ *            when the work runs: the host never waits for it, and a captured graph follows its values.  They must not decrease; values outside
+ *            [0, n] count as the nearer end.  Rows behind the last expert's give zeros in Y, T and dX and enter no gradient.
+ *   W        [experts][i, o], the type of X or RL_FP8_B128 (then as above: X and dY rounded in the large products)
+ *   A, B     [experts][i, r], [experts][r, o], the type of X; both NULL: no adapter (dA and dB must be NULL too)
+ *   T        [n, r] or NULL.  Forward: s X A is left there.  Backward: s X A as a forward left it; NULL: it is formed again if dB is
+ *            asked for.
+ *   opts     required: workspace of runlora_experts_workspace_bytes(); scale (of both passes: there is no record between them); bias
+ *            (forward only) = [experts, o], dense; dropout_p must be 0.
+ *   dX, dA, dB  overwritten; any may be NULL (skipped).
+ * RL_F16 / RL_BF16; n >= 1; i, o, r multiples of 8 (i and o of 16 for an RL_FP8_B128 W); experts in [1, 65535]; leading dimensions up to
+ * 4194304.  Sums run in a fixed order: the same call gives the same bits.
+ *
+ * rl_stack_t: as rl_tensor_t, `experts` matrices `stride` elements apart (a multiple of 8, for RL_FP8_B128 of 16; inputs may have stride 0,
+ * one matrix for all).  The scale bytes of an RL_FP8_B128 stack are dense, [experts][ceil(rows/128)][ceil(cols/128)]
+ * (with stride 0 those of the one matrix).
+ */
+typedef struct {
+  void* data;
+  int64_t experts, rows, cols, ld, stride;
+  int32_t dtype;
+  void* scales;
+  int32_t group;
+} rl_stack_t;
+
+int runlora_experts_forward(const rl_tensor_t* X, const int32_t* ends, const rl_stack_t* W, const rl_stack_t* A, const rl_stack_t* B,
+                            rl_tensor_t* Y, rl_tensor_t* T, const rl_opts_t* opts);
+int runlora_experts_backward(const rl_tensor_t* dY, const rl_tensor_t* X, const int32_t* ends, const rl_stack_t* W, const rl_stack_t* A,
+                             const rl_stack_t* B, const rl_tensor_t* T, rl_tensor_t* dX, rl_stack_t* dA, rl_stack_t* dB,
+                             const rl_opts_t* opts);
+/* the most that any call of these sizes takes (backward = 0: forward); r = 0: no adapter.  0 for what the calls refuse. */
+size_t runlora_experts_workspace_bytes(int backward, int64_t n, int64_t experts, int64_t i, int64_t o, int64_t r, int dtype, int w_dtype);
+
+/*
  * Choose the (forward, backward) pair of computation graphs for one layer shape, by estimated time
  * or by operation count (the selection step named in the abstract).  Pure host function,
  * thread-safe, no HIP call.  Uses the time model unless the environment variable
  * RUNLORA_CRITERION=flops asks for the Table 1 FLOP criterion.  dtype is the activation dtype;
- * pass RL_INT4_G64 to restrict the choice to the graphs an int4 W supports.
+ * pass RL_INT4_G64 or RL_FP8_B128 to restrict the choice to the graphs such a W supports.
  * Debugging overrides: RUNLORA_FORCE_FWD=<rl_fwd_variant_t id> and RUNLORA_FORCE_BWD=<rl_bwd_variant_t
  * id> in the environment pin that side of the pair.  The other side stays the selector's, except that
  * it is moved to keep the pair legal (a forced default backward takes the default forward with it; a
@@ -344,7 +400,7 @@ size_t runlora_saved_bytes(int fwd, int64_t n, int64_t i, int64_t o, int64_t r, 
  * RL_ERR_WORKSPACE and runlora_last_hip_error() names the size.  0 for an unknown variant or dtype. */
 size_t runlora_workspace_bytes(int fwd, int bwd, int64_t n, int64_t i, int64_t o, int64_t r,
                                int dtype);
-/* Same with W's dtype explicit: w_dtype = dtype (dense) or RL_INT4_G64. */
+/* Same with W's dtype explicit: w_dtype = dtype (dense), RL_INT4_G64 or RL_FP8_B128. */
 size_t runlora_workspace_bytes_w(int fwd, int bwd, int64_t n, int64_t i, int64_t o, int64_t r,
                                  int dtype, int w_dtype);
 /* Same for one call whose choices are known (dense W; dense rows), never more than the above: a bit set of

@@ -17,7 +17,7 @@ import os
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "librunlora.so")
 
-RL_F32, RL_F16, RL_BF16, RL_INT4_G64 = 0, 1, 2, 3
+RL_F32, RL_F16, RL_BF16, RL_INT4_G64, RL_FP8_B128 = 0, 1, 2, 3, 4
 FWD_DEFAULT, FWD1, FWD2, FWD3 = 0, 1, 2, 3
 BWD_DEFAULT, BWD1, BWD2, BWD3, BWD4, BWD5, BWD6, BWD7, BWD8 = 0, 1, 2, 3, 4, 5, 6, 7, 8
 FWD_VARIANTS = (FWD_DEFAULT, FWD1, FWD2, FWD3)
@@ -37,12 +37,19 @@ EXPORTS = (
     "runlora_probe_mfma",
     "runlora_vera_forward", "runlora_vera_backward", "runlora_vera_workspace_bytes",
     "runlora_dora_forward", "runlora_dora_backward", "runlora_dora_workspace_bytes",
+    "runlora_fp8_quantize", "runlora_experts_forward", "runlora_experts_backward", "runlora_experts_workspace_bytes",
 )
 
 
 class rl_tensor_t(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
                 ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("scales", ctypes.c_void_p),
+                ("group", ctypes.c_int32)]
+
+
+class rl_stack_t(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("experts", ctypes.c_int64), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld", ctypes.c_int64), ("stride", ctypes.c_int64), ("dtype", ctypes.c_int32), ("scales", ctypes.c_void_p),
                 ("group", ctypes.c_int32)]
 
 
@@ -122,6 +129,15 @@ def lib():
     L.runlora_dora_backward.restype = ci
     L.runlora_dora_workspace_bytes.argtypes = [ci, ci, i64, i64, i64, i64, ci]
     L.runlora_dora_workspace_bytes.restype = ctypes.c_size_t
+    kp = ctypes.POINTER(rl_stack_t)
+    L.runlora_fp8_quantize.argtypes = [tp, tp, op]
+    L.runlora_fp8_quantize.restype = ci
+    L.runlora_experts_forward.argtypes = [tp, vp, kp, kp, kp, tp, tp, op]
+    L.runlora_experts_forward.restype = ci
+    L.runlora_experts_backward.argtypes = [tp, tp, vp, kp, kp, kp, tp, tp, kp, kp, op]
+    L.runlora_experts_backward.restype = ci
+    L.runlora_experts_workspace_bytes.argtypes = [ci, i64, i64, i64, i64, i64, ci, ci]
+    L.runlora_experts_workspace_bytes.restype = ctypes.c_size_t
     L.runlora_select.argtypes = [i64, i64, i64, i64, ci, ip, ip]
     L.runlora_select.restype = ci
     L.runlora_select_by.argtypes = [ci, i64, i64, i64, i64, ci, ip, ip]
@@ -198,7 +214,7 @@ def _current_stream():
 
 
 def dtype_from_name(name):
-    return {"f32": RL_F32, "f16": RL_F16, "bf16": RL_BF16, "int4": RL_INT4_G64}[name]
+    return {"f32": RL_F32, "f16": RL_F16, "bf16": RL_BF16, "int4": RL_INT4_G64, "fp8": RL_FP8_B128}[name]
 
 
 class Int4Weight:
@@ -225,10 +241,47 @@ class Int4Weight:
                           torch.from_numpy(np.ascontiguousarray(scale)).to(device), rows, cols)
 
 
+class Fp8Weight:
+    """A frozen W [rows, cols], or a stack of `experts` of them, in e4m3 with one power-of-two scale per 128 x 128 block
+    (RL_FP8_B128): `data` holds the bytes, a uint8 or float8_e4m3fn device tensor [rows, ld] or [experts, rows, ld], `scales` the scale
+    bytes, uint8 [ceil(rows/128), ceil(cols/128)] or one more dimension in front; value = e4m3 * 2^(byte - 127)."""
+
+    def __init__(self, data, scales, rows, cols):
+        blocks = ((rows + 127) // 128, (cols + 127) // 128)
+        if data.dim() not in (2, 3) or data.element_size() != 1 or data.stride(-1) != 1 or data.shape[-2] != rows or data.shape[-1] < cols:
+            raise ValueError("data must be bytes [rows, >= cols], with a leading dimension for a stack")
+        if tuple(scales.shape) != tuple(data.shape[:-2]) + blocks or scales.element_size() != 1 or not scales.is_contiguous():
+            raise ValueError(f"scales must be dense bytes {blocks}, with data's leading dimension for a stack")
+        if scales.device != data.device:
+            raise ValueError("data and scales must be on one device")
+        self.data, self.scales, self.rows, self.cols = data, scales, rows, cols
+        self.ld = data.stride(-2)
+        self.experts = data.shape[0] if data.dim() == 3 else None  # None: a single matrix
+
+    @property
+    def shape(self):
+        return (self.rows, self.cols) if self.experts is None else (self.experts, self.rows, self.cols)
+
+    @staticmethod
+    def quantize(w, stream=None):
+        """The nearest such weight to a float tensor [rows, cols] or [experts, rows, cols] (runlora_fp8_quantize)."""
+        import torch
+        rows, cols = w.shape[-2:]
+        q = torch.empty(w.shape, dtype=torch.uint8, device=w.device)
+        s = torch.empty(tuple(w.shape[:-2]) + ((rows + 127) // 128, (cols + 127) // 128), dtype=torch.uint8, device=w.device)
+        for src, dst, sc in zip(w, q, s) if w.dim() == 3 else ((w, q, s),):
+            runlora_fp8_quantize(src, dst, sc, stream)
+        return Fp8Weight(q, s, rows, cols)
+
+
 def tensor_desc(t):
-    """rl_tensor_t view of a 2-D torch tensor or an Int4Weight (None -> NULL pointer argument)."""
+    """rl_tensor_t view of a 2-D torch tensor, an Int4Weight or an Fp8Weight (None -> NULL pointer argument)."""
     if t is None:
         return None
+    if isinstance(t, Fp8Weight):
+        if t.experts is not None:
+            raise ValueError("expected a single matrix, not a stack")
+        return rl_tensor_t(t.data.data_ptr(), t.rows, t.cols, t.ld, RL_FP8_B128, t.scales.data_ptr(), 128)
     if isinstance(t, Int4Weight):
         return rl_tensor_t(t.packed.data_ptr(), t.rows, t.cols, t.ld, RL_INT4_G64, t.scales.data_ptr(), 64)
     strides = t.stride()
@@ -236,6 +289,28 @@ def tensor_desc(t):
         raise ValueError("expected a 2-D tensor with contiguous rows")
     rows, cols = t.shape
     return rl_tensor_t(t.data_ptr(), rows, cols, strides[0], dtype_code(t.dtype), None, 0)
+
+
+def stack_desc(t):
+    """rl_stack_t view of a 3-D torch tensor [experts, rows, cols] or an Fp8Weight stack (None -> NULL pointer argument)."""
+    if t is None:
+        return None
+    if isinstance(t, Fp8Weight):
+        if t.experts is None:
+            raise ValueError("expected a stack of weights")
+        return rl_stack_t(t.data.data_ptr(), t.experts, t.rows, t.cols, t.ld, t.data.stride(0), RL_FP8_B128, t.scales.data_ptr(), 128)
+    strides = t.stride()
+    if len(strides) != 3 or strides[2] != 1:
+        raise ValueError("expected a 3-D tensor with contiguous rows")
+    experts, rows, cols = t.shape
+    return rl_stack_t(t.data_ptr(), experts, rows, cols, strides[1], strides[0], dtype_code(t.dtype), None, 0)
+
+
+def _ends(ends, experts):
+    import torch
+    if ends.dtype != torch.int32 or ends.dim() != 1 or ends.numel() != experts or ends.stride(0) != 1:
+        raise ValueError("ends must be a dense int32 vector with one element per expert")
+    return ends.data_ptr()
 
 
 def _opts(workspace, stream, scale=None, bias=None, dropout_p=None, dropout_seed=0):
@@ -364,6 +439,47 @@ def runlora_dora_backward(variant, dY, saved, W, A, B, m, c, Y, dX, dA, dB, dm, 
 
 def runlora_dora_workspace_bytes(fwd, bwd, n, i, o, r, dtype):
     return int(lib().runlora_dora_workspace_bytes(fwd, bwd, n, i, o, r, dtype))
+
+
+def runlora_fp8_quantize(src, data, scales, stream=None):
+    """src [rows, cols] (f32 / f16 / bf16) rounded to e4m3 bytes `data` [rows, cols] with scale bytes `scales` per 128 x 128 block."""
+    rows, cols = src.shape
+    if data.element_size() != 1 or tuple(data.shape) != (rows, cols) or data.stride(1) != 1:
+        raise ValueError("data must be bytes of src's shape with contiguous rows")
+    if scales.element_size() != 1 or tuple(scales.shape) != ((rows + 127) // 128, (cols + 127) // 128) or not scales.is_contiguous():
+        raise ValueError("scales must be dense bytes, one per 128 x 128 block")
+    d = rl_tensor_t(data.data_ptr(), rows, cols, data.stride(0), RL_FP8_B128, scales.data_ptr(), 128)
+    o = _opts(None, stream)
+    _check(lib().runlora_fp8_quantize(_ref(tensor_desc(src)), ctypes.byref(d), ctypes.byref(o)))
+    return data, scales
+
+
+def runlora_experts_forward(X, ends, W, A, B, Y, T=None, workspace=None, stream=None, scale=None, bias=None):
+    """Y_t = X_t W_e (+ bias_e) + scale (X_t A_e) B_e for every row t of expert e; rows are sorted by expert and `ends` (int32 [experts], on
+    the device) holds where each expert's rows end.  W, A, B: [experts, ., .] (W also an Fp8Weight stack); A = B = None: no adapter.
+    T: [n, r] buffer that receives scale XA, or None.  workspace: runlora_experts_workspace_bytes bytes."""
+    if bias is not None:
+        if bias.dtype != X.dtype or tuple(bias.shape) != (W.shape[0], Y.shape[1]) or not bias.is_contiguous():
+            raise ValueError("bias must be dense [experts, d_out] of the activation dtype")
+        bias = bias.view(-1)
+    dx, dw, da, db, dy, dt = tensor_desc(X), stack_desc(W), stack_desc(A), stack_desc(B), tensor_desc(Y), tensor_desc(T)
+    o = _opts(workspace, stream, scale, bias)
+    _check(lib().runlora_experts_forward(_ref(dx), _ends(ends, W.shape[0]), _ref(dw), _ref(da), _ref(db), _ref(dy), _ref(dt), ctypes.byref(o)))
+    return Y
+
+
+def runlora_experts_backward(dY, X, ends, W, A, B, dX, dA, dB, T=None, workspace=None, stream=None, scale=None):
+    """Gradients of runlora_experts_forward; any of dX / dA / dB may be None.  T: scale XA as the forward left it, or None."""
+    ddy, dx, dw, da, db, dt = tensor_desc(dY), tensor_desc(X), stack_desc(W), stack_desc(A), stack_desc(B), tensor_desc(T)
+    gx, ga, gb = tensor_desc(dX), stack_desc(dA), stack_desc(dB)
+    o = _opts(workspace, stream, scale)
+    _check(lib().runlora_experts_backward(_ref(ddy), _ref(dx), _ends(ends, W.shape[0]), _ref(dw), _ref(da), _ref(db), _ref(dt), _ref(gx), _ref(ga),
+                                          _ref(gb), ctypes.byref(o)))
+    return dX, dA, dB
+
+
+def runlora_experts_workspace_bytes(backward, n, experts, i, o, r, dtype, w_dtype=None):
+    return int(lib().runlora_experts_workspace_bytes(int(bool(backward)), n, experts, i, o, r, dtype, dtype if w_dtype is None else w_dtype))
 
 
 def runlora_select(n_tokens, d_in, d_out, r, dtype, criterion=None):

@@ -7,6 +7,8 @@
 #include "../../include/runlora.h"
 #include "schedule.hpp"
 #include "dora.hpp"
+#include "fp8.hpp"
+#include "grouped.hpp"
 #include "vera.hpp"
 
 using namespace rl;
@@ -278,12 +280,277 @@ int check_workspace(const Schedule& sch, const rl_opts_t* opts) {
 
 }  // namespace
 
+// ---- layers over an 8-bit weight, and over stacks of expert weights (grouped.hpp) ---------------------------
+namespace {
+
+constexpr int64_t kMaxLd = 1LL << 22;      // tiles are addressed by 32-bit offsets over 128 rows
+constexpr int64_t kMaxExperts = 65535;
+
+int check_fp8(const rl_tensor_t* W, int64_t rows, int64_t cols) {
+  if (!W || !W->data || !W->scales) return RL_ERR_NULL;
+  if (W->group != 128) return RL_ERR_UNSUPPORTED;
+  if (W->rows != rows || W->cols != cols || W->ld < W->cols) return RL_ERR_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(W->data) & 15) != 0 || W->ld % 16 != 0 || cols % 16 != 0) return RL_ERR_ALIGN;
+  return RL_OK;
+}
+int64_t scale_bytes(int64_t rows, int64_t cols) { return (rows + 127) / 128 * ((cols + 127) / 128); }
+
+// one matrix of a stack as rl_tensor_t; RL_OK if the stack has `experts` of them, [rows, cols], of that dtype
+int check_stack(const rl_stack_t* t, int64_t experts, int64_t rows, int64_t cols, int dtype, bool output) {
+  if (!t || !t->data) return RL_ERR_NULL;
+  if (t->dtype != dtype) return RL_ERR_DTYPE;
+  if (t->experts != experts) return RL_ERR_SHAPE;
+  const rl_tensor_t one{t->data, t->rows, t->cols, t->ld, t->dtype, t->scales, t->group};
+  const int rc = dtype == RL_FP8_B128 ? check_fp8(&one, rows, cols) : check_tensor(&one, rows, cols, dtype);
+  if (rc != RL_OK) return rc;
+  if (t->stride < 0 || (output && experts > 1 && t->stride < (rows - 1) * t->ld + cols)) return RL_ERR_SHAPE;
+  if (t->stride % (dtype == RL_FP8_B128 ? 16 : 8) != 0) return RL_ERR_ALIGN;
+  return t->ld > kMaxLd ? RL_ERR_UNSUPPORTED : RL_OK;
+}
+Range stack_range(const rl_stack_t* t, size_t esz) {
+  const char* lo = static_cast<const char*>(t->data);
+  return {lo, lo + ((size_t)((t->experts - 1) * t->stride) + (size_t)((t->rows - 1) * t->ld + t->cols)) * esz};
+}
+
+// the sizes of a call (checks that need no pointer)
+int check_sizes(int64_t n, int64_t experts, int64_t i, int64_t o, int64_t r, int dtype, int w_dtype) {
+  if (dtype != RL_F16 && dtype != RL_BF16) return internal_dtype(dtype) < 0 ? RL_ERR_DTYPE : RL_ERR_UNSUPPORTED;
+  if (w_dtype != dtype && w_dtype != RL_FP8_B128) return RL_ERR_DTYPE;
+  if (experts < 1 || r < 0) return RL_ERR_SHAPE;
+  const int rc = check_dims(n, i, o, r > 0 ? r : 8, dtype);
+  if (rc != RL_OK) return rc;
+  if (w_dtype == RL_FP8_B128 && (i % 16 != 0 || o % 16 != 0)) return RL_ERR_ALIGN;
+  return experts > kMaxExperts || i > kMaxLd || o > kMaxLd || r > kMaxLd ? RL_ERR_UNSUPPORTED : RL_OK;
+}
+
+ExpertsDesc experts_desc(int64_t n, int64_t experts, int64_t i, int64_t o, int64_t r, int dtype, int w_dtype) {
+  ExpertsDesc d;
+  d.dtype = internal_dtype(dtype);
+  d.f8 = w_dtype == RL_FP8_B128;
+  d.n = n; d.experts = experts; d.i = i; d.o = o; d.r = r;
+  return d;
+}
+void set_weights(ExpertsDesc* d, const rl_stack_t* W, const rl_stack_t* A, const rl_stack_t* B) {
+  d->W = W->data; d->ldw = W->ld; d->sw = W->stride;
+  if (d->f8) {
+    d->w_scales = static_cast<const uint8_t*>(W->scales);
+    d->s_scales = W->stride != 0 || W->experts == 1 ? scale_bytes(W->rows, W->cols) : 0;
+  }
+  if (A) { d->A = A->data; d->lda = A->ld; d->sa = A->stride; }
+  if (B) { d->B = B->data; d->ldb = B->ld; d->sb = B->stride; }
+}
+
+int check_space(size_t need, const rl_opts_t* opts) {
+  if (need == 0) return RL_OK;
+  if (!opts || !opts->workspace || opts->workspace_bytes < need) {
+    std::snprintf(g_hip_error, sizeof(g_hip_error), "this call needs a workspace of %zu bytes", need);
+    return RL_ERR_WORKSPACE;
+  }
+  return (reinterpret_cast<uintptr_t>(opts->workspace) & 255) != 0 ? RL_ERR_ALIGN : RL_OK;
+}
+
+rl_stack_t stack_of(const rl_tensor_t* t) { return rl_stack_t{t->data, 1, t->rows, t->cols, t->ld, 0, t->dtype, t->scales, t->group}; }
+
+// checks shared by the two families' forwards and backwards: everything but the outputs
+int check_inputs(const rl_tensor_t* rows, int64_t width, const int32_t* ends, const rl_stack_t* W, const rl_stack_t* A, const rl_stack_t* B, int64_t* r) {
+  if (!rows || !W || (A == nullptr) != (B == nullptr)) return RL_ERR_NULL;
+  const int64_t E = W->experts, i = W->rows, o = W->cols;
+  *r = A ? A->cols : 0;
+  if (A && *r < 1) return RL_ERR_SHAPE;
+  int rc = check_sizes(rows->rows, E, i, o, *r, rows->dtype, W->dtype);
+  if (rc != RL_OK) return rc;
+  if ((rc = check_tensor(rows, rows->rows, width, rows->dtype)) != RL_OK) return rc;
+  if (rows->ld > kMaxLd) return RL_ERR_UNSUPPORTED;
+  if ((rc = check_stack(W, E, i, o, W->dtype, false)) != RL_OK) return rc;
+  if (A && (rc = check_stack(A, E, i, *r, rows->dtype, false)) != RL_OK) return rc;
+  if (B && (rc = check_stack(B, E, *r, o, rows->dtype, false)) != RL_OK) return rc;
+  if (!ends && E > 1) return RL_ERR_NULL;
+  return (reinterpret_cast<uintptr_t>(ends) & 3) != 0 ? RL_ERR_ALIGN : RL_OK;
+}
+
+struct Ranges {
+  Range r[12];
+  int k = 0;
+  void add(Range x) { if (x.lo) r[k++] = x; }
+  bool hit(Range x) const {
+    for (int j = 0; j < k; ++j)
+      if (overlap(x, r[j])) return true;
+    return false;
+  }
+};
+void add_inputs(Ranges* in, const int32_t* ends, const rl_stack_t* W, const rl_stack_t* A, const rl_stack_t* B) {
+  in->add(stack_range(W, W->dtype == RL_FP8_B128 ? 1 : 2));
+  if (W->dtype == RL_FP8_B128) in->add(range_of(W->scales, 1, 0, (W->stride != 0 ? W->experts : 1) * scale_bytes(W->rows, W->cols), 1));
+  if (A) in->add(stack_range(A, 2));
+  if (B) in->add(stack_range(B, 2));
+  if (ends) in->add(range_of(ends, 1, 0, W->experts, 4));
+}
+
+int experts_forward_impl(const rl_tensor_t* X, const int32_t* ends, const rl_stack_t* W, const rl_stack_t* A, const rl_stack_t* B, rl_tensor_t* Y,
+                         rl_tensor_t* T, const rl_opts_t* opts, bool use_static) {
+  if (!X || !W || !Y) return RL_ERR_NULL;
+  int64_t r = 0;
+  int rc = check_inputs(X, W->rows, ends, W, A, B, &r);
+  if (rc != RL_OK) return rc;
+  const int64_t n = X->rows, o = W->cols;
+  if ((rc = check_tensor(Y, n, o, X->dtype)) != RL_OK) return rc;
+  if (T && !A) return RL_ERR_SHAPE;
+  if (T && (rc = check_tensor(T, n, r, X->dtype)) != RL_OK) return rc;
+  if (opts && opts->dropout_p != 0.f) return RL_ERR_UNSUPPORTED;
+  const void* bias = opts ? opts->bias : nullptr;
+  if ((reinterpret_cast<uintptr_t>(bias) & 15) != 0) return RL_ERR_ALIGN;
+  Ranges in;
+  add_inputs(&in, ends, W, A, B);
+  in.add(range_of(X->data, n, X->ld, X->cols, 2));
+  if (bias) in.add(range_of(bias, 1, 0, W->experts * o, 2));
+  const Range ry = range_of(Y->data, n, Y->ld, o, 2);
+  if (in.hit(ry)) return RL_ERR_ALIAS;
+  if (T) {
+    const Range rt = range_of(T->data, n, T->ld, r, 2);
+    if (in.hit(rt) || overlap(rt, ry)) return RL_ERR_ALIAS;
+  }
+  ExpertsDesc d = experts_desc(n, W->experts, W->rows, o, r, X->dtype, W->dtype);
+  set_weights(&d, W, A, B);
+  d.ends = ends;
+  d.X = X->data; d.ldx = X->ld;
+  d.Y = Y->data; d.ldy = Y->ld;
+  if (T) { d.T = T->data; d.ldt = T->ld; }
+  d.bias = bias;
+  d.scale = opts && opts->scale != 0.f ? opts->scale : 1.f;
+  const size_t need = experts_workspace(d, false);
+  void* ws = opts ? opts->workspace : nullptr;
+  if (use_static) {
+    if (need > kStaticScratchBytes) {
+      std::snprintf(g_hip_error, sizeof(g_hip_error), "runlora_forward_static: this call needs %zu bytes of scratch, the fixed array holds %zu", need, kStaticScratchBytes);
+      return RL_ERR_WORKSPACE;
+    }
+    if (g_dry_run) return RL_OK;
+    if ((rc = static_scratch(&ws)) != RL_OK) return rc;
+  } else if ((rc = check_space(need, opts)) != RL_OK) {
+    return rc;
+  }
+  if (g_dry_run) return RL_OK;
+  const hipError_t e = experts_forward(d, ws, opts ? static_cast<hipStream_t>(opts->stream) : nullptr);
+  return e == hipSuccess ? RL_OK : set_hip_error(e, "experts forward");
+}
+
+int experts_backward_impl(const rl_tensor_t* dY, const rl_tensor_t* X, const int32_t* ends, const rl_stack_t* W, const rl_stack_t* A, const rl_stack_t* B,
+                          const rl_tensor_t* T, rl_tensor_t* dX, rl_stack_t* dA, rl_stack_t* dB, float scale, const rl_opts_t* opts) {
+  if (!dY || !W) return RL_ERR_NULL;
+  int64_t r = 0;
+  int rc = check_inputs(dY, W->cols, ends, W, A, B, &r);
+  if (rc != RL_OK) return rc;
+  const int dtype = dY->dtype;
+  const int64_t n = dY->rows, E = W->experts, i = W->rows, o = W->cols;
+  if ((dA || dB || T) && !A) return RL_ERR_SHAPE;
+  const bool need_X = dA || (dB && !T);
+  if (need_X && !X) return RL_ERR_NULL;
+  if (X && (rc = check_tensor(X, n, i, dtype)) != RL_OK) return rc;
+  if (X && X->ld > kMaxLd) return RL_ERR_UNSUPPORTED;
+  if (T && (rc = check_tensor(T, n, r, dtype)) != RL_OK) return rc;
+  if (T && T->ld > kMaxLd) return RL_ERR_UNSUPPORTED;
+  if (dX && (rc = check_tensor(dX, n, i, dtype)) != RL_OK) return rc;
+  if (dA && (rc = check_stack(dA, E, i, r, dtype, true)) != RL_OK) return rc;
+  if (dB && (rc = check_stack(dB, E, r, o, dtype, true)) != RL_OK) return rc;
+  Ranges in;
+  add_inputs(&in, ends, W, A, B);
+  in.add(range_of(dY->data, n, dY->ld, o, 2));
+  if (X) in.add(range_of(X->data, n, X->ld, i, 2));
+  if (T) in.add(range_of(T->data, n, T->ld, r, 2));
+  if (dX) { const Range x = range_of(dX->data, n, dX->ld, i, 2); if (in.hit(x)) return RL_ERR_ALIAS; in.add(x); }
+  if (dA) { const Range x = stack_range(dA, 2); if (in.hit(x)) return RL_ERR_ALIAS; in.add(x); }
+  if (dB && in.hit(stack_range(dB, 2))) return RL_ERR_ALIAS;
+  ExpertsDesc d = experts_desc(n, E, i, o, r, dtype, W->dtype);
+  set_weights(&d, W, A, B);
+  d.ends = ends;
+  d.dY = dY->data; d.lddy = dY->ld;
+  if (X) { d.X = X->data; d.ldx = X->ld; }
+  if (T) { d.T = T->data; d.ldt = T->ld; d.has_T = true; }
+  if (dX) { d.dX = dX->data; d.lddx = dX->ld; }
+  if (dA) { d.dA = dA->data; d.ldda = dA->ld; d.sda = dA->stride; }
+  if (dB) { d.dB = dB->data; d.lddb = dB->ld; d.sdb = dB->stride; }
+  d.scale = scale != 0.f ? scale : 1.f;
+  if ((rc = check_space(experts_workspace(d, true), opts)) != RL_OK) return rc;
+  if (g_dry_run) return RL_OK;
+  const hipError_t e = experts_backward(d, opts ? opts->workspace : nullptr, opts ? static_cast<hipStream_t>(opts->stream) : nullptr);
+  return e == hipSuccess ? RL_OK : set_hip_error(e, "experts backward");
+}
+
+// the layer calls on an RL_FP8_B128 weight: a stack of one
+int fp8_forward(int variant, const rl_tensor_t* X, const rl_tensor_t* W, const rl_tensor_t* A, const rl_tensor_t* B, rl_tensor_t* Y, rl_saved_t* saved,
+                const rl_opts_t* opts, bool use_static) {
+  if (variant != RL_FWD1 && variant != RL_FWD3) return RL_ERR_UNSUPPORTED;
+  if (W->group != 128) return RL_ERR_UNSUPPORTED;
+  const rl_stack_t w = stack_of(W), a = stack_of(A), b = stack_of(B);
+  if (A->cols < 1) return RL_ERR_SHAPE;
+  rl_tensor_t T{saved->T, X->rows, A->cols, saved->ldt, X->dtype, nullptr, 0};
+  const int rc = experts_forward_impl(X, nullptr, &w, &a, &b, Y, saved->T ? &T : nullptr, opts, use_static);
+  if (rc != RL_OK) return rc;
+  saved->fwd_variant = variant;
+  saved->dtype = X->dtype;
+  saved->n = X->rows; saved->i = W->rows; saved->o = W->cols; saved->r = A->cols;
+  saved->X = X->data; saved->ldx = X->ld;
+  saved->scale = opts && opts->scale != 0.f ? opts->scale : 1.f;
+  saved->dropout_thr = saved->dropout_seed = 0u;
+  if (!saved->T) saved->ldt = 0;
+  saved->M = nullptr;
+  saved->ldm = 0;
+  return RL_OK;
+}
+int fp8_backward(int variant, const rl_tensor_t* dY, const rl_saved_t* saved, const rl_tensor_t* W, const rl_tensor_t* A, const rl_tensor_t* B, rl_tensor_t* dX,
+                 rl_tensor_t* dA, rl_tensor_t* dB, const rl_opts_t* opts) {
+  if (variant != RL_BWD1) return RL_ERR_UNSUPPORTED;
+  if (saved->fwd_variant < RL_FWD_DEFAULT || saved->fwd_variant > RL_FWD3 || saved->dropout_thr != 0u) return RL_ERR_SAVED_MISMATCH;
+  if (saved->dtype != dY->dtype || saved->n != dY->rows || saved->i != W->rows || saved->o != W->cols || saved->r != A->cols) return RL_ERR_SAVED_MISMATCH;
+  if (!saved->X) return RL_ERR_NULL;
+  const rl_stack_t w = stack_of(W), a = stack_of(A), b = stack_of(B);
+  const rl_tensor_t X{const_cast<void*>(saved->X), saved->n, saved->i, saved->ldx, saved->dtype, nullptr, 0};
+  const rl_tensor_t T{saved->T, saved->n, saved->r, saved->ldt, saved->dtype, nullptr, 0};
+  rl_stack_t ga, gb;
+  if (dA) ga = stack_of(dA);
+  if (dB) gb = stack_of(dB);
+  return experts_backward_impl(dY, &X, nullptr, &w, &a, &b, saved->T ? &T : nullptr, dX, dA ? &ga : nullptr, dB ? &gb : nullptr, saved->scale, opts);
+}
+
+}  // namespace
+
+extern "C" int runlora_experts_forward(const rl_tensor_t* X, const int32_t* ends, const rl_stack_t* W, const rl_stack_t* A, const rl_stack_t* B, rl_tensor_t* Y,
+                                       rl_tensor_t* T, const rl_opts_t* opts) {
+  return experts_forward_impl(X, ends, W, A, B, Y, T, opts, false);
+}
+extern "C" int runlora_experts_backward(const rl_tensor_t* dY, const rl_tensor_t* X, const int32_t* ends, const rl_stack_t* W, const rl_stack_t* A,
+                                        const rl_stack_t* B, const rl_tensor_t* T, rl_tensor_t* dX, rl_stack_t* dA, rl_stack_t* dB, const rl_opts_t* opts) {
+  return experts_backward_impl(dY, X, ends, W, A, B, T, dX, dA, dB, opts ? opts->scale : 1.f, opts);
+}
+extern "C" size_t runlora_experts_workspace_bytes(int backward, int64_t n, int64_t experts, int64_t i, int64_t o, int64_t r, int dtype, int w_dtype) {
+  if (check_sizes(n, experts, i, o, r, dtype, w_dtype) != RL_OK) return 0;
+  return experts_workspace(experts_desc(n, experts, i, o, r, dtype, w_dtype), backward != 0);
+}
+
+extern "C" int runlora_fp8_quantize(const rl_tensor_t* src, rl_tensor_t* dst, const rl_opts_t* opts) {
+  if (!src || !dst || !src->data) return RL_ERR_NULL;
+  const int dt = internal_dtype(src->dtype);
+  if (dt < 0 || dst->dtype != RL_FP8_B128) return RL_ERR_DTYPE;
+  if (src->rows < 1 || src->cols < 1) return RL_ERR_SHAPE;
+  if (src->rows > kMaxLd || src->cols > kMaxLd) return RL_ERR_UNSUPPORTED;
+  int rc = check_tensor(src, src->rows, src->cols, src->dtype);
+  if (rc != RL_OK) return rc;
+  if ((rc = check_fp8(dst, src->rows, src->cols)) != RL_OK) return rc;
+  const Range rq = range_of(dst->data, src->rows, dst->ld, src->cols, 1), rs = range_of(dst->scales, 1, 0, scale_bytes(src->rows, src->cols), 1);
+  const Range in = range_of(src->data, src->rows, src->ld, src->cols, dtype_size(dt));
+  if (overlap(rq, in) || overlap(rs, in) || overlap(rq, rs)) return RL_ERR_ALIAS;
+  const hipError_t e = fp8_blocks_run(dt, src->data, src->ld, src->rows, src->cols, dst->data, dst->ld, static_cast<uint8_t*>(dst->scales),
+                                      opts ? static_cast<hipStream_t>(opts->stream) : nullptr);
+  return e == hipSuccess ? RL_OK : set_hip_error(e, "fp8 quantize");
+}
+
 namespace {
 // use_static: the scratch is this device's copy of the library's fixed array instead of opts->workspace
 int forward_impl(int variant, const rl_tensor_t* X, const rl_tensor_t* W, const rl_tensor_t* A, const rl_tensor_t* B,
                  rl_tensor_t* Y, rl_saved_t* saved, const rl_opts_t* opts, bool use_static) {
   if (!X || !W || !A || !B || !Y || !saved) return RL_ERR_NULL;
   if (variant < RL_FWD_DEFAULT || variant > RL_FWD3) return RL_ERR_VARIANT;
+  if (W->dtype == RL_FP8_B128) return fp8_forward(variant, X, W, A, B, Y, saved, opts, use_static);
   const int dtype = X->dtype;
   const int dt = internal_dtype(dtype);
   if (dt < 0) return RL_ERR_DTYPE;
@@ -408,6 +675,7 @@ extern "C" int runlora_backward(int variant, const rl_tensor_t* dY, const rl_sav
                                 rl_tensor_t* dB, const rl_opts_t* opts) {
   if (!dY || !saved || !W || !A || !B) return RL_ERR_NULL;
   if (variant < RL_BWD_DEFAULT || variant > RL_BWD8) return RL_ERR_VARIANT;
+  if (W->dtype == RL_FP8_B128) return fp8_backward(variant, dY, saved, W, A, B, dX, dA, dB, opts);
   const int dtype = dY->dtype;
   const int dt = internal_dtype(dtype);
   if (dt < 0) return RL_ERR_DTYPE;
@@ -845,6 +1113,12 @@ extern "C" size_t runlora_workspace_bytes_w(int fwd, int bwd, int64_t n, int64_t
                                             int w_dtype) {
   const int dt = internal_dtype(dtype);
   if (dt < 0 || n < 1 || i < 1 || o < 1 || r < 1) return 0;
+  if (w_dtype == RL_FP8_B128) {
+    if (check_sizes(n, 1, i, o, r, dtype, w_dtype) != RL_OK) return 0;
+    const ExpertsDesc d = experts_desc(n, 1, i, o, r, dtype, w_dtype);
+    const size_t f = fwd == RL_FWD1 || fwd == RL_FWD3 ? experts_workspace(d, false) : 0, b = bwd == RL_BWD1 ? experts_workspace(d, true) : 0;
+    return f > b ? f : b;
+  }
   if (w_dtype != dtype && w_dtype != RL_INT4_G64) return 0;
   LayerDims L{n, i, o, r, dt, w_dtype == RL_INT4_G64};
   size_t need = 0;

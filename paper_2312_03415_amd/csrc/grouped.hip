@@ -1,0 +1,426 @@
+// Layers over stacks of expert weights and over an 8-bit weight: launches of a forward and a backward (grouped.hpp), and the small
+// kernels between the products.
+#include "grouped.hpp"
+
+#include "fp8.hpp"
+#include "gemm_engine.hpp"
+
+namespace rl {
+namespace {
+
+constexpr int kThreads = 256;
+typedef __attribute__((__vector_size__(4 * sizeof(int)))) int v4;
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t pad256(int64_t b) { return (b + 255) / 256 * 256; }
+
+// out_e[o][k] = in_e[k][o]: the factor B with the contraction in its rows.  Eight k a thread, loads along o.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void turn_kernel(const T* __restrict__ in, int64_t ld, int64_t stride, T* __restrict__ out, int R, int O) {
+  const int c = (int)blockIdx.x * kThreads + threadIdx.x, k0 = (int)blockIdx.y * 8;
+  if (c >= O) return;
+  const T* p = in + blockIdx.z * stride + (int64_t)k0 * ld + c;
+  T v[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = p[k * ld];
+  *reinterpret_cast<v4*>(out + ((int64_t)blockIdx.z * O + c) * R + k0) = *reinterpret_cast<const v4*>(v);
+}
+
+// out[e][m][0..N) = alpha * sum over slices of partial[slice][e][m][0..N), in slice order; eight columns a thread
+template <typename T>
+__global__ __launch_bounds__(kThreads) void slices_kernel(const float* __restrict__ partial, int splits, int64_t rows, int M, int N, float alpha, T* __restrict__ out,
+                                                          int64_t ldo, int64_t so) {
+  const int64_t c = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 8, row = c / N;
+  if (row >= rows) return;
+  const int col = (int)(c - row * N);
+  const float* p = partial + row * N + col;
+  f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+#pragma unroll 4
+  for (int k = 0; k < splits; ++k) {
+    a += *reinterpret_cast<const f32x4*>(p);
+    b += *reinterpret_cast<const f32x4*>(p + 4);
+    p += rows * N;
+  }
+  const int64_t e = row / M, m = row - e * M;
+  T o[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) { o[k] = from_f32<T>(a[k] * alpha); o[4 + k] = from_f32<T>(b[k] * alpha); }
+  *reinterpret_cast<v4*>(out + e * so + m * ldo + col) = *reinterpret_cast<const v4*>(o);
+}
+
+// expert of a row (experts: behind the last one's), the same on every lane
+__device__ __forceinline__ int expert_of(const int32_t* ends, int experts, int row, int lane) {
+  if (ends == nullptr) return 0;
+  int e = 0;
+  for (int base = 0; base < experts; base += 64) {
+    const bool before = base + lane < experts && ends[base + lane] <= row;
+    e += __popcll(__ballot(before));
+  }
+  return e;
+}
+
+struct FewArgs {
+  const void *X, *A, *B, *bias;
+  int64_t ldx, lda, sa, ldb, sb;
+  float *part_t, *part;  // [slices][n][R], [splits][n][N]
+  void *Y, *T;
+  int64_t ldy, ldt;
+  const int32_t* ends;
+  int experts, n, K, N, R, slices, splits;
+  float scale;
+};
+
+// Few rows: X A in slices of K.  A workgroup takes one row and one slice; R / 8 threads side by side take eight columns of A each.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void few_rank_kernel(FewArgs g) {
+  __shared__ float sum[kThreads][8];
+  const int row = (int)blockIdx.x, e = expert_of(g.ends, g.experts, row, threadIdx.x & 63);
+  if (e >= g.experts) return;
+  const int cg = g.R / 8, kl = kThreads / cg, c = threadIdx.x % cg, k0 = threadIdx.x / cg;
+  const int each = (g.K / 8 + g.slices - 1) / g.slices * 8, lo = (int)blockIdx.y * each, hi = lo + each < g.K ? lo + each : g.K;
+  const T* const x = static_cast<const T*>(g.X) + (int64_t)row * g.ldx;
+  const T* const a = static_cast<const T*>(g.A) + e * g.sa + c * 8;
+  float acc[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+  if (k0 < kl) {
+#pragma unroll 4
+    for (int k = lo + k0; k < hi; k += kl) {
+      const v4 v = *reinterpret_cast<const v4*>(a + (int64_t)k * g.lda);
+      const T* const t = reinterpret_cast<const T*>(&v);
+      const float xk = (float)x[k];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] += xk * (float)t[j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sum[threadIdx.x][j] = acc[j];
+  __syncthreads();
+  if ((int)threadIdx.x < g.R) {
+    float s = 0.f;
+    for (int k = 0; k < kl; ++k) s += sum[k * cg + threadIdx.x / 8][threadIdx.x & 7];
+    g.part_t[((int64_t)blockIdx.y * g.n + row) * g.R + threadIdx.x] = s;
+  }
+}
+
+// Few rows: Y = the slices of X W + T B + bias, T = s * the slices of X A rounded to the storage type.  A workgroup takes 512 columns of a row.
+template <typename T>
+__global__ __launch_bounds__(64) void few_finish_kernel(FewArgs g) {
+  __shared__ float t[256];
+  const int row = (int)blockIdx.y, lane = threadIdx.x, e = expert_of(g.ends, g.experts, row, lane);
+  const int col = ((int)blockIdx.x * 64 + lane) * 8;
+  const bool rest = e >= g.experts;
+  for (int k = lane; k < g.R; k += 64) {
+    float s = 0.f;
+    if (!rest)
+      for (int j = 0; j < g.slices; ++j) s += g.part_t[((int64_t)j * g.n + row) * g.R + k];
+    const T r = from_f32<T>(s * g.scale);
+    t[k] = (float)r;
+    if (g.T != nullptr && blockIdx.x == 0) static_cast<T*>(g.T)[(int64_t)row * g.ldt + k] = r;
+  }
+  __syncthreads();
+  if (col >= g.N) return;
+  f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+  const float* p = g.part + (int64_t)row * g.N + col;
+#pragma unroll 4
+  for (int j = 0; j < g.splits; ++j) {
+    a += *reinterpret_cast<const f32x4*>(p + (int64_t)j * g.n * g.N);
+    b += *reinterpret_cast<const f32x4*>(p + (int64_t)j * g.n * g.N + 4);
+  }
+  if (!rest) {
+    const T* const bp = static_cast<const T*>(g.B) + e * g.sb + col;
+#pragma unroll 8
+    for (int k = 0; k < g.R; ++k) {
+      const v4 v = *reinterpret_cast<const v4*>(bp + (int64_t)k * g.ldb);
+      const T* const w = reinterpret_cast<const T*>(&v);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { a[j] += t[k] * (float)w[j]; b[j] += t[k] * (float)w[4 + j]; }
+    }
+    if (g.bias != nullptr) {
+      const v4 v = *reinterpret_cast<const v4*>(static_cast<const T*>(g.bias) + (int64_t)e * g.N + col);
+      const T* const w = reinterpret_cast<const T*>(&v);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { a[j] += (float)w[j]; b[j] += (float)w[4 + j]; }
+    }
+  }
+  T o[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) { o[j] = from_f32<T>(a[j]); o[4 + j] = from_f32<T>(b[j]); }
+  *reinterpret_cast<v4*>(static_cast<T*>(g.Y) + (int64_t)row * g.ldy + col) = *reinterpret_cast<const v4*>(o);
+}
+
+template <template <typename> class F, typename... Args>
+hipError_t by_type(int dtype, Args... args) {
+  return dtype == DT_BF16 ? F<__bf16>::run(args...) : F<_Float16>::run(args...);
+}
+template <typename T>
+struct Turn {
+  static hipError_t run(const void* in, int64_t ld, int64_t stride, void* out, int64_t R, int64_t O, int64_t E, hipStream_t s) {
+    launch_timed(turn_kernel<T>, dim3((unsigned)ceil_div(O, kThreads), (unsigned)(R / 8), (unsigned)E), dim3(kThreads), 0, s, static_cast<const T*>(in), ld, stride,
+                 static_cast<T*>(out), (int)R, (int)O);
+    return hipGetLastError();
+  }
+};
+template <typename T>
+struct Slices {
+  static hipError_t run(const float* p, int splits, int64_t rows, int64_t M, int64_t N, float alpha, void* out, int64_t ldo, int64_t so, hipStream_t s) {
+    launch_timed(slices_kernel<T>, dim3((unsigned)ceil_div(rows * N / 8, kThreads)), dim3(kThreads), 0, s, p, splits, rows, (int)M, (int)N, alpha, static_cast<T*>(out), ldo, so);
+    return hipGetLastError();
+  }
+};
+template <typename T>
+struct FewRank {
+  static hipError_t run(const FewArgs& g, hipStream_t s) {
+    launch_timed(few_rank_kernel<T>, dim3((unsigned)g.n, (unsigned)g.slices), dim3(kThreads), 0, s, g);
+    return hipGetLastError();
+  }
+};
+template <typename T>
+struct FewFinish {
+  static hipError_t run(const FewArgs& g, hipStream_t s) {
+    launch_timed(few_finish_kernel<T>, dim3((unsigned)ceil_div(g.N, 512), (unsigned)g.n), dim3(64), 0, s, g);
+    return hipGetLastError();
+  }
+};
+
+hipError_t launch(int dtype, bool f8, int al, int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s) {
+  return dtype == DT_BF16 ? grouped_launch_bf16(f8, al, bl, tile, a, grid, s) : grouped_launch_f16(f8, al, bl, tile, a, grid, s);
+}
+
+// ---- plans: functions of sizes alone, shared by the workspace query and the call ----------------------
+
+constexpr int64_t kFill = 512;  // workgroups that fill the chip, two to a compute unit
+
+// rows of an expert that gets its share
+int64_t share(const ExpertsDesc& d) { return ceil_div(d.n, d.experts < d.n ? d.experts : d.n); }
+
+bool few(const ExpertsDesc& d) { return d.n <= 64 && d.r <= 256; }
+
+// the large product of a forward (K = i) or a backward (K = o)
+struct MainPlan { int tile, splits, per; unsigned gx; };
+MainPlan main_plan(const ExpertsDesc& d, int64_t N, int64_t K, bool split) {
+  MainPlan p;
+  const int64_t rows = share(d);
+  p.tile = rows <= 32 ? GT_32x128 : (rows <= 96 ? GT_64x128 : GT_128x128);
+  const GroupedTileInfo t = grouped_tile(p.tile);
+  const int64_t tiles = grouped_row_tiles(d.n, d.experts, t.bm, d.f8) * ceil_div(N, t.bn), nk = ceil_div(K, d.f8 ? 128 : 64);
+  p.gx = (unsigned)tiles;
+  int64_t s = split ? kFill / tiles : 1;
+  if (s > nk / 4) s = nk / 4;
+  if (s < 1) s = 1;
+  p.per = (int)ceil_div(nk, s);
+  p.splits = (int)ceil_div(nk, p.per);
+  return p;
+}
+
+// T = s X A, Z = s dY B^T
+struct RankPlan { int tile, splits, per; unsigned gx; };
+RankPlan rank_plan(const ExpertsDesc& d, int64_t K) {
+  RankPlan p;
+  p.tile = d.r <= 32 ? GT_64x32 : (d.r <= 64 ? GT_64x64 : GT_64x128T);
+  const GroupedTileInfo t = grouped_tile(p.tile);
+  const int64_t tiles = grouped_row_tiles(d.n, d.experts, t.bm, false) * ceil_div(d.r, t.bn), nk = ceil_div(K, 64);
+  p.gx = (unsigned)tiles;
+  int64_t s = kFill / tiles;
+  if (s > nk / 4) s = nk / 4;
+  if (s < 1) s = 1;
+  p.per = (int)ceil_div(nk, s);
+  p.splits = (int)ceil_div(nk, p.per);
+  return p;
+}
+size_t rank_bytes(const ExpertsDesc& d, const RankPlan& p) { return p.splits > 1 ? (size_t)p.splits * d.n * d.r * 4 : 0; }
+
+// dA = X^T Z (wide = i), dB = T^T dY (wide = o)
+struct GradPlan { int tile, splits; unsigned gx; };
+GradPlan grad_plan(const ExpertsDesc& d, int64_t wide, bool wide_rows) {
+  GradPlan p;
+  p.tile = d.r <= 32 ? (wide_rows ? GT_128x32 : GT_32x128) : (d.r <= 64 ? (wide_rows ? GT_128x64 : GT_64x128) : GT_128x128);
+  const GroupedTileInfo t = grouped_tile(p.tile);
+  const int64_t tiles = d.experts * ceil_div(wide_rows ? wide : d.r, t.bm) * ceil_div(wide_rows ? d.r : wide, t.bn);
+  p.gx = (unsigned)tiles;
+  int64_t s = kFill / tiles;
+  const int64_t nk = ceil_div(share(d), 64);
+  if (s > nk / 4) s = nk / 4;
+  if (s > 16) s = 16;
+  p.splits = (int)(s < 1 ? 1 : s);
+  return p;
+}
+size_t grad_bytes(const ExpertsDesc& d, const GradPlan& p, int64_t wide) { return p.splits > 1 ? (size_t)p.splits * d.experts * wide * d.r * 4 : 0; }
+
+// workspace layout
+struct Carver {
+  char* base;
+  size_t used = 0;
+  void* take(size_t bytes) {
+    void* p = base ? base + used : nullptr;
+    used += (size_t)pad256((int64_t)bytes);
+    return p;
+  }
+};
+struct Space {
+  uint8_t *q = nullptr, *s = nullptr;  // the rounded X or dY
+  int64_t ldq = 0, lds = 0;
+  void *turned = nullptr, *T = nullptr, *Z = nullptr;
+  float *part = nullptr, *part_t = nullptr;
+  int slices = 0;
+  size_t bytes = 0;
+};
+Space space(const ExpertsDesc& d, bool backward, void* workspace) {
+  Carver c{static_cast<char*>(workspace)};
+  Space w;
+  const int64_t K = backward ? d.o : d.i, N = backward ? d.i : d.o;
+  if (d.f8 && (!backward || d.dX != nullptr || workspace == nullptr)) {
+    w.ldq = fp8_row_bytes(K);
+    w.lds = fp8_scale_ld(d.n);
+    w.q = static_cast<uint8_t*>(c.take((size_t)(d.n * w.ldq)));
+    w.s = static_cast<uint8_t*>(c.take((size_t)(w.ldq / 128 * w.lds)));
+  }
+  if (!backward && few(d)) {
+    const MainPlan m = main_plan(d, N, K, true);
+    w.part = static_cast<float*>(c.take((size_t)m.splits * d.n * N * 4));
+    if (d.r > 0) {
+      w.slices = (int)(d.n >= 32 ? 8 : (d.n >= 8 ? 16 : 32));
+      w.part_t = static_cast<float*>(c.take((size_t)w.slices * d.n * d.r * 4));
+    }
+  } else if (d.r > 0) {
+    size_t part = rank_bytes(d, rank_plan(d, d.i));
+    w.T = c.take((size_t)(d.n * d.r) * 2);
+    if (!backward) {
+      w.turned = c.take((size_t)(d.experts * d.o * d.r) * 2);
+    } else {
+      w.Z = c.take((size_t)(d.n * d.r) * 2);
+      const size_t more[3] = {rank_bytes(d, rank_plan(d, d.o)), grad_bytes(d, grad_plan(d, d.i, true), d.i), grad_bytes(d, grad_plan(d, d.o, false), d.o)};
+      for (size_t b : more) part = part > b ? part : b;
+    }
+    w.part = static_cast<float*>(c.take(part));
+  }
+  w.bytes = c.used;
+  return w;
+}
+
+GroupedArgs rows_args(const ExpertsDesc& d) {
+  GroupedArgs a{};
+  a.ends = d.ends;
+  a.experts = (int)d.experts;
+  a.n = (int)d.n;
+  a.alpha = 1.f;
+  a.splits = 1;
+  return a;
+}
+
+// T [n, r] = s A_rows F:  F = A [i, r] (X's rows) or B [r, o] read as its transpose (dY's rows)
+hipError_t rank_run(const ExpertsDesc& d, const void* rows, int64_t ldrows, int64_t K, bool backward, void* out, int64_t ldo, float* part, hipStream_t stream) {
+  const RankPlan p = rank_plan(d, K);
+  GroupedArgs a = rows_args(d);
+  a.A = rows; a.lda = ldrows;
+  a.B = backward ? d.B : d.A; a.ldb = backward ? d.ldb : d.lda; a.sb = backward ? d.sb : d.sa;
+  a.C = out; a.ldc = ldo;
+  a.N = (int)d.r; a.K = (int)K;
+  a.alpha = d.scale;
+  a.splits = p.splits; a.tiles_per_split = p.per;
+  a.partial = p.splits > 1 ? part : nullptr;
+  hipError_t e = launch(d.dtype, false, 0, backward ? 1 : 0, p.tile, a, dim3(p.gx, (unsigned)p.splits), stream);
+  if (e == hipSuccess && p.splits > 1) e = by_type<Slices>(d.dtype, (const float*)part, p.splits, d.n, d.n, d.r, d.scale, out, ldo, (int64_t)0, stream);
+  return e;
+}
+
+hipError_t grad_run(const ExpertsDesc& d, bool of_A, const void* T, int64_t ldt, const void* Z, float* part, hipStream_t stream) {
+  const int64_t wide = of_A ? d.i : d.o;
+  const GradPlan p = grad_plan(d, wide, of_A);
+  GroupedArgs a = rows_args(d);
+  if (of_A) {
+    a.A = d.X; a.lda = d.ldx; a.B = Z; a.ldb = d.r;
+    a.M = (int)d.i; a.N = (int)d.r;
+    a.C = d.dA; a.ldc = d.ldda; a.sc = d.sda;
+  } else {
+    a.A = T; a.lda = ldt; a.B = d.dY; a.ldb = d.lddy;
+    a.M = (int)d.r; a.N = (int)d.o;
+    a.C = d.dB; a.ldc = d.lddb; a.sc = d.sdb;
+  }
+  a.splits = p.splits;
+  a.partial = p.splits > 1 ? part : nullptr;
+  hipError_t e = launch(d.dtype, false, 1, 0, p.tile, a, dim3(p.gx, (unsigned)p.splits), stream);
+  if (e == hipSuccess && p.splits > 1)
+    e = by_type<Slices>(d.dtype, (const float*)part, p.splits, d.experts * a.M, (int64_t)a.M, (int64_t)a.N, 1.f, a.C, a.ldc, a.sc, stream);
+  return e;
+}
+
+// the large product: rows (rounded first where W is e4m3) times W or its transpose, the adapter's product TA TB^T and the bias behind it
+hipError_t main_run(const ExpertsDesc& d, bool backward, const Space& w, const void* TA, int64_t ldta, const void* TB, int64_t ldtb, int64_t stb, void* out, int64_t ldo,
+                    bool slices, hipStream_t stream) {
+  const int64_t K = backward ? d.o : d.i, N = backward ? d.i : d.o;
+  const MainPlan p = main_plan(d, N, K, slices);
+  GroupedArgs a = rows_args(d);
+  a.A = backward ? d.dY : d.X;
+  a.lda = backward ? d.lddy : d.ldx;
+  a.B = d.W; a.ldb = d.ldw; a.sb = d.sw;
+  if (d.f8) {
+    hipError_t e = fp8_rows_run(d.dtype, a.A, a.lda, d.n, K, w.q, w.ldq, w.s, w.lds, stream);
+    if (e != hipSuccess) return e;
+    a.A = w.q; a.lda = w.ldq;
+    a.SA = w.s; a.ldsa = w.lds;
+    a.SB = d.w_scales; a.ssb = d.s_scales;
+    a.scols = (int)ceil_div(d.o, 128);
+  }
+  a.C = out; a.ldc = ldo;
+  a.N = (int)N; a.K = (int)K;
+  a.splits = p.splits; a.tiles_per_split = p.per;
+  if (slices) {
+    a.partial = w.part;
+  } else {
+    a.bias = backward ? nullptr : d.bias;
+    if (d.r > 0) { a.TA = TA; a.ldta = ldta; a.TB = TB; a.ldtb = ldtb; a.stb = stb; a.R = (int)d.r; }
+  }
+  return launch(d.dtype, d.f8, 0, backward ? 1 : 0, p.tile, a, dim3(p.gx, (unsigned)p.splits), stream);
+}
+
+}  // namespace
+
+size_t experts_workspace(const ExpertsDesc& d, bool backward) { return space(d, backward, nullptr).bytes; }
+
+hipError_t experts_forward(const ExpertsDesc& d, void* workspace, hipStream_t stream) {
+  const Space w = space(d, false, workspace);
+  hipError_t e;
+  if (few(d)) {
+    FewArgs f{};
+    f.X = d.X; f.A = d.A; f.B = d.B; f.bias = d.bias;
+    f.ldx = d.ldx; f.lda = d.lda; f.sa = d.sa; f.ldb = d.ldb; f.sb = d.sb;
+    f.part_t = w.part_t; f.part = w.part;
+    f.Y = d.Y; f.ldy = d.ldy; f.T = d.T; f.ldt = d.ldt;
+    f.ends = d.ends; f.experts = (int)d.experts;
+    f.n = (int)d.n; f.K = (int)d.i; f.N = (int)d.o; f.R = (int)d.r;
+    f.slices = w.slices; f.splits = main_plan(d, d.o, d.i, true).splits;
+    f.scale = d.scale;
+    if (d.r > 0 && (e = by_type<FewRank>(d.dtype, f, stream)) != hipSuccess) return e;
+    if ((e = main_run(d, false, w, nullptr, 0, nullptr, 0, 0, nullptr, 0, true, stream)) != hipSuccess) return e;
+    return by_type<FewFinish>(d.dtype, f, stream);
+  }
+  void* T = d.T ? d.T : w.T;
+  const int64_t ldt = d.T ? d.ldt : d.r;
+  if (d.r > 0) {
+    if ((e = by_type<Turn>(d.dtype, d.B, d.ldb, d.sb, w.turned, d.r, d.o, d.experts, stream)) != hipSuccess) return e;
+    if ((e = rank_run(d, d.X, d.ldx, d.i, false, T, ldt, w.part, stream)) != hipSuccess) return e;
+  }
+  return main_run(d, false, w, T, ldt, w.turned, d.r, d.o * d.r, d.Y, d.ldy, false, stream);
+}
+
+hipError_t experts_backward(const ExpertsDesc& d, void* workspace, hipStream_t stream) {
+  const Space w = space(d, true, workspace);
+  hipError_t e;
+  const void* T = d.T;
+  int64_t ldt = d.ldt;
+  if (d.r > 0) {
+    if ((d.dX || d.dA) && (e = rank_run(d, d.dY, d.lddy, d.o, true, w.Z, d.r, w.part, stream)) != hipSuccess) return e;
+    if (d.dB && !d.has_T) {
+      if ((e = rank_run(d, d.X, d.ldx, d.i, false, w.T, d.r, w.part, stream)) != hipSuccess) return e;
+      T = w.T;
+      ldt = d.r;
+    }
+    if (d.dA && (e = grad_run(d, true, T, ldt, w.Z, w.part, stream)) != hipSuccess) return e;
+    if (d.dB && (e = grad_run(d, false, T, ldt, w.Z, w.part, stream)) != hipSuccess) return e;
+  }
+  if (d.dX) return main_run(d, true, w, w.Z, d.r, d.A, d.lda, d.sa, d.dX, d.lddx, false, stream);
+  return hipSuccess;
+}
+
+}  // namespace rl

@@ -1,0 +1,3 @@
+#define RL_T __bf16
+#define RL_GROUPED_FN grouped_launch_bf16
+#include "grouped_launch.inc"

@@ -1,0 +1,3 @@
+#define RL_T _Float16
+#define RL_GROUPED_FN grouped_launch_f16
+#include "grouped_launch.inc"

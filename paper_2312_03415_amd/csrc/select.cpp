@@ -185,6 +185,12 @@ extern "C" int runlora_select_by(int criterion, int64_t n, int64_t i, int64_t o,
                                  int* fwd, int* bwd) {
   if (!fwd || !bwd) return RL_ERR_NULL;
   if (n < 1 || i < 1 || o < 1 || r < 1) return RL_ERR_SHAPE;
+  if (dtype == RL_FP8_B128) {  // the one pair that exists for such a W
+    if (criterion < 0 || criterion > 3) return RL_ERR_VARIANT;
+    *fwd = RL_FWD1;
+    *bwd = RL_BWD1;
+    return RL_OK;
+  }
   int dt = to_internal_dtype(dtype);
   if (dt < 0) return RL_ERR_DTYPE;
   if (criterion < 0 || criterion > 3) return RL_ERR_VARIANT;
@@ -274,6 +280,7 @@ extern "C" int runlora_select(int64_t n, int64_t i, int64_t o, int64_t r, int dt
     }
     const bool merged = *fwd == RL_FWD2 || *bwd == RL_BWD4 || *bwd == RL_BWD5 || *bwd == RL_BWD7 || *bwd == RL_BWD8;
     if (dtype == RL_INT4_G64 && merged) return RL_ERR_UNSUPPORTED;
+    if (dtype == RL_FP8_B128 && ((*fwd != RL_FWD1 && *fwd != RL_FWD3) || *bwd != RL_BWD1)) return RL_ERR_UNSUPPORTED;
   }
   return RL_OK;
 }

@@ -12,6 +12,9 @@ for the calls that have to see a Python-level function (tracing, functorch trans
     y = layer(x)                                                     # x [..., d_in] -> [..., d_out]
     wrap_linears(model, r=16, alpha=32, targets=("q_proj", "v_proj"))
     vera = RunVeRALinear(weight, A_shared, B_shared)                 # frozen A, B; trainable vectors d, b
+    layer8 = RunLoRAFp8Linear.from_linear(nn_linear, r=16, alpha=32) # the frozen W in 8 bits
+    experts = RunLoRAExperts(weight_stack, r=16, alpha=32)           # one adapted layer per expert
+    y = experts(x_sorted, ends)                                      # rows sorted by expert, ends[e] = where expert e's rows end
 """
 import ctypes
 import math
@@ -381,6 +384,151 @@ class RunDoRALinear(nn.Module):
 
     def extra_repr(self):
         return f"d_in={self.d_in}, d_out={self.d_out}, r={self.r}, scale={self.scale:g}, bias={self.bias is not None}"
+
+
+def _rows(x, width):
+    """x as a matrix [n, width] that the library can read."""
+    x2 = x.reshape(-1, width)
+    if x2.stride(-1) != 1 or x2.stride(0) % 8 != 0 or x2.stride(0) < width or x2.data_ptr() % 16 != 0:
+        x2 = x2.contiguous()
+    return x2
+
+
+def _w_code(W, code):
+    return rl.RL_FP8_B128 if isinstance(W, rl.Fp8Weight) else code
+
+
+class RunLoRAFp8Function(torch.autograd.Function):
+    """y = Q(x) W + bias + scale (x A) B over an Fp8Weight (runlora.h); gradients for x, A and B, the large product of dx on Q(dy).
+    scale XA (n*r elements) is kept for the backward."""
+
+    @staticmethod
+    def forward(ctx, x, W, A, B, bias, scale):
+        x2 = _rows(x, W.rows)
+        n, r, code = x2.shape[0], A.shape[1], rl.dtype_code(x.dtype)
+        y = torch.empty((n, W.cols), dtype=x.dtype, device=x.device)
+        T = torch.empty((n, r), dtype=x.dtype, device=x.device)
+        ctx.saved, ctx.W, ctx.x_shape = rl.new_saved(T), W, x.shape
+        if n > 0:
+            ws = _workspace(x.device, rl.runlora_workspace_bytes(rl.FWD1, -1, n, W.rows, W.cols, r, code, rl.RL_FP8_B128))
+            rl.runlora_forward(rl.FWD1, x2, W, A, B, y, ctx.saved, workspace=ws, scale=scale, bias=bias)
+        ctx.save_for_backward(x2, A, B, T)
+        return y.view(*x.shape[:-1], W.cols)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x2, A, B, T = ctx.saved_tensors
+        W, (n, i), r = ctx.W, x2.shape, A.shape[1]
+        dy2 = _rows(dy, W.cols)
+        need_x, _, need_a, need_b = ctx.needs_input_grad[:4]
+        dx = torch.empty((n, i), dtype=x2.dtype, device=x2.device) if need_x else None
+        make = torch.empty_like if n > 0 else torch.zeros_like
+        dA, dB = make(A) if need_a else None, make(B) if need_b else None
+        if n > 0:
+            saved, x2 = _reread(ctx.saved, dy2, x2, A, B, T)
+            if saved.T != T.data_ptr() or saved.ldt != T.stride(0):
+                saved = type(saved).from_buffer_copy(saved)
+                saved.T, saved.ldt = T.data_ptr(), T.stride(0)
+            code = rl.dtype_code(dy.dtype)
+            ws = _workspace(dy.device, rl.runlora_workspace_bytes(-1, rl.BWD1, n, i, W.cols, r, code, rl.RL_FP8_B128))
+            rl.runlora_backward(rl.BWD1, dy2, saved, W, A, B, dx, dA, dB, workspace=ws)
+        return dx.view(ctx.x_shape) if need_x else None, None, dA, dB, None, None
+
+
+class RunLoRAExpertsFunction(torch.autograd.Function):
+    """y_t = x_t W_e + bias_e + scale (x_t A_e) B_e over rows sorted by expert (runlora_experts_forward / _backward); gradients for x, A and
+    B.  W: [experts, d_in, d_out] or an Fp8Weight stack; A = B = None: no adapter.  scale XA is kept for the backward."""
+
+    @staticmethod
+    def forward(ctx, x, ends, W, A, B, bias, scale):
+        E, i, o = W.shape
+        x2 = _rows(x, i)
+        n, r, code = x2.shape[0], 0 if A is None else A.shape[2], rl.dtype_code(x.dtype)
+        y = torch.empty((n, o), dtype=x.dtype, device=x.device)
+        T = torch.empty((n, r), dtype=x.dtype, device=x.device) if r else None
+        if n > 0:
+            ws = _workspace(x.device, rl.runlora_experts_workspace_bytes(False, n, E, i, o, r, code, _w_code(W, code)))
+            rl.runlora_experts_forward(x2, ends, W, A, B, y, T, workspace=ws, scale=scale, bias=bias)
+        ctx.W, ctx.scale, ctx.x_shape = W, scale, x.shape
+        ctx.save_for_backward(x2, ends, A, B, T)
+        return y.view(*x.shape[:-1], o)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x2, ends, A, B, T = ctx.saved_tensors
+        E, i, o = ctx.W.shape
+        n, r = x2.shape[0], 0 if A is None else A.shape[2]
+        dy2, x2 = _rows(dy, o), _rows(x2, i)
+        need = ctx.needs_input_grad
+        dx = torch.empty((n, i), dtype=x2.dtype, device=x2.device) if need[0] else None
+        make = torch.empty if n > 0 else torch.zeros
+        dA = make(A.shape, dtype=A.dtype, device=A.device) if need[3] else None
+        dB = make(B.shape, dtype=B.dtype, device=B.device) if need[4] else None
+        if n > 0:
+            code = rl.dtype_code(dy.dtype)
+            ws = _workspace(dy.device, rl.runlora_experts_workspace_bytes(True, n, E, i, o, r, code, _w_code(ctx.W, code)))
+            rl.runlora_experts_backward(dy2, x2, ends, ctx.W, A, B, dx, dA, dB, T, workspace=ws, scale=ctx.scale)
+        return dx.view(ctx.x_shape) if need[0] else None, None, None, dA, dB, None, None
+
+
+class RunLoRAFp8Linear(nn.Module):
+    """LoRA-augmented linear layer over a frozen weight kept in 8 bits (binding.Fp8Weight); otherwise as RunLoRALinear."""
+
+    def __init__(self, weight, r, alpha=None, bias=None, dtype=torch.bfloat16):
+        super().__init__()
+        (self.d_in, self.d_out), self.r = weight.shape, r
+        self.scale = 1.0 if alpha is None else float(alpha) / r
+        device = weight.data.device
+        self.register_buffer("weight_data", weight.data)
+        self.register_buffer("weight_scales", weight.scales)
+        self.bias = nn.Parameter(bias.contiguous(), requires_grad=False) if bias is not None else None
+        self.lora_A = nn.Parameter(torch.randn(self.d_in, r, dtype=dtype, device=device) / math.sqrt(self.d_in))
+        self.lora_B = nn.Parameter(torch.zeros(r, self.d_out, dtype=dtype, device=device))
+
+    @classmethod
+    def from_linear(cls, linear, r, alpha=None):
+        """nn.Linear keeps its weight as [d_out, d_in]; the layer holds the transposed copy, rounded."""
+        b = linear.bias.detach() if linear.bias is not None else None
+        return cls(rl.Fp8Weight.quantize(linear.weight.detach().t().contiguous()), r, alpha, b, linear.weight.dtype)
+
+    @property
+    def weight(self):
+        return rl.Fp8Weight(self.weight_data, self.weight_scales, self.d_in, self.d_out)
+
+    def forward(self, x):
+        return RunLoRAFp8Function.apply(x, self.weight, self.lora_A, self.lora_B, self.bias, self.scale)
+
+    def extra_repr(self):
+        return f"d_in={self.d_in}, d_out={self.d_out}, r={self.r}, scale={self.scale:g}, bias={self.bias is not None}"
+
+
+class RunLoRAExperts(nn.Module):
+    """One adapted linear layer per expert, on rows sorted by expert: frozen weight [experts, d_in, d_out] (a tensor or an Fp8Weight stack) and
+    bias [experts, d_out], trainable A [experts, d_in, r] and B [experts, r, d_out]; layer(x [n, d_in], ends), ends (int32, on the
+    device) = where each expert's rows end, e.g. torch.bincount(expert_of_row, minlength=experts).cumsum(0, dtype=torch.int32)."""
+
+    def __init__(self, weight, r, alpha=None, bias=None, dtype=None):
+        super().__init__()
+        self.experts, self.d_in, self.d_out = weight.shape
+        self.r, self.scale = r, 1.0 if alpha is None else float(alpha) / r
+        self.fp8 = isinstance(weight, rl.Fp8Weight)
+        if self.fp8:
+            self.register_buffer("weight_data", weight.data)
+            self.register_buffer("weight_scales", weight.scales)
+            device, dtype = weight.data.device, dtype or torch.bfloat16
+        else:
+            self.weight = nn.Parameter(weight.contiguous(), requires_grad=False)
+            device, dtype = weight.device, weight.dtype
+        self.bias = nn.Parameter(bias.contiguous(), requires_grad=False) if bias is not None else None
+        self.lora_A = nn.Parameter(torch.randn(self.experts, self.d_in, r, dtype=dtype, device=device) / math.sqrt(self.d_in))
+        self.lora_B = nn.Parameter(torch.zeros(self.experts, r, self.d_out, dtype=dtype, device=device))
+
+    def forward(self, x, ends):
+        W = rl.Fp8Weight(self.weight_data, self.weight_scales, self.d_in, self.d_out) if self.fp8 else self.weight
+        return RunLoRAExpertsFunction.apply(x, ends, W, self.lora_A, self.lora_B, self.bias, self.scale)
+
+    def extra_repr(self):
+        return f"experts={self.experts}, d_in={self.d_in}, d_out={self.d_out}, r={self.r}, scale={self.scale:g}, bias={self.bias is not None}"
 
 
 def wrap_linears(model, r, alpha=None, targets=None, pair=None, keep_merged=False, dropout=0.0, adapter="lora"):

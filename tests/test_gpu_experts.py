@@ -1,0 +1,410 @@
+"""Layers over stacks of expert weights (16-bit and 8-bit) and the layer over an 8-bit weight, through the C ABI and the modules, against a
+float64 reference.  Bounds: the relative 2-norm error of helpers.py per output, and the per-element bounds that experts_oracle.py derives."""
+import numpy as np
+import pytest
+
+import experts_oracle as ref
+from helpers import TOL, relerr, to_f64, torch_dtype
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+def _rl():
+    from paper_2312_03415_amd import binding
+    return binding
+
+
+class Case:
+    """Inputs on the device and as float64, from the sizes alone."""
+
+    def __init__(self, dtype, fp8, n, experts, i, o, r, kind="uneven", bias=False, seed=0, pad=0, outliers=True):
+        rng = np.random.default_rng(1000 * seed + n + 7 * experts + i + o + r)
+        td = torch_dtype(dtype)
+        self.__dict__.update(dtype=dtype, fp8=fp8, n=n, experts=experts, i=i, o=o, r=r, td=td)
+
+        def dev(shape, var, width_pad=0):
+            host = rng.standard_normal(shape) * np.sqrt(var)
+            if width_pad:
+                buf = torch.full(shape[:-1] + (shape[-1] + width_pad,), float("nan"), dtype=td, device="cuda")
+                t = buf[..., :shape[-1]]
+                t.copy_(torch.from_numpy(host))
+            else:
+                t = torch.from_numpy(host).to(td).cuda()
+            return t, to_f64(t)
+
+        x = rng.standard_normal((n, i))
+        if outliers:
+            x[:, :: max(1, i // 3)] *= 8.0
+        buf = torch.full((n, i + pad), float("nan"), dtype=td, device="cuda")
+        self.X = buf[:, :i]
+        self.X.copy_(torch.from_numpy(x))
+        self.hX = to_f64(self.X)
+        self.dY, self.hdY = dev((n, o), 1.0, pad)
+        if n > 3:
+            self.dY[::4] = 0.0
+            self.hdY[::4] = 0.0
+        self.A, self.hA = dev((experts, i, r), 1.0 / i, pad) if r else (None, None)
+        self.B, self.hB = dev((experts, r, o), 0.5 / r, pad) if r else (None, None)
+        self.bias, self.hbias = dev((experts, o), 0.1) if bias else (None, None)
+        self.ends_host = np.cumsum(ref.counts(kind, n, experts, rng))
+        self.ends = torch.from_numpy(self.ends_host.astype(np.int32)).cuda()
+        w = rng.standard_normal((experts, i, o)) / np.sqrt(i)
+        if fp8:
+            rl = _rl()
+            self.W = rl.Fp8Weight.quantize(torch.from_numpy(w).float().cuda())
+            data, scales = self.W.data.cpu().numpy(), self.W.scales.cpu().numpy()
+            self.hW = np.stack([ref.weight_value(data[e], scales[e]) for e in range(experts)])
+        else:
+            wb = torch.full((experts, i, o + pad), float("nan"), dtype=td, device="cuda")
+            self.W = wb[..., :o]
+            self.W.copy_(torch.from_numpy(w))
+            self.hW = to_f64(self.W)
+
+    def workspace(self, backward):
+        rl = _rl()
+        code = rl.dtype_code(self.td)
+        size = rl.runlora_experts_workspace_bytes(backward, self.n, self.experts, self.i, self.o, self.r, code, rl.RL_FP8_B128 if self.fp8 else code)
+        return torch.full((max(size, 256),), 255, dtype=torch.uint8, device="cuda")  # (every value a NaN: nothing may rely on scratch)
+
+    def forward(self, s=1.5, keep=True):
+        rl = _rl()
+        Y = torch.full((self.n, self.o), float("nan"), dtype=self.td, device="cuda")
+        T = torch.full((self.n, self.r), float("nan"), dtype=self.td, device="cuda") if keep and self.r else None
+        rl.runlora_experts_forward(self.X, self.ends, self.W, self.A, self.B, Y, T, workspace=self.workspace(False), scale=s, bias=self.bias)
+        return Y, T
+
+    def backward(self, T, s=1.5):
+        rl = _rl()
+        nan = lambda shape: torch.full(shape, float("nan"), dtype=self.td, device="cuda")
+        dX = nan((self.n, self.i))
+        dA, dB = (nan((self.experts, self.i, self.r)), nan((self.experts, self.r, self.o))) if self.r else (None, None)
+        rl.runlora_experts_backward(self.dY, self.X, self.ends, self.W, self.A, self.B, dX, dA, dB, T, workspace=self.workspace(True), scale=s)
+        return dX, dA, dB
+
+    def want_forward(self, s=1.5):
+        return ref.forward(self.hX, self.ends_host, self.hW, self.hA, self.hB, self.hbias, s, self.fp8, self.dtype)
+
+    def want_backward(self, s=1.5):
+        return ref.backward(self.hdY, self.hX, self.ends_host, self.hW, self.hA, self.hB, s, self.fp8, self.dtype)
+
+
+def close(name, got, want, bound, dtype):
+    g = to_f64(got).reshape(want.shape)
+    assert np.isfinite(g).all(), f"{name}: not finite"
+    assert relerr(g, want) <= TOL[dtype], f"{name}: rel. Frobenius error {relerr(g, want):.2e}"
+    over = np.abs(g - want) > bound
+    assert not over.any(), f"{name}: {int(over.sum())} elements out of bounds, first at {np.argwhere(over)[0]}, {np.max(np.abs(g - want)[over] / bound[over])} times"
+
+
+def close_all(names, got, want, dtype):
+    for name, g, w, b in zip(names, got, *want):
+        if w is not None and w.size:
+            close(name, g, w, b, dtype)
+
+
+def check(c):
+    Y, T = c.forward()
+    close_all(("Y", "T"), (Y, T), c.want_forward(), c.dtype)
+    want = c.want_backward()
+    for kept in ((T, None) if c.r else (None,)):
+        close_all(("dX", "dA", "dB"), c.backward(kept), want, c.dtype)
+
+
+SIZES = [
+    # n, experts, i, o, r, rows per expert
+    (1, 1, 128, 128, 8, "even"),           # a single row
+    (1, 5, 272, 144, 16, "one"),
+    (7, 3, 144, 400, 8, "uneven"),
+    (33, 8, 256, 512, 16, "uneven"),       # few rows, empty experts
+    (64, 64, 128, 256, 32, "even"),        # one row each
+    (50, 4, 384, 272, 24, "rest"),         # rows behind the last expert's
+    (65, 2, 528, 400, 40, "even"),
+    (200, 130, 144, 272, 8, "uneven"),     # more experts than a wave has lanes, twice
+    (300, 7, 336, 592, 64, "uneven"),
+    (257, 3, 640, 656, 72, "one"),
+    (515, 5, 1040, 272, 128, "rest"),
+    (700, 2, 272, 1168, 136, "even"),      # a rank above a tile's width
+    (400, 3, 256, 256, 264, "uneven"),
+    (40, 3, 256, 256, 264, "uneven"),
+    (90, 4, 144, 144, 16, "none"),         # nobody gets a row
+    (1100, 3, 528, 784, 16, "uneven"),
+]
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+@pytest.mark.parametrize("n,experts,i,o,r,kind", SIZES)
+def test_forward_and_backward(n, experts, i, o, r, kind, fp8):
+    check(Case("bf16", fp8, n, experts, i, o, r, kind, bias=(n % 2 == 1)))
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+@pytest.mark.parametrize("n,experts,i,o,r,kind", [SIZES[3], SIZES[8], SIZES[15]])
+def test_fp16(n, experts, i, o, r, kind, fp8):
+    check(Case("f16", fp8, n, experts, i, o, r, kind, bias=True))
+
+
+@pytest.mark.parametrize("n,experts,i,o,r,kind", [(20, 3, 136, 264, 8, "uneven"), (333, 3, 136, 264, 24, "uneven"), (150, 2, 1032, 648, 56, "rest")])
+def test_dense_widths_in_steps_of_eight(n, experts, i, o, r, kind):
+    check(Case("bf16", False, n, experts, i, o, r, kind, bias=True))
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+@pytest.mark.parametrize("n", [5, 300])
+def test_no_adapter(n, fp8):
+    check(Case("bf16", fp8, n, 4, 256, 400, 0, "uneven", bias=True))
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+@pytest.mark.parametrize("n", [12, 300])
+def test_padded_rows(n, fp8):
+    """Leading dimensions above the widths, with NaN between the rows."""
+    check(Case("bf16", fp8, n, 3, 272, 400, 24, "uneven", pad=24))
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+@pytest.mark.parametrize("n", [9, 260])
+def test_shared_adapter_and_strided_gradients(n, fp8):
+    """One A and B for all experts (stride 0); dA and dB into a larger buffer."""
+    rl = _rl()
+    c = Case("bf16", fp8, n, 4, 256, 272, 16, "uneven")
+    c.A, c.B = c.A[1:2].expand(4, -1, -1), c.B[2:3].expand(4, -1, -1)
+    c.hA, c.hB = np.repeat(c.hA[1:2], 4, 0), np.repeat(c.hB[2:3], 4, 0)
+    Y, T = c.forward()
+    close_all(("Y", "T"), (Y, T), c.want_forward(), "bf16")
+    big_A, big_B = (torch.full((9,) + s, 7.0, dtype=c.td, device="cuda") for s in ((256, 24), (16, 280)))
+    dA, dB = big_A[:8:2, :, :16], big_B[1::2, :, :272]
+    rl.runlora_experts_backward(c.dY, c.X, c.ends, c.W, c.A, c.B, None, dA, dB, T, workspace=c.workspace(True), scale=1.5)
+    close_all(("", "dA", "dB"), (None, dA, dB), tuple((None,) + w[1:] for w in c.want_backward()), "bf16")
+    assert (big_A[1::2] == 7.0).all() and (big_A[..., 16:] == 7.0).all() and (big_B[::2] == 7.0).all() and (big_B[..., 272:] == 7.0).all()
+
+
+def test_subsets_of_gradients_give_the_same_bits():
+    rl = _rl()
+    c = Case("bf16", True, 300, 3, 256, 400, 16)
+    _, T = c.forward()
+    dX, dA, dB = c.backward(T)
+    for want in ((1, 0, 0), (0, 1, 0), (0, 0, 1), (1, 1, 0)):
+        outs = [torch.empty_like(t) if w else None for t, w in zip((dX, dA, dB), want)]
+        rl.runlora_experts_backward(c.dY, c.X, c.ends, c.W, c.A, c.B, *outs, T, workspace=c.workspace(True), scale=1.5)
+        for got, full in zip(outs, (dX, dA, dB)):
+            assert got is None or torch.equal(got, full)
+
+
+@pytest.mark.parametrize("n", [40, 900])
+def test_repeated_calls_give_the_same_bits(n):
+    c = Case("bf16", True, n, 5, 400, 528, 16)
+    Y, T = c.forward()
+    grads = c.backward(T)
+    for _ in range(5):
+        Y2, T2 = c.forward()
+        assert torch.equal(Y, Y2) and torch.equal(T, T2)
+        assert all(torch.equal(a, b) for a, b in zip(grads, c.backward(T)))
+
+
+@pytest.mark.parametrize("n", [20, 400])
+def test_ends_outside_the_rows_count_as_the_nearer_end(n):
+    c = Case("bf16", False, n, 4, 256, 256, 8, "even")
+    c.ends_host = np.array([0, n // 2, n, n])
+    c.ends = torch.tensor([-5, n // 2, n + 1000, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    check(c)
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+@pytest.mark.parametrize("n", [24, 300])
+def test_rows_of_other_experts_do_not_matter(n, fp8):
+    """Infinities and NaN in one expert's rows and weights stay in its outputs."""
+    c = Case("bf16", fp8, n, 3, 256, 272, 16, "even")
+    Y0, T0 = c.forward()
+    g0 = c.backward(T0)
+    lo, hi = int(c.ends_host[0]), int(c.ends_host[1])
+    c.X[lo] = float("inf")
+    c.X[lo + 1, 5] = float("nan")
+    c.dY[hi - 1] = float("nan")
+    c.B[1, 0, 0] = float("nan")
+    Y, T = c.forward()
+    keep = torch.ones(n, dtype=torch.bool, device="cuda")
+    keep[lo:hi] = False
+    assert torch.equal(Y[keep], Y0[keep]) and torch.equal(T[keep], T0[keep])
+    assert not torch.isfinite(Y[lo]).any() and torch.isnan(Y[lo + 1]).all()
+    dX, dA, dB = c.backward(T)
+    assert torch.equal(dX[keep], g0[0][keep])
+    for g, w in ((dA, g0[1]), (dB, g0[2])):
+        assert torch.equal(g[0], w[0]) and torch.equal(g[2], w[2])
+    assert torch.isnan(dX[hi - 1]).all()
+
+
+@pytest.mark.parametrize("n", [16, 500])
+def test_captured_graph_follows_the_ends(n):
+    """The row counts are read when the work runs: a captured call replayed with other ends."""
+    rl = _rl()
+    c = Case("bf16", True, n, 4, 256, 272, 16, "even")
+    ws, Y = c.workspace(False), torch.empty((n, 272), dtype=c.td, device="cuda")
+    call = lambda: rl.runlora_experts_forward(c.X, c.ends, c.W, c.A, c.B, Y, workspace=ws, scale=1.5)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for ends in ([n // 4, n // 2, n // 2, n], [0, 0, 0, n], [n, n, n, n], [1, 2, 3, n // 2]):
+        c.ends_host = np.array(ends)
+        c.ends.copy_(torch.tensor(ends, dtype=torch.int32))
+        Y.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = Y.clone()
+        close_all(("Y",), (got,), c.want_forward(), "bf16")
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(got, Y)
+
+
+def test_another_stream():
+    c = Case("bf16", True, 300, 4, 256, 272, 16)
+    Y0, T0 = c.forward()
+    g0 = c.backward(T0)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        Y, T = c.forward()
+        g = c.backward(T)
+    side.synchronize()
+    assert torch.equal(Y, Y0) and all(torch.equal(a, b) for a, b in zip(g, g0))
+
+
+# ---- the modules ---------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+@pytest.mark.parametrize("n", [0, 30, 300])
+def test_experts_module(n, fp8):
+    from paper_2312_03415_amd.module import RunLoRAExperts
+    c = Case("bf16", fp8, max(n, 1), 4, 256, 272, 16, "uneven", bias=True)
+    layer = RunLoRAExperts(c.W, 16, 24.0, c.bias)
+    with torch.no_grad():
+        layer.lora_A.copy_(c.A)
+        layer.lora_B.copy_(c.B)
+    x = c.X[:n].contiguous().requires_grad_(True)
+    y = layer(x, c.ends if n else torch.zeros_like(c.ends))
+    dx, dA, dB = torch.autograd.grad(y, (x, layer.lora_A, layer.lora_B), c.dY[:n])
+    assert y.shape == (n, 272) and dx.shape == x.shape
+    if n == 0:
+        assert (dA == 0).all() and (dB == 0).all()
+        return
+    close_all(("Y",), (y,), c.want_forward(), "bf16")
+    close_all(("dX", "dA", "dB"), (dx, dA, dB), c.want_backward(), "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("n", [3, 400])
+def test_fp8_layer_module_and_abi(n, dtype):
+    """RunLoRAFp8Linear (autograd) and runlora_forward / runlora_backward on an Fp8Weight give the same bits and meet the reference."""
+    from paper_2312_03415_amd.module import RunLoRAFp8Linear
+    rl = _rl()
+    c = Case(dtype, True, n, 1, 528, 784, 24, "even", bias=True)
+    W = rl.Fp8Weight(c.W.data[0], c.W.scales[0], 528, 784)
+    layer = RunLoRAFp8Linear(W, 24, 36.0, c.bias[0], dtype=c.td)
+    with torch.no_grad():
+        layer.lora_A.copy_(c.A[0])
+        layer.lora_B.copy_(c.B[0])
+    x = c.X.clone().requires_grad_(True)
+    y = layer(x)
+    grads = torch.autograd.grad(y, (x, layer.lora_A, layer.lora_B), c.dY)
+    close_all(("Y",), (y,), c.want_forward(), dtype)
+    close_all(("dX", "dA", "dB"), grads, c.want_backward(), dtype)
+    code = rl.dtype_code(c.td)
+    assert rl.runlora_select(n, 528, 784, 24, rl.RL_FP8_B128) == (rl.FWD1, rl.BWD1)
+    ws = rl.new_workspace(rl.FWD1, rl.BWD1, n, 528, 784, 24, code, w_dtype=rl.RL_FP8_B128)
+    T, Y = torch.empty((n, 24), dtype=c.td, device="cuda"), torch.empty((n, 784), dtype=c.td, device="cuda")
+    saved = rl.new_saved(T)
+    rl.runlora_forward(rl.FWD1, c.X, W, c.A[0], c.B[0], Y, saved, workspace=ws, scale=1.5, bias=c.bias[0])
+    assert torch.equal(Y, y)
+    Y2 = torch.empty_like(Y)
+    rl.runlora_forward_static(rl.FWD1, c.X, W, c.A[0], c.B[0], Y2, rl.new_saved(), scale=1.5, bias=c.bias[0])
+    assert torch.equal(Y, Y2)
+    outs = [torch.empty_like(g) for g in grads]
+    rl.runlora_backward(rl.BWD1, c.dY, saved, W, c.A[0], c.B[0], *outs, workspace=ws)
+    assert all(torch.equal(a, b) for a, b in zip(outs, grads))
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+def test_gradients_against_differences(fp8):
+    """<dA, D> and <dB, D> against the change of <Y, G>: Y is linear in A and in B, so that a step of any size measures the derivative.  Y is
+    rounded (relative 2^-9 per element, independent), so the difference of two sums of N products is off by about 2^-9 sqrt(2 N) rms(Y) rms(G),
+    which four times over is the bound."""
+    c = Case("bf16", fp8, 200, 3, 256, 272, 16, "even", outliers=False)
+    rng = np.random.default_rng(5)
+    _, T = c.forward()
+    _, dA, dB = c.backward(T)
+    for which, grad in (("A", dA), ("B", dB)):
+        factor = getattr(c, which)
+        step = torch.from_numpy(rng.standard_normal(factor.shape)).to(c.td).cuda()
+        base, ys = factor.clone(), []
+        for sign in (1.0, -1.0):
+            factor.copy_(base + sign * step)
+            moved = to_f64(factor) - to_f64(base)
+            ys.append((to_f64(c.forward()[0]), moved))
+        factor.copy_(base)
+        got = ((ys[0][0] - ys[1][0]) * c.hdY).sum()
+        want = (to_f64(grad) * (ys[0][1] - ys[1][1])).sum()
+        y = np.sqrt((ys[0][0] ** 2).mean())
+        noise = 4 * 2.0 ** -9 * np.sqrt(2 * c.hdY.size) * y * np.sqrt((c.hdY ** 2).mean())
+        assert abs(got - want) <= noise + 4 * 2.0 ** -9 * abs(want), (which, got, want, noise)
+
+
+# ---- the quantisers ------------------------------------------------------------------------------------------------
+
+def _awkward(rows, cols, rng):
+    """Values over the whole range: zero blocks, denormals, exact ties, the largest values, blocks that end at 448 and just above."""
+    x = rng.standard_normal((rows, cols)) * 2.0 ** rng.integers(-30, 30, (rows, 1))
+    x[1 % rows] = 0.0
+    if rows > 4:
+        x[2, :] = 2.0 ** -133          # a bf16 denormal
+        x[3, ::2] = 448.0
+        x[4, ::3] = 450.0
+        x[4, 1] = 17.0                 # a tie between 16 and 18
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 16), (128, 128), (130, 272), (500, 1040)])
+def test_weight_quantiser(rows, cols, dtype):
+    rl = _rl()
+    rng = np.random.default_rng(rows + cols)
+    x = _awkward(rows, cols, rng)
+    if dtype == "f16":
+        x = np.clip(x, -60000, 60000)
+    src = torch.from_numpy(x).to(torch_dtype(dtype)).cuda()
+    W = rl.Fp8Weight.quantize(src)
+    want, exps = ref.round_blocks(to_f64(src), 128, 128)
+    scales = W.scales.cpu().numpy().astype(np.int64) - 127
+    assert np.array_equal(scales, exps)
+    assert np.array_equal(ref.weight_value(W.data.cpu().numpy(), W.scales.cpu().numpy()), want)
+
+
+def test_blocks_with_infinities_or_nan_become_nan():
+    rl = _rl()
+    src = torch.ones((256, 256), device="cuda")
+    src[3, 130] = float("inf")
+    src[200, 10] = float("nan")
+    W = rl.Fp8Weight.quantize(src)
+    v = ref.weight_value(W.data.cpu().numpy(), W.scales.cpu().numpy())
+    assert np.isnan(v[:128, 128:]).all() and np.isnan(v[128:, :128]).all() and (v[:128, :128] == 1).all() and (v[128:, 128:] == 1).all()
+
+
+@pytest.mark.parametrize("n", [1, 5, 70, 2050])
+def test_rows_are_rounded_as_defined(n):
+    """Through W = 1 the layer returns Q(X): e4m3 values times powers of two, which bf16 holds exactly."""
+    rl = _rl()
+    k = 272
+    x = _awkward(n, k, np.random.default_rng(n))
+    x[x != 0] = np.clip(np.abs(x[x != 0]), 2.0 ** -100, None) * np.sign(x[x != 0])   # (sums of products stay normal numbers)
+    X = torch.from_numpy(x).to(torch.bfloat16).cuda()
+    data = torch.zeros((1, k, k), dtype=torch.uint8, device="cuda")
+    data[0].fill_diagonal_(0x38)
+    W = rl.Fp8Weight(data, torch.full((1, 3, 3), 127, dtype=torch.uint8, device="cuda"), k, k)
+    Y = torch.empty((n, k), dtype=torch.bfloat16, device="cuda")
+    ends = torch.tensor([n], dtype=torch.int32, device="cuda")
+    ws = torch.empty(rl.runlora_experts_workspace_bytes(False, n, 1, k, k, 0, rl.RL_BF16, rl.RL_FP8_B128), dtype=torch.uint8, device="cuda")
+    rl.runlora_experts_forward(X, ends, W, None, None, Y, workspace=ws)
+    want, _ = ref.round_blocks(to_f64(X), 1, 128)
+    assert np.array_equal(to_f64(Y), want)
