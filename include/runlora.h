@@ -324,7 +324,7 @@ int runlora_fp8_quantize(const rl_tensor_t* src, rl_tensor_t* dst, const rl_opts
  *            (forward only) = [experts, o], dense; dropout_p must be 0.
  *   dX, dA, dB  overwritten; any may be NULL (skipped).
  * RL_F16 / RL_BF16; n >= 1; i, o, r multiples of 8 (i and o of 16 for an RL_FP8_B128 W); experts in [1, 65535]; leading dimensions up to
- * 4194304.  Sums run in a fixed order: the same call gives the same bits.
+ * 2097152.  Sums run in a fixed order: the same call gives the same bits.
  *
  * rl_stack_t: as rl_tensor_t, `experts` matrices `stride` elements apart (a multiple of 8, for RL_FP8_B128 of 16; inputs may have stride 0,
  * one matrix for all).  The scale bytes of an RL_FP8_B128 stack are dense, [experts][ceil(rows/128)][ceil(cols/128)]

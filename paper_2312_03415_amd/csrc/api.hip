@@ -283,7 +283,7 @@ int check_workspace(const Schedule& sch, const rl_opts_t* opts) {
 // ---- layers over an 8-bit weight, and over stacks of expert weights (grouped.hpp) ---------------------------
 namespace {
 
-constexpr int64_t kMaxLd = 1LL << 22;      // tiles are addressed by 32-bit offsets over 128 rows
+constexpr int64_t kMaxLd = 1LL << 21;      // tiles are addressed by 31-bit byte offsets over 256 rows
 constexpr int64_t kMaxExperts = 65535;
 
 int check_fp8(const rl_tensor_t* W, int64_t rows, int64_t cols) {

@@ -189,7 +189,8 @@ hipError_t launch(int dtype, bool f8, int al, int bl, int tile, const GroupedArg
 
 // ---- plans: functions of sizes alone, shared by the workspace query and the call ----------------------
 
-constexpr int64_t kFill = 512;  // workgroups that fill the chip, two to a compute unit
+constexpr int64_t kUnits = 256;  // compute units
+constexpr int64_t kFill = 512;   // workgroups that fill the chip, two to a compute unit
 
 // rows of an expert that gets its share
 int64_t share(const ExpertsDesc& d) { return ceil_div(d.n, d.experts < d.n ? d.experts : d.n); }
@@ -202,9 +203,10 @@ MainPlan main_plan(const ExpertsDesc& d, int64_t N, int64_t K, bool split) {
   MainPlan p;
   const int64_t rows = share(d);
   p.tile = rows <= 32 ? GT_32x128 : (rows <= 96 ? GT_64x128 : GT_128x128);
+  if (!split && rows > 160 && grouped_row_tiles(d.n, d.experts, 256, d.f8) * ceil_div(N, 256) >= 128 && (!d.f8 || K <= 128 * 128)) p.tile = GT_256x256;
   const GroupedTileInfo t = grouped_tile(p.tile);
   const int64_t tiles = grouped_row_tiles(d.n, d.experts, t.bm, d.f8) * ceil_div(N, t.bn), nk = ceil_div(K, d.f8 ? 128 : 64);
-  p.gx = (unsigned)tiles;
+  p.gx = (unsigned)(p.tile == GT_256x256 && tiles > kUnits ? kUnits : tiles);
   int64_t s = split ? kFill / tiles : 1;
   if (s > nk / 4) s = nk / 4;
   if (s < 1) s = 1;

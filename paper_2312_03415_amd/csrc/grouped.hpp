@@ -43,10 +43,10 @@ struct GroupedArgs {
 };
 
 // what a launch runs on
-enum GroupedTile { GT_32x128 = 0, GT_64x128, GT_128x128, GT_64x32, GT_64x64, GT_64x128T, GT_128x32, GT_128x64, GT_COUNT };
+enum GroupedTile { GT_32x128 = 0, GT_64x128, GT_128x128, GT_64x32, GT_64x64, GT_64x128T, GT_128x32, GT_128x64, GT_256x256, GT_COUNT };
 struct GroupedTileInfo { int bm, bn; };
 inline GroupedTileInfo grouped_tile(int t) {
-  static const GroupedTileInfo k[GT_COUNT] = {{32, 128}, {64, 128}, {128, 128}, {64, 32}, {64, 64}, {64, 128}, {128, 32}, {128, 64}};
+  static const GroupedTileInfo k[GT_COUNT] = {{32, 128}, {64, 128}, {128, 128}, {64, 32}, {64, 64}, {64, 128}, {128, 32}, {128, 64}, {256, 256}};
   return k[t];
 }
 

@@ -144,6 +144,46 @@ def test_fp16(n, experts, i, o, r, kind, fp8):
     check(Case("f16", fp8, n, experts, i, o, r, kind, bias=True))
 
 
+LARGE = [
+    # enough 256 x 256 tiles in both directions, several a compute unit: ragged rows and columns, K that ends inside a tile, long K
+    (2100, 1, 2320, 4112, 24, "even"),
+    (2600, 3, 2576, 3856, 40, "uneven"),
+    (3000, 5, 2320, 2832, 136, "rest"),
+    (3500, 2, 3088, 5136, 0, "uneven"),
+    (20000, 70, 528, 1040, 8, "even"),
+]
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+@pytest.mark.parametrize("n,experts,i,o,r,kind", LARGE)
+def test_large_tiles(n, experts, i, o, r, kind, fp8):
+    check(Case("f16" if experts == 3 else "bf16", fp8, n, experts, i, o, r, kind, bias=(n % 1000 != 0)))
+
+
+def test_large_tiles_give_the_same_bits_again_and_under_capture():
+    rl = _rl()
+    n = 2600
+    c = Case("bf16", True, n, 3, 2576, 3856, 40, "uneven")
+    ws, Y = c.workspace(False), torch.empty((n, 3856), dtype=c.td, device="cuda")
+    call = lambda: rl.runlora_experts_forward(c.X, c.ends, c.W, c.A, c.B, Y, workspace=ws, scale=1.5)
+    call()
+    torch.cuda.synchronize()
+    first = Y.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(4):
+        Y.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(Y, first)
+    c.ends_host = np.array([n, n, n])
+    c.ends.fill_(n)
+    graph.replay()
+    torch.cuda.synchronize()
+    close_all(("Y",), (Y,), c.want_forward(), "bf16")
+
+
 @pytest.mark.parametrize("n,experts,i,o,r,kind", [(20, 3, 136, 264, 8, "uneven"), (333, 3, 136, 264, 24, "uneven"), (150, 2, 1032, 648, 56, "rest")])
 def test_dense_widths_in_steps_of_eight(n, experts, i, o, r, kind):
     check(Case("bf16", False, n, experts, i, o, r, kind, bias=True))
