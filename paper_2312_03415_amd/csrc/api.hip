@@ -412,6 +412,7 @@ int experts_forward_impl(const rl_tensor_t* X, const int32_t* ends, const rl_sta
   ExpertsDesc d = experts_desc(n, W->experts, W->rows, o, r, X->dtype, W->dtype);
   set_weights(&d, W, A, B);
   d.ends = ends;
+  d.has_ends = ends != nullptr;
   d.X = X->data; d.ldx = X->ld;
   d.Y = Y->data; d.ldy = Y->ld;
   if (T) { d.T = T->data; d.ldt = T->ld; }
@@ -463,6 +464,7 @@ int experts_backward_impl(const rl_tensor_t* dY, const rl_tensor_t* X, const int
   ExpertsDesc d = experts_desc(n, E, i, o, r, dtype, W->dtype);
   set_weights(&d, W, A, B);
   d.ends = ends;
+  d.has_ends = ends != nullptr;
   d.dY = dY->data; d.lddy = dY->ld;
   if (X) { d.X = X->data; d.ldx = X->ld; }
   if (T) { d.T = T->data; d.ldt = T->ld; d.has_T = true; }
@@ -524,7 +526,14 @@ extern "C" int runlora_experts_backward(const rl_tensor_t* dY, const rl_tensor_t
 }
 extern "C" size_t runlora_experts_workspace_bytes(int backward, int64_t n, int64_t experts, int64_t i, int64_t o, int64_t r, int dtype, int w_dtype) {
   if (check_sizes(n, experts, i, o, r, dtype, w_dtype) != RL_OK) return 0;
-  return experts_workspace(experts_desc(n, experts, i, o, r, dtype, w_dtype), backward != 0);
+  ExpertsDesc d = experts_desc(n, experts, i, o, r, dtype, w_dtype);
+  size_t need = experts_workspace(d, backward != 0);
+  if (experts == 1) {  // a call may leave the ends out
+    d.has_ends = false;
+    const size_t b = experts_workspace(d, backward != 0);
+    need = b > need ? b : need;
+  }
+  return need;
 }
 
 extern "C" int runlora_fp8_quantize(const rl_tensor_t* src, rl_tensor_t* dst, const rl_opts_t* opts) {
@@ -1115,7 +1124,8 @@ extern "C" size_t runlora_workspace_bytes_w(int fwd, int bwd, int64_t n, int64_t
   if (dt < 0 || n < 1 || i < 1 || o < 1 || r < 1) return 0;
   if (w_dtype == RL_FP8_B128) {
     if (check_sizes(n, 1, i, o, r, dtype, w_dtype) != RL_OK) return 0;
-    const ExpertsDesc d = experts_desc(n, 1, i, o, r, dtype, w_dtype);
+    ExpertsDesc d = experts_desc(n, 1, i, o, r, dtype, w_dtype);
+    d.has_ends = false;
     const size_t f = fwd == RL_FWD1 || fwd == RL_FWD3 ? experts_workspace(d, false) : 0, b = bwd == RL_BWD1 ? experts_workspace(d, true) : 0;
     return f > b ? f : b;
   }

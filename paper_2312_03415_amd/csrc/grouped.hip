@@ -68,16 +68,26 @@ struct FewArgs {
   const int32_t* ends;
   int experts, n, K, N, R, slices, splits;
   float scale;
+  uint8_t *q, *qs;  // e4m3 W: X rounded
+  int64_t ldq, ldqs;
+  int qx, qy;       // its workgroups
 };
 
-// Few rows: X A in slices of K.  A workgroup takes one row and one slice; R / 8 threads side by side take eight columns of A each.
+// Few rows, first launch: X rounded to e4m3 (workgroups [0, qx qy), where W is e4m3) and X A in slices of K (the others: one row and one slice
+// each, R / 8 threads side by side for eight columns of A each).
 template <typename T>
-__global__ __launch_bounds__(kThreads) void few_rank_kernel(FewArgs g) {
-  __shared__ float sum[kThreads][8];
-  const int row = (int)blockIdx.x, e = expert_of(g.ends, g.experts, row, threadIdx.x & 63);
+__global__ __launch_bounds__(kThreads) void few_prepare_kernel(FewArgs g) {
+  __shared__ union { float sum[kThreads][9]; uint8_t sc[4][4]; } sh;  // (rows of nine: columns of eight would share banks)
+  int bx = (int)blockIdx.x;
+  if (bx < g.qx * g.qy) {
+    fp8_rows_tile<T, 1>(static_cast<const T*>(g.X), g.ldx, g.n, g.K, g.q, g.ldq, g.qs, g.ldqs, bx % g.qx, bx / g.qx, sh.sc);
+    return;
+  }
+  bx -= g.qx * g.qy;
+  const int row = bx % g.n, slice = bx / g.n, e = expert_of(g.ends, g.experts, row, threadIdx.x & 63);
   if (e >= g.experts) return;
   const int cg = g.R / 8, kl = kThreads / cg, c = threadIdx.x % cg, k0 = threadIdx.x / cg;
-  const int each = (g.K / 8 + g.slices - 1) / g.slices * 8, lo = (int)blockIdx.y * each, hi = lo + each < g.K ? lo + each : g.K;
+  const int each = (g.K / 8 + g.slices - 1) / g.slices * 8, lo = slice * each, hi = lo + each < g.K ? lo + each : g.K;
   const T* const x = static_cast<const T*>(g.X) + (int64_t)row * g.ldx;
   const T* const a = static_cast<const T*>(g.A) + e * g.sa + c * 8;
   float acc[8];
@@ -94,54 +104,90 @@ __global__ __launch_bounds__(kThreads) void few_rank_kernel(FewArgs g) {
     }
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j) sum[threadIdx.x][j] = acc[j];
-  __syncthreads();
-  if ((int)threadIdx.x < g.R) {
-    float s = 0.f;
-    for (int k = 0; k < kl; ++k) s += sum[k * cg + threadIdx.x / 8][threadIdx.x & 7];
-    g.part_t[((int64_t)blockIdx.y * g.n + row) * g.R + threadIdx.x] = s;
+  for (int j = 0; j < 8; ++j) sh.sum[threadIdx.x][j] = acc[j];
+  // the kl sums of a column, eight at a time
+  for (int left = kl; left > 1; left = (left + 7) / 8) {
+    __syncthreads();
+    const int next = (left + 7) / 8;
+    float s[8];
+    if (k0 < next) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = 0.f;
+      for (int k = 8 * k0; k < 8 * k0 + 8 && k < left; ++k)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] += sh.sum[k * cg + c][j];
+    }
+    __syncthreads();
+    if (k0 < next)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sh.sum[threadIdx.x][j] = s[j];
   }
+  __syncthreads();
+  if ((int)threadIdx.x < g.R) g.part_t[((int64_t)slice * g.n + row) * g.R + threadIdx.x] = sh.sum[threadIdx.x / 8][threadIdx.x & 7];
 }
 
-// Few rows: Y = the slices of X W + T B + bias, T = s * the slices of X A rounded to the storage type.  A workgroup takes 512 columns of a row.
+// Few rows, last launch: Y = the slices of X W + T B + bias, T = s * the slices of X A rounded to the storage type.  A workgroup takes 512
+// columns of a row; slices and rows of B are dealt out to its four waves, so that every trip to memory is on its way at once.
+// Bound by latency: a wave a workgroup, walking everything in turn, took 8.8 us for 1 x 4096 -> 4096 r 16 and 6.6 for 48 x 4096 ->
+// 11008 r 32.
 template <typename T>
-__global__ __launch_bounds__(64) void few_finish_kernel(FewArgs g) {
-  __shared__ float t[256];
-  const int row = (int)blockIdx.y, lane = threadIdx.x, e = expert_of(g.ends, g.experts, row, lane);
+__global__ __launch_bounds__(kThreads) void few_finish_kernel(FewArgs g) {
+  constexpr int AHEAD = 4;  // rows of B that a wave requests ahead of T
+  __shared__ float part[kThreads], t[256];
+  __shared__ f32x4 sums[3][2][64];
+  const int row = (int)blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, e = expert_of(g.ends, g.experts, row, lane);
   const int col = ((int)blockIdx.x * 64 + lane) * 8;
-  const bool rest = e >= g.experts;
-  for (int k = lane; k < g.R; k += 64) {
-    float s = 0.f;
-    if (!rest)
-      for (int j = 0; j < g.slices; ++j) s += g.part_t[((int64_t)j * g.n + row) * g.R + k];
-    const T r = from_f32<T>(s * g.scale);
-    t[k] = (float)r;
-    if (g.T != nullptr && blockIdx.x == 0) static_cast<T*>(g.T)[(int64_t)row * g.ldt + k] = r;
-  }
-  __syncthreads();
-  if (col >= g.N) return;
+  const bool rest = e >= g.experts, ok = col < g.N;
+  const T* const bp = static_cast<const T*>(g.B) + (rest ? 0 : e * g.sb) + (ok ? col : 0);
+  v4 ahead[AHEAD];
+#pragma unroll
+  for (int j = 0; j < AHEAD; ++j) ahead[j] = wave + 4 * j < g.R ? *reinterpret_cast<const v4*>(bp + (int64_t)(wave + 4 * j) * g.ldb) : v4{0, 0, 0, 0};
   f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
-  const float* p = g.part + (int64_t)row * g.N + col;
+  const float* p = g.part + (int64_t)row * g.N + (ok ? col : 0);
 #pragma unroll 4
-  for (int j = 0; j < g.splits; ++j) {
+  for (int j = wave; j < g.splits; j += 4) {
     a += *reinterpret_cast<const f32x4*>(p + (int64_t)j * g.n * g.N);
     b += *reinterpret_cast<const f32x4*>(p + (int64_t)j * g.n * g.N + 4);
   }
-  if (!rest) {
-    const T* const bp = static_cast<const T*>(g.B) + e * g.sb + col;
+  if (g.R > 0) {
+    const int groups = kThreads / g.R, k = tid % g.R, q = tid / g.R;
+    float s = 0.f;
+    if (q < groups && !rest) {
 #pragma unroll 8
-    for (int k = 0; k < g.R; ++k) {
-      const v4 v = *reinterpret_cast<const v4*>(bp + (int64_t)k * g.ldb);
+      for (int j = q; j < g.slices; j += groups) s += g.part_t[((int64_t)j * g.n + row) * g.R + k];
+    }
+    part[tid] = s;
+    __syncthreads();
+    if (tid < g.R) {
+      for (int j = 1; j < groups; ++j) s += part[j * g.R + tid];
+      const T r = from_f32<T>(s * g.scale);
+      t[tid] = (float)r;
+      if (g.T != nullptr && blockIdx.x == 0) static_cast<T*>(g.T)[(int64_t)row * g.ldt + tid] = r;
+    }
+    __syncthreads();
+    auto add = [&](const v4& v, float x) {
       const T* const w = reinterpret_cast<const T*>(&v);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { a[j] += t[k] * (float)w[j]; b[j] += t[k] * (float)w[4 + j]; }
-    }
-    if (g.bias != nullptr) {
-      const v4 v = *reinterpret_cast<const v4*>(static_cast<const T*>(g.bias) + (int64_t)e * g.N + col);
-      const T* const w = reinterpret_cast<const T*>(&v);
+      for (int j = 0; j < 4; ++j) { a[j] += x * (float)w[j]; b[j] += x * (float)w[4 + j]; }
+    };
+    if (!rest) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { a[j] += (float)w[j]; b[j] += (float)w[4 + j]; }
+      for (int j = 0; j < AHEAD; ++j)
+        if (wave + 4 * j < g.R) add(ahead[j], t[wave + 4 * j]);
+#pragma unroll 4
+      for (int kk = wave + 4 * AHEAD; kk < g.R; kk += 4) add(*reinterpret_cast<const v4*>(bp + (int64_t)kk * g.ldb), t[kk]);
     }
+  }
+  if (wave > 0) { sums[wave - 1][0][lane] = a; sums[wave - 1][1][lane] = b; }
+  __syncthreads();
+  if (wave > 0 || !ok) return;
+#pragma unroll
+  for (int w = 0; w < 3; ++w) { a += sums[w][0][lane]; b += sums[w][1][lane]; }
+  if (g.bias != nullptr && !rest) {
+    const v4 v = *reinterpret_cast<const v4*>(static_cast<const T*>(g.bias) + (int64_t)e * g.N + col);
+    const T* const w = reinterpret_cast<const T*>(&v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { a[j] += (float)w[j]; b[j] += (float)w[4 + j]; }
   }
   T o[8];
 #pragma unroll
@@ -169,16 +215,18 @@ struct Slices {
   }
 };
 template <typename T>
-struct FewRank {
+struct FewPrepare {
   static hipError_t run(const FewArgs& g, hipStream_t s) {
-    launch_timed(few_rank_kernel<T>, dim3((unsigned)g.n, (unsigned)g.slices), dim3(kThreads), 0, s, g);
+    const unsigned grid = (unsigned)(g.qx * g.qy + (g.R > 0 ? g.n * g.slices : 0));
+    if (grid == 0) return hipSuccess;
+    launch_timed(few_prepare_kernel<T>, dim3(grid), dim3(kThreads), 0, s, g);
     return hipGetLastError();
   }
 };
 template <typename T>
 struct FewFinish {
   static hipError_t run(const FewArgs& g, hipStream_t s) {
-    launch_timed(few_finish_kernel<T>, dim3((unsigned)ceil_div(g.N, 512), (unsigned)g.n), dim3(64), 0, s, g);
+    launch_timed(few_finish_kernel<T>, dim3((unsigned)ceil_div(g.N, 512), (unsigned)g.n), dim3(kThreads), 0, s, g);
     return hipGetLastError();
   }
 };
@@ -203,9 +251,9 @@ MainPlan main_plan(const ExpertsDesc& d, int64_t N, int64_t K, bool split) {
   MainPlan p;
   const int64_t rows = share(d);
   p.tile = rows <= 32 ? GT_32x128 : (rows <= 96 ? GT_64x128 : GT_128x128);
-  if (!split && rows > 160 && grouped_row_tiles(d.n, d.experts, 256, d.f8) * ceil_div(N, 256) >= 128 && (!d.f8 || K <= 128 * 128)) p.tile = GT_256x256;
+  if (!split && rows > 160 && grouped_row_tiles(d.n, d.experts, d.has_ends, 256, d.f8) * ceil_div(N, 256) >= 128 && (!d.f8 || K <= 128 * 128)) p.tile = GT_256x256;
   const GroupedTileInfo t = grouped_tile(p.tile);
-  const int64_t tiles = grouped_row_tiles(d.n, d.experts, t.bm, d.f8) * ceil_div(N, t.bn), nk = ceil_div(K, d.f8 ? 128 : 64);
+  const int64_t tiles = grouped_row_tiles(d.n, d.experts, d.has_ends, t.bm, d.f8) * ceil_div(N, t.bn), nk = ceil_div(K, d.f8 ? 128 : 64);
   p.gx = (unsigned)(p.tile == GT_256x256 && tiles > kUnits ? kUnits : tiles);
   int64_t s = split ? kFill / tiles : 1;
   if (s > nk / 4) s = nk / 4;
@@ -219,15 +267,15 @@ MainPlan main_plan(const ExpertsDesc& d, int64_t N, int64_t K, bool split) {
 struct RankPlan { int tile, splits, per; unsigned gx; };
 RankPlan rank_plan(const ExpertsDesc& d, int64_t K) {
   RankPlan p;
-  p.tile = d.r <= 32 ? GT_64x32 : (d.r <= 64 ? GT_64x64 : GT_64x128T);
+  p.tile = d.r <= 32 ? GT_64x32 : (d.r <= 64 ? GT_64x64 : (d.n >= 4096 ? GT_128x128 : GT_64x128T));
   const GroupedTileInfo t = grouped_tile(p.tile);
-  const int64_t tiles = grouped_row_tiles(d.n, d.experts, t.bm, false) * ceil_div(d.r, t.bn), nk = ceil_div(K, 64);
+  const int64_t tiles = grouped_row_tiles(d.n, d.experts, d.has_ends, t.bm, false) * ceil_div(d.r, t.bn), nk = ceil_div(K, 128);  // (slices end on a scale block)
   p.gx = (unsigned)tiles;
   int64_t s = kFill / tiles;
-  if (s > nk / 4) s = nk / 4;
+  if (s > nk / 2) s = nk / 2;
   if (s < 1) s = 1;
-  p.per = (int)ceil_div(nk, s);
-  p.splits = (int)ceil_div(nk, p.per);
+  p.per = 2 * (int)ceil_div(nk, s);
+  p.splits = (int)ceil_div(nk * 2, p.per);
   return p;
 }
 size_t rank_bytes(const ExpertsDesc& d, const RankPlan& p) { return p.splits > 1 ? (size_t)p.splits * d.n * d.r * 4 : 0; }
@@ -311,7 +359,9 @@ GroupedArgs rows_args(const ExpertsDesc& d) {
 }
 
 // T [n, r] = s A_rows F:  F = A [i, r] (X's rows) or B [r, o] read as its transpose (dY's rows)
-hipError_t rank_run(const ExpertsDesc& d, const void* rows, int64_t ldrows, int64_t K, bool backward, void* out, int64_t ldo, float* part, hipStream_t stream) {
+// `round`: the rows are also rounded to e4m3 into w.q and w.s
+hipError_t rank_run(const ExpertsDesc& d, const Space& w, const void* rows, int64_t ldrows, int64_t K, bool backward, bool round, void* out, int64_t ldo, hipStream_t stream) {
+  float* const part = w.part;
   const RankPlan p = rank_plan(d, K);
   GroupedArgs a = rows_args(d);
   a.A = rows; a.lda = ldrows;
@@ -321,7 +371,14 @@ hipError_t rank_run(const ExpertsDesc& d, const void* rows, int64_t ldrows, int6
   a.alpha = d.scale;
   a.splits = p.splits; a.tiles_per_split = p.per;
   a.partial = p.splits > 1 ? part : nullptr;
-  hipError_t e = launch(d.dtype, false, 0, backward ? 1 : 0, p.tile, a, dim3(p.gx, (unsigned)p.splits), stream);
+  const dim3 grid(p.gx, (unsigned)p.splits);
+  hipError_t e;
+  if (round) {
+    a.Q = w.q; a.ldq = w.ldq; a.QS = w.s; a.ldqs = w.lds;
+    e = d.dtype == DT_BF16 ? grouped_rows_launch_bf16(backward ? 1 : 0, p.tile, a, grid, stream) : grouped_rows_launch_f16(backward ? 1 : 0, p.tile, a, grid, stream);
+  } else {
+    e = launch(d.dtype, false, 0, backward ? 1 : 0, p.tile, a, grid, stream);
+  }
   if (e == hipSuccess && p.splits > 1) e = by_type<Slices>(d.dtype, (const float*)part, p.splits, d.n, d.n, d.r, d.scale, out, ldo, (int64_t)0, stream);
   return e;
 }
@@ -347,9 +404,9 @@ hipError_t grad_run(const ExpertsDesc& d, bool of_A, const void* T, int64_t ldt,
   return e;
 }
 
-// the large product: rows (rounded first where W is e4m3) times W or its transpose, the adapter's product TA TB^T and the bias behind it
+// the large product: rows (rounded first where W is e4m3 and they are not yet) times W or its transpose, the adapter's product TA TB^T and the bias behind it
 hipError_t main_run(const ExpertsDesc& d, bool backward, const Space& w, const void* TA, int64_t ldta, const void* TB, int64_t ldtb, int64_t stb, void* out, int64_t ldo,
-                    bool slices, hipStream_t stream) {
+                    bool slices, bool rounded, hipStream_t stream) {
   const int64_t K = backward ? d.o : d.i, N = backward ? d.i : d.o;
   const MainPlan p = main_plan(d, N, K, slices);
   GroupedArgs a = rows_args(d);
@@ -357,8 +414,10 @@ hipError_t main_run(const ExpertsDesc& d, bool backward, const Space& w, const v
   a.lda = backward ? d.lddy : d.ldx;
   a.B = d.W; a.ldb = d.ldw; a.sb = d.sw;
   if (d.f8) {
-    hipError_t e = fp8_rows_run(d.dtype, a.A, a.lda, d.n, K, w.q, w.ldq, w.s, w.lds, stream);
-    if (e != hipSuccess) return e;
+    if (!rounded) {
+      hipError_t e = fp8_rows_run(d.dtype, a.A, a.lda, d.n, K, w.q, w.ldq, w.s, w.lds, stream);
+      if (e != hipSuccess) return e;
+    }
     a.A = w.q; a.lda = w.ldq;
     a.SA = w.s; a.ldsa = w.lds;
     a.SB = d.w_scales; a.ssb = d.s_scales;
@@ -393,17 +452,22 @@ hipError_t experts_forward(const ExpertsDesc& d, void* workspace, hipStream_t st
     f.n = (int)d.n; f.K = (int)d.i; f.N = (int)d.o; f.R = (int)d.r;
     f.slices = w.slices; f.splits = main_plan(d, d.o, d.i, true).splits;
     f.scale = d.scale;
-    if (d.r > 0 && (e = by_type<FewRank>(d.dtype, f, stream)) != hipSuccess) return e;
-    if ((e = main_run(d, false, w, nullptr, 0, nullptr, 0, 0, nullptr, 0, true, stream)) != hipSuccess) return e;
+    if (d.f8) {
+      f.q = w.q; f.qs = w.s; f.ldq = w.ldq; f.ldqs = w.lds;
+      f.qx = (int)ceil_div(d.n, 4);
+      f.qy = (int)ceil_div(w.ldq, 512);
+    }
+    if ((e = by_type<FewPrepare>(d.dtype, f, stream)) != hipSuccess) return e;
+    if ((e = main_run(d, false, w, nullptr, 0, nullptr, 0, 0, nullptr, 0, true, true, stream)) != hipSuccess) return e;
     return by_type<FewFinish>(d.dtype, f, stream);
   }
   void* T = d.T ? d.T : w.T;
   const int64_t ldt = d.T ? d.ldt : d.r;
   if (d.r > 0) {
     if ((e = by_type<Turn>(d.dtype, d.B, d.ldb, d.sb, w.turned, d.r, d.o, d.experts, stream)) != hipSuccess) return e;
-    if ((e = rank_run(d, d.X, d.ldx, d.i, false, T, ldt, w.part, stream)) != hipSuccess) return e;
+    if ((e = rank_run(d, w, d.X, d.ldx, d.i, false, d.f8, T, ldt, stream)) != hipSuccess) return e;
   }
-  return main_run(d, false, w, T, ldt, w.turned, d.r, d.o * d.r, d.Y, d.ldy, false, stream);
+  return main_run(d, false, w, T, ldt, w.turned, d.r, d.o * d.r, d.Y, d.ldy, false, d.r > 0, stream);
 }
 
 hipError_t experts_backward(const ExpertsDesc& d, void* workspace, hipStream_t stream) {
@@ -412,16 +476,16 @@ hipError_t experts_backward(const ExpertsDesc& d, void* workspace, hipStream_t s
   const void* T = d.T;
   int64_t ldt = d.ldt;
   if (d.r > 0) {
-    if ((d.dX || d.dA) && (e = rank_run(d, d.dY, d.lddy, d.o, true, w.Z, d.r, w.part, stream)) != hipSuccess) return e;
+    if ((d.dX || d.dA) && (e = rank_run(d, w, d.dY, d.lddy, d.o, true, d.f8 && d.dX != nullptr, w.Z, d.r, stream)) != hipSuccess) return e;
     if (d.dB && !d.has_T) {
-      if ((e = rank_run(d, d.X, d.ldx, d.i, false, w.T, d.r, w.part, stream)) != hipSuccess) return e;
+      if ((e = rank_run(d, w, d.X, d.ldx, d.i, false, false, w.T, d.r, stream)) != hipSuccess) return e;
       T = w.T;
       ldt = d.r;
     }
     if (d.dA && (e = grad_run(d, true, T, ldt, w.Z, w.part, stream)) != hipSuccess) return e;
     if (d.dB && (e = grad_run(d, false, T, ldt, w.Z, w.part, stream)) != hipSuccess) return e;
   }
-  if (d.dX) return main_run(d, true, w, w.Z, d.r, d.A, d.lda, d.sa, d.dX, d.lddx, false, stream);
+  if (d.dX) return main_run(d, true, w, w.Z, d.r, d.A, d.lda, d.sa, d.dX, d.lddx, false, d.r > 0, stream);
   return hipSuccess;
 }
 

@@ -40,6 +40,9 @@ struct GroupedArgs {
   int n, M, N, K, R;
   int splits, tiles_per_split;
   float alpha;  // C = alpha (A B) + TA TB + bias
+  // builds that round A on the way (AL = 0, 16-bit): e4m3 bytes [n][ldq], zeros behind K, and scale bytes [ldq / 128][ldqs]
+  uint8_t *Q, *QS;
+  int64_t ldq, ldqs;
 };
 
 // what a launch runs on
@@ -50,12 +53,16 @@ inline GroupedTileInfo grouped_tile(int t) {
   return k[t];
 }
 
-// largest number of row tiles that n rows of up to `experts` groups (and the rest behind them) can make
-inline int64_t grouped_row_tiles(int64_t n, int64_t experts, int bm, bool f8) {
+// largest number of row tiles that n rows of up to `experts` groups (and the rest behind them) can make; one group without ends: all rows
+inline int64_t grouped_row_tiles(int64_t n, int64_t experts, bool ends, int bm, bool f8) {
+  if (!ends) return (n + bm - 1) / bm;
   const int64_t groups = (experts + 1 < n ? experts + 1 : n);
   return (n + groups * (bm - 1 + (f8 ? 3 : 0))) / bm;  // (an e4m3 group's first tile starts up to three rows early)
 }
 
+// rows: A is rounded on the way (GroupedArgs::Q)
+hipError_t grouped_rows_launch_bf16(int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s);
+hipError_t grouped_rows_launch_f16(int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s);
 hipError_t grouped_launch_bf16(bool f8, int al, int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s);
 hipError_t grouped_launch_f16(bool f8, int al, int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s);
 
@@ -65,6 +72,7 @@ struct ExpertsDesc {
   bool f8 = false;
   int64_t n = 0, experts = 1, i = 0, o = 0, r = 0;
   const int32_t* ends = nullptr;
+  bool has_ends = true;  // false: one expert, all rows its (sizes are asked for without ends)
   const void *W = nullptr, *A = nullptr, *B = nullptr, *bias = nullptr;
   int64_t ldw = 0, sw = 0, lda = 0, sa = 0, ldb = 0, sb = 0;
   const uint8_t* w_scales = nullptr;

@@ -15,6 +15,7 @@
 #include <type_traits>
 #include <utility>
 
+#include "fp8.hpp"
 #include "gemm_mt.hpp"
 #include "grouped.hpp"
 
@@ -105,8 +106,13 @@ __device__ __forceinline__ int grouped_swz(int q) {
   else return mt_swz<BX>(q);
 }
 
-template <typename T, bool F8, int AL, int BL, int BM, int BN, int WM, int NS>
+// ROWS: A, which a rank-r product reads once (X in T = s X A, dY in Z = s dY B^T), is rounded to e4m3 for the large product on the way: a
+// thread takes the 16-byte chunks of the tile that it loaded, keeps those of every other K tile, and rounds both halves of a block
+// of 128 columns together, the eight lanes of a row agreeing on its largest magnitude.  The pass over A that rounding would take is saved:
+// dY of 8192 x 11008 r 32 54 + 56 us in two, of 16384 x 11008 r 128 126 + 186.
+template <typename T, bool F8, int AL, int BL, int BM, int BN, int WM, int NS, bool ROWS = false>
 __device__ __forceinline__ void grouped_mt_body(const GroupedArgs& g, const int bx, const int by) {
+  static_assert(!ROWS || (!F8 && AL == 0), "a 16-bit A by rows");
   using P = GroupedTileShape<F8, AL, BL, BM, BN, WM, NS>;
   constexpr int EB = P::EB, KE = P::KE, TM = P::TM, TN = P::TN;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem_raw[];
@@ -287,6 +293,7 @@ __device__ __forceinline__ void grouped_mt_body(const GroupedArgs& g, const int 
 
   if (u0 < u1) {
     for (int s = 0; s < NS - 1; ++s) issue_tile(s);
+    [[maybe_unused]] i32x4 kept[P::IA];  // ROWS: this thread's chunks of the even K tile of a pair (u0 is even)
     [[maybe_unused]] int wscale = 0;  // scale bytes of W for 64 K tiles, one per lane
     int st = 0, fill = NS - 1;
     for (int u = u0; u < u1; ++u) {
@@ -322,6 +329,11 @@ __device__ __forceinline__ void grouped_mt_body(const GroupedArgs& g, const int 
         else if constexpr (TM == 2) asm volatile("ds_read_u16 %0, %1" : "=v"(sa) : "v"(addr));
         else asm volatile("ds_read_b32 %0, %1" : "=v"(sa) : "v"(addr));
       }
+      [[maybe_unused]] i32x4 chunk[P::IA];
+      if constexpr (ROWS) {
+        const uint32_t at = lds_base + soff + (uint32_t)(wave * (P::IA * 1024) + lane * 16);
+        static_for<P::IA>([&](auto j) { auto& c = chunk[j]; const uint32_t a = at; asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(c) : "v"(a), "i"(decltype(j)::value * 1024)); });
+      }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       static_for<2>([&](auto h) {
         static_for<TN>([&](auto b) { fb[b][h].touch(); });
@@ -344,6 +356,47 @@ __device__ __forceinline__ void grouped_mt_body(const GroupedArgs& g, const int 
             acc[a][b] = Mma16<T>::mma(fb[b][h].get(), fa[a][h].get(), acc[a][b]);
           });
         });
+      }
+      if constexpr (ROWS) {
+        static_for<P::IA>([&](auto j) { auto& c = chunk[j]; asm volatile("" : "+v"(c)); });
+        const bool odd = (u & 1) != 0;
+        if (odd || u + 1 == u1) {  // the block's second half, or none of it lies inside K
+#pragma unroll
+          for (int j = 0; j < P::IA; ++j) {
+            const i32x4 none = {0, 0, 0, 0}, half[2] = {odd ? kept[j] : chunk[j], odd ? chunk[j] : none};
+            float v[16];
+            uint32_t top = 0;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              v[k] = (float)reinterpret_cast<const T*>(&half[k >> 3])[k & 7];
+              const uint32_t bits = __float_as_uint(v[k]) & 0x7FFFFFFFu;
+              top = top > bits ? top : bits;
+            }
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) {
+              const uint32_t other = (uint32_t)__shfl_xor((int)top, d);
+              top = top > other ? top : other;
+            }
+            uint32_t byte;
+            float mul;
+            bool nan;
+            fp8_block_scale(top, &byte, &mul, &nan);
+            const int p = (wave * P::IA + j) * 64 + lane, row = p >> 3, m = m0 + row, kb = u >> 1;
+            const int col = kb * 128 + (((p & 7) ^ ((row >> 1) & 7)) << 3);
+            if (n0 == 0 && m >= gt.lo && m < gt.hi) {
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                i32x2 out = {fp8_pack4(v[8 * h] * mul, v[8 * h + 1] * mul, v[8 * h + 2] * mul, v[8 * h + 3] * mul),
+                             fp8_pack4(v[8 * h + 4] * mul, v[8 * h + 5] * mul, v[8 * h + 6] * mul, v[8 * h + 7] * mul)};
+                if (nan) out = i32x2{0x7F7F7F7F, 0x7F7F7F7F};
+                *reinterpret_cast<i32x2*>(g.Q + (int64_t)m * g.ldq + col + 64 * h) = out;
+              }
+              if ((lane & 7) == 0) g.QS[(int64_t)kb * g.ldqs + m] = (uint8_t)byte;
+            }
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < P::IA; ++j) kept[j] = chunk[j];
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -428,9 +481,9 @@ __device__ __forceinline__ void grouped_mt_body(const GroupedArgs& g, const int 
   }
 }
 
-template <typename T, bool F8, int AL, int BL, int BM, int BN, int WM, int NS>
+template <typename T, bool F8, int AL, int BL, int BM, int BN, int WM, int NS, bool ROWS>
 __global__ __launch_bounds__(256, 2) void grouped_mt_kernel(GroupedArgs g) {
-  grouped_mt_body<T, F8, AL, BL, BM, BN, WM, NS>(g, (int)blockIdx.x, (int)blockIdx.y);
+  grouped_mt_body<T, F8, AL, BL, BM, BN, WM, NS, ROWS>(g, (int)blockIdx.x, (int)blockIdx.y);
 }
 
 }  // namespace rl
