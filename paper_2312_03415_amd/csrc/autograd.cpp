@@ -8,7 +8,10 @@
 // r 64 196 -> 114, 1237 x 2056 -> 5464 197 -> 122.  Likewise VeRA (448 x 768 -> 768 r 128
 // 196 -> 109, 623 x 4352 -> 4096 r 64 200 -> 117) and DoRA (765 x 1280 -> 7328 r 64 216 -> 135).
 //
-// lora(...), vera(...) and dora(...) return None where their node does not apply, and the caller then takes the Python node: tensor subclasses, torch
+// ExpertsNode is the same for RunLoRAExpertsFunction and RunLoRAFp8Function (999 rows of 12 experts 1032 -> 2744 r 8, forward +
+// backward: 168 us a pass with the Python node, 86 of them the GPU's).
+//
+// lora(...), vera(...), dora(...) and experts(...) return None where their node does not apply, and the caller then takes the Python node: tensor subclasses, torch
 // function / dispatch modes, functorch transforms and tracing (all of which have to see a Python-level function), devices
 // other than the current GPU, and operands that only the Python path's checks describe properly.  Forward-mode gradients are
 // refused by either node, saved-tensor hooks apply to both (the same tensors are saved in the same order).
@@ -41,6 +44,9 @@ decltype(&runlora_vera_workspace_bytes) p_vera_workspace_bytes = nullptr;
 decltype(&runlora_dora_forward) p_dora_forward = nullptr;
 decltype(&runlora_dora_backward) p_dora_backward = nullptr;
 decltype(&runlora_dora_workspace_bytes) p_dora_workspace_bytes = nullptr;
+decltype(&runlora_experts_forward) p_experts_forward = nullptr;
+decltype(&runlora_experts_backward) p_experts_backward = nullptr;
+decltype(&runlora_experts_workspace_bytes) p_experts_workspace_bytes = nullptr;
 PyObject* g_check = nullptr;
 
 void check(int rc) {
@@ -337,6 +343,80 @@ struct DoRANode : public torch::autograd::Function<DoRANode> {
   }
 };
 
+// a stack of matrices (or one): what the forward checked is checked again, as in saved_desc
+rl_stack_t stack_desc(const at::Tensor& t, const at::Tensor& x, int code, int64_t cols = -1, const at::Tensor& scales = at::Tensor()) {
+  TORCH_CHECK_VALUE((t.dim() == 2 || t.dim() == 3) && t.stride(-1) == 1, "expected a matrix or a stack of matrices with contiguous rows");
+  TORCH_CHECK_VALUE(t.device() == x.device(), "a saved tensor came back on another device: ", t.device(), ", not ", x.device());
+  const bool many = t.dim() == 3;
+  const bool fp8 = scales.defined();
+  if (fp8)
+    TORCH_CHECK_VALUE(scales.device() == x.device() && scales.is_contiguous() && scales.element_size() == 1 && t.element_size() == 1,
+                      "an 8-bit weight came back with other bytes or scales");
+  return rl_stack_t{t.data_ptr(), many ? t.size(0) : 1, t.size(-2), cols < 0 ? t.size(-1) : cols, t.stride(-2), many ? t.stride(0) : 0,
+                    fp8 ? (int32_t)RL_FP8_B128 : code, fp8 ? scales.data_ptr() : nullptr, fp8 ? 128 : 0};
+}
+
+const int32_t* ends_of(const at::Tensor& ends, int64_t experts, const at::Tensor& x) {
+  if (!ends.defined()) return nullptr;
+  TORCH_CHECK_VALUE(ends.device() == x.device() && ends.dim() == 1 && ends.numel() == experts && ends.scalar_type() == at::kInt && ends.stride(0) == 1,
+                    "ends must be a dense int32 vector with one element per expert");
+  return ends.data_ptr<int32_t>();
+}
+
+// W: the stack [E, i, o] (or a matrix, one expert) in x's type, or the bytes of an 8-bit weight with `scales`; ends undefined: one expert
+struct ExpertsNode : public torch::autograd::Function<ExpertsNode> {
+  static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& A, const at::Tensor& B, const at::Tensor& W,
+                            const std::optional<at::Tensor>& scales, const std::optional<at::Tensor>& ends, const std::optional<at::Tensor>& bias,
+                            double scale, int64_t o) {
+    const int code = dtype_code(x.scalar_type());
+    const at::Tensor s = scales.has_value() ? *scales : at::Tensor(), e = ends.has_value() ? *ends : at::Tensor();
+    const rl_stack_t dw = stack_desc(W, x, code, o, s), da = stack_desc(A, x, code), db = stack_desc(B, x, code);
+    const at::Tensor x2 = rows(x, dw.rows);
+    const int64_t n = x2.size(0), r = da.cols;
+    at::Tensor y = at::empty({n, o}, x.options());
+    const at::Tensor T = at::empty({n, r}, x.options());
+    const at::Tensor ws = scratch(p_experts_workspace_bytes(0, n, dw.experts, dw.rows, o, r, code, dw.dtype), x);
+    const rl_opts_t opts = options(x, ws, bias, scale);
+    const rl_tensor_t dx = desc(x2, code);
+    rl_tensor_t dy = desc(y, code), dt = desc(T, code);
+    check(p_experts_forward(&dx, ends_of(e, dw.experts, x), &dw, &da, &db, &dy, &dt, &opts));
+    ctx->save_for_backward({x2, A, B, W, s, e});
+    ctx->saved_data["T"] = T;
+    ctx->saved_data["scale"] = scale;
+    ctx->saved_data["o"] = o;
+    ctx->saved_data["x_shape"] = x.sizes().vec();
+    return shaped(y, x);
+  }
+
+  static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+    const auto vars = ctx->get_saved_variables();
+    TORCH_CHECK_VALUE(vars[0].is_cuda(), "the saved input came back on ", vars[0].device());
+    const at::Tensor &A = vars[1], &B = vars[2];
+    const int64_t o = ctx->saved_data["o"].toInt();
+    const rl_stack_t dw = stack_desc(vars[3], vars[0], dtype_code(vars[3].scalar_type()), o, vars[4]), da = stack_desc(A, vars[0], dtype_code(A.scalar_type())),
+                     db = stack_desc(B, vars[0], dtype_code(B.scalar_type()));
+    const at::Tensor x2 = rows(vars[0], dw.rows);
+    const int64_t n = x2.size(0), i = dw.rows, r = da.cols;
+    const int code = dtype_code(x2.scalar_type());
+    const c10::OptionalDeviceGuard guard(x2.device());
+    const at::Tensor dy2 = rows(grads[0], o), T = ctx->saved_data["T"].toTensor();
+    at::Tensor dx, dA, dB;
+    rl_tensor_t tx{};
+    rl_stack_t ta{}, tb{};
+    if (ctx->needs_input_grad(0)) { dx = at::empty({n, i}, x2.options()); tx = desc(dx, code); }
+    if (ctx->needs_input_grad(1)) { dA = at::empty(A.sizes(), A.options()); ta = stack_desc(dA, x2, da.dtype); }
+    if (ctx->needs_input_grad(2)) { dB = at::empty(B.sizes(), B.options()); tb = stack_desc(dB, x2, db.dtype); }
+    const at::Tensor ws = scratch(p_experts_workspace_bytes(1, n, dw.experts, i, o, r, code, dw.dtype), x2);
+    const rl_opts_t opts = options(x2, ws, std::nullopt, ctx->saved_data["scale"].toDouble());
+    const rl_tensor_t ddy = desc(dy2, dtype_code(dy2.scalar_type())), dx2 = desc(x2, code), dt = desc(T, dtype_code(T.scalar_type()));
+    check(p_experts_backward(&ddy, &dx2, ends_of(vars[5], dw.experts, x2), &dw, &da, &db, &dt, dx.defined() ? &tx : nullptr, dA.defined() ? &ta : nullptr,
+                             dB.defined() ? &tb : nullptr, &opts));
+    if (dx.defined()) dx = dx.view(ctx->saved_data["x_shape"].toIntVector());
+    at::Tensor none;
+    return {dx, dA, dB, none, none, none, none, none, none};
+  }
+};
+
 bool plain_2d(const at::Tensor& t, const at::Tensor& x) {
   return t.dim() == 2 && t.stride(1) == 1 && t.scalar_type() == x.scalar_type() && t.device() == x.device() && t.layout() == at::kStrided;
 }
@@ -466,11 +546,53 @@ PyObject* py_dora(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-// init((forward, backward, workspace_bytes addresses of LoRA, of VeRA, of DoRA: nine in all), check)
+// experts(x, A, B, W, scales, ends, bias, scale, d_out): y, or None; scales, ends and bias may be None.  W, A and B are stacks, or with ends
+// None matrices; the library's checks have the messages for sizes that do not fit
+PyObject* py_experts(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 9 || p_experts_forward == nullptr || !PyFloat_CheckExact(args[7]) || !PyLong_CheckExact(args[8])) Py_RETURN_NONE;
+  const int64_t o = PyLong_AsLongLong(args[8]);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    Py_RETURN_NONE;
+  }
+  if (torch::jit::tracer::isTracing() || at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set() ||
+      c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode))
+    Py_RETURN_NONE;
+  for (int k = 0; k < 7; ++k) {
+    if (k >= 4 && args[k] == Py_None) continue;
+    if (!THPVariable_CheckExact(args[k])) Py_RETURN_NONE;
+    const at::Tensor& t = THPVariable_Unpack(args[k]);
+    if (!t.is_cuda() || t.layout() != at::kStrided || t.numel() == 0 || t.device().index() != c10::hip::current_device() || t.is_conj() || t.is_neg() ||
+        t._is_zerotensor())
+      Py_RETURN_NONE;
+  }
+  const at::Tensor &x = THPVariable_Unpack(args[0]), &A = THPVariable_Unpack(args[1]), &B = THPVariable_Unpack(args[2]), &W = THPVariable_Unpack(args[3]);
+  const std::optional<at::Tensor> scales = optional_tensor(args[4]), ends = optional_tensor(args[5]), bias = optional_tensor(args[6]);
+  const int64_t dim = ends.has_value() ? 3 : 2;
+  for (const at::Tensor* t : {&A, &B, &W})
+    if (t->dim() != dim || t->stride(-1) != 1) Py_RETURN_NONE;
+  if (dtype_code(x.scalar_type()) < 0 || A.scalar_type() != x.scalar_type() || B.scalar_type() != x.scalar_type() || x.dim() < 1 || x.size(-1) != W.size(-2)) Py_RETURN_NONE;
+  if (scales.has_value() ? (scales->dim() != dim || scales->element_size() != 1 || W.element_size() != 1 || W.size(-1) < o ||
+                            scales->size(-2) != (W.size(-2) + 127) / 128 || scales->size(-1) != (o + 127) / 128 || (dim == 3 && scales->size(0) != W.size(0)))
+                         : (W.scalar_type() != x.scalar_type() || W.size(-1) != o))
+    Py_RETURN_NONE;
+  if (ends.has_value() && (ends->dim() != 1 || ends->numel() != W.size(0) || ends->scalar_type() != at::kInt || ends->stride(0) != 1)) Py_RETURN_NONE;
+  if (bias.has_value() && (bias->scalar_type() != x.scalar_type() || !bias->is_contiguous() || bias->numel() != (dim == 3 ? W.size(0) : 1) * o)) Py_RETURN_NONE;
+  at::Tensor y;
+  {
+    pybind11::gil_scoped_release release;
+    y = ExpertsNode::apply(x, A, B, W, scales, ends, bias, PyFloat_AS_DOUBLE(args[7]), o);
+  }
+  return THPVariable_Wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+// init((forward, backward, workspace_bytes addresses of LoRA, of VeRA, of DoRA, of the experts: twelve in all), check)
 PyObject* py_init(PyObject*, PyObject* args) {
-  unsigned long long a[9];
+  unsigned long long a[12];
   PyObject* chk;
-  if (!PyArg_ParseTuple(args, "(KKKKKKKKK)O", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &chk)) return nullptr;
+  if (!PyArg_ParseTuple(args, "(KKKKKKKKKKKK)O", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &a[9], &a[10], &a[11], &chk)) return nullptr;
   p_forward = reinterpret_cast<decltype(p_forward)>(a[0]);
   p_backward = reinterpret_cast<decltype(p_backward)>(a[1]);
   p_workspace_bytes = reinterpret_cast<decltype(p_workspace_bytes)>(a[2]);
@@ -480,6 +602,9 @@ PyObject* py_init(PyObject*, PyObject* args) {
   p_dora_forward = reinterpret_cast<decltype(p_dora_forward)>(a[6]);
   p_dora_backward = reinterpret_cast<decltype(p_dora_backward)>(a[7]);
   p_dora_workspace_bytes = reinterpret_cast<decltype(p_dora_workspace_bytes)>(a[8]);
+  p_experts_forward = reinterpret_cast<decltype(p_experts_forward)>(a[9]);
+  p_experts_backward = reinterpret_cast<decltype(p_experts_backward)>(a[10]);
+  p_experts_workspace_bytes = reinterpret_cast<decltype(p_experts_workspace_bytes)>(a[11]);
   Py_INCREF(chk);
   Py_XDECREF(g_check);
   g_check = chk;
@@ -489,6 +614,7 @@ PyObject* py_init(PyObject*, PyObject* args) {
 PyMethodDef methods[] = {{"lora", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_lora)), METH_FASTCALL, "LoRA layer as a native autograd node, or None"},
                          {"vera", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_vera)), METH_FASTCALL, "VeRA layer as a native autograd node, or None"},
                          {"dora", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_dora)), METH_FASTCALL, "DoRA layer as a native autograd node, or None"},
+                         {"experts", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_experts)), METH_FASTCALL, "layer over expert stacks or an 8-bit weight as a native autograd node, or None"},
                          {"init", py_init, METH_VARARGS, "hand over librunlora's entry points"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_autograd", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -45,7 +45,8 @@ def _native():
         from . import _autograd
         address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
         entries = (lib.runlora_forward, lib.runlora_backward, lib.runlora_call_workspace_bytes, lib.runlora_vera_forward, lib.runlora_vera_backward,
-                   lib.runlora_vera_workspace_bytes, lib.runlora_dora_forward, lib.runlora_dora_backward, lib.runlora_dora_workspace_bytes)
+                   lib.runlora_vera_workspace_bytes, lib.runlora_dora_forward, lib.runlora_dora_backward, lib.runlora_dora_workspace_bytes,
+                   lib.runlora_experts_forward, lib.runlora_experts_backward, lib.runlora_experts_workspace_bytes)
         _autograd.init(tuple(address(f) for f in entries), rl._check)
         _native_module = _autograd
     return _native_module
@@ -398,46 +399,19 @@ def _w_code(W, code):
     return rl.RL_FP8_B128 if isinstance(W, rl.Fp8Weight) else code
 
 
-class RunLoRAFp8Function(torch.autograd.Function):
-    """y = Q(x) W + bias + scale (x A) B over an Fp8Weight (runlora.h); gradients for x, A and B, the large product of dx on Q(dy).
-    scale XA (n*r elements) is kept for the backward."""
-
-    @staticmethod
-    def forward(ctx, x, W, A, B, bias, scale):
-        x2 = _rows(x, W.rows)
-        n, r, code = x2.shape[0], A.shape[1], rl.dtype_code(x.dtype)
-        y = torch.empty((n, W.cols), dtype=x.dtype, device=x.device)
-        T = torch.empty((n, r), dtype=x.dtype, device=x.device)
-        ctx.saved, ctx.W, ctx.x_shape = rl.new_saved(T), W, x.shape
-        if n > 0:
-            ws = _workspace(x.device, rl.runlora_workspace_bytes(rl.FWD1, -1, n, W.rows, W.cols, r, code, rl.RL_FP8_B128))
-            rl.runlora_forward(rl.FWD1, x2, W, A, B, y, ctx.saved, workspace=ws, scale=scale, bias=bias)
-        ctx.save_for_backward(x2, A, B, T)
-        return y.view(*x.shape[:-1], W.cols)
-
-    @staticmethod
-    def backward(ctx, dy):
-        x2, A, B, T = ctx.saved_tensors
-        W, (n, i), r = ctx.W, x2.shape, A.shape[1]
-        dy2 = _rows(dy, W.cols)
-        need_x, _, need_a, need_b = ctx.needs_input_grad[:4]
-        dx = torch.empty((n, i), dtype=x2.dtype, device=x2.device) if need_x else None
-        make = torch.empty_like if n > 0 else torch.zeros_like
-        dA, dB = make(A) if need_a else None, make(B) if need_b else None
-        if n > 0:
-            saved, x2 = _reread(ctx.saved, dy2, x2, A, B, T)
-            if saved.T != T.data_ptr() or saved.ldt != T.stride(0):
-                saved = type(saved).from_buffer_copy(saved)
-                saved.T, saved.ldt = T.data_ptr(), T.stride(0)
-            code = rl.dtype_code(dy.dtype)
-            ws = _workspace(dy.device, rl.runlora_workspace_bytes(-1, rl.BWD1, n, i, W.cols, r, code, rl.RL_FP8_B128))
-            rl.runlora_backward(rl.BWD1, dy2, saved, W, A, B, dx, dA, dB, workspace=ws)
-        return dx.view(ctx.x_shape) if need_x else None, None, dA, dB, None, None
-
-
 class RunLoRAExpertsFunction(torch.autograd.Function):
     """y_t = x_t W_e + bias_e + scale (x_t A_e) B_e over rows sorted by expert (runlora_experts_forward / _backward); gradients for x, A and
-    B.  W: [experts, d_in, d_out] or an Fp8Weight stack; A = B = None: no adapter.  scale XA is kept for the backward."""
+    B.  W: [experts, d_in, d_out] or an Fp8Weight stack; A = B = None: no adapter.  scale XA (n*r elements) is kept for the backward."""
+
+    @classmethod
+    def apply(cls, x, ends, W, A, B, bias, scale):
+        if cls is RunLoRAExpertsFunction:
+            fp8 = isinstance(W, rl.Fp8Weight)
+            if A is not None:
+                y = _native().experts(x, A, B, W.data if fp8 else W, W.scales if fp8 else None, ends, bias, scale, W.shape[-1])
+                if y is not None:
+                    return y
+        return super().apply(x, ends, W, A, B, bias, scale)
 
     @staticmethod
     def forward(ctx, x, ends, W, A, B, bias, scale):
@@ -449,14 +423,17 @@ class RunLoRAExpertsFunction(torch.autograd.Function):
         if n > 0:
             ws = _workspace(x.device, rl.runlora_experts_workspace_bytes(False, n, E, i, o, r, code, _w_code(W, code)))
             rl.runlora_experts_forward(x2, ends, W, A, B, y, T, workspace=ws, scale=scale, bias=bias)
-        ctx.W, ctx.scale, ctx.x_shape = W, scale, x.shape
-        ctx.save_for_backward(x2, ends, A, B, T)
+        fp8 = isinstance(W, rl.Fp8Weight)
+        ctx.scale, ctx.x_shape, ctx.w_shape = scale, x.shape, (E, i, o)
+        ctx.save_for_backward(x2, ends, A, B, T, W.data if fp8 else W, W.scales if fp8 else None)
         return y.view(*x.shape[:-1], o)
 
     @staticmethod
     def backward(ctx, dy):
-        x2, ends, A, B, T = ctx.saved_tensors
-        E, i, o = ctx.W.shape
+        x2, ends, A, B, T, W, scales = ctx.saved_tensors
+        E, i, o = ctx.w_shape
+        if scales is not None:
+            W = rl.Fp8Weight(W, scales, i, o)
         n, r = x2.shape[0], 0 if A is None else A.shape[2]
         dy2, x2 = _rows(dy, o), _rows(x2, i)
         need = ctx.needs_input_grad
@@ -465,10 +442,60 @@ class RunLoRAExpertsFunction(torch.autograd.Function):
         dA = make(A.shape, dtype=A.dtype, device=A.device) if need[3] else None
         dB = make(B.shape, dtype=B.dtype, device=B.device) if need[4] else None
         if n > 0:
+            for t in (x2, ends, A, B, T):
+                if t is not None and t.device != dy.device:
+                    raise ValueError(f"a saved tensor came back on another device: {t.device}, not {dy.device}")
             code = rl.dtype_code(dy.dtype)
-            ws = _workspace(dy.device, rl.runlora_experts_workspace_bytes(True, n, E, i, o, r, code, _w_code(ctx.W, code)))
-            rl.runlora_experts_backward(dy2, x2, ends, ctx.W, A, B, dx, dA, dB, T, workspace=ws, scale=ctx.scale)
+            ws = _workspace(dy.device, rl.runlora_experts_workspace_bytes(True, n, E, i, o, r, code, _w_code(W, code)))
+            rl.runlora_experts_backward(dy2, x2, ends, W, A, B, dx, dA, dB, T, workspace=ws, scale=ctx.scale)
         return dx.view(ctx.x_shape) if need[0] else None, None, None, dA, dB, None, None
+
+
+class RunLoRAFp8Function(torch.autograd.Function):
+    """y = Q(x) W + bias + scale (x A) B over an Fp8Weight (runlora.h); gradients for x, A and B, the large product of dx on Q(dy).
+    scale XA (n*r elements) is kept for the backward."""
+
+    @classmethod
+    def apply(cls, x, W, A, B, bias, scale):
+        if cls is RunLoRAFp8Function and isinstance(W, rl.Fp8Weight):
+            y = _native().experts(x, A, B, W.data, W.scales, None, bias, scale, W.cols)
+            if y is not None:
+                return y
+        return super().apply(x, W, A, B, bias, scale)
+
+    @staticmethod
+    def forward(ctx, x, W, A, B, bias, scale):
+        x2 = _rows(x, W.rows)
+        n, r, code = x2.shape[0], A.shape[1], rl.dtype_code(x.dtype)
+        y = torch.empty((n, W.cols), dtype=x.dtype, device=x.device)
+        T = torch.empty((n, r), dtype=x.dtype, device=x.device)
+        ctx.saved, ctx.w_shape, ctx.x_shape = rl.new_saved(T), W.shape, x.shape
+        if n > 0:
+            ws = _workspace(x.device, rl.runlora_workspace_bytes(rl.FWD1, -1, n, W.rows, W.cols, r, code, rl.RL_FP8_B128))
+            rl.runlora_forward(rl.FWD1, x2, W, A, B, y, ctx.saved, workspace=ws, scale=scale, bias=bias)
+        ctx.save_for_backward(x2, A, B, T, W.data, W.scales)
+        return y.view(*x.shape[:-1], W.cols)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x2, A, B, T, data, scales = ctx.saved_tensors
+        (i, o), n, r = ctx.w_shape, x2.shape[0], A.shape[1]
+        W = rl.Fp8Weight(data, scales, i, o)
+        dy2 = _rows(dy, o)
+        need_x, _, need_a, need_b = ctx.needs_input_grad[:4]
+        dx = torch.empty((n, i), dtype=x2.dtype, device=x2.device) if need_x else None
+        make = torch.empty if n > 0 else torch.zeros
+        dA = make(A.shape, dtype=A.dtype, device=A.device) if need_a else None
+        dB = make(B.shape, dtype=B.dtype, device=B.device) if need_b else None
+        if n > 0:
+            saved, x2 = _reread(ctx.saved, dy2, x2, A, B, T)
+            if saved.T != T.data_ptr() or saved.ldt != T.stride(0):
+                saved = type(saved).from_buffer_copy(saved)
+                saved.T, saved.ldt = T.data_ptr(), T.stride(0)
+            code = rl.dtype_code(dy.dtype)
+            ws = _workspace(dy.device, rl.runlora_workspace_bytes(-1, rl.BWD1, n, i, o, r, code, rl.RL_FP8_B128))
+            rl.runlora_backward(rl.BWD1, dy2, saved, W, A, B, dx, dA, dB, workspace=ws)
+        return dx.view(ctx.x_shape) if need_x else None, None, dA, dB, None, None
 
 
 class RunLoRAFp8Linear(nn.Module):

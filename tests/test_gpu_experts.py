@@ -334,6 +334,60 @@ def test_experts_module(n, fp8):
     close_all(("dX", "dA", "dB"), (dx, dA, dB), c.want_backward(), "bf16")
 
 
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+@pytest.mark.parametrize("n", [20, 300])
+def test_native_and_python_nodes_give_the_same_bits(n, fp8, monkeypatch):
+    """The Python node (here: what a subclass of the function runs) and the native one, in several input shapes; a tensor that autograd keeps may
+    not change between the passes, with either."""
+    from paper_2312_03415_amd import module
+    c = Case("bf16", fp8, n, 4, 256, 272, 16, "uneven", bias=True)
+
+    class PythonExperts(module.RunLoRAExpertsFunction):
+        pass
+
+    class PythonFp8(module.RunLoRAFp8Function):
+        pass
+
+    def one(fn, shape):
+        x = c.X.reshape(shape).clone().requires_grad_(True)
+        A, B = c.A.clone().requires_grad_(True), c.B.clone().requires_grad_(True)
+        y = fn.apply(x, c.ends, c.W, A, B, c.bias, 1.5)
+        assert ("ExpertsNode" in type(y.grad_fn).__name__ or "ExpertsNode" in str(y.grad_fn.name())) == (fn is module.RunLoRAExpertsFunction)
+        return (y,) + torch.autograd.grad(y, (x, A, B), c.dY.reshape(y.shape))
+
+    for shape in ((n, 256), (2, n // 2, 256)):
+        for a, b in zip(one(module.RunLoRAExpertsFunction, shape), one(PythonExperts, shape)):
+            assert a.shape == b.shape and torch.equal(a, b)
+    x = c.X.clone().requires_grad_(True)
+    for fn in (module.RunLoRAExpertsFunction, PythonExperts):
+        ends = c.ends.clone()
+        y = fn.apply(x, ends, c.W, c.A, c.B, c.bias, 1.5)
+        ends.add_(0)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.backward(c.dY)
+    if fp8:
+        rl = _rl()
+        W = rl.Fp8Weight(c.W.data[1], c.W.scales[1], 256, 272)
+        outs = []
+        for fn in (module.RunLoRAFp8Function, PythonFp8):
+            x = c.X.clone().requires_grad_(True)
+            A, B = c.A[1].clone().requires_grad_(True), c.B[1].clone().requires_grad_(True)
+            y = fn.apply(x, W, A, B, c.bias[1], 1.5)
+            outs.append((y,) + torch.autograd.grad(y, (x, A, B), c.dY))
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def test_native_node_reports_the_librarys_errors():
+    from paper_2312_03415_amd import module
+    rl = _rl()
+    c = Case("bf16", False, 40, 4, 256, 272, 16, "uneven")
+    with pytest.raises(rl.RunLoRAError) as e:
+        module.RunLoRAExpertsFunction.apply(c.X, c.ends, c.W, c.A, c.B[:, :8], None, 1.0)
+    assert e.value.code == rl.RL_ERR_SHAPE
+    with pytest.raises(ValueError):
+        module.RunLoRAExpertsFunction.apply(c.X, c.ends.long(), c.W, c.A, c.B, None, 1.0)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("n", [3, 400])
 def test_fp8_layer_module_and_abi(n, dtype):
