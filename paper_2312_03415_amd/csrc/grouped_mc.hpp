@@ -11,7 +11,8 @@
 //  - No LDS read is in flight where the code branches (the end of a K tile): the compiler may copy registers there.
 //  - Output tiles are those of the experts' rows; tile counts stay in registers, one expert a lane, so that finding the next tile is
 //    a ballot.  Rows and columns outside the operands are fetched from past the buffers' ends, which gives zeros.
-//  - The adapter's product runs behind the K loop, fragments straight from memory, see grouped_mt.hpp.
+//  - The adapter's product is one more run of K tiles in the same stream (T and the other factor, both with the rank in their rows).
+//    With its fragments straight from memory behind the K loop, as grouped_mt.hpp has it, an output tile of r = 128 took 20 us more.
 #pragma once
 #include "grouped_mt.hpp"
 
@@ -75,84 +76,148 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
     const int band_rows = (nbm - first_m) < BAND ? (nbm - first_m) : BAND, in_band = id - band * per_band;
     n0 = (in_band / band_rows) * 256;
     const int t = first_m + in_band % band_rows;
-    if (!one_scan) return group_find<256, F8>(g.ends, g.experts, g.n, lane, t);
     GroupTile out;
-    const int l = __builtin_ctzll(__ballot(gsum > t));
-    out.e = l;
-    out.lo = __builtin_amdgcn_readlane(glo, l);
-    out.hi = __builtin_amdgcn_readlane(ghi, l);
-    out.m0 = (F8 ? out.lo & ~3 : out.lo) + (t - (__builtin_amdgcn_readlane(gsum, l) - __builtin_amdgcn_readlane(gtiles, l))) * 256;
+    if (one_scan) {
+      const int l = __builtin_ctzll(__ballot(gsum > t));
+      out.e = l;
+      out.lo = __builtin_amdgcn_readlane(glo, l);
+      out.hi = __builtin_amdgcn_readlane(ghi, l);
+      out.m0 = (F8 ? out.lo & ~3 : out.lo) + (t - (__builtin_amdgcn_readlane(gsum, l) - __builtin_amdgcn_readlane(gtiles, l))) * 256;
+    } else {
+      out = group_find<256, F8>(g.ends, g.experts, g.n, lane, t);
+    }
+    // (said to the compiler: with a descriptor that it takes for a lane's own, every load becomes a loop over the lanes)
+    out.e = __builtin_amdgcn_readfirstlane(out.e);
+    out.lo = __builtin_amdgcn_readfirstlane(out.lo);
+    out.hi = __builtin_amdgcn_readfirstlane(out.hi);
+    out.m0 = __builtin_amdgcn_readfirstlane(out.m0);
+    n0 = __builtin_amdgcn_readfirstlane(n0);
     return out;
   };
 
-  // ---- load cursor: the K tile of the output tile that is fetched next
+  // ---- load cursor: the K tile of the output tile that is fetched next.  An output tile's K tiles are the nt of the large product and then
+  // the ntail of the adapter's (64 of the rank each, 16-bit, both factors with the rank in their rows).
   constexpr uint32_t OOB = 0x80000000u, kBias = 3 * 1024;  // (four loads share an LDS base and differ in the immediate offset, see gemm_mc64.hpp)
   uint32_t offA[IPW], offB[IPW];
   const unsigned char *pA = nullptr, *pB = nullptr, *pS = nullptr;
-  int64_t leftA = 0, leftB = 0;
-  const int64_t stepB = B_STR ? (int64_t)KE * g.ldb * EB : 128;
-  int cw = blockIdx.x, cu = 0, leftS = 0;
-  bool clive = true;
-  const int ktail = g.K - g.K / KE * KE;
-  auto partial_tile = [&]() RL_INLINE {  // the cursor is at a partial K tile: chunks beyond K read zeros
-    if constexpr (!F8) {
-#pragma unroll
-      for (int j = 0; j < IPW; ++j) {
-        const int p = (wave * IPW + j) * 64 + lane;
-        if (((p & 7) ^ ((p >> 4) & 7)) * (16 / EB) >= ktail) offA[j] |= OOB;
-      }
-    }
-    if constexpr (!B_STR) {
-#pragma unroll
-      for (int j = 0; j < IPW; ++j) {
-        const int p = (wave * IPW + j) * 64 + lane;
-        if (((p & 7) ^ ((p >> 4) & 7)) * (16 / EB) >= ktail) offB[j] |= OOB;
-      }
-    }
+  int64_t leftA = 0, leftB = 0, stepB = 0;
+  const int ntail = (g.R + 63) >> 6;
+  int cw = blockIdx.x, cu = 0, cnext = 0, leftS = 0, ce = 0, cm0 = 0, cn0 = 0;  // cnext: the K tile at which something changes
+  bool clive = true, in_tail = false;
+  const int kpart = g.K - g.K / KE * KE, rpart = g.R & 63;  // what the last K tile of each kind holds, 0: all of it
+  // (what follows from the lane alone is not worth registers across the K loop)
+  auto opaque_lane = [&]() RL_INLINE {
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    return ln;
   };
-  auto cursor_open = [&]() RL_INLINE {  // the first K tile of output tile cw, or of the next that has any; none left: loads of nothing
-    GroupTile t{};
-    int n0 = 0;
-    for (;; cw += gridDim.x) {
-      if (cw >= total || nt == 0) { clive = false; break; }
-      t = tile_of(cw, n0);
-      if (t.e < g.experts) break;
-    }
-    cu = 0;
-    if (!clive) {
-      leftA = leftB = 0;
-      leftS = 0;
-      return;
-    }
-    const int rows = g.n - t.m0;
-    pA = static_cast<const unsigned char*>(g.A) + (int64_t)t.m0 * g.lda * EB;
-    leftA = ((int64_t)(rows - 1) * g.lda + (F8 ? (int64_t)((g.K + 127) / 128) * 128 : g.K)) * EB;
-    const unsigned char* const Be = static_cast<const unsigned char*>(g.B) + (int64_t)t.e * g.sb * EB;
-    pB = Be + (B_STR ? (int64_t)n0 * EB : (int64_t)n0 * g.ldb * EB);
-    leftB = (B_STR ? (int64_t)(g.K - 1) * g.ldb + g.N - n0 : (int64_t)(g.N - n0 - 1) * g.ldb + g.K) * EB;
+  auto k_contiguous = [&](uint32_t (&off)[IPW], bool dealt, int rows, int ld, int eb) RL_INLINE {
+    const int ln = opaque_lane();
 #pragma unroll
     for (int j = 0; j < IPW; ++j) {
-      const int p = (wave * IPW + j) * 64 + lane;
-      {
-        int row = p >> 3;
-        const int col = ((p & 7) ^ ((row >> 1) & 7)) * (16 / EB);
-        if constexpr (F8) row = (row & 128) + (row & 15) * 8 + ((row & 127) >> 4);  // the wave's rows are dealt out to its blocks
-        offA[j] = row < rows ? (uint32_t)((row * (int)g.lda + col) * EB) + (kBias - 1024u * (j & 3)) : OOB;
-      }
-      if constexpr (!B_STR) {
-        const int row = p >> 3, col = ((p & 7) ^ ((row >> 1) & 7)) * (16 / EB);
-        offB[j] = n0 + row < g.N ? (uint32_t)((row * (int)g.ldb + col) * EB) + (kBias - 1024u * (j & 3)) : OOB;
-      } else {
-        const int row = F8 ? p >> 4 : p >> 5;
+      const int p = (wave * IPW + j) * 64 + ln;
+      int row = p >> 3;
+      const int byte = ((p & 7) ^ ((row >> 1) & 7)) * 16;
+      if (dealt) row = (row & 128) + (row & 15) * 8 + ((row & 127) >> 4);  // the wave's rows are dealt out to its blocks
+      off[j] = row < rows ? (uint32_t)(row * ld * eb + byte) + (kBias - 1024u * (j & 3)) : OOB;
+    }
+  };
+  auto cut = [&](uint32_t (&off)[IPW], int bytes) RL_INLINE {  // chunks that lie `bytes` or more into the row of a K tile read zeros
+    const int ln = opaque_lane();
+#pragma unroll
+    for (int j = 0; j < IPW; ++j) {
+      const int p = (wave * IPW + j) * 64 + ln;
+      if (((p & 7) ^ ((p >> 4) & 7)) * 16 >= bytes) off[j] |= OOB;
+    }
+  };
+  auto cursor_main = [&]() RL_INLINE {  // the first K tile of output tile cw, or of the next that has any; none left: loads of nothing
+    GroupTile t{};
+    for (;; cw += gridDim.x) {
+      if (cw >= total) { clive = false; break; }
+      t = tile_of(cw, cn0);
+      if (t.e < g.experts) break;
+    }
+    if (!clive) {
+      leftA = leftB = 0;
+      return;
+    }
+    ce = t.e;
+    cm0 = t.m0;
+    const int rows = g.n - cm0;
+    pA = static_cast<const unsigned char*>(g.A) + (int64_t)cm0 * g.lda * EB;
+    leftA = ((int64_t)(rows - 1) * g.lda + (F8 ? (int64_t)((g.K + 127) / 128) * 128 : g.K)) * EB;
+    k_contiguous(offA, F8, rows, (int)g.lda, EB);
+    const unsigned char* const Be = static_cast<const unsigned char*>(g.B) + (int64_t)ce * g.sb * EB;
+    if constexpr (!B_STR) {
+      pB = Be + (int64_t)cn0 * g.ldb * EB;
+      leftB = ((int64_t)(g.N - cn0 - 1) * g.ldb + g.K) * EB;
+      stepB = 128;
+      k_contiguous(offB, false, g.N - cn0, (int)g.ldb, EB);
+    } else {
+      pB = Be + (int64_t)cn0 * EB;
+      leftB = ((int64_t)(g.K - 1) * g.ldb + g.N - cn0) * EB;
+      stepB = (int64_t)KE * g.ldb * EB;
+      const int ln = opaque_lane();
+#pragma unroll
+      for (int j = 0; j < IPW; ++j) {
+        const int p = (wave * IPW + j) * 64 + ln, row = F8 ? p >> 4 : p >> 5;
         const int col = F8 ? ((p & 15) ^ grouped_swz<true, 256>(row)) * 16 : ((p & 31) ^ (4 * (row & 3))) * 8;
-        offB[j] = n0 + col < g.N ? (uint32_t)((row * (int)g.ldb + col) * EB) + (kBias - 1024u * (j & 3)) : OOB;
+        offB[j] = cn0 + col < g.N ? (uint32_t)((row * (int)g.ldb + col) * EB) + (kBias - 1024u * (j & 3)) : OOB;
       }
     }
     if constexpr (F8) {
-      pS = g.SA + t.m0;
-      leftS = (int)(g.ldsa - t.m0);
+      pS = g.SA + cm0;
+      leftS = (int)(g.ldsa - cm0);
     }
-    if (ktail != 0 && nt == 1) partial_tile();
+    in_tail = false;
+  };
+  auto cursor_tail = [&]() RL_INLINE {  // the first K tile of the adapter's product
+    const int rows = g.n - cm0;
+    pA = static_cast<const unsigned char*>(g.TA) + (int64_t)cm0 * g.ldta * 2;
+    leftA = ((int64_t)(rows - 1) * g.ldta + g.R) * 2;
+    k_contiguous(offA, F8, rows, (int)g.ldta, 2);
+    pB = static_cast<const unsigned char*>(g.TB) + (ce * g.stb + (int64_t)cn0 * g.ldtb) * 2;
+    leftB = ((int64_t)(g.N - cn0 - 1) * g.ldtb + g.R) * 2;
+    stepB = 128;
+    k_contiguous(offB, false, g.N - cn0, (int)g.ldtb, 2);
+    in_tail = true;
+  };
+  auto cut_main = [&]() RL_INLINE {  // the large product's partial K tile
+    if constexpr (!F8) cut(offA, kpart * EB);  // (rows of a rounded A are whole scale blocks, zeros behind K)
+    if constexpr (!B_STR) cut(offB, kpart * EB);
+  };
+  auto cut_tail = [&]() RL_INLINE {
+    cut(offA, rpart * 2);
+    cut(offB, rpart * 2);
+  };
+  // The cursor has reached cnext, and it lies ahead of the cursor again afterwards, or nothing is left.  (What several branches would assign
+  // is assigned behind them: the compiler folds their stores into one through a choice of addresses, and the variables stay in memory.)
+  auto cursor_event = [&]() RL_INLINE {
+    int at = cu, next = nt;
+    if (cu < nt) {
+      cut_main();
+    } else if (!in_tail && ntail > 0) {
+      cursor_tail();
+      next = nt + ntail - (rpart != 0);
+      if (next == at) {
+        cut_tail();
+        next = nt + ntail;
+      }
+    } else if (cu < nt + ntail) {
+      cut_tail();
+      next = nt + ntail;
+    } else {
+      cw += gridDim.x;
+      cursor_main();
+      at = 0;
+      next = nt - (kpart != 0);
+      if (next == 0) {
+        if (clive) cut_main();
+        next = nt;
+      }
+    }
+    cu = at;
+    cnext = next;
   };
   auto rsrc = [&](const unsigned char* base, int64_t left) RL_INLINE {
     const int size = left <= 0 ? 0 : (left > 0x7fff0000 ? 0x7fff0000 : (int)left) + (int)kBias;
@@ -160,7 +225,12 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
   };
   __amdgpu_buffer_rsrc_t rsA, rsB;
   auto cursor_point = [&]() RL_INLINE { rsA = rsrc(pA, leftA); rsB = rsrc(pB, leftB); };
-  cursor_open();
+  cursor_main();
+  cnext = nt - (kpart != 0);
+  if (clive && cnext == 0) {
+    cut_main();
+    cnext = nt;
+  }
   cursor_point();
   // load j of the cursor's K tile into stage `st`: 0..7 the A half, 8..15 the B half, 16 the scales of A
   auto issue_load = [&](int st, auto j_c) RL_INLINE {
@@ -171,7 +241,7 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
       unsigned char* const dst = smem + st * P::STAGE_BYTES + (isB ? P::A_BYTES : 0) + wave * (IPW * 1024) + (jj >> 2) * 4096;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(isB ? rsB : rsA, (mc_lds_void_t*)dst, 16, isB ? offB[jj] : offA[jj], 0, (jj & 3) * 1024, 0);
     } else if constexpr (F8) {
-      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(pS), 0, leftS > 0 ? leftS : 0, 0x00020000);
+      const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(pS), 0, clive && !in_tail ? leftS : 0, 0x00020000);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (mc_lds_void_t*)(smem + P::SCALES + st * 1024 + wave * 256), 4, 4 * lane, 0, 0, 0);
     }
   };
@@ -183,19 +253,6 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
     if constexpr (F8) pS += g.ldsa;
     cursor_point();
   };
-  const int nlast = nt - (ktail != 0);
-  auto cursor_event = [&]() RL_INLINE {
-    if (__builtin_expect(clive && cu >= nlast, 0)) {
-      if (cu == nt) {
-        cw += gridDim.x;
-        cursor_open();
-      } else {
-        partial_tile();
-      }
-      cursor_point();
-    }
-  };
-
   // ---- fragment addresses inside a stage (half h of a fragment: k 32 h + 8 grp .. + 7, or 64 h + 16 grp .. + 15 for e4m3)
   uint32_t fragA[2], fragB[B_STR ? 8 : 2];
   {
@@ -225,15 +282,23 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
     asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(f.h0) : "v"(at0), "i"(a * 2048));
     asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(f.h1) : "v"(at1), "i"(a * 2048));
   };
-  auto read_B = [&](auto b_c, uint32_t soff) RL_INLINE {
+  auto read_B = [&](auto tail_c, auto b_c, uint32_t soff) RL_INLINE {  // TAIL: a K-contiguous 16-bit tile whatever W's layout
     constexpr int b = decltype(b_c)::value;
+    constexpr bool TAIL = decltype(tail_c)::value;
     auto& f = fb[b];
     const uint32_t base = lds_base + soff;
     const auto& fr = fragB;
+    [[maybe_unused]] const uint32_t fragT = (uint32_t)(P::A_BYTES + (wn - wm) * 16384);  // the same lanes' rows of the B half
     if constexpr (!B_STR) {
       const uint32_t at0 = base + fr[0], at1 = base + fr[1];
       asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(f.h0) : "v"(at0), "i"(b * 2048));
       asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(f.h1) : "v"(at1), "i"(b * 2048));
+    } else if constexpr (TAIL) {
+      const uint32_t at0 = base + fragA[0] + fragT, at1 = base + fragA[1] + fragT;
+      asm volatile("ds_read_b64 %0, %1 offset:%2" : "=v"(f.q[0]) : "v"(at0), "i"(b * 2048));
+      asm volatile("ds_read_b64 %0, %1 offset:%2" : "=v"(f.q[1]) : "v"(at0), "i"(b * 2048 + 8));
+      asm volatile("ds_read_b64 %0, %1 offset:%2" : "=v"(f.q[2]) : "v"(at1), "i"(b * 2048));
+      asm volatile("ds_read_b64 %0, %1 offset:%2" : "=v"(f.q[3]) : "v"(at1), "i"(b * 2048 + 8));
     } else {
       const uint32_t at = base + fr[b];
       if constexpr (F8) {
@@ -264,11 +329,12 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
   int wsc = 0;      // scale byte of W, this K tile
 #define MC_FENCE() __builtin_amdgcn_sched_barrier(0)
   // products of A block a with B blocks B0 .. B0 + 3; slot(j) is called behind each quarter of them
-  auto row_products = [&](auto a_c, auto b0_c, auto slot) RL_INLINE {
+  auto row_products = [&](auto tail_c, auto a_c, auto b0_c, auto slot) RL_INLINE {
     constexpr int a = decltype(a_c)::value, B0 = decltype(b0_c)::value;
+    constexpr bool TAIL = decltype(tail_c)::value;
     static_for<4>([&](auto j_c) RL_INLINE {
       constexpr int j = decltype(j_c)::value;
-      if constexpr (F8) {
+      if constexpr (F8 && !TAIL) {
         mma_f8<a & 3>(acc[a][B0 + j], __builtin_shufflevector(half(fb[B0 + j], H0{}), half(fb[B0 + j], H1{}), 0, 1, 2, 3, 4, 5, 6, 7),
                       __builtin_shufflevector(fa[a].h0, fa[a].h1, 0, 1, 2, 3, 4, 5, 6, 7), wsc, sa[a >> 2]);
       } else {
@@ -289,14 +355,17 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
   for (int s = 0; s < 2; ++s) {
     static_for<LPT>([&](auto j) RL_INLINE { issue_load(s, j); });
     cursor_step();
-    cursor_event();
+    if (clive && cu >= cnext) {
+      cursor_event();
+      cursor_point();
+    }
   }
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(mc_wait_imm(0, true));
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   MC_FENCE();
-  static_for<4>([&](auto b) RL_INLINE { read_B(b, 0u); });
+  static_for<4>([&](auto b) RL_INLINE { read_B(std::false_type{}, b, 0u); });
   static_for<6>([&](auto a) RL_INLINE { read_A(a, 0u); });
   read_scales(0);
   auto wait_next = [&]() RL_INLINE {  // the fragments fetched across the end of a K tile
@@ -316,7 +385,6 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
     int n0;
     const GroupTile t = tile_of(w, n0);
     const bool rest = t.e >= g.experts;
-    const int ntk = rest ? 0 : nt;
     [[maybe_unused]] int wscale0 = 127, wscale1 = 127;  // scale bytes of W, a K tile a lane
     if constexpr (F8) {
       if (!rest) {
@@ -359,21 +427,17 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
       constexpr int s = decltype(s_c)::value, j = (s - kFirst) / 2;
       if constexpr (s >= kFirst && (s - kFirst) % 2 == 0 && j < LPT) issue_load(st, std::integral_constant<int, j>{});
     };
-    for (int u = 0; u < ntk; ++u) {
+    // one K tile; TAIL, NEXT: it, and the one behind it in the load stream, are of the adapter's product
+    auto k_tile = [&](auto tail_c, auto next_c) RL_INLINE {
       const uint32_t soff = (uint32_t)(st * P::STAGE_BYTES), soffn = (uint32_t)((st ^ 1) * P::STAGE_BYTES);
-      if constexpr (F8) {
-        if (__builtin_expect(u == 64, 0)) wscale0 = wscale1;
-        wsc = __builtin_amdgcn_readlane(wscale0, u & 63);
-        asm volatile("s_nop 4" : "+v"(wsc));  // (in a vector register, ahead of the products that the compiler does not know to guard)
-      }
       MC_FENCE();
       // Step 0: B blocks 0..3; A blocks 6, 7 and B blocks 4..7 are fetched, the last reads of this tile's stage.
       static_for<8>([&](auto a_c) RL_INLINE {
         constexpr int a = decltype(a_c)::value;
-        row_products(a_c, H0{}, [&](auto j_c) RL_INLINE {
+        row_products(tail_c, a_c, H0{}, [&](auto j_c) RL_INLINE {
           constexpr int s = 4 * a + decltype(j_c)::value;
           if constexpr (s < 2) read_A(std::integral_constant<int, 6 + s>{}, soff);
-          if constexpr (s >= 1 && s < 5) read_B(std::integral_constant<int, 3 + s>{}, soff);
+          if constexpr (s >= 1 && s < 5) read_B(tail_c, std::integral_constant<int, 3 + s>{}, soff);
           if constexpr (s == kFree) {  // everyone has read this tile: its stage may be refilled
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             fa[6].touch(); fa[7].touch();
@@ -387,7 +451,7 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
       // Step 1: B blocks 4..7; behind the first products the next tile has landed, and its first fragments are fetched.
       static_for<8>([&](auto a_c) RL_INLINE {
         constexpr int a = decltype(a_c)::value;
-        row_products(a_c, std::integral_constant<int, 4>{}, [&](auto j_c) RL_INLINE {
+        row_products(tail_c, a_c, std::integral_constant<int, 4>{}, [&](auto j_c) RL_INLINE {
           constexpr int s = 4 * a + decltype(j_c)::value;
           if constexpr (s == 0) {
             asm volatile("" ::: "memory");
@@ -397,52 +461,47 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
             MC_FENCE();
             read_scales(st ^ 1);
           }
-          if constexpr (s >= 1 && s < 5) read_B(std::integral_constant<int, s - 1>{}, soffn);
+          if constexpr (s >= 1 && s < 5) read_B(next_c, std::integral_constant<int, s - 1>{}, soffn);
           if constexpr (s % 4 == 3 && s < 24) read_A(std::integral_constant<int, s / 4>{}, soffn);
           refill(std::integral_constant<int, 32 + s>{});
           if constexpr (32 + s == kFirst + 2 * LPT) cursor_step();
         });
       });
       wait_next();
-      cursor_event();
-      st ^= 1;
-    }
-
-    // ---- the adapter's product (the next tile's first K tiles keep arriving meanwhile); rows and columns outside the factors and k
-    // beyond R lie past the buffers' ends
-    if (g.R > 0 && !rest) {
-      const auto factor = [&](const void* p, int64_t ld, int rows) RL_INLINE {
-        const int64_t size = ((int64_t)(rows - 1) * ld + g.R) * 2;
-        return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(size < 0x7fff0000 ? size : 0x7fff0000), 0x00020000);
-      };
-      const __amdgpu_buffer_rsrc_t rsX = factor(static_cast<const T*>(g.TA) + (int64_t)t.m0 * g.ldta, g.ldta, g.n - t.m0);
-      const __amdgpu_buffer_rsrc_t rsW = factor(static_cast<const T*>(g.TB) + t.e * g.stb + (int64_t)n0 * g.ldtb, g.ldtb, g.N - n0);
-      const int ldx = 2 * (int)g.ldta, ldw = 2 * (int)g.ldtb;
-      const int stepx = F8 ? ldx : 16 * ldx, stepw = 16 * ldw;
-#pragma unroll 1
-      for (int k0 = 0; k0 < g.R; k0 += 32) {
-        const int k = k0 + 8 * grp;
-        uint32_t offx = (uint32_t)((wm * 128 + (F8 ? 8 * s16 : s16)) * ldx + 2 * k), offw = (uint32_t)((wn * 128 + s16) * ldw + 2 * k);
-        if (k >= g.R) { offx = OOB; offw = OOB; }
-        i32x4 xb[8];
-#pragma unroll
-        for (int b = 0; b < 8; ++b) xb[b] = __builtin_amdgcn_raw_buffer_load_b128(rsW, offw + b * stepw, 0, 0);
-        static_for<2>([&](auto h_c) RL_INLINE {
-          constexpr int h = decltype(h_c)::value;
-          i32x4 xa[4];
-#pragma unroll
-          for (int a = 0; a < 4; ++a) xa[a] = __builtin_amdgcn_raw_buffer_load_b128(rsX, offx + (4 * h + a) * stepx, 0, 0);
-          // (waited for here, and not among the products, which are not the compiler's to guard)
-          asm volatile("s_nop 7" : "+v"(xb[0]), "+v"(xb[1]), "+v"(xb[2]), "+v"(xb[3]), "+v"(xb[4]), "+v"(xb[5]), "+v"(xb[6]), "+v"(xb[7]), "+v"(xa[0]), "+v"(xa[1]),
-                       "+v"(xa[2]), "+v"(xa[3]));
-          MC_FENCE();
-          static_for<32>([&](auto q_c) RL_INLINE {
-            constexpr int a = decltype(q_c)::value >> 3, b = decltype(q_c)::value & 7;
-            Elem16<T>::mma(acc[4 * h + a][b], xb[b], xa[a]);
-            MC_FENCE();
-          });
-        });
+    };
+    using Main = std::false_type;
+    using Tail = std::true_type;
+    auto scale_of = [&](int u) RL_INLINE {
+      if constexpr (F8) {
+        if (__builtin_expect(u == 64, 0)) wscale0 = wscale1;
+        wsc = __builtin_amdgcn_readlane(wscale0, u & 63);
+        asm volatile("s_nop 4" : "+v"(wsc));  // (in a vector register, ahead of the products that the compiler does not know to guard)
       }
+    };
+    // (in sequence, and not one loop over kinds: where different products meet, the compiler moves accumulators)
+    const int before = rest ? 0 : (ntail > 0 ? nt - 1 : nt);  // K tiles with another of the large product's behind them in the stream
+    auto next_tile = [&]() RL_INLINE {
+      if (__builtin_expect(clive && cu >= cnext, 0)) {
+        cursor_event();
+        cursor_point();
+      }
+      st ^= 1;
+    };
+    for (int u = 0; u < before; ++u) {
+      scale_of(u);
+      k_tile(Main{}, Main{});
+      next_tile();
+    }
+    if (ntail > 0 && !rest) {
+      scale_of(nt - 1);
+      k_tile(Main{}, Tail{});
+      next_tile();
+      for (int u = 1; u < ntail; ++u) {
+        k_tile(Tail{}, Tail{});
+        next_tile();
+      }
+      k_tile(Tail{}, Main{});
+      next_tile();
     }
     asm volatile("s_nop 7\n\ts_nop 7");  // the last products' results, read by hand below
     // ---- epilogue: 16 rows x 128 columns of the wave at a time through LDS, 16-byte pieces of 4 rows x 256 bytes out (gemm_mc64.hpp)
