@@ -246,15 +246,42 @@ int64_t share(const ExpertsDesc& d) { return ceil_div(d.n, d.experts < d.n ? d.e
 bool few(const ExpertsDesc& d) { return d.n <= 64 && d.r <= 256; }
 
 // the large product of a forward (K = i) or a backward (K = o)
-struct MainPlan { int tile, splits, per; unsigned gx; };
+struct MainPlan { int tile, splits, per; unsigned gx; bool join; };
 MainPlan main_plan(const ExpertsDesc& d, int64_t N, int64_t K, bool split) {
   MainPlan p;
   const int64_t rows = share(d);
-  p.tile = rows <= 32 ? GT_32x128 : (rows <= 96 ? GT_64x128 : GT_128x128);
-  if (!split && rows > 160 && grouped_row_tiles(d.n, d.experts, d.has_ends, 256, d.f8) * ceil_div(N, 256) >= 128 && (!d.f8 || K <= 128 * 128)) p.tile = GT_256x256;
-  const GroupedTileInfo t = grouped_tile(p.tile);
-  const int64_t tiles = grouped_row_tiles(d.n, d.experts, d.has_ends, t.bm, d.f8) * ceil_div(N, t.bn), nk = ceil_div(K, d.f8 ? 128 : 64);
+  auto tiles_of = [&](int tile) {
+    const GroupedTileInfo t = grouped_tile(tile);
+    return grouped_row_tiles(d.n, d.experts, d.has_ends, t.bm, d.f8) * ceil_div(N, t.bn);
+  };
+  // The largest tile that an expert's rows fill and of which there are enough.  Measured without adapters, 16-bit / 8-bit weights:
+  //  256 x 256 from about 200 tiles: Y of 4000 x 4096 -> 4096 (256 tiles) 107 / 70 us against 127 / 84 in 128 x 128 tiles, of 2000 rows
+  //    (128 tiles) 94 / 58 against 68 / 46;
+  //  128 x 128 from about 384: Y of 1237 x 2064 -> 5456 (430 tiles) 43 / 31 us against 58 / 42 in 64 x 128 tiles; dX of 600 x 5456 -> 2064
+  //    (85 tiles) 71 / 46 against 41 / 31;
+  //  64 x 128 from about 160: 300 x 4096 -> 4096 (160 tiles) 33 / 24 against 34 / 25 in 32 x 128 tiles, 200 x 2048 -> 2048 (64) 18 / 15
+  //    against 15.5 / 13.
+  // In between, where 64 x 128 tiles are more than the compute units and K is long enough to split 256 x 256 ones over them (below),
+  // those are faster with 16-bit weights: dX of 1237 x 5456 -> 2064 (340 tiles, 45 of them) 54 us against 74, Y of 3000 rows of 8 experts
+  // 8192 -> 1024 75 against 88; with 8-bit weights 73 against 46 and 70 against 65.
+  const int64_t nk = ceil_div(K, d.f8 ? 128 : 64);
+  const bool long_k = 3 * nk >= 160;
+  p.tile = GT_32x128;
+  if (rows > 32 && tiles_of(GT_64x128) >= 160) p.tile = GT_64x128;
+  if (rows > 96 && tiles_of(GT_128x128) >= 384) p.tile = GT_128x128;
+  if (!split && rows > 160 && (!d.f8 || K <= 128 * 128) &&
+      (tiles_of(GT_256x256) >= 208 || (p.tile == GT_64x128 && !d.f8 && long_k && tiles_of(GT_64x128) > kUnits))) p.tile = GT_256x256;
+  const int64_t tiles = tiles_of(p.tile);
   p.gx = (unsigned)(p.tile == GT_256x256 && tiles > kUnits ? kUnits : tiles);
+  p.join = false;
+  if (p.tile == GT_256x256) {  // the last round of tiles may be worth splitting; how many tiles there are only the device knows, unless all rows are one group's
+    const int64_t left = tiles % kUnits;
+    p.join = long_k && (d.has_ends || (left > 0 && left <= kUnits / 2));
+    if (p.join) p.gx = (unsigned)kUnits;
+    p.splits = 1;
+    p.per = (int)nk;
+    return p;
+  }
   int64_t s = split ? kFill / tiles : 1;
   if (s > nk / 4) s = nk / 4;
   if (s < 1) s = 1;
@@ -278,6 +305,7 @@ RankPlan rank_plan(const ExpertsDesc& d, int64_t K) {
   p.splits = (int)ceil_div(nk * 2, p.per);
   return p;
 }
+constexpr size_t kJoinBytes = (size_t)kUnits * 256 * 256 * 4;  // a tile's fp32 sums for every compute unit
 size_t rank_bytes(const ExpertsDesc& d, const RankPlan& p) { return p.splits > 1 ? (size_t)p.splits * d.n * d.r * 4 : 0; }
 
 // dA = X^T Z (wide = i), dB = T^T dY (wide = o)
@@ -311,7 +339,7 @@ struct Space {
   uint8_t *q = nullptr, *s = nullptr;  // the rounded X or dY
   int64_t ldq = 0, lds = 0;
   void *turned = nullptr, *T = nullptr, *Z = nullptr;
-  float *part = nullptr, *part_t = nullptr;
+  float *part = nullptr, *part_t = nullptr, *join = nullptr;
   int slices = 0;
   size_t bytes = 0;
 };
@@ -344,6 +372,7 @@ Space space(const ExpertsDesc& d, bool backward, void* workspace) {
     }
     w.part = static_cast<float*>(c.take(part));
   }
+  if (!(!backward && few(d)) && (!backward || d.dX != nullptr || workspace == nullptr) && main_plan(d, N, K, false).join) w.join = static_cast<float*>(c.take(kJoinBytes));
   w.bytes = c.used;
   return w;
 }
@@ -355,6 +384,7 @@ GroupedArgs rows_args(const ExpertsDesc& d) {
   a.n = (int)d.n;
   a.alpha = 1.f;
   a.splits = 1;
+  a.band = 8;
   return a;
 }
 
@@ -426,9 +456,13 @@ hipError_t main_run(const ExpertsDesc& d, bool backward, const Space& w, const v
   a.C = out; a.ldc = ldo;
   a.N = (int)N; a.K = (int)K;
   a.splits = p.splits; a.tiles_per_split = p.per;
+  // where an expert's rows are one tile, its W is read once, column tiles in order (64 rows of 16 experts 4096 -> 11008: 127 us in bands
+  // of 8 experts, 117 so); otherwise bands of row tiles share what they read of it
+  if (share(d) <= grouped_tile(p.tile).bm) a.band = 1;
   if (slices) {
     a.partial = w.part;
   } else {
+    a.partial = p.join ? w.join : nullptr;
     a.bias = backward ? nullptr : d.bias;
     if (d.r > 0) { a.TA = TA; a.ldta = ldta; a.TB = TB; a.ldtb = ldtb; a.stb = stb; a.R = (int)d.r; }
   }

@@ -39,13 +39,14 @@ struct GroupedArgs {
   int experts;
   int n, M, N, K, R;
   int splits, tiles_per_split;
+  int band;  // row tiles per band in which the output tiles are walked
   float alpha;  // C = alpha (A B) + TA TB + bias
   // builds that round A on the way (AL = 0, 16-bit): e4m3 bytes [n][ldq], zeros behind K, and scale bytes [ldq / 128][ldqs]
   uint8_t *Q, *QS;
   int64_t ldq, ldqs;
 };
 
-// what a launch runs on
+// what a launch runs on (T: a rank-r product's)
 enum GroupedTile { GT_32x128 = 0, GT_64x128, GT_128x128, GT_64x32, GT_64x64, GT_64x128T, GT_128x32, GT_128x64, GT_256x256, GT_COUNT };
 struct GroupedTileInfo { int bm, bn; };
 inline GroupedTileInfo grouped_tile(int t) {

@@ -49,8 +49,71 @@ struct GroupedMcShape {
   static constexpr int kMaxScaleTiles = 128;                 // K tiles whose scales of W two registers hold
 };
 
+// Where the output tiles are: the groups' row tiles times nbn, walked in bands of 8 row tiles, a contiguous run per XCD (gemm_mc64.hpp).
+// The tile counts of up to 64 experts stay in registers.
+template <bool F8>
+struct GroupedOrder {
+  GroupScan<256, F8> groups;
+  int nbm, nbn, total;
+  __device__ __forceinline__ void open(const GroupedArgs& g, int lane) {
+    nbn = (g.N + 255) >> 8;
+    groups.open(g.ends, g.experts, g.n, lane);
+    nbm = groups.total;
+    total = nbm * nbn;
+  }
+  template <typename Args>  // (in any address space)
+  __device__ __forceinline__ GroupTile at(const Args& g, int lane, int seq, int& n0) const {
+    const int x = seq & 7, slot = seq >> 3, q = total >> 3, rem = total & 7;
+    const int id = x * q + (x < rem ? x : rem) + slot;
+    constexpr int BAND = 8;
+    const int per_band = BAND * nbn, band = id / per_band, first_m = band * BAND;
+    const int band_rows = (nbm - first_m) < BAND ? (nbm - first_m) : BAND, in_band = id - band * per_band;
+    GroupTile out = groups.find(g.ends, g.experts, g.n, lane, first_m + in_band % band_rows);
+    // (said to the compiler: with a descriptor that it takes for a lane's own, every load becomes a loop over the lanes)
+    out.e = __builtin_amdgcn_readfirstlane(out.e);
+    out.lo = __builtin_amdgcn_readfirstlane(out.lo);
+    out.hi = __builtin_amdgcn_readfirstlane(out.hi);
+    out.m0 = __builtin_amdgcn_readfirstlane(out.m0);
+    n0 = __builtin_amdgcn_readfirstlane((in_band / band_rows) * 256);
+    return out;
+  }
+};
+
+// The last round of one tile per compute unit, where it is at most half full, has its tiles' K tiles dealt out to `splits` workgroups each,
+// which leave fp32 sums for grouped_mc_join_kernel: (1 - 1 / splits) of a round of nt K tiles of 1.5 us for a round trip of up to
+// 64 MB and a launch, together about 40 us; worth it from 60 us saved.  8192 rows of 8 experts, K = 8192 (about 288 tiles), bf16: 257 + 12 us in
+// place of 384; 16384 x 11008 -> 4096 e4m3: 735 + 14 in place of 807; where it would save 48 us (K = 4096, bf16) it gains nothing.
+// The tile count is the device's to know: both kernels decide here.
+struct GroupedSplit {
+  int whole, splits, per;  // tiles [0, whole) by themselves; the others' K tiles in `splits` runs of `per`
+};
+__device__ __forceinline__ GroupedSplit grouped_split(const GroupedArgs& g, int total, int nt) {
+  const int left = total & 255;
+  GroupedSplit s{total, 1, nt};
+  if (g.partial == nullptr || left == 0 || left > 128) return s;
+  int k = 256 / left;
+  if (k > 8) k = 8;
+  s.per = (nt + k - 1) / k;
+  s.splits = (nt + s.per - 1) / s.per;
+  if ((nt - s.per) * 3 < 120 || s.per < 4) return GroupedSplit{total, 1, nt};
+  s.whole = total - left;
+  return s;
+}
+
 template <typename T, bool F8, int BL>
-__global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
+__global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs args) {
+  // The arguments are read from the kernel's argument segment where they are used: kept in scalar registers across the K loop, they push the
+  // loop's own state out of them (17 v_readlane a K tile to fetch it back, e4m3 8 % slower).
+  typedef const __attribute__((address_space(4))) GroupedArgs* ArgPtr;
+  auto fresh = []() RL_INLINE -> ArgPtr {
+#if defined(__HIP_DEVICE_COMPILE__)
+    ArgPtr p = (ArgPtr)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return p;
+#else
+    return nullptr;
+#endif
+  };
   using P = GroupedMcShape;
   constexpr int EB = F8 ? 1 : 2, KE = 128 / EB, IPW = 8;
   constexpr bool B_STR = BL == 0;
@@ -60,39 +123,19 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1;
   const int s16 = lane & 15, grp = lane >> 4;
-  const int nbn = (g.N + 255) >> 8, nt = (g.K + KE - 1) / KE;
-
-  // ---- output tiles: the groups' row tiles times nbn, walked in bands of 8 row tiles, a contiguous run per XCD (gemm_mc64.hpp)
-  int glo, ghi, gtiles, gsum;
-  const bool one_scan = g.experts < 64;
-  gsum = group_scan<256, F8>(g.ends, g.experts, g.n, 0, lane, glo, ghi, gtiles);
-  const int nbm = one_scan ? __builtin_amdgcn_readlane(gsum, 63) : group_total<256, F8>(g.ends, g.experts, g.n, lane);
-  const int total = nbm * nbn;
-  auto tile_of = [&](int seq, int& n0) RL_INLINE -> GroupTile {
-    const int x = seq & 7, slot = seq >> 3, q = total >> 3, rem = total & 7;
-    const int id = x * q + (x < rem ? x : rem) + slot;
-    constexpr int BAND = 8;
-    const int per_band = BAND * nbn, band = id / per_band, first_m = band * BAND;
-    const int band_rows = (nbm - first_m) < BAND ? (nbm - first_m) : BAND, in_band = id - band * per_band;
-    n0 = (in_band / band_rows) * 256;
-    const int t = first_m + in_band % band_rows;
-    GroupTile out;
-    if (one_scan) {
-      const int l = __builtin_ctzll(__ballot(gsum > t));
-      out.e = l;
-      out.lo = __builtin_amdgcn_readlane(glo, l);
-      out.hi = __builtin_amdgcn_readlane(ghi, l);
-      out.m0 = (F8 ? out.lo & ~3 : out.lo) + (t - (__builtin_amdgcn_readlane(gsum, l) - __builtin_amdgcn_readlane(gtiles, l))) * 256;
-    } else {
-      out = group_find<256, F8>(g.ends, g.experts, g.n, lane, t);
-    }
-    // (said to the compiler: with a descriptor that it takes for a lane's own, every load becomes a loop over the lanes)
-    out.e = __builtin_amdgcn_readfirstlane(out.e);
-    out.lo = __builtin_amdgcn_readfirstlane(out.lo);
-    out.hi = __builtin_amdgcn_readfirstlane(out.hi);
-    out.m0 = __builtin_amdgcn_readfirstlane(out.m0);
-    n0 = __builtin_amdgcn_readfirstlane(n0);
-    return out;
+  const GroupedArgs& g0 = args;
+  const int nt = (g0.K + KE - 1) / KE;
+  GroupedOrder<F8> order;
+  order.open(g0, lane);
+  const GroupedSplit split = grouped_split(g0, order.total, nt);
+  const int nwork = split.whole + (order.total - split.whole) * split.splits;
+  // work item w: an output tile and its K tiles [u0, u1); the adapter's follow the last of them
+  auto item = [&](int w, int& n0, int& u0, int& u1) RL_INLINE -> GroupTile {
+    const bool part = w >= split.whole;
+    const int j = part ? w - split.whole : 0, tile = j / split.splits, run = j - tile * split.splits;
+    u0 = run * split.per;
+    u1 = part && u0 + split.per < nt ? u0 + split.per : nt;
+    return order.at(*fresh(), lane, part ? split.whole + tile : w, n0);
   };
 
   // ---- load cursor: the K tile of the output tile that is fetched next.  An output tile's K tiles are the nt of the large product and then
@@ -101,10 +144,11 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
   uint32_t offA[IPW], offB[IPW];
   const unsigned char *pA = nullptr, *pB = nullptr, *pS = nullptr;
   int64_t leftA = 0, leftB = 0, stepB = 0;
-  const int ntail = (g.R + 63) >> 6;
-  int cw = blockIdx.x, cu = 0, cnext = 0, leftS = 0, ce = 0, cm0 = 0, cn0 = 0;  // cnext: the K tile at which something changes
+  const int ntail = (g0.R + 63) >> 6, experts = g0.experts;
+  int cw = blockIdx.x, cu = 0, cnext = 0, cend = 0, leftS = 0, ce = 0, cm0 = 0, cn0 = 0;  // cnext: the K tile at which something changes
+  const int64_t ldsa = F8 ? g0.ldsa : 0;
   bool clive = true, in_tail = false;
-  const int kpart = g.K - g.K / KE * KE, rpart = g.R & 63;  // what the last K tile of each kind holds, 0: all of it
+  const int kpart = g0.K - g0.K / KE * KE, rpart = g0.R & 63;  // what the last K tile of each kind holds, 0: all of it
   // (what follows from the lane alone is not worth registers across the K loop)
   auto opaque_lane = [&]() RL_INLINE {
     int ln = lane;
@@ -130,56 +174,64 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
       if (((p & 7) ^ ((p >> 4) & 7)) * 16 >= bytes) off[j] |= OOB;
     }
   };
-  auto cursor_main = [&]() RL_INLINE {  // the first K tile of output tile cw, or of the next that has any; none left: loads of nothing
+  auto cursor_main = [&]() RL_INLINE -> int {  // the first K tile of work item cw, or of the next that has any; none left: loads of nothing
     GroupTile t{};
+    int u0 = 0, u1 = nt;
     for (;; cw += gridDim.x) {
-      if (cw >= total) { clive = false; break; }
-      t = tile_of(cw, cn0);
-      if (t.e < g.experts) break;
+      if (cw >= nwork) { clive = false; break; }
+      t = item(cw, cn0, u0, u1);
+      if (t.e < experts) break;
     }
+    cend = u1;
     if (!clive) {
       leftA = leftB = 0;
-      return;
+      return u0;
     }
+    const ArgPtr ga = fresh();
     ce = t.e;
     cm0 = t.m0;
-    const int rows = g.n - cm0;
-    pA = static_cast<const unsigned char*>(g.A) + (int64_t)cm0 * g.lda * EB;
-    leftA = ((int64_t)(rows - 1) * g.lda + (F8 ? (int64_t)((g.K + 127) / 128) * 128 : g.K)) * EB;
-    k_contiguous(offA, F8, rows, (int)g.lda, EB);
-    const unsigned char* const Be = static_cast<const unsigned char*>(g.B) + (int64_t)ce * g.sb * EB;
+    const int rows = ga->n - cm0;
+    pA = static_cast<const unsigned char*>(ga->A) + (int64_t)cm0 * ga->lda * EB;
+    leftA = ((int64_t)(rows - 1) * ga->lda + (F8 ? (int64_t)((ga->K + 127) / 128) * 128 : ga->K)) * EB;
+    k_contiguous(offA, F8, rows, (int)ga->lda, EB);
+    const unsigned char* const Be = static_cast<const unsigned char*>(ga->B) + (int64_t)ce * ga->sb * EB;
     if constexpr (!B_STR) {
-      pB = Be + (int64_t)cn0 * g.ldb * EB;
-      leftB = ((int64_t)(g.N - cn0 - 1) * g.ldb + g.K) * EB;
+      pB = Be + (int64_t)cn0 * ga->ldb * EB;
+      leftB = ((int64_t)(ga->N - cn0 - 1) * ga->ldb + ga->K) * EB;
       stepB = 128;
-      k_contiguous(offB, false, g.N - cn0, (int)g.ldb, EB);
+      k_contiguous(offB, false, ga->N - cn0, (int)ga->ldb, EB);
     } else {
       pB = Be + (int64_t)cn0 * EB;
-      leftB = ((int64_t)(g.K - 1) * g.ldb + g.N - cn0) * EB;
-      stepB = (int64_t)KE * g.ldb * EB;
+      leftB = ((int64_t)(ga->K - 1) * ga->ldb + ga->N - cn0) * EB;
+      stepB = (int64_t)KE * ga->ldb * EB;
       const int ln = opaque_lane();
 #pragma unroll
       for (int j = 0; j < IPW; ++j) {
         const int p = (wave * IPW + j) * 64 + ln, row = F8 ? p >> 4 : p >> 5;
         const int col = F8 ? ((p & 15) ^ grouped_swz<true, 256>(row)) * 16 : ((p & 31) ^ (4 * (row & 3))) * 8;
-        offB[j] = cn0 + col < g.N ? (uint32_t)((row * (int)g.ldb + col) * EB) + (kBias - 1024u * (j & 3)) : OOB;
+        offB[j] = cn0 + col < ga->N ? (uint32_t)((row * (int)ga->ldb + col) * EB) + (kBias - 1024u * (j & 3)) : OOB;
       }
     }
     if constexpr (F8) {
-      pS = g.SA + cm0;
-      leftS = (int)(g.ldsa - cm0);
+      pS = ga->SA + cm0;
+      leftS = (int)(ga->ldsa - cm0);
+      pS += u0 * ga->ldsa;
     }
+    pA += u0 * 128; leftA -= u0 * 128;
+    pB += u0 * stepB; leftB -= u0 * stepB;
     in_tail = false;
+    return u0;
   };
   auto cursor_tail = [&]() RL_INLINE {  // the first K tile of the adapter's product
-    const int rows = g.n - cm0;
-    pA = static_cast<const unsigned char*>(g.TA) + (int64_t)cm0 * g.ldta * 2;
-    leftA = ((int64_t)(rows - 1) * g.ldta + g.R) * 2;
-    k_contiguous(offA, F8, rows, (int)g.ldta, 2);
-    pB = static_cast<const unsigned char*>(g.TB) + (ce * g.stb + (int64_t)cn0 * g.ldtb) * 2;
-    leftB = ((int64_t)(g.N - cn0 - 1) * g.ldtb + g.R) * 2;
+    const ArgPtr ga = fresh();
+    const int rows = ga->n - cm0;
+    pA = static_cast<const unsigned char*>(ga->TA) + (int64_t)cm0 * ga->ldta * 2;
+    leftA = ((int64_t)(rows - 1) * ga->ldta + ga->R) * 2;
+    k_contiguous(offA, F8, rows, (int)ga->ldta, 2);
+    pB = static_cast<const unsigned char*>(ga->TB) + (ce * ga->stb + (int64_t)cn0 * ga->ldtb) * 2;
+    leftB = ((int64_t)(ga->N - cn0 - 1) * ga->ldtb + ga->R) * 2;
     stepB = 128;
-    k_contiguous(offB, false, g.N - cn0, (int)g.ldtb, 2);
+    k_contiguous(offB, false, ga->N - cn0, (int)ga->ldtb, 2);
     in_tail = true;
   };
   auto cut_main = [&]() RL_INLINE {  // the large product's partial K tile
@@ -193,27 +245,26 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
   // The cursor has reached cnext, and it lies ahead of the cursor again afterwards, or nothing is left.  (What several branches would assign
   // is assigned behind them: the compiler folds their stores into one through a choice of addresses, and the variables stay in memory.)
   auto cursor_event = [&]() RL_INLINE {
-    int at = cu, next = nt;
-    if (cu < nt) {
+    int at = cu, next = cend;
+    if (cu < cend) {
       cut_main();
-    } else if (!in_tail && ntail > 0) {
+    } else if (!in_tail && ntail > 0 && cend == nt) {
       cursor_tail();
       next = nt + ntail - (rpart != 0);
       if (next == at) {
         cut_tail();
         next = nt + ntail;
       }
-    } else if (cu < nt + ntail) {
+    } else if (in_tail && cu < nt + ntail) {
       cut_tail();
       next = nt + ntail;
     } else {
       cw += gridDim.x;
-      cursor_main();
-      at = 0;
-      next = nt - (kpart != 0);
-      if (next == 0) {
+      at = cursor_main();
+      next = cend - (kpart != 0 && cend == nt);
+      if (next == at) {
         if (clive) cut_main();
-        next = nt;
+        next = cend;
       }
     }
     cu = at;
@@ -225,11 +276,11 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
   };
   __amdgpu_buffer_rsrc_t rsA, rsB;
   auto cursor_point = [&]() RL_INLINE { rsA = rsrc(pA, leftA); rsB = rsrc(pB, leftB); };
-  cursor_main();
-  cnext = nt - (kpart != 0);
-  if (clive && cnext == 0) {
+  cu = cursor_main();
+  cnext = cend - (kpart != 0 && cend == nt);
+  if (clive && cnext == cu) {
     cut_main();
-    cnext = nt;
+    cnext = cend;
   }
   cursor_point();
   // load j of the cursor's K tile into stage `st`: 0..7 the A half, 8..15 the B half, 16 the scales of A
@@ -250,7 +301,7 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
     ++cu;
     pA += 128; leftA -= 128;
     pB += stepB; leftB -= stepB;
-    if constexpr (F8) pS += g.ldsa;
+    if constexpr (F8) pS += ldsa;
     cursor_point();
   };
   // ---- fragment addresses inside a stage (half h of a fragment: k 32 h + 8 grp .. + 7, or 64 h + 16 grp .. + 15 for e4m3)
@@ -381,18 +432,19 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
   wait_next();
   int st = 0;
 
-  for (int w = blockIdx.x; w < total; w += gridDim.x) {
-    int n0;
-    const GroupTile t = tile_of(w, n0);
-    const bool rest = t.e >= g.experts;
+  for (int w = blockIdx.x; w < nwork; w += gridDim.x) {
+    int n0, u0, u1;
+    const GroupTile t = item(w, n0, u0, u1);
+    const bool rest = t.e >= experts;
+    ArgPtr ga = fresh();
     [[maybe_unused]] int wscale0 = 127, wscale1 = 127;  // scale bytes of W, a K tile a lane
     if constexpr (F8) {
       if (!rest) {
-        const int nb = (n0 >> 7) + wn, blocks = B_STR ? (g.K + 127) >> 7 : (g.N + 127) >> 7;
+        const int nb = (n0 >> 7) + wn, blocks = B_STR ? (ga->K + 127) >> 7 : (ga->N + 127) >> 7;
         auto scale = [&](int kb) RL_INLINE {
           kb = kb < nt ? kb : nt - 1;
           const int ib = B_STR ? kb : nb, ob = B_STR ? nb : kb;
-          return ib < blocks && ob < g.scols ? (int)g.SB[t.e * g.ssb + (int64_t)ib * g.scols + ob] : 127;
+          return ib < blocks && ob < ga->scols ? (int)ga->SB[t.e * ga->ssb + (int64_t)ib * ga->scols + ob] : 127;
         };
         wscale0 = scale(lane);
         if (nt > 64) wscale1 = scale(64 + lane);
@@ -401,12 +453,12 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
     f32x4 start[8];  // the accumulators start with the bias
 #pragma unroll
     for (int b = 0; b < 8; ++b) start[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (g.bias != nullptr && !rest) {
+    if (ga->bias != nullptr && !rest && u0 == 0) {
 #pragma unroll
       for (int b = 0; b < 8; ++b) {
         int c = n0 + wn * 128 + 16 * b + 4 * grp;
-        c = c < g.N ? c : g.N - 4;  // (columns beyond N are never stored)
-        const i32x2 v = *reinterpret_cast<const i32x2*>(static_cast<const T*>(g.bias) + (int64_t)t.e * g.N + c);
+        c = c < ga->N ? c : ga->N - 4;  // (columns beyond N are never stored)
+        const i32x2 v = *reinterpret_cast<const i32x2*>(static_cast<const T*>(ga->bias) + (int64_t)t.e * ga->N + c);
         const T* const b4 = reinterpret_cast<const T*>(&v);
 #pragma unroll
         for (int e = 0; e < 4; ++e) start[b][e] = (float)b4[e];
@@ -416,6 +468,7 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
     if constexpr (F8) {
       __builtin_amdgcn_s_waitcnt(mc_wait_imm(0, false));
       asm volatile("" : "+v"(wscale0), "+v"(wscale1));
+      if (u0 > 64) wscale0 = wscale1;
     }
 
     // A K tile is 64 slots of 32 cycles, two steps.  Its stage is free once every wave has read its last fragments (slot kFree), and the
@@ -479,7 +532,8 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
       }
     };
     // (in sequence, and not one loop over kinds: where different products meet, the compiler moves accumulators)
-    const int before = rest ? 0 : (ntail > 0 ? nt - 1 : nt);  // K tiles with another of the large product's behind them in the stream
+    const bool tail = ntail > 0 && u1 == nt && !rest;
+    const int before = rest ? u0 : (tail ? u1 - 1 : u1);  // K tiles with another of the large product's behind them in the stream
     auto next_tile = [&]() RL_INLINE {
       if (__builtin_expect(clive && cu >= cnext, 0)) {
         cursor_event();
@@ -487,12 +541,12 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
       }
       st ^= 1;
     };
-    for (int u = 0; u < before; ++u) {
+    for (int u = u0; u < before; ++u) {
       scale_of(u);
       k_tile(Main{}, Main{});
       next_tile();
     }
-    if (ntail > 0 && !rest) {
+    if (tail) {
       scale_of(nt - 1);
       k_tile(Main{}, Tail{});
       next_tile();
@@ -504,12 +558,27 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
       next_tile();
     }
     asm volatile("s_nop 7\n\ts_nop 7");  // the last products' results, read by hand below
+    ga = fresh();
+    if (w >= split.whole) {  // fp32 sums of a run of K tiles, as the accumulators lie
+      f32x4* const part = reinterpret_cast<f32x4*>(ga->partial) + ((int64_t)(w - split.whole) * 4 + wave) * 4096 + lane;
+      static_for<64>([&](auto e_c) RL_INLINE {
+        constexpr int e = decltype(e_c)::value;
+        float x0, x1, x2, x3;
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x0) : "a"(acc[e >> 3][e & 7][0]));
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x1) : "a"(acc[e >> 3][e & 7][1]));
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x2) : "a"(acc[e >> 3][e & 7][2]));
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x3) : "a"(acc[e >> 3][e & 7][3]));
+        part[e * 64] = f32x4{x0, x1, x2, x3};
+        MC_FENCE();
+      });
+      continue;
+    }
     // ---- epilogue: 16 rows x 128 columns of the wave at a time through LDS, 16-byte pieces of 4 rows x 256 bytes out (gemm_mc64.hpp)
     const uint32_t stg = lds_base + (uint32_t)(P::STAGING + wave * 4096);
     const int rr = lane >> 4, rc = lane & 15;
     const int ncol = n0 + wn * 128 + rc * 8;
-    const bool n_ok = ncol < g.N;
-    T* const C = static_cast<T*>(g.C) + ncol;
+    const bool n_ok = ncol < ga->N;
+    T* const C = static_cast<T*>(ga->C) + ncol;
     static_for<8>([&](auto a_c) RL_INLINE {
       constexpr int a = decltype(a_c)::value;
       const uint32_t wr = stg + (uint32_t)s16 * 256u, wsw = 2u * (uint32_t)s16;
@@ -542,7 +611,7 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int r = 4 * k + rr, m = t.m0 + wm * 128 + (F8 ? 8 * r + a : 16 * a + r);
-        if (n_ok && m >= t.lo && m < t.hi) *reinterpret_cast<i32x4*>(C + (int64_t)m * g.ldc) = o[k];
+        if (n_ok && m >= t.lo && m < t.hi) *reinterpret_cast<i32x4*>(C + (int64_t)m * ga->ldc) = o[k];
       }
       MC_FENCE();
     });
@@ -552,5 +621,38 @@ __global__ __launch_bounds__(256, 1) void grouped_mc_kernel(GroupedArgs g) {
 #undef MC_FENCE
 }
 #undef RL_INLINE
+
+// The split tiles' sums added up in order, rounded and stored: a workgroup takes a sixteenth of a tile (16 of its 256 accumulator blocks).
+constexpr int kJoinPieces = 16;
+template <typename T, bool F8>
+__global__ __launch_bounds__(256) void grouped_mc_join_kernel(GroupedArgs g) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  GroupedOrder<F8> order;
+  order.open(g, lane);
+  const GroupedSplit split = grouped_split(g, order.total, (g.K + (F8 ? 127 : 63)) / (F8 ? 128 : 64));
+  const int tile = (int)blockIdx.x / kJoinPieces, piece = (int)blockIdx.x % kJoinPieces;
+  if (tile >= order.total - split.whole) return;
+  int n0;
+  const GroupTile t = order.at(g, lane, split.whole + tile, n0);
+  const f32x4* part = reinterpret_cast<const f32x4*>(g.partial) + (int64_t)tile * split.splits * 16384;
+  f32x4 sum[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) sum[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < split.splits; ++s, part += 16384) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum[k] += part[((piece * 4 + wave) * 4 + k) * 64 + lane];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int block = (piece * 4 + wave) * 4 + k;  // [wave of the tile][row block][column block]
+    const int w = block >> 6, a = (block >> 3) & 7, b = block & 7, r = lane & 15;
+    const int m = t.m0 + (w >> 1) * 128 + (F8 ? 8 * r + a : 16 * a + r), n = n0 + (w & 1) * 128 + 16 * b + 4 * (lane >> 4);
+    if (m < t.lo || m >= t.hi || n >= g.N) continue;
+    T o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = from_f32<T>(sum[k][e]);
+    *reinterpret_cast<i32x2*>(static_cast<T*>(g.C) + (int64_t)m * g.ldc + n) = *reinterpret_cast<const i32x2*>(o);
+  }
+}
 
 }  // namespace rl

@@ -29,59 +29,71 @@ struct GroupTile {
   int e, m0, lo, hi;
 };
 template <int BM, bool F8>
-__device__ __forceinline__ int group_scan(const int32_t* ends, int experts, int n, int base, int lane, int& lo, int& hi, int& tiles) {
-  const int e = base + lane;
-  auto clamped = [&](int v) { return v < 0 ? 0 : (v > n ? n : v); };
-  lo = 0;
-  hi = 0;
-  if (e < experts) {
-    hi = ends == nullptr ? n : clamped(ends[e]);
-    lo = e == 0 ? 0 : clamped(ends[e - 1]);
-  } else if (e == experts) {
-    hi = n;
-    lo = ends == nullptr ? n : clamped(ends[experts - 1]);
-  }
-  if (hi < lo) hi = lo;
-  const int first = F8 ? lo & ~3 : lo;
-  tiles = hi > lo ? (hi - first + BM - 1) / BM : 0;
-  int sum = tiles;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int v = __shfl_up(sum, d);
-    if (lane >= d) sum += v;
-  }
-  return sum;  // inclusive
+__device__ __forceinline__ int group_tiles(int lo, int hi) {
+  return hi > lo ? (hi - (F8 ? lo & ~3 : lo) + BM - 1) / BM : 0;
 }
+// The row tiles of up to 64 experts, one a lane, and of all together; further experts are scanned 64 at a time wherever a tile is looked up.
 template <int BM, bool F8>
-__device__ __forceinline__ int group_total(const int32_t* ends, int experts, int n, int lane) {
-  int total = 0;
-  for (int base = 0; base <= experts; base += 64) {
-    int lo, hi, tiles;
-    const int sum = group_scan<BM, F8>(ends, experts, n, base, lane, lo, hi, tiles);
-    total += __builtin_amdgcn_readlane(sum, 63);
-  }
-  return total;
-}
-template <int BM, bool F8>
-__device__ __forceinline__ GroupTile group_find(const int32_t* ends, int experts, int n, int lane, int t) {
-  GroupTile out{experts, 0, 0, 0};
-  for (int base = 0; base <= experts; base += 64) {
-    int lo, hi, tiles;
-    const int sum = group_scan<BM, F8>(ends, experts, n, base, lane, lo, hi, tiles);
-    const int all = __builtin_amdgcn_readlane(sum, 63);
-    if (t < all) {
-      const int l = __builtin_ctzll(__ballot(sum > t));
-      out.e = base + l;
-      out.lo = __builtin_amdgcn_readlane(lo, l);
-      out.hi = __builtin_amdgcn_readlane(hi, l);
-      const int before = __builtin_amdgcn_readlane(sum, l) - __builtin_amdgcn_readlane(tiles, l);
-      out.m0 = (F8 ? out.lo & ~3 : out.lo) + (t - before) * BM;
-      return out;
+struct GroupScan {
+  int lo, hi, tiles, sum;     // of the first 64: rows, row tiles, row tiles up to and with this one
+  int total, rest_lo;         // row tiles of all groups; where the rows behind the last expert's begin
+  __device__ __forceinline__ void scan(const int32_t* ends, int experts, int n, int base, int lane) {
+    const int e = base + lane;
+    auto clamped = [&](int v) { return v < 0 ? 0 : (v > n ? n : v); };
+    lo = hi = 0;
+    if (e < experts) {
+      hi = ends == nullptr ? n : clamped(ends[e]);
+      lo = ends == nullptr || e == 0 ? 0 : clamped(ends[e - 1]);
+      if (hi < lo) hi = lo;
     }
-    t -= all;
+    tiles = group_tiles<BM, F8>(lo, hi);
+    sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int v = __shfl_up(sum, d);
+      if (lane >= d) sum += v;
+    }
   }
-  return out;
-}
+  __device__ __forceinline__ void open(const int32_t* ends, int experts, int n, int lane) {
+    if (ends == nullptr) {  // one expert, all rows
+      const bool first = lane == 0;
+      lo = 0;
+      hi = first ? n : 0;
+      tiles = first ? (n + BM - 1) / BM : 0;
+      sum = total = (n + BM - 1) / BM;
+      rest_lo = n;
+      return;
+    }
+    total = 0;
+    for (int base = (experts - 1) & ~63; base >= 0; base -= 64) {  // (the first 64 last: theirs stay)
+      scan(ends, experts, n, base, lane);
+      total += __builtin_amdgcn_readlane(sum, 63);
+      if (base == ((experts - 1) & ~63)) rest_lo = __builtin_amdgcn_readlane(hi, (experts - 1) & 63);
+    }
+    total += group_tiles<BM, F8>(rest_lo, n);
+  }
+  // row tile t
+  __device__ __forceinline__ GroupTile find(const int32_t* ends, int experts, int n, int lane, int t) const {
+    GroupScan s = *this;
+    GroupTile out{experts, 0, rest_lo, n};
+    int before = 0;
+    for (int base = 0; base < experts; base += 64) {
+      if (base > 0) s.scan(ends, experts, n, base, lane);
+      const int all = __builtin_amdgcn_readlane(s.sum, 63);
+      if (t < before + all) {
+        const int l = __builtin_ctzll(__ballot(s.sum > t - before));
+        out.e = base + l;
+        out.lo = __builtin_amdgcn_readlane(s.lo, l);
+        out.hi = __builtin_amdgcn_readlane(s.hi, l);
+        before += __builtin_amdgcn_readlane(s.sum, l) - __builtin_amdgcn_readlane(s.tiles, l);
+        break;
+      }
+      before += all;
+    }
+    out.m0 = (F8 ? out.lo & ~3 : out.lo) + (t - before) * BM;
+    return out;
+  }
+};
 
 template <bool F8, int AL, int BL, int BM_, int BN_, int WM_, int NS_>
 struct GroupedTileShape {
@@ -127,14 +139,15 @@ __device__ __forceinline__ void grouped_mt_body(const GroupedArgs& g, const int 
   GroupTile gt;
   int m0, n0, u0, u1;
   if constexpr (AL == 0) {
-    const int nbm = group_total<BM, F8>(g.ends, g.experts, g.n, lane), total = nbm * nbn;
+    GroupScan<BM, F8> groups;
+    groups.open(g.ends, g.experts, g.n, lane);
+    const int nbm = groups.total, total = nbm * nbn;
     if (bx >= total) return;
     const int x = bx & 7, slot = bx >> 3, q = total >> 3, rem = total & 7;
-    const int id = x * q + (x < rem ? x : rem) + slot;  // a contiguous run of tiles per XCD, walked in bands of 8 row tiles
-    constexpr int BAND = 8;
-    const int per_band = BAND * nbn, band = id / per_band, first_m = band * BAND;
-    const int band_rows = (nbm - first_m) < BAND ? (nbm - first_m) : BAND, in_band = id - band * per_band;
-    gt = group_find<BM, F8>(g.ends, g.experts, g.n, lane, first_m + in_band % band_rows);
+    const int id = x * q + (x < rem ? x : rem) + slot;  // a contiguous run of tiles per XCD, walked in bands of row tiles
+    const int per_band = g.band * nbn, band = id / per_band, first_m = band * g.band;
+    const int band_rows = (nbm - first_m) < g.band ? (nbm - first_m) : g.band, in_band = id - band * per_band;
+    gt = groups.find(g.ends, g.experts, g.n, lane, first_m + in_band % band_rows);
     m0 = gt.m0;
     n0 = (in_band / band_rows) * BN;
     const int nt = gt.e < g.experts ? (g.K + KE - 1) / KE : 0;
@@ -288,6 +301,31 @@ __device__ __forceinline__ void grouped_mt_body(const GroupedArgs& g, const int 
     }
   };
 
+  // the adapter's factors, 32 of the rank at a time, straight from memory; the first ones are on their way ahead of the K loop
+  constexpr bool TAIL = AL == 0 && !ROWS && BN >= 128;
+  const bool has_tail = TAIL && g.R > 0 && !rest;
+  // row of the wave's tile that element r of block a is
+  auto row_of = [&](int a, int r) { return F8 ? r * TM + a : 16 * a + r; };
+  i32x4 tailA_regs[TAIL ? TM : 1], tailB_regs[TAIL ? TN : 1];
+  [[maybe_unused]] auto load_tail = [&](int k0) __attribute__((always_inline)) {
+    if constexpr (TAIL) {
+      const int k = k0 + 8 * grp;
+      const i32x4 zero = {0, 0, 0, 0};
+      const T* const tb = static_cast<const T*>(g.TB) + gt.e * g.stb;
+#pragma unroll
+      for (int b = 0; b < TN; ++b) {
+        const int c = n0 + wn * P::WTN + 16 * b + s16;
+        tailB_regs[b] = k < g.R && c < g.N ? *reinterpret_cast<const i32x4*>(tb + (int64_t)c * g.ldtb + k) : zero;
+      }
+#pragma unroll
+      for (int a = 0; a < TM; ++a) {
+        const int m = m0 + wm * P::WTM + row_of(a, s16);
+        tailA_regs[a] = k < g.R && m < g.n ? *reinterpret_cast<const i32x4*>(static_cast<const T*>(g.TA) + (int64_t)m * g.ldta + k) : zero;
+      }
+    }
+  };
+  if (has_tail) load_tail(0);
+
   f32x4 acc[TM][TN];  // lane l: row l % 16, columns 4 (l / 16) .. + 3 of each 16x16 block
   static_for<TM * TN>([&](auto e) { acc[decltype(e)::value / TN][decltype(e)::value % TN] = f32x4{0.f, 0.f, 0.f, 0.f}; });
 
@@ -407,30 +445,17 @@ __device__ __forceinline__ void grouped_mt_body(const GroupedArgs& g, const int 
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 
-  // row of the wave's tile that element r of block a is
-  auto row_of = [&](int a, int r) { return F8 ? r * TM + a : 16 * a + r; };
-
   // ---- the adapter's product
-  if (AL == 0 && g.R > 0 && !rest) {
-    for (int k0 = 0; k0 < g.R; k0 += 32) {
-      const int k = k0 + 8 * grp;
-      i32x4 fa[TM], fb[TN];
-      const i32x4 zero = {0, 0, 0, 0};
-      const T* const tb = static_cast<const T*>(g.TB) + gt.e * g.stb;
-#pragma unroll
-      for (int b = 0; b < TN; ++b) {
-        const int c = n0 + wn * P::WTN + 16 * b + s16;
-        fb[b] = k < g.R && c < g.N ? *reinterpret_cast<const i32x4*>(tb + (int64_t)c * g.ldtb + k) : zero;
+  if constexpr (TAIL) {
+    if (has_tail) {
+      for (int k0 = 0;;) {
+        static_for<TM * TN>([&](auto q) {
+          constexpr int a = decltype(q)::value / TN, b = decltype(q)::value % TN;
+          acc[a][b] = Mma16<T>::mma(tailB_regs[b], tailA_regs[a], acc[a][b]);
+        });
+        if ((k0 += 32) >= g.R) break;
+        load_tail(k0);
       }
-#pragma unroll
-      for (int a = 0; a < TM; ++a) {
-        const int m = m0 + wm * P::WTM + row_of(a, s16);
-        fa[a] = k < g.R && m < g.n ? *reinterpret_cast<const i32x4*>(static_cast<const T*>(g.TA) + (int64_t)m * g.ldta + k) : zero;
-      }
-      static_for<TM * TN>([&](auto q) {
-        constexpr int a = decltype(q)::value / TN, b = decltype(q)::value % TN;
-        acc[a][b] = Mma16<T>::mma(fb[b], fa[a], acc[a][b]);
-      });
     }
   }
 

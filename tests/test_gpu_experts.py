@@ -160,6 +160,63 @@ def test_large_tiles(n, experts, i, o, r, kind, fp8):
     check(Case("f16" if experts == 3 else "bf16", fp8, n, experts, i, o, r, kind, bias=(n % 1000 != 0)))
 
 
+# tiles beyond whole rounds whose K tiles are dealt out to several workgroups, in either direction: (n, experts, i, o, r, rows per expert)
+SPLIT = [(2048, 1, 4112, 9008, 24, "even"), (2500, 3, 9008, 3856, 72, "rest"), (2500, 3, 3856, 9008, 136, "uneven"), (9000, 1, 8080, 2064, 0, "even")]
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+@pytest.mark.parametrize("n,experts,i,o,r,kind", SPLIT)
+def test_split_last_round(n, experts, i, o, r, kind, fp8):
+    """Against a float64 product on the device (the host's takes minutes), on the 2-norm bound, and the same bits when called again."""
+    rl = _rl()
+    td, code = torch.bfloat16, rl.RL_BF16
+    g = torch.Generator(device="cuda").manual_seed(n)
+    X, dY = (torch.randn((n, w), generator=g, device="cuda").to(td) for w in (i, o))
+    A, B = ((torch.randn(s, generator=g, device="cuda") * v).to(td) for s, v in (((experts, i, r), i ** -0.5), ((experts, r, o), 0.3 * max(r, 1) ** -0.5)))
+    if r == 0:
+        A = B = None
+    bias = torch.randn((experts, o), generator=g, device="cuda").to(td)
+    w = torch.randn((experts, i, o), generator=g, device="cuda") * i ** -0.5
+    W = rl.Fp8Weight.quantize(w) if fp8 else w.to(td)
+    if fp8:
+        sc = torch.exp2(W.scales.double() - 127).repeat_interleave(128, 1)[:, :i].repeat_interleave(128, 2)[:, :, :o]
+        hW = W.data.view(torch.float8_e4m3fn).double() * sc
+
+        def q(x):
+            p = torch.zeros((x.shape[0], -(-x.shape[1] // 128) * 128), dtype=torch.float64, device="cuda")
+            p[:, :x.shape[1]] = x
+            p = p.view(x.shape[0], -1, 128)
+            m, e = torch.frexp(p.abs().amax(2, keepdim=True))
+            e = (e - torch.where(m > 0.875, 8, 9)).double()
+            return ((p * torch.exp2(-e)).float().to(torch.float8_e4m3fn).double() * torch.exp2(e)).view(x.shape[0], -1)[:, :x.shape[1]]
+    else:
+        hW, q = W.double(), lambda x: x
+    ends_host = np.cumsum(ref.counts(kind, n, experts, np.random.default_rng(n)))
+    ends = torch.from_numpy(ends_host.astype(np.int32)).cuda()
+    wY, wX = torch.zeros((n, o), dtype=torch.float64, device="cuda"), torch.zeros((n, i), dtype=torch.float64, device="cuda")
+    Xq, dYq, lo = q(X.double()), q(dY.double()), 0
+    for e, hi in enumerate(ends_host):
+        wY[lo:hi] = Xq[lo:hi] @ hW[e] + bias[e].double()
+        wX[lo:hi] = dYq[lo:hi] @ hW[e].t().contiguous()
+        if r:
+            wY[lo:hi] += 1.5 * (X[lo:hi].double() @ A[e].double()) @ B[e].double()
+            wX[lo:hi] += 1.5 * (dY[lo:hi].double() @ B[e].double().t().contiguous()) @ A[e].double().t().contiguous()
+        lo = hi
+    for _ in range(2):
+        Y, dX = (torch.full((n, w_), float("nan"), dtype=td, device="cuda") for w_ in (o, i))
+        ws = [torch.full((rl.runlora_experts_workspace_bytes(b, n, experts, i, o, r, code, rl.RL_FP8_B128 if fp8 else code) + 256,), 255, dtype=torch.uint8,
+                         device="cuda") for b in (False, True)]
+        rl.runlora_experts_forward(X, ends, W, A, B, Y, workspace=ws[0], scale=1.5, bias=bias)
+        rl.runlora_experts_backward(dY, X, ends, W, A, B, dX, None, None, workspace=ws[1], scale=1.5)
+        for got, want in ((Y, wY), (dX, wX)):
+            assert float((got.double() - want).norm() / want.norm()) <= TOL["bf16"]
+            rows = want.norm(dim=1)
+            assert float(((got.double() - want).norm(dim=1) - 2 * TOL["bf16"] * rows).max()) <= 0.0   # ... and no row twice that off
+        if _ == 0:
+            first = (Y, dX)
+    assert torch.equal(first[0], Y) and torch.equal(first[1], dX)
+
+
 def test_large_tiles_give_the_same_bits_again_and_under_capture():
     rl = _rl()
     n = 2600
