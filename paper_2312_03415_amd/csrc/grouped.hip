@@ -14,38 +14,57 @@ typedef __attribute__((__vector_size__(4 * sizeof(int)))) int v4;
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t pad256(int64_t b) { return (b + 255) / 256 * 256; }
 
-// out_e[o][k] = in_e[k][o]: the factor B with the contraction in its rows.  Eight k a thread, loads along o.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void turn_kernel(const T* __restrict__ in, int64_t ld, int64_t stride, T* __restrict__ out, int R, int O) {
-  const int c = (int)blockIdx.x * kThreads + threadIdx.x, k0 = (int)blockIdx.y * 8;
-  if (c >= O) return;
-  const T* p = in + blockIdx.z * stride + (int64_t)k0 * ld + c;
-  T v[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) v[k] = p[k * ld];
-  *reinterpret_cast<v4*>(out + ((int64_t)blockIdx.z * O + c) * R + k0) = *reinterpret_cast<const v4*>(v);
-}
+// Joins behind rank-r products, in one launch: up to two sets of slices, and a factor turned for the large product.
 
 // out[e][m][0..N) = alpha * sum over slices of partial[slice][e][m][0..N), in slice order; eight columns a thread
+struct SliceSum {
+  const float* partial;
+  void* out;
+  int64_t ldo, so, rows;  // rows: of all e
+  int splits, M, N, groups;  // groups: its workgroups (0: none)
+  float alpha;
+};
+// out_e[o][k] = in_e[k][o]: the factor B with the contraction in its rows; eight k a thread, loads along o
+struct Turn {
+  const void* in;
+  void* out;
+  int64_t ld, stride;
+  int R, O, groups;
+};
 template <typename T>
-__global__ __launch_bounds__(kThreads) void slices_kernel(const float* __restrict__ partial, int splits, int64_t rows, int M, int N, float alpha, T* __restrict__ out,
-                                                          int64_t ldo, int64_t so) {
-  const int64_t c = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 8, row = c / N;
-  if (row >= rows) return;
-  const int col = (int)(c - row * N);
-  const float* p = partial + row * N + col;
+__global__ __launch_bounds__(kThreads) void join_kernel(SliceSum p, SliceSum q, Turn t) {
+  int id = (int)blockIdx.x;
+  if (id < t.groups) {
+    const int cols = (t.O + kThreads - 1) / kThreads, eights = t.R / 8;
+    const int c = id % cols * kThreads + threadIdx.x, k0 = id / cols % eights * 8, e = id / cols / eights;
+    if (c >= t.O) return;
+    const T* const in = static_cast<const T*>(t.in) + e * t.stride + (int64_t)k0 * t.ld + c;
+    T v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = in[k * t.ld];
+    *reinterpret_cast<v4*>(static_cast<T*>(t.out) + ((int64_t)e * t.O + c) * t.R + k0) = *reinterpret_cast<const v4*>(v);
+    return;
+  }
+  id -= t.groups;
+  const bool second = id >= p.groups;
+  if (second) id -= p.groups;
+  const SliceSum& g = second ? q : p;
+  const int64_t c = ((int64_t)id * kThreads + threadIdx.x) * 8, row = c / g.N;
+  if (row >= g.rows) return;
+  const int col = (int)(c - row * g.N);
+  const float* part = g.partial + row * g.N + col;
   f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
 #pragma unroll 4
-  for (int k = 0; k < splits; ++k) {
-    a += *reinterpret_cast<const f32x4*>(p);
-    b += *reinterpret_cast<const f32x4*>(p + 4);
-    p += rows * N;
+  for (int k = 0; k < g.splits; ++k) {
+    a += *reinterpret_cast<const f32x4*>(part);
+    b += *reinterpret_cast<const f32x4*>(part + 4);
+    part += g.rows * g.N;
   }
-  const int64_t e = row / M, m = row - e * M;
+  const int64_t e = row / g.M, m = row - e * g.M;
   T o[8];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) { o[k] = from_f32<T>(a[k] * alpha); o[4 + k] = from_f32<T>(b[k] * alpha); }
-  *reinterpret_cast<v4*>(out + e * so + m * ldo + col) = *reinterpret_cast<const v4*>(o);
+  for (int k = 0; k < 4; ++k) { o[k] = from_f32<T>(a[k] * g.alpha); o[4 + k] = from_f32<T>(b[k] * g.alpha); }
+  *reinterpret_cast<v4*>(static_cast<T*>(g.out) + e * g.so + m * g.ldo + col) = *reinterpret_cast<const v4*>(o);
 }
 
 // expert of a row (experts: behind the last one's), the same on every lane
@@ -199,18 +218,15 @@ template <template <typename> class F, typename... Args>
 hipError_t by_type(int dtype, Args... args) {
   return dtype == DT_BF16 ? F<__bf16>::run(args...) : F<_Float16>::run(args...);
 }
+SliceSum slice_sum(const float* partial, int splits, int64_t rows, int64_t M, int64_t N, float alpha, void* out, int64_t ldo, int64_t so) {
+  return SliceSum{partial, out, ldo, so, rows, splits, (int)M, (int)N, (int)ceil_div(rows * N / 8, kThreads), alpha};
+}
 template <typename T>
-struct Turn {
-  static hipError_t run(const void* in, int64_t ld, int64_t stride, void* out, int64_t R, int64_t O, int64_t E, hipStream_t s) {
-    launch_timed(turn_kernel<T>, dim3((unsigned)ceil_div(O, kThreads), (unsigned)(R / 8), (unsigned)E), dim3(kThreads), 0, s, static_cast<const T*>(in), ld, stride,
-                 static_cast<T*>(out), (int)R, (int)O);
-    return hipGetLastError();
-  }
-};
-template <typename T>
-struct Slices {
-  static hipError_t run(const float* p, int splits, int64_t rows, int64_t M, int64_t N, float alpha, void* out, int64_t ldo, int64_t so, hipStream_t s) {
-    launch_timed(slices_kernel<T>, dim3((unsigned)ceil_div(rows * N / 8, kThreads)), dim3(kThreads), 0, s, p, splits, rows, (int)M, (int)N, alpha, static_cast<T*>(out), ldo, so);
+struct Join {
+  static hipError_t run(const SliceSum& p, const SliceSum& q, const Turn& t, hipStream_t s) {
+    const unsigned grid = (unsigned)(p.groups + q.groups + t.groups);
+    if (grid == 0) return hipSuccess;
+    launch_timed(join_kernel<T>, dim3(grid), dim3(kThreads), 0, s, p, q, t);
     return hipGetLastError();
   }
 };
@@ -231,8 +247,8 @@ struct FewFinish {
   }
 };
 
-hipError_t launch(int dtype, bool f8, int al, int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s) {
-  return dtype == DT_BF16 ? grouped_launch_bf16(f8, al, bl, tile, a, grid, s) : grouped_launch_f16(f8, al, bl, tile, a, grid, s);
+hipError_t launch(int dtype, bool f8, int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s) {
+  return dtype == DT_BF16 ? grouped_launch_bf16(f8, bl, tile, a, grid, s) : grouped_launch_f16(f8, bl, tile, a, grid, s);
 }
 
 // ---- plans: functions of sizes alone, shared by the workspace query and the call ----------------------
@@ -308,14 +324,13 @@ RankPlan rank_plan(const ExpertsDesc& d, int64_t K) {
 constexpr size_t kJoinBytes = (size_t)kUnits * 256 * 256 * 4;  // a tile's fp32 sums for every compute unit
 size_t rank_bytes(const ExpertsDesc& d, const RankPlan& p) { return p.splits > 1 ? (size_t)p.splits * d.n * d.r * 4 : 0; }
 
-// dA = X^T Z (wide = i), dB = T^T dY (wide = o)
-struct GradPlan { int tile, splits; unsigned gx; };
-GradPlan grad_plan(const ExpertsDesc& d, int64_t wide, bool wide_rows) {
+// dA = X^T Z (wide = i), dB = T^T dY (wide = o): tiles of 128 by up to 128 of the rank
+struct GradPlan { int width, splits, gx; };
+GradPlan grad_plan(const ExpertsDesc& d, int64_t wide) {
   GradPlan p;
-  p.tile = d.r <= 32 ? (wide_rows ? GT_128x32 : GT_32x128) : (d.r <= 64 ? (wide_rows ? GT_128x64 : GT_64x128) : GT_128x128);
-  const GroupedTileInfo t = grouped_tile(p.tile);
-  const int64_t tiles = d.experts * ceil_div(wide_rows ? wide : d.r, t.bm) * ceil_div(wide_rows ? d.r : wide, t.bn);
-  p.gx = (unsigned)tiles;
+  p.width = d.r <= 32 ? 32 : (d.r <= 64 ? 64 : 128);
+  const int64_t tiles = d.experts * ceil_div(wide, 128) * ceil_div(d.r, p.width);
+  p.gx = (int)tiles;
   int64_t s = kFill / tiles;
   const int64_t nk = ceil_div(share(d), 64);
   if (s > nk / 4) s = nk / 4;
@@ -367,7 +382,7 @@ Space space(const ExpertsDesc& d, bool backward, void* workspace) {
       w.turned = c.take((size_t)(d.experts * d.o * d.r) * 2);
     } else {
       w.Z = c.take((size_t)(d.n * d.r) * 2);
-      const size_t more[3] = {rank_bytes(d, rank_plan(d, d.o)), grad_bytes(d, grad_plan(d, d.i, true), d.i), grad_bytes(d, grad_plan(d, d.o, false), d.o)};
+      const size_t more[2] = {rank_bytes(d, rank_plan(d, d.o)), grad_bytes(d, grad_plan(d, d.i), d.i) + grad_bytes(d, grad_plan(d, d.o), d.o)};
       for (size_t b : more) part = part > b ? part : b;
     }
     w.part = static_cast<float*>(c.take(part));
@@ -390,7 +405,7 @@ GroupedArgs rows_args(const ExpertsDesc& d) {
 
 // T [n, r] = s A_rows F:  F = A [i, r] (X's rows) or B [r, o] read as its transpose (dY's rows)
 // `round`: the rows are also rounded to e4m3 into w.q and w.s
-hipError_t rank_run(const ExpertsDesc& d, const Space& w, const void* rows, int64_t ldrows, int64_t K, bool backward, bool round, void* out, int64_t ldo, hipStream_t stream) {
+hipError_t rank_run(const ExpertsDesc& d, const Space& w, const void* rows, int64_t ldrows, int64_t K, bool backward, bool round, void* out, int64_t ldo, const Turn& turn, hipStream_t stream) {
   float* const part = w.part;
   const RankPlan p = rank_plan(d, K);
   GroupedArgs a = rows_args(d);
@@ -407,31 +422,44 @@ hipError_t rank_run(const ExpertsDesc& d, const Space& w, const void* rows, int6
     a.Q = w.q; a.ldq = w.ldq; a.QS = w.s; a.ldqs = w.lds;
     e = d.dtype == DT_BF16 ? grouped_rows_launch_bf16(backward ? 1 : 0, p.tile, a, grid, stream) : grouped_rows_launch_f16(backward ? 1 : 0, p.tile, a, grid, stream);
   } else {
-    e = launch(d.dtype, false, 0, backward ? 1 : 0, p.tile, a, grid, stream);
+    e = launch(d.dtype, false, backward ? 1 : 0, p.tile, a, grid, stream);
   }
-  if (e == hipSuccess && p.splits > 1) e = by_type<Slices>(d.dtype, (const float*)part, p.splits, d.n, d.n, d.r, d.scale, out, ldo, (int64_t)0, stream);
-  return e;
+  if (e != hipSuccess) return e;
+  const SliceSum sum = p.splits > 1 ? slice_sum(part, p.splits, d.n, d.n, d.r, d.scale, out, ldo, 0) : SliceSum{};
+  return by_type<Join>(d.dtype, sum, SliceSum{}, turn, stream);
 }
 
-hipError_t grad_run(const ExpertsDesc& d, bool of_A, const void* T, int64_t ldt, const void* Z, float* part, hipStream_t stream) {
-  const int64_t wide = of_A ? d.i : d.o;
-  const GradPlan p = grad_plan(d, wide, of_A);
-  GroupedArgs a = rows_args(d);
-  if (of_A) {
+// dA and dB, those that are wanted
+hipError_t grads_run(const ExpertsDesc& d, const void* T, int64_t ldt, const void* Z, float* part, hipStream_t stream) {
+  GroupedArgs a = rows_args(d), b = rows_args(d);
+  const GradPlan pa = grad_plan(d, d.i), pb = grad_plan(d, d.o);
+  SliceSum sa{}, sb{};
+  int ax = 0, bx = 0;
+  if (d.dA) {
     a.A = d.X; a.lda = d.ldx; a.B = Z; a.ldb = d.r;
     a.M = (int)d.i; a.N = (int)d.r;
     a.C = d.dA; a.ldc = d.ldda; a.sc = d.sda;
-  } else {
-    a.A = T; a.lda = ldt; a.B = d.dY; a.ldb = d.lddy;
-    a.M = (int)d.r; a.N = (int)d.o;
-    a.C = d.dB; a.ldc = d.lddb; a.sc = d.sdb;
+    a.splits = pa.splits;
+    ax = pa.gx;
+    if (pa.splits > 1) {
+      a.partial = part;
+      sa = slice_sum(part, pa.splits, d.experts * d.i, d.i, d.r, 1.f, d.dA, d.ldda, d.sda);
+      part += pa.splits * d.experts * d.i * d.r;
+    }
   }
-  a.splits = p.splits;
-  a.partial = p.splits > 1 ? part : nullptr;
-  hipError_t e = launch(d.dtype, false, 1, 0, p.tile, a, dim3(p.gx, (unsigned)p.splits), stream);
-  if (e == hipSuccess && p.splits > 1)
-    e = by_type<Slices>(d.dtype, (const float*)part, p.splits, d.experts * a.M, (int64_t)a.M, (int64_t)a.N, 1.f, a.C, a.ldc, a.sc, stream);
-  return e;
+  if (d.dB) {
+    b.A = T; b.lda = ldt; b.B = d.dY; b.ldb = d.lddy;
+    b.M = (int)d.r; b.N = (int)d.o;
+    b.C = d.dB; b.ldc = d.lddb; b.sc = d.sdb;
+    b.splits = pb.splits;
+    bx = pb.gx;
+    if (pb.splits > 1) {
+      b.partial = part;
+      sb = slice_sum(part, pb.splits, d.experts * d.r, d.r, d.o, 1.f, d.dB, d.lddb, d.sdb);
+    }
+  }
+  hipError_t e = d.dtype == DT_BF16 ? grouped_grads_launch_bf16(pa.width, a, ax, b, bx, stream) : grouped_grads_launch_f16(pa.width, a, ax, b, bx, stream);
+  return e != hipSuccess ? e : by_type<Join>(d.dtype, sa, sb, Turn{}, stream);
 }
 
 // the large product: rows (rounded first where W is e4m3 and they are not yet) times W or its transpose, the adapter's product TA TB^T and the bias behind it
@@ -466,7 +494,7 @@ hipError_t main_run(const ExpertsDesc& d, bool backward, const Space& w, const v
     a.bias = backward ? nullptr : d.bias;
     if (d.r > 0) { a.TA = TA; a.ldta = ldta; a.TB = TB; a.ldtb = ldtb; a.stb = stb; a.R = (int)d.r; }
   }
-  return launch(d.dtype, d.f8, 0, backward ? 1 : 0, p.tile, a, dim3(p.gx, (unsigned)p.splits), stream);
+  return launch(d.dtype, d.f8, backward ? 1 : 0, p.tile, a, dim3(p.gx, (unsigned)p.splits), stream);
 }
 
 }  // namespace
@@ -498,8 +526,8 @@ hipError_t experts_forward(const ExpertsDesc& d, void* workspace, hipStream_t st
   void* T = d.T ? d.T : w.T;
   const int64_t ldt = d.T ? d.ldt : d.r;
   if (d.r > 0) {
-    if ((e = by_type<Turn>(d.dtype, d.B, d.ldb, d.sb, w.turned, d.r, d.o, d.experts, stream)) != hipSuccess) return e;
-    if ((e = rank_run(d, w, d.X, d.ldx, d.i, false, d.f8, T, ldt, stream)) != hipSuccess) return e;
+    const Turn turn{d.B, w.turned, d.ldb, d.sb, (int)d.r, (int)d.o, (int)(ceil_div(d.o, kThreads) * (d.r / 8) * d.experts)};
+    if ((e = rank_run(d, w, d.X, d.ldx, d.i, false, d.f8, T, ldt, turn, stream)) != hipSuccess) return e;
   }
   return main_run(d, false, w, T, ldt, w.turned, d.r, d.o * d.r, d.Y, d.ldy, false, d.r > 0, stream);
 }
@@ -510,14 +538,13 @@ hipError_t experts_backward(const ExpertsDesc& d, void* workspace, hipStream_t s
   const void* T = d.T;
   int64_t ldt = d.ldt;
   if (d.r > 0) {
-    if ((d.dX || d.dA) && (e = rank_run(d, w, d.dY, d.lddy, d.o, true, d.f8 && d.dX != nullptr, w.Z, d.r, stream)) != hipSuccess) return e;
+    if ((d.dX || d.dA) && (e = rank_run(d, w, d.dY, d.lddy, d.o, true, d.f8 && d.dX != nullptr, w.Z, d.r, Turn{}, stream)) != hipSuccess) return e;
     if (d.dB && !d.has_T) {
-      if ((e = rank_run(d, w, d.X, d.ldx, d.i, false, false, w.T, d.r, stream)) != hipSuccess) return e;
+      if ((e = rank_run(d, w, d.X, d.ldx, d.i, false, false, w.T, d.r, Turn{}, stream)) != hipSuccess) return e;
       T = w.T;
       ldt = d.r;
     }
-    if (d.dA && (e = grad_run(d, true, T, ldt, w.Z, w.part, stream)) != hipSuccess) return e;
-    if (d.dB && (e = grad_run(d, false, T, ldt, w.Z, w.part, stream)) != hipSuccess) return e;
+    if ((d.dA || d.dB) && (e = grads_run(d, T, ldt, w.Z, w.part, stream)) != hipSuccess) return e;
   }
   if (d.dX) return main_run(d, true, w, w.Z, d.r, d.A, d.lda, d.sa, d.dX, d.lddx, false, d.r > 0, stream);
   return hipSuccess;

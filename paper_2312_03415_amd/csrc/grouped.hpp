@@ -47,10 +47,10 @@ struct GroupedArgs {
 };
 
 // what a launch runs on (T: a rank-r product's)
-enum GroupedTile { GT_32x128 = 0, GT_64x128, GT_128x128, GT_64x32, GT_64x64, GT_64x128T, GT_128x32, GT_128x64, GT_256x256, GT_COUNT };
+enum GroupedTile { GT_32x128 = 0, GT_64x128, GT_128x128, GT_64x32, GT_64x64, GT_64x128T, GT_256x256, GT_COUNT };
 struct GroupedTileInfo { int bm, bn; };
 inline GroupedTileInfo grouped_tile(int t) {
-  static const GroupedTileInfo k[GT_COUNT] = {{32, 128}, {64, 128}, {128, 128}, {64, 32}, {64, 64}, {64, 128}, {128, 32}, {128, 64}, {256, 256}};
+  static const GroupedTileInfo k[GT_COUNT] = {{32, 128}, {64, 128}, {128, 128}, {64, 32}, {64, 64}, {64, 128}, {256, 256}};
   return k[t];
 }
 
@@ -64,8 +64,11 @@ inline int64_t grouped_row_tiles(int64_t n, int64_t experts, bool ends, int bm, 
 // rows: A is rounded on the way (GroupedArgs::Q)
 hipError_t grouped_rows_launch_bf16(int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s);
 hipError_t grouped_rows_launch_f16(int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s);
-hipError_t grouped_launch_bf16(bool f8, int al, int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s);
-hipError_t grouped_launch_f16(bool f8, int al, int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s);
+hipError_t grouped_launch_bf16(bool f8, int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s);
+hipError_t grouped_launch_f16(bool f8, int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s);
+// tiles of 128 x width of dA and width x 128 of dB: ax and bx of them, in their splits (0: not wanted)
+hipError_t grouped_grads_launch_bf16(int width, const GroupedArgs& ga, int ax, const GroupedArgs& gb, int bx, hipStream_t s);
+hipError_t grouped_grads_launch_f16(int width, const GroupedArgs& ga, int ax, const GroupedArgs& gb, int bx, hipStream_t s);
 
 // one layer call (experts = 1, ends = nullptr: an ordinary layer)
 struct ExpertsDesc {

@@ -511,4 +511,13 @@ __global__ __launch_bounds__(256, 2) void grouped_mt_kernel(GroupedArgs g) {
   grouped_mt_body<T, F8, AL, BL, BM, BN, WM, NS, ROWS>(g, (int)blockIdx.x, (int)blockIdx.y);
 }
 
+// dA = X^T Z and dB = T^T dY in one launch: the first ax ga.splits workgroups take dA, the others dB.  One of them alone is a launch without the
+// other's workgroups.
+template <typename T, int R, int WM, int NS, int NS2>
+__global__ __launch_bounds__(256, 2) void grouped_mt_grads_kernel(GroupedArgs ga, GroupedArgs gb, int ax, int bx) {
+  const int id = (int)blockIdx.x, first = ax * ga.splits;
+  if (id < first) grouped_mt_body<T, false, 1, 0, 128, R, WM, NS>(ga, id % ax, id / ax);
+  else grouped_mt_body<T, false, 1, 0, R, 128, (R < 64 ? 1 : 2), NS2>(gb, (id - first) % bx, (id - first) / bx);
+}
+
 }  // namespace rl
