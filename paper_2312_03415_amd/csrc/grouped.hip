@@ -283,8 +283,10 @@ MainPlan main_plan(const ExpertsDesc& d, int64_t N, int64_t K, bool split) {
   const int64_t nk = ceil_div(K, d.f8 ? 128 : 64);
   const bool long_k = 3 * nk >= 160;
   p.tile = GT_32x128;
-  if (rows > 32 && tiles_of(GT_64x128) >= 160) p.tile = GT_64x128;
-  if (rows > 96 && tiles_of(GT_128x128) >= 384) p.tile = GT_128x128;
+  // In slices of K (few rows) 64 x 128 tiles pay from 32 K tiles: 64 rows 4096 -> 11008 29 us against 33, 11008 -> 4096 33 against 35, but
+  // 2064 -> 5456 19.3 against 18.0.
+  if (rows > 32 && (split ? nk >= 32 : tiles_of(GT_64x128) >= 160)) p.tile = GT_64x128;
+  if (!split && rows > 96 && tiles_of(GT_128x128) >= 384) p.tile = GT_128x128;
   if (!split && rows > 160 && (!d.f8 || K <= 128 * 128) &&
       (tiles_of(GT_256x256) >= 208 || (p.tile == GT_64x128 && !d.f8 && long_k && tiles_of(GT_64x128) > kUnits))) p.tile = GT_256x256;
   const int64_t tiles = tiles_of(p.tile);
@@ -298,7 +300,9 @@ MainPlan main_plan(const ExpertsDesc& d, int64_t N, int64_t K, bool split) {
     p.per = (int)nk;
     return p;
   }
-  int64_t s = split ? kFill / tiles : 1;
+  // A workgroup a compute unit: what two would load faster, the sum over twice the slices takes (with the small launches around it, 64 rows
+  // 4096 -> 11008 2 slices 28.8 us, 5 30.7; 40 rows 25.0 and 26.1; 5 rows of 8 experts 2048 -> 2048 3 slices 17.2, 6 18.4).
+  int64_t s = split ? kUnits / tiles : 1;
   if (s > nk / 4) s = nk / 4;
   if (s < 1) s = 1;
   p.per = (int)ceil_div(nk, s);
@@ -340,6 +344,14 @@ GradPlan grad_plan(const ExpertsDesc& d, int64_t wide) {
 }
 size_t grad_bytes(const ExpertsDesc& d, const GradPlan& p, int64_t wide) { return p.splits > 1 ? (size_t)p.splits * d.experts * wide * d.r * 4 : 0; }
 
+// Few rows: slices of K in X A.  A workgroup's threads go around about six times at most (64 rows 11008 -> 4096 r 64 in 8 slices 41 us, in 32 35;
+// 48 rows 4096 -> 11008 r 32 in 8 28.6, in 16 27.7; 64 rows 2064 -> 5456 r 16 in 8 18.6, in 32 20.5).
+int few_slices(const ExpertsDesc& d) {
+  int s = d.n < 32 ? 16 : 8;
+  while (s < 32 && d.i * d.r > (int64_t)s * 8 * kThreads * 6) s *= 2;
+  return s;
+}
+
 // workspace layout
 struct Carver {
   char* base;
@@ -372,7 +384,7 @@ Space space(const ExpertsDesc& d, bool backward, void* workspace) {
     const MainPlan m = main_plan(d, N, K, true);
     w.part = static_cast<float*>(c.take((size_t)m.splits * d.n * N * 4));
     if (d.r > 0) {
-      w.slices = (int)(d.n >= 32 ? 8 : (d.n >= 8 ? 16 : 32));
+      w.slices = few_slices(d);
       w.part_t = static_cast<float*>(c.take((size_t)w.slices * d.n * d.r * 4));
     }
   } else if (d.r > 0) {
