@@ -13,6 +13,8 @@
 //    a ballot.  Rows and columns outside the operands are fetched from past the buffers' ends, which gives zeros.
 //  - The adapter's product is one more run of K tiles in the same stream (T and the other factor, both with the rank in their rows).
 //    With its fragments straight from memory behind the K loop, as grouped_mt.hpp has it, an output tile of r = 128 took 20 us more.
+// Rates of 8192 x 8192 -> 8192 without adapters: bf16 1.46 (Y) and 1.48 (dX) PFLOP/s, e4m3 2.50 and 2.55 with the rounding of the rows; a library
+// product reaches 1.21 / 1.36 and 2.69 on this card.
 #pragma once
 #include "grouped_mt.hpp"
 

@@ -9,8 +9,14 @@
 //  - e4m3: v_mfma_scale_f32_16x16x128_f8f6f4 takes the power-of-two scales with the operands: no vector instruction is spent on
 //    them.  A lane wants the scales of row l % 16 of every 16-row block of the wave; the wave's rows are dealt out to the blocks in
 //    turn (block a holds rows TM s + a), so that they are consecutive bytes.
-//  - The adapter's product runs behind the K loop in the same accumulators, its fragments straight from memory: T is [n, R] and the
-//    other factor is laid out [N, R], both with the contraction in the rows.
+//  - The adapter's product runs behind the K loop in the same accumulators, its fragments straight from memory, the first 32 of the rank
+//    requested ahead of the loop: T is [n, R] and the other factor is laid out [N, R], both with the contraction in the rows.
+//
+// What bounds it: what a compute unit fetches through its L1 (33 to 45 B/ns), or memory.  One row tile an expert: 64 rows of 16 experts 4096 ->
+// 11008 e4m3, W at 6.2 TB/s (117 us).  More rows: 999 of 12 experts 1032 -> 2744 f16 23 us,
+// 2000 x 4096 -> 4096 bf16 68 us (1.0 PFLOP/s).  Two workgroups a compute unit hide each other's waits: one with a ring of four stages took
+// 117 us in place of 68 there, and a second set of operand registers, read while the first is multiplied, gained nothing (24.2 us
+// against 23.9 and 42.4 against 39.6 at two small shapes, 317 against 306 for 4096 rows of 64 experts 2048 -> 8192 e4m3).
 #pragma once
 #include <type_traits>
 #include <utility>
@@ -121,7 +127,7 @@ __device__ __forceinline__ int grouped_swz(int q) {
 // ROWS: A, which a rank-r product reads once (X in T = s X A, dY in Z = s dY B^T), is rounded to e4m3 for the large product on the way: a
 // thread takes the 16-byte chunks of the tile that it loaded, keeps those of every other K tile, and rounds both halves of a block
 // of 128 columns together, the eight lanes of a row agreeing on its largest magnitude.  The pass over A that rounding would take is saved:
-// dY of 8192 x 11008 r 32 54 + 56 us in two, of 16384 x 11008 r 128 126 + 186.
+// dY of 8192 x 11008 r 32 71 us in place of 54 + 56 in two, of 16384 x 11008 r 128 178 in place of 126 + 186.
 template <typename T, bool F8, int AL, int BL, int BM, int BN, int WM, int NS, bool ROWS = false>
 __device__ __forceinline__ void grouped_mt_body(const GroupedArgs& g, const int bx, const int by) {
   static_assert(!ROWS || (!F8 && AL == 0), "a 16-bit A by rows");

@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -10,6 +11,17 @@ if ROOT not in sys.path:
 
 def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a real MI355X (runs through the C-ABI HIP library)")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def fresh_gpu_memory():
+    """Every file starts with what it holds alone: tests that measure allocated memory would otherwise see garbage of earlier files collected while they
+    measure, or count an earlier file's cached block that the allocator hands out whole."""
+    torch = sys.modules.get("torch")
+    if torch is not None and torch.cuda.is_initialized():
+        gc.collect()
+        torch.cuda.empty_cache()
+    yield
 
 
 def load_table1():
