@@ -13,7 +13,7 @@
 //    requested ahead of the loop: T is [n, R] and the other factor is laid out [N, R], both with the contraction in the rows.
 //
 // What bounds it: what a compute unit fetches through its L1 (33 to 45 B/ns), or memory.  One row tile an expert: 64 rows of 16 experts 4096 ->
-// 11008 e4m3, W at 6.2 TB/s (117 us).  More rows: 999 of 12 experts 1032 -> 2744 f16 23 us,
+// 11008 e4m3, W at 6.2 TB/s (117 us); 16 rows of 8 experts 2048 -> 8192 bf16 39 us, 6.1 TB/s.  More rows: 999 of 12 experts 1032 -> 2744 f16 23 us,
 // 2000 x 4096 -> 4096 bf16 68 us (1.0 PFLOP/s).  Two workgroups a compute unit hide each other's waits: one with a ring of four stages took
 // 117 us in place of 68 there, and a second set of operand registers, read while the first is multiplied, gained nothing (24.2 us
 // against 23.9 and 42.4 against 39.6 at two small shapes, 317 against 306 for 4096 rows of 64 experts 2048 -> 8192 e4m3).
