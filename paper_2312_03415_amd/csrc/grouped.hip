@@ -24,7 +24,10 @@ struct SliceSum {
   int splits, M, N, groups;  // groups: its workgroups (0: none)
   float alpha;
 };
-// out_e[o][k] = in_e[k][o]: the factor B with the contraction in its rows; eight k a thread, loads along o
+// out_e[o][k] = in_e[k][o]: the factor B with the contraction in its rows.  From 64 rows a workgroup turns 64 x 64 in LDS, so that loads and
+// stores are runs of 128 bytes (8 experts, 128 x 11008, with the slices of 16384 x 128 beside it: 15 us, 28 directly); below that a thread
+// takes eight rows of a column (64 experts, 16 x 8192: 9 us, 12 through LDS).
+constexpr int kTurnRows = 64;
 struct Turn {
   const void* in;
   void* out;
@@ -33,8 +36,9 @@ struct Turn {
 };
 template <typename T>
 __global__ __launch_bounds__(kThreads) void join_kernel(SliceSum p, SliceSum q, Turn t) {
+  __shared__ __attribute__((aligned(16))) T tile[64][72];
   int id = (int)blockIdx.x;
-  if (id < t.groups) {
+  if (id < t.groups && t.R < kTurnRows) {
     const int cols = (t.O + kThreads - 1) / kThreads, eights = t.R / 8;
     const int c = id % cols * kThreads + threadIdx.x, k0 = id / cols % eights * 8, e = id / cols / eights;
     if (c >= t.O) return;
@@ -43,6 +47,26 @@ __global__ __launch_bounds__(kThreads) void join_kernel(SliceSum p, SliceSum q, 
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = in[k * t.ld];
     *reinterpret_cast<v4*>(static_cast<T*>(t.out) + ((int64_t)e * t.O + c) * t.R + k0) = *reinterpret_cast<const v4*>(v);
+    return;
+  }
+  if (id < t.groups) {
+    const int cols = (t.O + 63) / 64, ks = (t.R + 63) / 64;
+    const int c0 = id % cols * 64, k0 = id / cols % ks * 64, e = id / cols / ks, kn = t.R - k0 < 64 ? t.R - k0 : 64;
+    const T* const in = static_cast<const T*>(t.in) + e * t.stride + (int64_t)k0 * t.ld + c0;
+    for (int q = threadIdx.x; q < kn * 8; q += kThreads) {
+      const int k = q >> 3, c = (q & 7) * 8;
+      if (c0 + c >= t.O) continue;
+      const v4 v = *reinterpret_cast<const v4*>(in + k * t.ld + c);
+      const T* const w = reinterpret_cast<const T*>(&v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) tile[c + j][k] = w[j];
+    }
+    __syncthreads();
+    T* const out = static_cast<T*>(t.out) + ((int64_t)e * t.O + c0) * t.R + k0;
+    for (int q = threadIdx.x; q < 8 * kn; q += kThreads) {
+      const int c = q / (kn / 8), k = q % (kn / 8) * 8;
+      if (c0 + c < t.O) *reinterpret_cast<v4*>(out + (int64_t)c * t.R + k) = *reinterpret_cast<const v4*>(&tile[c][k]);
+    }
     return;
   }
   id -= t.groups;
@@ -538,7 +562,7 @@ hipError_t experts_forward(const ExpertsDesc& d, void* workspace, hipStream_t st
   void* T = d.T ? d.T : w.T;
   const int64_t ldt = d.T ? d.ldt : d.r;
   if (d.r > 0) {
-    const Turn turn{d.B, w.turned, d.ldb, d.sb, (int)d.r, (int)d.o, (int)(ceil_div(d.o, kThreads) * (d.r / 8) * d.experts)};
+    const Turn turn{d.B, w.turned, d.ldb, d.sb, (int)d.r, (int)d.o, (int)((d.r < kTurnRows ? ceil_div(d.o, kThreads) * (d.r / 8) : ceil_div(d.o, 64) * ceil_div(d.r, 64)) * d.experts)};
     if ((e = rank_run(d, w, d.X, d.ldx, d.i, false, d.f8, T, ldt, turn, stream)) != hipSuccess) return e;
   }
   return main_run(d, false, w, T, ldt, w.turned, d.r, d.o * d.r, d.Y, d.ldy, false, d.r > 0, stream);
