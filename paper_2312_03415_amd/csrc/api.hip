@@ -396,6 +396,7 @@ int experts_forward_impl(const rl_tensor_t* X, const int32_t* ends, const rl_sta
   if ((rc = check_tensor(Y, n, o, X->dtype)) != RL_OK) return rc;
   if (T && !A) return RL_ERR_SHAPE;
   if (T && (rc = check_tensor(T, n, r, X->dtype)) != RL_OK) return rc;
+  if (T && T->ld > kMaxLd) return RL_ERR_UNSUPPORTED;  // (the large product reads it)
   if (opts && opts->dropout_p != 0.f) return RL_ERR_UNSUPPORTED;
   const void* bias = opts ? opts->bias : nullptr;
   if ((reinterpret_cast<uintptr_t>(bias) & 15) != 0) return RL_ERR_ALIGN;
