@@ -306,6 +306,18 @@ def stack_desc(t):
     return rl_stack_t(t.data_ptr(), experts, rows, cols, strides[1], strides[0], dtype_code(t.dtype), None, 0)
 
 
+def _one_gpu(first, *others):
+    """Refuses operands (None, tensors, Fp8Weights) that are not all in one GPU's memory: a kernel would read an address of the host's."""
+    device = first.get_device()
+    if device < 0:
+        raise ValueError(f"operands must be on a GPU, not on {first.device}")
+    for t in others:
+        if isinstance(t, Fp8Weight):
+            t = t.data  # (its scales are where they are)
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"operands must be on one GPU: {t.device}, not {first.device}")
+
+
 def _ends(ends, experts):
     import torch
     if ends.dtype != torch.int32 or ends.dim() != 1 or ends.numel() != experts or ends.stride(0) != 1:
@@ -338,6 +350,8 @@ def runlora_forward(variant, X, W, A, B, Y, saved, workspace=None, stream=None, 
     dropout_p / dropout_seed: LoRA dropout on the adapter's input (mask defined in runlora.h), None = off."""
     if bias is not None and (bias.dtype != X.dtype or bias.numel() != Y.shape[1]):
         raise ValueError("bias must have d_out elements of the activation dtype")
+    if isinstance(W, Fp8Weight):
+        _one_gpu(X, W, A, B, Y, workspace, bias)
     dx, dw, da, db, dy = (tensor_desc(t) for t in (X, W, A, B, Y))
     o = _opts(workspace, stream, scale, bias, dropout_p, dropout_seed)
     _check(lib().runlora_forward(variant, _ref(dx), _ref(dw), _ref(da), _ref(db), _ref(dy), ctypes.byref(saved),
@@ -354,6 +368,8 @@ def runlora_forward_static(variant, X, W, A, B, Y, saved, stream=None, scale=Non
     device allocation); raises RL_ERR_WORKSPACE if the call needs more than STATIC_SCRATCH_BYTES."""
     if bias is not None and (bias.dtype != X.dtype or bias.numel() != Y.shape[1]):
         raise ValueError("bias must have d_out elements of the activation dtype")
+    if isinstance(W, Fp8Weight):
+        _one_gpu(X, W, A, B, Y, bias)
     dx, dw, da, db, dy = (tensor_desc(t) for t in (X, W, A, B, Y))
     o = _opts(None, stream, scale, bias, dropout_p, dropout_seed)
     _check(lib().runlora_forward_static(variant, _ref(dx), _ref(dw), _ref(da), _ref(db), _ref(dy), ctypes.byref(saved),
@@ -363,6 +379,8 @@ def runlora_forward_static(variant, X, W, A, B, Y, saved, stream=None, scale=Non
 
 def runlora_backward(variant, dY, saved, W, A, B, dX, dA, dB, workspace=None, stream=None):
     """Gradients of Eq. 3 in backward graph `variant`; any of dX/dA/dB may be None (skipped)."""
+    if isinstance(W, Fp8Weight):
+        _one_gpu(dY, W, A, B, dX, dA, dB, workspace)
     ddy, dw, da, db = (tensor_desc(t) for t in (dY, W, A, B))
     gx, ga, gb = tensor_desc(dX), tensor_desc(dA), tensor_desc(dB)
     o = _opts(workspace, stream)
@@ -448,6 +466,7 @@ def runlora_fp8_quantize(src, data, scales, stream=None):
         raise ValueError("data must be bytes of src's shape with contiguous rows")
     if scales.element_size() != 1 or tuple(scales.shape) != ((rows + 127) // 128, (cols + 127) // 128) or not scales.is_contiguous():
         raise ValueError("scales must be dense bytes, one per 128 x 128 block")
+    _one_gpu(src, data, scales)
     d = rl_tensor_t(data.data_ptr(), rows, cols, data.stride(0), RL_FP8_B128, scales.data_ptr(), 128)
     o = _opts(None, stream)
     _check(lib().runlora_fp8_quantize(_ref(tensor_desc(src)), ctypes.byref(d), ctypes.byref(o)))
@@ -462,6 +481,7 @@ def runlora_experts_forward(X, ends, W, A, B, Y, T=None, workspace=None, stream=
         if bias.dtype != X.dtype or tuple(bias.shape) != (W.shape[0], Y.shape[1]) or not bias.is_contiguous():
             raise ValueError("bias must be dense [experts, d_out] of the activation dtype")
         bias = bias.view(-1)
+    _one_gpu(X, ends, W, A, B, Y, T, workspace, bias)
     dx, dw, da, db, dy, dt = tensor_desc(X), stack_desc(W), stack_desc(A), stack_desc(B), tensor_desc(Y), tensor_desc(T)
     o = _opts(workspace, stream, scale, bias)
     _check(lib().runlora_experts_forward(_ref(dx), _ends(ends, W.shape[0]), _ref(dw), _ref(da), _ref(db), _ref(dy), _ref(dt), ctypes.byref(o)))
@@ -470,6 +490,7 @@ def runlora_experts_forward(X, ends, W, A, B, Y, T=None, workspace=None, stream=
 
 def runlora_experts_backward(dY, X, ends, W, A, B, dX, dA, dB, T=None, workspace=None, stream=None, scale=None):
     """Gradients of runlora_experts_forward; any of dX / dA / dB may be None.  T: scale XA as the forward left it, or None."""
+    _one_gpu(dY, X, ends, W, A, B, dX, dA, dB, T, workspace)
     ddy, dx, dw, da, db, dt = tensor_desc(dY), tensor_desc(X), stack_desc(W), stack_desc(A), stack_desc(B), tensor_desc(T)
     gx, ga, gb = tensor_desc(dX), stack_desc(dA), stack_desc(dB)
     o = _opts(workspace, stream, scale)

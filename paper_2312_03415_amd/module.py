@@ -442,7 +442,7 @@ class RunLoRAExpertsFunction(torch.autograd.Function):
         dA = make(A.shape, dtype=A.dtype, device=A.device) if need[3] else None
         dB = make(B.shape, dtype=B.dtype, device=B.device) if need[4] else None
         if n > 0:
-            for t in (x2, ends, A, B, T):
+            for t in ctx.saved_tensors:
                 if t is not None and t.device != dy.device:
                     raise ValueError(f"a saved tensor came back on another device: {t.device}, not {dy.device}")
             code = rl.dtype_code(dy.dtype)
@@ -488,7 +488,7 @@ class RunLoRAFp8Function(torch.autograd.Function):
         dA = make(A.shape, dtype=A.dtype, device=A.device) if need_a else None
         dB = make(B.shape, dtype=B.dtype, device=B.device) if need_b else None
         if n > 0:
-            saved, x2 = _reread(ctx.saved, dy2, x2, A, B, T)
+            saved, x2 = _reread(ctx.saved, dy2, x2, A, B, T, data, scales)
             if saved.T != T.data_ptr() or saved.ldt != T.stride(0):
                 saved = type(saved).from_buffer_copy(saved)
                 saved.T, saved.ldt = T.data_ptr(), T.stride(0)

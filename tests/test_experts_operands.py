@@ -26,3 +26,92 @@ def test_rows_of_a_kept_product_in_the_layer_call(ld, code):
     saved, opts = rl.rl_saved_t(), rl.rl_opts_t(None, next(ADDRESS), 16)
     saved.T, saved.ldt = 1 << 45, ld
     assert rl.lib().runlora_forward(rl.FWD1, *(ctypes.byref(t) for t in (X, W, A, B, Y, saved, opts))) == code
+
+
+# ---- operands in host memory, whose addresses a kernel must never get ----------------------------------------------------
+
+def _operands(torch, fp8):
+    """Operands of both directions by name, all on the host."""
+    n, E, i, o, r = 40, 3, 256, 272, 16
+    z = lambda *shape, dtype=torch.bfloat16: torch.zeros(shape, dtype=dtype)
+    W = rl.Fp8Weight(z(E, i, o, dtype=torch.uint8), z(E, 2, 3, dtype=torch.uint8), i, o) if fp8 else z(E, i, o)
+    return dict(X=z(n, i), ends=z(E, dtype=torch.int32), W=W, A=z(E, i, r), B=z(E, r, o), Y=z(n, o), T=z(n, r), dY=z(n, o), dX=z(n, i), dA=z(E, i, r),
+                dB=z(E, r, o), bias=z(E, o), workspace=z(1 << 20, dtype=torch.uint8))
+
+
+def _on(t, device):
+    """The operand as a tensor that says it is on `device`."""
+    return rl.Fp8Weight(t.data.to(device), t.scales.to(device), t.rows, t.cols) if isinstance(t, rl.Fp8Weight) else t.to(device)
+
+
+FORWARD = ("X", "ends", "W", "A", "B", "Y", "T", "workspace", "bias")
+BACKWARD = ("dY", "X", "ends", "W", "A", "B", "dX", "dA", "dB", "T", "workspace")
+
+
+@pytest.fixture
+def no_library(monkeypatch):
+    """No call may get as far as the library."""
+    def refuse():
+        raise AssertionError("the call was not refused")
+    monkeypatch.setattr(rl, "lib", refuse)
+    monkeypatch.setattr(rl, "_current_stream", refuse)
+
+
+def _fake_gpu(torch):
+    from torch._subclasses.fake_tensor import FakeTensorMode  # (tensors without storage that say they are on a GPU)
+    return FakeTensorMode(allow_non_fake_inputs=True)
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+@pytest.mark.parametrize("call,names", [("forward", FORWARD), ("backward", BACKWARD)])
+def test_an_operand_on_the_host_is_refused(call, names, fp8, no_library):
+    torch = pytest.importorskip("torch")
+    fn = getattr(rl, "runlora_experts_" + call)
+    t = _operands(torch, fp8)
+    with pytest.raises(ValueError, match="GPU"):
+        fn(**{k: t[k] for k in names})
+    with _fake_gpu(torch):
+        gpu = {k: _on(v, "cuda") for k, v in t.items()}
+        for name in names:
+            with pytest.raises(ValueError, match="GPU"):
+                fn(**{k: (t if k == name else gpu)[k] for k in names})
+
+
+@pytest.mark.parametrize("call", ["runlora_forward", "runlora_forward_static", "runlora_backward"])
+def test_an_operand_of_the_8_bit_layer_on_the_host_is_refused(call, no_library):
+    torch = pytest.importorskip("torch")
+    E = _operands(torch, True)
+    t = {k: (rl.Fp8Weight(E["W"].data[0], E["W"].scales[0], 256, 272) if k == "W" else E[k][0] if k in ("A", "B", "dA", "dB", "bias") else E[k]) for k in E}
+    names = {"runlora_forward": ("X", "W", "A", "B", "Y", "workspace", "bias"), "runlora_forward_static": ("X", "W", "A", "B", "Y", "bias"),
+             "runlora_backward": ("dY", "W", "A", "B", "dX", "dA", "dB", "workspace")}[call]
+    fn = lambda ops: getattr(rl, call)(1, saved=rl.rl_saved_t(), **ops)
+    with pytest.raises(ValueError, match="GPU"):
+        fn({k: t[k] for k in names})
+    with _fake_gpu(torch):
+        gpu = {k: _on(v, "cuda") for k, v in t.items()}
+        for name in names:
+            with pytest.raises(ValueError, match="GPU"):
+                fn({k: (t if k == name else gpu)[k] for k in names})
+
+
+def test_a_weight_on_the_host_is_not_quantised(no_library):
+    """A model is often built on the host and moved behind that: the layer over its 8-bit weight has to be made on the GPU."""
+    torch = pytest.importorskip("torch")
+    from paper_2312_03415_amd.module import RunLoRAFp8Linear
+    with pytest.raises(ValueError, match="GPU"):
+        rl.Fp8Weight.quantize(torch.zeros(2, 256, 272))
+    with pytest.raises(ValueError, match="GPU"):
+        RunLoRAFp8Linear.from_linear(torch.nn.Linear(256, 272).bfloat16(), 16)
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["dense", "fp8"])
+def test_layers_refuse_rows_on_the_host(fp8):
+    torch = pytest.importorskip("torch")
+    from paper_2312_03415_amd import module
+    t = _operands(torch, fp8)
+    with pytest.raises(ValueError, match="GPU"):
+        module.RunLoRAExpertsFunction.apply(t["X"], t["ends"], t["W"], t["A"], t["B"], None, 1.0)
+    if fp8:
+        W = rl.Fp8Weight(t["W"].data[0], t["W"].scales[0], 256, 272)
+        with pytest.raises(ValueError, match="GPU"):
+            module.RunLoRAFp8Function.apply(t["X"], W, t["A"][0], t["B"][0], None, 1.0)
