@@ -52,6 +52,14 @@ def _native():
     return _native_module
 
 
+def _rows(x, width):
+    """x as a matrix [n, width] that the library can read."""
+    x2 = x.reshape(-1, width)
+    if x2.stride(-1) != 1 or x2.stride(0) % 8 != 0 or x2.stride(0) < width or x2.data_ptr() % 16 != 0:
+        x2 = x2.contiguous()
+    return x2
+
+
 def _reread(saved, dy, x2, *others):
     """The forward's record for the input as autograd hands it back (and that input): a saved-tensor hook may have moved it or
     laid it out anew, so the pointer the forward recorded need not be x2's."""
@@ -61,8 +69,7 @@ def _reread(saved, dy, x2, *others):
             raise ValueError(f"a saved tensor came back on another device: {t.device}, not {dy.device}")
     if x2.data_ptr() == saved.X and x2.stride() == (saved.ldx, 1) and x2.dtype == dy.dtype:
         return saved, x2  # as it was
-    if x2.stride(-1) != 1 or x2.stride(0) % 8 != 0 or x2.data_ptr() % 16 != 0:
-        x2 = x2.contiguous()
+    x2 = _rows(x2, saved.i)
     saved = type(saved).from_buffer_copy(saved)
     saved.X, saved.ldx, saved.dtype = x2.data_ptr(), x2.stride(0), rl.dtype_code(x2.dtype)
     return saved, x2
@@ -91,9 +98,7 @@ class RunLoRAFunction(torch.autograd.Function):
         fwd, bwd = pair
         i, o = W.shape
         r = A.shape[1]
-        x2 = x.reshape(-1, i)
-        if x2.stride(-1) != 1 or x2.stride(0) % 8 != 0 or x2.data_ptr() % 16 != 0:
-            x2 = x2.contiguous()
+        x2 = _rows(x, i)
         n = x2.shape[0]
         code = rl.dtype_code(x.dtype)
         y = torch.empty((n, o), dtype=x.dtype, device=x.device)
@@ -120,9 +125,7 @@ class RunLoRAFunction(torch.autograd.Function):
         i, o = W.shape
         r = A.shape[1]
         n = x2.shape[0]
-        dy2 = dy.reshape(n, o)
-        if dy2.stride(-1) != 1 or dy2.stride(0) % 8 != 0 or dy2.data_ptr() % 16 != 0:
-            dy2 = dy2.contiguous()
+        dy2 = _rows(dy, o)
         need_x, _, need_a, need_b = ctx.needs_input_grad[:4]
         dx = torch.empty((n, i), dtype=x2.dtype, device=x2.device) if need_x else None
         dA = torch.empty_like(A) if need_a else None
@@ -211,9 +214,7 @@ class RunVeRAFunction(torch.autograd.Function):
         fwd, bwd = pair
         i, o = W.shape
         r = A.shape[1]
-        x2 = x.reshape(-1, i)
-        if x2.stride(-1) != 1 or x2.stride(0) % 8 != 0 or x2.data_ptr() % 16 != 0:
-            x2 = x2.contiguous()
+        x2 = _rows(x, i)
         n = x2.shape[0]
         code = rl.dtype_code(x.dtype)
         y = torch.empty((n, o), dtype=x.dtype, device=x.device)
@@ -235,9 +236,7 @@ class RunVeRAFunction(torch.autograd.Function):
         i, o = W.shape
         r = A.shape[1]
         n = x2.shape[0]
-        dy2 = dy.reshape(n, o)
-        if dy2.stride(-1) != 1 or dy2.stride(0) % 8 != 0 or dy2.data_ptr() % 16 != 0:
-            dy2 = dy2.contiguous()
+        dy2 = _rows(dy, o)
         need = ctx.needs_input_grad
         dx = torch.empty((n, i), dtype=x2.dtype, device=x2.device) if need[0] else None
         dd = torch.empty_like(d) if need[4] else None
@@ -304,9 +303,7 @@ class RunDoRAFunction(torch.autograd.Function):
     def forward(ctx, x, W, A, B, m, bias, scale, bwd):
         i, o = W.shape
         r = A.shape[1]
-        x2 = x.reshape(-1, i)
-        if x2.stride(-1) != 1 or x2.stride(0) % 8 != 0 or x2.data_ptr() % 16 != 0:
-            x2 = x2.contiguous()
+        x2 = _rows(x, i)
         n = x2.shape[0]
         code = rl.dtype_code(x.dtype)
         y = torch.empty((n, o), dtype=x.dtype, device=x.device)
@@ -328,9 +325,7 @@ class RunDoRAFunction(torch.autograd.Function):
         i, o = W.shape
         r = A.shape[1]
         n = x2.shape[0]
-        dy2 = dy.reshape(n, o)
-        if dy2.stride(-1) != 1 or dy2.stride(0) % 8 != 0 or dy2.data_ptr() % 16 != 0:
-            dy2 = dy2.contiguous()
+        dy2 = _rows(dy, o)
         need = ctx.needs_input_grad
         dx = torch.empty((n, i), dtype=x2.dtype, device=x2.device) if need[0] else None
         dA = torch.empty_like(A) if need[2] else None
@@ -385,14 +380,6 @@ class RunDoRALinear(nn.Module):
 
     def extra_repr(self):
         return f"d_in={self.d_in}, d_out={self.d_out}, r={self.r}, scale={self.scale:g}, bias={self.bias is not None}"
-
-
-def _rows(x, width):
-    """x as a matrix [n, width] that the library can read."""
-    x2 = x.reshape(-1, width)
-    if x2.stride(-1) != 1 or x2.stride(0) % 8 != 0 or x2.stride(0) < width or x2.data_ptr() % 16 != 0:
-        x2 = x2.contiguous()
-    return x2
 
 
 def _w_code(W, code):

@@ -115,3 +115,16 @@ def test_layers_refuse_rows_on_the_host(fp8):
         W = rl.Fp8Weight(t["W"].data[0], t["W"].scales[0], 256, 272)
         with pytest.raises(ValueError, match="GPU"):
             module.RunLoRAFp8Function.apply(t["X"], W, t["A"][0], t["B"][0], None, 1.0)
+
+
+def test_rows_that_the_library_does_not_read_are_laid_out_anew():
+    torch = pytest.importorskip("torch")
+    from paper_2312_03415_amd.module import _rows
+    dense = torch.randn(6, 48).bfloat16()
+    one = dense[0]
+    padded = torch.randn(6, 56).bfloat16()[:, :48]
+    assert _rows(dense, 48) is not None and _rows(dense, 48).data_ptr() == dense.data_ptr()
+    assert _rows(padded, 48).data_ptr() == padded.data_ptr()
+    for x in (one.expand(6, 48), dense.t().contiguous().t(), torch.randn(6, 50).bfloat16()[:, :48], padded[:, ::2]):
+        r = _rows(x, x.shape[-1])
+        assert torch.equal(r, x) and r.stride(1) == 1 and r.stride(0) >= x.shape[-1] and r.stride(0) % 8 == 0 and r.data_ptr() % 16 == 0
