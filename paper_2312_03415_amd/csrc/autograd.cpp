@@ -80,7 +80,8 @@ rl_tensor_t saved_desc(const at::Tensor& t, const at::Tensor& x) {
 // rows as the library takes them (the same test as the Python node's)
 at::Tensor rows(const at::Tensor& t, int64_t cols) {
   at::Tensor r = t.reshape({-1, cols});
-  if (r.stride(-1) != 1 || r.stride(0) % 8 != 0 || r.stride(0) < cols || reinterpret_cast<uintptr_t>(r.data_ptr()) % 16 != 0) r = r.contiguous();
+  if (r.stride(-1) != 1 || r.stride(0) % 8 != 0 || r.stride(0) < cols || reinterpret_cast<uintptr_t>(r.data_ptr()) % 16 != 0)
+    r = r.clone(at::MemoryFormat::Contiguous);  // (contiguous() would hand dense rows at an odd address back as they are)
   return r;
 }
 

@@ -56,7 +56,7 @@ def _rows(x, width):
     """x as a matrix [n, width] that the library can read."""
     x2 = x.reshape(-1, width)
     if x2.stride(-1) != 1 or x2.stride(0) % 8 != 0 or x2.stride(0) < width or x2.data_ptr() % 16 != 0:
-        x2 = x2.contiguous()
+        x2 = x2.clone(memory_format=torch.contiguous_format)  # (contiguous() would hand dense rows at an odd address back as they are)
     return x2
 
 

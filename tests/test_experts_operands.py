@@ -128,3 +128,12 @@ def test_rows_that_the_library_does_not_read_are_laid_out_anew():
     for x in (one.expand(6, 48), dense.t().contiguous().t(), torch.randn(6, 50).bfloat16()[:, :48], padded[:, ::2]):
         r = _rows(x, x.shape[-1])
         assert torch.equal(r, x) and r.stride(1) == 1 and r.stride(0) >= x.shape[-1] and r.stride(0) % 8 == 0 and r.data_ptr() % 16 == 0
+
+
+def test_rows_that_only_look_dense_are_laid_out_anew():
+    """Dense rows at an odd address, and a single row whose distance to the next (that is not there) is odd: contiguous as torch counts."""
+    torch = pytest.importorskip("torch")
+    from paper_2312_03415_amd.module import _rows
+    for x in (torch.randn(6 * 48 + 8).bfloat16()[1:1 + 6 * 48].view(6, 48), torch.randn(2, 49).bfloat16()[:1, :48]):
+        r = _rows(x, 48)
+        assert x.is_contiguous() and torch.equal(r, x) and r.stride(0) % 8 == 0 and r.data_ptr() % 16 == 0

@@ -66,3 +66,34 @@ def test_an_input_that_repeats_over_the_rows(kind, node):
     got, = torch.autograd.grad(f(a.expand(90, -1)), a, dy)
     want, = torch.autograd.grad(f(b), b, dy)
     assert torch.equal(got, want.sum(0, keepdim=True))
+
+
+def odd_address(t):
+    """The same dense rows at an address that is two bytes off."""
+    flat = torch.empty(t.numel() + 8, dtype=t.dtype, device=t.device)
+    out = flat[1:1 + t.numel()].view(t.shape)
+    out.copy_(t)
+    assert out.is_contiguous() and out.data_ptr() % 16 != 0
+    return out
+
+
+def odd_distance(t):
+    """One row of a matrix with a column more (which counts as contiguous, whatever its rows' distance)."""
+    assert t.shape[0] == 1
+    out = torch.empty(2, t.shape[1] + 1, dtype=t.dtype, device=t.device)[:1, :t.shape[1]]
+    out.copy_(t)
+    assert out.is_contiguous() and out.stride(0) % 8 != 0
+    return out
+
+
+@pytest.mark.parametrize("node", ["native", "python"])
+@pytest.mark.parametrize("kind", LAYERS)
+@pytest.mark.parametrize("n,off", [(90, odd_address), (1, odd_address), (1, odd_distance)])
+def test_rows_that_only_look_dense(kind, node, n, off):
+    f, x, dy = layer(kind, node, n), rows(n, D_IN, 2).requires_grad_(True), rows(n, D_OUT, 1)
+    y = f(x)
+    want, = torch.autograd.grad(y, x, dy)
+    xo = off(x.detach()).requires_grad_(True)
+    got = f(xo)
+    assert torch.equal(got, y)
+    assert torch.equal(torch.autograd.grad(got, xo, off(dy))[0], want)
