@@ -381,8 +381,7 @@ struct ExpertsNode : public torch::autograd::Function<ExpertsNode> {
     const rl_tensor_t dx = desc(x2, code);
     rl_tensor_t dy = desc(y, code), dt = desc(T, code);
     check(p_experts_forward(&dx, ends_of(e, dw.experts, x), &dw, &da, &db, &dy, &dt, &opts));
-    ctx->save_for_backward({x2, A, B, W, s, e});
-    ctx->saved_data["T"] = T;
+    ctx->save_for_backward({x2, e, A, B, T, W, s});  // (the Python nodes' order; what a call lacks is skipped by both)
     ctx->saved_data["scale"] = scale;
     ctx->saved_data["o"] = o;
     ctx->saved_data["x_shape"] = x.sizes().vec();
@@ -392,15 +391,16 @@ struct ExpertsNode : public torch::autograd::Function<ExpertsNode> {
   static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
     const auto vars = ctx->get_saved_variables();
     TORCH_CHECK_VALUE(vars[0].is_cuda(), "the saved input came back on ", vars[0].device());
-    const at::Tensor &A = vars[1], &B = vars[2];
+    const at::Tensor &ends = vars[1], &A = vars[2], &B = vars[3], &T = vars[4], &W = vars[5], &scales = vars[6];
     const int64_t o = ctx->saved_data["o"].toInt();
-    const rl_stack_t dw = stack_desc(vars[3], vars[0], dtype_code(vars[3].scalar_type()), o, vars[4]), da = stack_desc(A, vars[0], dtype_code(A.scalar_type())),
+    const rl_stack_t dw = stack_desc(W, vars[0], dtype_code(W.scalar_type()), o, scales), da = stack_desc(A, vars[0], dtype_code(A.scalar_type())),
                      db = stack_desc(B, vars[0], dtype_code(B.scalar_type()));
+    const rl_tensor_t dt = saved_desc(T, vars[0]);
     const at::Tensor x2 = rows(vars[0], dw.rows);
     const int64_t n = x2.size(0), i = dw.rows, r = da.cols;
     const int code = dtype_code(x2.scalar_type());
     const c10::OptionalDeviceGuard guard(x2.device());
-    const at::Tensor dy2 = rows(grads[0], o), T = ctx->saved_data["T"].toTensor();
+    const at::Tensor dy2 = rows(grads[0], o);
     at::Tensor dx, dA, dB;
     rl_tensor_t tx{};
     rl_stack_t ta{}, tb{};
@@ -409,8 +409,8 @@ struct ExpertsNode : public torch::autograd::Function<ExpertsNode> {
     if (ctx->needs_input_grad(2)) { dB = at::empty(B.sizes(), B.options()); tb = stack_desc(dB, x2, db.dtype); }
     const at::Tensor ws = scratch(p_experts_workspace_bytes(1, n, dw.experts, i, o, r, code, dw.dtype), x2);
     const rl_opts_t opts = options(x2, ws, std::nullopt, ctx->saved_data["scale"].toDouble());
-    const rl_tensor_t ddy = desc(dy2, dtype_code(dy2.scalar_type())), dx2 = desc(x2, code), dt = desc(T, dtype_code(T.scalar_type()));
-    check(p_experts_backward(&ddy, &dx2, ends_of(vars[5], dw.experts, x2), &dw, &da, &db, &dt, dx.defined() ? &tx : nullptr, dA.defined() ? &ta : nullptr,
+    const rl_tensor_t ddy = desc(dy2, dtype_code(dy2.scalar_type())), dx2 = desc(x2, code);
+    check(p_experts_backward(&ddy, &dx2, ends_of(ends, dw.experts, x2), &dw, &da, &db, &dt, dx.defined() ? &tx : nullptr, dA.defined() ? &ta : nullptr,
                              dB.defined() ? &tb : nullptr, &opts));
     if (dx.defined()) dx = dx.view(ctx->saved_data["x_shape"].toIntVector());
     at::Tensor none;
