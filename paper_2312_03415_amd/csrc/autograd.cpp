@@ -351,7 +351,8 @@ rl_stack_t stack_desc(const at::Tensor& t, const at::Tensor& x, int code, int64_
   const bool many = t.dim() == 3;
   const bool fp8 = scales.defined();
   if (fp8)
-    TORCH_CHECK_VALUE(scales.device() == x.device() && scales.is_contiguous() && scales.element_size() == 1 && t.element_size() == 1,
+    TORCH_CHECK_VALUE(scales.device() == x.device() && scales.is_contiguous() && scales.element_size() == 1 && t.element_size() == 1 && t.size(-1) >= cols &&
+                          scales.numel() == (many ? t.size(0) : 1) * ((t.size(-2) + 127) / 128) * ((cols + 127) / 128),
                       "an 8-bit weight came back with other bytes or scales");
   return rl_stack_t{t.data_ptr(), many ? t.size(0) : 1, t.size(-2), cols < 0 ? t.size(-1) : cols, t.stride(-2), many ? t.stride(0) : 0,
                     fp8 ? (int32_t)RL_FP8_B128 : code, fp8 ? scales.data_ptr() : nullptr, fp8 ? 128 : 0};

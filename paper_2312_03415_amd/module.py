@@ -476,6 +476,8 @@ class RunLoRAFp8Function(torch.autograd.Function):
         dB = make(B.shape, dtype=B.dtype, device=B.device) if need_b else None
         if n > 0:
             saved, x2 = _reread(ctx.saved, dy2, x2, A, B, T, data, scales)
+            if tuple(T.shape) != (n, r) or T.dtype != x2.dtype or T.stride(1) != 1:
+                raise ValueError("scale XA came back from the saved tensors as another matrix")
             if saved.T != T.data_ptr() or saved.ldt != T.stride(0):
                 saved = type(saved).from_buffer_copy(saved)
                 saved.T, saved.ldt = T.data_ptr(), T.stride(0)

@@ -80,6 +80,32 @@ def test_the_kept_product_goes_with_the_graph(kind, node):
         del y, g
 
 
+@pytest.mark.parametrize("node", ["native", "python"])
+@pytest.mark.parametrize("kind", KINDS)
+def test_saved_tensors_that_come_back_changed(kind, node):
+    """Rows apart are read as they are; a device, layout, type or size that the forward would refuse is refused before anything is launched."""
+    ops, fn = Operands(kind), functions(kind)[node]
+    plain = packed(ops, fn)[1]
+    wide = lambda t: torch.cat([t.cuda()] * 2, -1)[..., :t.shape[-1]] if t.dim() >= 2 and t.dtype != torch.uint8 else t.cuda()
+    assert all(torch.equal(a, b) for a, b in zip(packed(ops, fn, wide)[1], plain))
+    odd = lambda t: t.cuda().repeat_interleave(2, -1)[..., ::2]
+    x, T, A = (N, I), (N, R), tuple(ops.A.shape)
+    W = tuple((ops.W if kind == "experts" else ops.W.data).shape)
+    changes = [(x, lambda t: t.cpu()), (T, lambda t: t.cpu()), (A, lambda t: t.cpu()), (W, lambda t: t.cpu()), (A, odd), (T, odd), (W, odd)]
+    if kind != "fp8":
+        changes += [((E,), lambda t: t.cpu()), ((E,), lambda t: t.cuda().long()), ((E,), lambda t: t.cuda()[:2])]
+    if kind != "experts":
+        S = tuple(ops.W.scales.shape)
+        changes += [(S, lambda t: t.cpu()), (S, lambda t: t.cuda()[..., :1].contiguous()), (W, lambda t: t.cuda()[..., :I]), (W, lambda t: t.cuda().float())]
+    changes += [(x, lambda t: t.cuda().float()), (T, lambda t: t.cuda().half()), (T, lambda t: t.cuda()[:-1]), (T, lambda t: t.cuda()[:, :8]),
+                (A, lambda t: t.cuda().half()), (A, lambda t: t.cuda()[..., :-8].contiguous())]
+    assert all(sum(s == shape for s, _ in packed(ops, fn)[0]) == 1 for shape, _ in changes)
+    for k, (shape, change) in enumerate(changes):
+        with pytest.raises((ValueError, rl.RunLoRAError)):
+            packed(ops, fn, lambda t: change(t) if tuple(t.shape) == shape else t.cuda())
+            pytest.fail(f"change {k} of a saved tensor {shape} was taken")
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_a_saved_tensor_that_changes_in_place(kind):
     messages = []
