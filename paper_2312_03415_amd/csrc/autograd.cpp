@@ -580,7 +580,9 @@ PyObject* py_experts(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                          : (W.scalar_type() != x.scalar_type() || W.size(-1) != o))
     Py_RETURN_NONE;
   if (ends.has_value() && (ends->dim() != 1 || ends->numel() != W.size(0) || ends->scalar_type() != at::kInt || ends->stride(0) != 1)) Py_RETURN_NONE;
-  if (bias.has_value() && (bias->scalar_type() != x.scalar_type() || !bias->is_contiguous() || bias->numel() != (dim == 3 ? W.size(0) : 1) * o)) Py_RETURN_NONE;
+  if (bias.has_value() && (bias->scalar_type() != x.scalar_type() || !bias->is_contiguous() || bias->dim() != dim - 1 || bias->size(-1) != o ||
+                            (dim == 3 && bias->size(0) != W.size(0))))
+    Py_RETURN_NONE;
   at::Tensor y;
   {
     pybind11::gil_scoped_release release;

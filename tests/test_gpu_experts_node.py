@@ -151,3 +151,14 @@ def test_both_nodes_on_streams_and_threads(kind):
             t.join()
         assert not errors, errors
         assert all(torch.equal(a, b) for k in range(4) for a, b in zip(out[k], alone[k]))
+
+
+@pytest.mark.parametrize("node", ["native", "python"])
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_bias_of_another_shape_is_refused(kind, node):
+    """As many elements in another order are not a bias for every expert."""
+    ops, fn = Operands(kind), functions(kind)[node]
+    for shape in ((1, O),) if kind == "fp8" else ((O, E), (E * O,), (E, 1, O)):
+        ops.bias = torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+        with pytest.raises(ValueError, match="bias"):
+            ops.run(fn)
