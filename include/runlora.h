@@ -300,7 +300,8 @@ size_t runlora_dora_workspace_bytes(int fwd, int bwd, int64_t n, int64_t i, int6
  *     Y = Q(X) W + 1 b^T + s (X A) B,     dX = Q(dY) W^T + s (dY B^T) A^T,     dA, dB as ever (from X and dY themselves),
  * Q(x) = e4m3(x / 2^e) 2^e with e the smallest integer >= -127 for which the block's largest magnitude is at most 448 * 2^e (rounding to
  * nearest, ties to even; a block holding an infinity or a NaN becomes NaN).  RL_F16 / RL_BF16 activations, i and o multiples of 16; graphs
- * RL_FWD1 (also asked for as RL_FWD3) and RL_BWD1, no LoRA dropout; everything else returns RL_ERR_UNSUPPORTED.  Workspace:
+ * RL_FWD1 (also asked for as RL_FWD3) and RL_BWD1, no LoRA dropout; everything else returns RL_ERR_UNSUPPORTED (runlora_vera_* too;
+ * runlora_dora_* take W in the type of A and B only).  Workspace:
  * runlora_workspace_bytes_w with w_dtype = RL_FP8_B128.  runlora_select takes RL_FP8_B128 as its dtype.
  *
  * runlora_fp8_quantize rounds a dense matrix (RL_F32 / RL_F16 / RL_BF16, [rows, cols]) to the same values in blocks of 128 x 128:

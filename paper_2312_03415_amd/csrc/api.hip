@@ -809,6 +809,7 @@ extern "C" int runlora_vera_forward(int variant, const rl_tensor_t* X, const rl_
                                     const rl_tensor_t* B, const void* d, const void* b, rl_tensor_t* Y,
                                     rl_saved_t* saved, const rl_opts_t* opts) {
   if (!X || !W || !A || !B || !Y || !saved) return RL_ERR_NULL;
+  if (W->dtype == RL_FP8_B128) return RL_ERR_UNSUPPORTED;
   VeraLayout v;
   int rc = vera_layout(B, d, b, opts, &v);
   if (rc != RL_OK) return rc;
@@ -836,6 +837,7 @@ extern "C" int runlora_vera_backward(int variant, const rl_tensor_t* dY, const r
                                      const rl_tensor_t* A, const rl_tensor_t* B, const void* d, const void* b,
                                      rl_tensor_t* dX, void* dd, void* db, const rl_opts_t* opts) {
   if (!dY || !saved || !W || !A || !B) return RL_ERR_NULL;
+  if (W->dtype == RL_FP8_B128) return RL_ERR_UNSUPPORTED;
   VeraLayout v;
   int rc = vera_layout(B, d, b, opts, &v);
   if (rc != RL_OK) return rc;

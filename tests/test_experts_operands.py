@@ -137,3 +137,21 @@ def test_rows_that_only_look_dense_are_laid_out_anew():
     for x in (torch.randn(6 * 48 + 8).bfloat16()[1:1 + 6 * 48].view(6, 48), torch.randn(2, 49).bfloat16()[:1, :48]):
         r = _rows(x, 48)
         assert x.is_contiguous() and torch.equal(r, x) and r.stride(0) % 8 == 0 and r.data_ptr() % 16 == 0
+
+
+# ---- what does not take an 8-bit weight ------------------------------------------------------------------------------
+
+def test_the_other_layers_refuse_an_8_bit_weight():
+    """VeRA's and DoRA's entries are built on the layer call, which takes one, without scratch or ranges for it."""
+    n, i, o, r = 64, 256, 272, 16
+    W = rl.rl_tensor_t(next(ADDRESS), i, o, o, rl.RL_FP8_B128, next(ADDRESS), 128)
+    X, A, B, Y, dX, dA, dB = tensor(n, i), tensor(i, r), tensor(r, o), tensor(n, o), tensor(n, i), tensor(i, r), tensor(r, o)
+    opts = rl.rl_opts_t(None, next(ADDRESS), 1 << 27)
+    saved = rl.rl_saved_t()
+    p = ctypes.byref
+    L, vec = rl.lib(), lambda: ctypes.c_void_p(next(ADDRESS))
+    assert L.runlora_vera_forward(rl.FWD1, p(X), p(W), p(A), p(B), vec(), vec(), p(Y), p(saved), p(opts)) == rl.RL_ERR_UNSUPPORTED
+    assert L.runlora_dora_forward(rl.FWD2, p(X), p(W), p(A), p(B), vec(), p(Y), p(saved), vec(), p(opts)) == rl.RL_ERR_DTYPE
+    saved.fwd_variant, saved.dtype, saved.n, saved.i, saved.o, saved.r, saved.X, saved.ldx = rl.FWD1, rl.RL_BF16, n, i, o, r, X.data, i
+    assert L.runlora_vera_backward(rl.BWD1, p(Y), p(saved), p(W), p(A), p(B), vec(), vec(), p(dX), vec(), vec(), p(opts)) == rl.RL_ERR_UNSUPPORTED
+    assert L.runlora_dora_backward(rl.BWD4, p(Y), p(saved), p(W), p(A), p(B), vec(), vec(), p(Y), p(dX), p(dA), p(dB), vec(), p(opts)) == rl.RL_ERR_DTYPE
