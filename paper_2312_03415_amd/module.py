@@ -487,6 +487,21 @@ class RunLoRAFp8Function(torch.autograd.Function):
         return dx.view(ctx.x_shape) if need_x else None, None, dA, dB, None, None
 
 
+def _bytes_of_state(module, state, prefix, *_):
+    for name in ("weight_data", "weight_scales"):
+        t = state.get(prefix + name)
+        if isinstance(t, torch.Tensor) and t.element_size() == 1:
+            state[prefix + name] = t.view(torch.uint8)
+
+
+def _register_bytes(module, weight):
+    """An Fp8Weight as a module's buffers.  They hold whole numbers: converting a module converts its floating-point tensors, 8-bit ones among
+    them; a state that holds them as such is read as bytes."""
+    module.register_buffer("weight_data", weight.data.view(torch.uint8))
+    module.register_buffer("weight_scales", weight.scales.view(torch.uint8))
+    module.register_load_state_dict_pre_hook(_bytes_of_state)
+
+
 class RunLoRAFp8Linear(nn.Module):
     """LoRA-augmented linear layer over a frozen weight kept in 8 bits (binding.Fp8Weight); otherwise as RunLoRALinear."""
 
@@ -495,8 +510,7 @@ class RunLoRAFp8Linear(nn.Module):
         (self.d_in, self.d_out), self.r = weight.shape, r
         self.scale = 1.0 if alpha is None else float(alpha) / r
         device = weight.data.device
-        self.register_buffer("weight_data", weight.data)
-        self.register_buffer("weight_scales", weight.scales)
+        _register_bytes(self, weight)
         self.bias = nn.Parameter(bias.contiguous(), requires_grad=False) if bias is not None else None
         self.lora_A = nn.Parameter(torch.randn(self.d_in, r, dtype=dtype, device=device) / math.sqrt(self.d_in))
         self.lora_B = nn.Parameter(torch.zeros(r, self.d_out, dtype=dtype, device=device))
@@ -529,8 +543,7 @@ class RunLoRAExperts(nn.Module):
         self.r, self.scale = r, 1.0 if alpha is None else float(alpha) / r
         self.fp8 = isinstance(weight, rl.Fp8Weight)
         if self.fp8:
-            self.register_buffer("weight_data", weight.data)
-            self.register_buffer("weight_scales", weight.scales)
+            _register_bytes(self, weight)
             device, dtype = weight.data.device, dtype or torch.bfloat16
         else:
             self.weight = nn.Parameter(weight.contiguous(), requires_grad=False)

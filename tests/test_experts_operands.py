@@ -155,3 +155,33 @@ def test_the_other_layers_refuse_an_8_bit_weight():
     saved.fwd_variant, saved.dtype, saved.n, saved.i, saved.o, saved.r, saved.X, saved.ldx = rl.FWD1, rl.RL_BF16, n, i, o, r, X.data, i
     assert L.runlora_vera_backward(rl.BWD1, p(Y), p(saved), p(W), p(A), p(B), vec(), vec(), p(dX), vec(), vec(), p(opts)) == rl.RL_ERR_UNSUPPORTED
     assert L.runlora_dora_backward(rl.BWD4, p(Y), p(saved), p(W), p(A), p(B), vec(), vec(), p(Y), p(dX), p(dA), p(dB), vec(), p(opts)) == rl.RL_ERR_DTYPE
+
+
+# ---- 8-bit weights in modules ------------------------------------------------------------------------------------------
+
+def _bytes(torch, *shape):
+    return torch.randint(0, 120, shape, generator=torch.Generator().manual_seed(4), dtype=torch.uint8)
+
+
+@pytest.mark.parametrize("experts", [0, 3])
+def test_an_8_bit_weight_stays_in_8_bits_whatever_the_module_is_turned_to(experts):
+    """Converting a module converts its floating-point buffers: the bytes are held as whole numbers, also where they came as float8_e4m3fn."""
+    torch = pytest.importorskip("torch")
+    from paper_2312_03415_amd.module import RunLoRAExperts, RunLoRAFp8Linear
+    lead = (experts,) if experts else ()
+    data, scales = _bytes(torch, *lead, 256, 272), _bytes(torch, *lead, 2, 3)
+    make = lambda d, s: (RunLoRAExperts if experts else RunLoRAFp8Linear)(rl.Fp8Weight(d, s, 256, 272), 16)
+    as_float = lambda t: t.view(torch.float8_e4m3fn)
+    for d in (data, as_float(data)):
+        for turn in (lambda m: m, lambda m: m.half(), lambda m: m.to(torch.float32), lambda m: torch.nn.Sequential(m).bfloat16()[0]):
+            layer = turn(make(d.clone(), scales.clone()))
+            assert torch.equal(layer.weight_data.view(torch.uint8), data) and torch.equal(layer.weight_scales.view(torch.uint8), scales)
+            if not experts:
+                assert torch.equal(layer.weight.data.view(torch.uint8), data)
+    # a state with the bytes in either type
+    for d in (data, as_float(data)):
+        layer = make(torch.zeros_like(data), torch.zeros_like(scales))
+        state = dict(layer.state_dict(), weight_data=d, weight_scales=scales)
+        torch.nn.Sequential(layer).load_state_dict({"0." + k: v for k, v in state.items()})
+        assert torch.equal(layer.weight_data.view(torch.uint8), data) and torch.equal(layer.weight_scales.view(torch.uint8), scales)
+        assert state["weight_data"].dtype == d.dtype
