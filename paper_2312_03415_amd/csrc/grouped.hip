@@ -285,40 +285,48 @@ int64_t share(const ExpertsDesc& d) { return ceil_div(d.n, d.experts < d.n ? d.e
 
 bool few(const ExpertsDesc& d) { return d.n <= 64 && d.r <= 256; }
 
-// the large product of a forward (K = i) or a backward (K = o)
-struct MainPlan { int tile, splits, per; unsigned gx; bool join; };
-MainPlan main_plan(const ExpertsDesc& d, int64_t N, int64_t K, bool split) {
-  MainPlan p;
-  const int64_t rows = share(d);
-  auto tiles_of = [&](int tile) {
+}  // namespace
+
+GroupedPlan grouped_plan(const ExpertsDesc& d, int64_t N, int64_t K, bool slices) {
+  GroupedPlan p;
+  const int64_t rows = share(d), some = d.experts < d.n ? d.experts : d.n;
+  auto most = [&](int tile) {  // tiles that there can be: what is launched
     const GroupedTileInfo t = grouped_tile(tile);
     return grouped_row_tiles(d.n, d.experts, d.has_ends, t.bm, d.f8) * ceil_div(N, t.bn);
   };
-  // The largest tile that an expert's rows fill and of which there are enough.  Measured without adapters, 16-bit / 8-bit weights:
-  //  256 x 256 from about 200 tiles: Y of 4000 x 4096 -> 4096 (256 tiles) 107 / 70 us against 127 / 84 in 128 x 128 tiles, of 2000 rows
-  //    (128 tiles) 94 / 58 against 68 / 46;
-  //  128 x 128 from about 384: Y of 1237 x 2064 -> 5456 (430 tiles) 43 / 31 us against 58 / 42 in 64 x 128 tiles; dX of 600 x 5456 -> 2064
-  //    (85 tiles) 71 / 46 against 41 / 31;
+  auto expected = [&](int tile) {  // tiles that there will be: an expert's last row tile is half full on average (not said of experts below half a tile)
+    const GroupedTileInfo t = grouped_tile(tile);
+    return (d.has_ends ? (d.n + (some + 1) * (t.bm / 2)) / t.bm : ceil_div(d.n, t.bm)) * ceil_div(N, t.bn);
+  };
+  // A larger tile costs less a product, as long as it is filled: it is taken where the next smaller ones are more than one round, two to a compute
+  // unit (kFill).  Measured without adapters, 16-bit / 8-bit weights, us:
+  //  128 x 128 for 64 x 128, K 768 to 8192: 540 to 672 of the smaller (270 to 336 of the larger; 8 shapes, one group) 16-28 % / 7-30 % faster, e.g. Y of 2100 x 4096 ->
+  //    2320 56 / 43 in place of 75 / 56; 500 and fewer (4 shapes of 3 to 8 uneven experts) the same to 30 % slower, 2000 rows of 8 experts 4096 -> 1792
+  //    60 / 41 in place of 46 / 33.
+  //  256 x 256 for 128 x 128, K 1536 to 8192: 576 to 768 of the smaller (144 to 192 of the larger; 6 shapes) 7-18 % / up to 22 % faster, 2300 x 4096 -> 4096 93 / 61 in place
+  //    of 108 / 70, and with 4, 8 and 16 uneven experts (540 to 672) 9-30 % / 4-28 %, 2400 rows of 4 experts 4096 -> 4096 97 / 62 in place of 136 / 73; 512 and fewer
+  //    slower, 1600 rows of 8 experts 4096 -> 4096 99 / 59 in place of 91 / 54.  A K below 1024 only where they fill a round by themselves:
+  //    3000 x 768 -> 4096 (192 of the larger) 26.4 / 28.4 in place of 25.8 / 25.9; 3000 rows of 12 experts 1032 -> 2744 38 / 31, 42 / 33 in the smaller.
   //  64 x 128 from about 160: 300 x 4096 -> 4096 (160 tiles) 33 / 24 against 34 / 25 in 32 x 128 tiles, 200 x 2048 -> 2048 (64) 18 / 15
   //    against 15.5 / 13.
-  // In between, where 64 x 128 tiles are more than the compute units and K is long enough to split 256 x 256 ones over them (below),
-  // those are faster with 16-bit weights: dX of 1237 x 5456 -> 2064 (340 tiles, 45 of them) 54 us against 74, Y of 3000 rows of 8 experts
-  // 8192 -> 1024 75 against 88; with 8-bit weights 73 against 46 and 70 against 65.
+  // With 16-bit weights and a long K, fewer than half a round of 256 x 256 tiles whose K is split over the compute units are faster than one round of smaller ones:
+  // 1237 x 5456 -> 2064 (45 tiles, 86 K tiles) 51 against 64, 3000 rows of 8 experts 8192 -> 1024 (60, 128) 79 against 108, 2560 x 8192 -> 2816 (110, 128) 111
+  // against 115; not with 64 K tiles, 2048 x 4096 -> 2048 51 against 43, or with 80, 2048 x 5120 -> 3584 80 against 75; with 8-bit weights 73 against 46 and 70 against 65.
   const int64_t nk = ceil_div(K, d.f8 ? 128 : 64);
-  const bool long_k = 3 * nk >= 160;
   p.tile = GT_32x128;
   // In slices of K (few rows) 64 x 128 tiles pay from 32 K tiles: 64 rows 4096 -> 11008 29 us against 33, 11008 -> 4096 33 against 35, but
   // 2064 -> 5456 19.3 against 18.0.
-  if (rows > 32 && (split ? nk >= 32 : tiles_of(GT_64x128) >= 160)) p.tile = GT_64x128;
-  if (!split && rows > 96 && tiles_of(GT_128x128) >= 384) p.tile = GT_128x128;
-  if (!split && rows > 160 && (!d.f8 || K <= 128 * 128) &&
-      (tiles_of(GT_256x256) >= 208 || (p.tile == GT_64x128 && !d.f8 && long_k && tiles_of(GT_64x128) > kUnits))) p.tile = GT_256x256;
-  const int64_t tiles = tiles_of(p.tile);
+  if (rows > 32 && (slices ? nk >= 32 : expected(GT_64x128) >= 160)) p.tile = GT_64x128;
+  if (!slices && rows > 96 && expected(GT_64x128) > kFill) p.tile = GT_128x128;
+  if (!slices && rows > 160 && (!d.f8 || K <= 128 * 128)) {
+    const bool few_split = !d.f8 && nk > 80 && expected(GT_64x128) > kUnits && grouped_split_round((int)expected(GT_256x256), (int)nk).splits > 1;
+    if ((expected(GT_128x128) > kFill && (K >= 1024 || expected(GT_256x256) >= 208)) || few_split) p.tile = GT_256x256;
+  }
+  const int64_t tiles = most(p.tile);
   p.gx = (unsigned)(p.tile == GT_256x256 && tiles > kUnits ? kUnits : tiles);
   p.join = false;
   if (p.tile == GT_256x256) {  // the last round of tiles may be worth splitting; how many tiles there are only the device knows, unless all rows are one group's
-    const int64_t left = tiles % kUnits;
-    p.join = long_k && (d.has_ends || (left > 0 && left <= kUnits / 2));
+    p.join = d.has_ends ? 3 * nk >= 160 : grouped_split_round((int)tiles, (int)nk).splits > 1;
     if (p.join) p.gx = (unsigned)kUnits;
     p.splits = 1;
     p.per = (int)nk;
@@ -326,13 +334,15 @@ MainPlan main_plan(const ExpertsDesc& d, int64_t N, int64_t K, bool split) {
   }
   // A workgroup a compute unit: what two would load faster, the sum over twice the slices takes (with the small launches around it, 64 rows
   // 4096 -> 11008 2 slices 28.8 us, 5 30.7; 40 rows 25.0 and 26.1; 5 rows of 8 experts 2048 -> 2048 3 slices 17.2, 6 18.4).
-  int64_t s = split ? kUnits / tiles : 1;
+  int64_t s = slices ? kUnits / tiles : 1;
   if (s > nk / 4) s = nk / 4;
   if (s < 1) s = 1;
   p.per = (int)ceil_div(nk, s);
   p.splits = (int)ceil_div(nk, p.per);
   return p;
 }
+
+namespace {
 
 // T = s X A, Z = s dY B^T
 struct RankPlan { int tile, splits, per; unsigned gx; };
@@ -405,7 +415,7 @@ Space space(const ExpertsDesc& d, bool backward, void* workspace) {
     w.s = static_cast<uint8_t*>(c.take((size_t)(w.ldq / 128 * w.lds)));
   }
   if (!backward && few(d)) {
-    const MainPlan m = main_plan(d, N, K, true);
+    const GroupedPlan m = grouped_plan(d, N, K, true);
     w.part = static_cast<float*>(c.take((size_t)m.splits * d.n * N * 4));
     if (d.r > 0) {
       w.slices = few_slices(d);
@@ -423,7 +433,7 @@ Space space(const ExpertsDesc& d, bool backward, void* workspace) {
     }
     w.part = static_cast<float*>(c.take(part));
   }
-  if (!(!backward && few(d)) && (!backward || d.dX != nullptr || workspace == nullptr) && main_plan(d, N, K, false).join) w.join = static_cast<float*>(c.take(kJoinBytes));
+  if (!(!backward && few(d)) && (!backward || d.dX != nullptr || workspace == nullptr) && grouped_plan(d, N, K, false).join) w.join = static_cast<float*>(c.take(kJoinBytes));
   w.bytes = c.used;
   return w;
 }
@@ -502,7 +512,7 @@ hipError_t grads_run(const ExpertsDesc& d, const void* T, int64_t ldt, const voi
 hipError_t main_run(const ExpertsDesc& d, bool backward, const Space& w, const void* TA, int64_t ldta, const void* TB, int64_t ldtb, int64_t stb, void* out, int64_t ldo,
                     bool slices, bool rounded, hipStream_t stream) {
   const int64_t K = backward ? d.o : d.i, N = backward ? d.i : d.o;
-  const MainPlan p = main_plan(d, N, K, slices);
+  const GroupedPlan p = grouped_plan(d, N, K, slices);
   GroupedArgs a = rows_args(d);
   a.A = backward ? d.dY : d.X;
   a.lda = backward ? d.lddy : d.ldx;
@@ -548,7 +558,7 @@ hipError_t experts_forward(const ExpertsDesc& d, void* workspace, hipStream_t st
     f.Y = d.Y; f.ldy = d.ldy; f.T = d.T; f.ldt = d.ldt;
     f.ends = d.ends; f.experts = (int)d.experts;
     f.n = (int)d.n; f.K = (int)d.i; f.N = (int)d.o; f.R = (int)d.r;
-    f.slices = w.slices; f.splits = main_plan(d, d.o, d.i, true).splits;
+    f.slices = w.slices; f.splits = grouped_plan(d, d.o, d.i, true).splits;
     f.scale = d.scale;
     if (d.f8) {
       f.q = w.q; f.qs = w.s; f.ldq = w.ldq; f.ldqs = w.lds;

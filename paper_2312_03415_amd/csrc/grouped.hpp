@@ -61,6 +61,26 @@ inline int64_t grouped_row_tiles(int64_t n, int64_t experts, bool ends, int bm, 
   return (n + groups * (bm - 1 + (f8 ? 3 : 0))) / bm;  // (an e4m3 group's first tile starts up to three rows early)
 }
 
+// The last round of 256 x 256 tiles, one per compute unit, where it is at most half full, has its tiles' K tiles dealt out to `splits` workgroups
+// each, which leave fp32 sums for grouped_mc_join_kernel: (1 - 1 / splits) of a round of nt K tiles of 1.5 us for a round trip of up to
+// 64 MB and a launch, together about 40 us; worth it from 60 us saved.  8192 rows of 8 experts, K = 8192 (about 288 tiles), bf16: 257 + 12 us in
+// place of 384; 16384 x 11008 -> 4096 e4m3: 735 + 14 in place of 807; where it would save 48 us (K = 4096, bf16) it gains nothing.
+struct GroupedSplit {
+  int whole, splits, per;  // tiles [0, whole) by themselves; the others' K tiles in `splits` runs of `per`
+};
+__host__ __device__ inline GroupedSplit grouped_split_round(int total, int nt) {
+  const int left = total & 255;
+  GroupedSplit s{total, 1, nt};
+  if (left == 0 || left > 128) return s;
+  int k = 256 / left;
+  if (k > 8) k = 8;
+  s.per = (nt + k - 1) / k;
+  s.splits = (nt + s.per - 1) / s.per;
+  if ((nt - s.per) * 3 < 120 || s.per < 4) return GroupedSplit{total, 1, nt};
+  s.whole = total - left;
+  return s;
+}
+
 // rows: A is rounded on the way (GroupedArgs::Q)
 hipError_t grouped_rows_launch_bf16(int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s);
 hipError_t grouped_rows_launch_f16(int bl, int tile, const GroupedArgs& a, dim3 grid, hipStream_t s);
@@ -90,6 +110,10 @@ struct ExpertsDesc {
   bool has_T = false;  // backward: T holds s X A already
   float scale = 1.f;
 };
+// what a large product of K into N columns runs on: a function of sizes alone, shared by the workspace query and the call.  slices: K in `splits`
+// slices that a launch of its own sums (few rows); join: 256 x 256 tiles whose last round may be split
+struct GroupedPlan { int tile, splits, per; unsigned gx; bool join; };
+GroupedPlan grouped_plan(const ExpertsDesc& d, int64_t N, int64_t K, bool slices);
 size_t experts_workspace(const ExpertsDesc& d, bool backward);
 hipError_t experts_forward(const ExpertsDesc& d, void* workspace, hipStream_t stream);
 hipError_t experts_backward(const ExpertsDesc& d, void* workspace, hipStream_t stream);

@@ -81,25 +81,9 @@ struct GroupedOrder {
   }
 };
 
-// The last round of one tile per compute unit, where it is at most half full, has its tiles' K tiles dealt out to `splits` workgroups each,
-// which leave fp32 sums for grouped_mc_join_kernel: (1 - 1 / splits) of a round of nt K tiles of 1.5 us for a round trip of up to
-// 64 MB and a launch, together about 40 us; worth it from 60 us saved.  8192 rows of 8 experts, K = 8192 (about 288 tiles), bf16: 257 + 12 us in
-// place of 384; 16384 x 11008 -> 4096 e4m3: 735 + 14 in place of 807; where it would save 48 us (K = 4096, bf16) it gains nothing.
-// The tile count is the device's to know: both kernels decide here.
-struct GroupedSplit {
-  int whole, splits, per;  // tiles [0, whole) by themselves; the others' K tiles in `splits` runs of `per`
-};
+// With experts the tile count is the device's to know: the product and the join decide here, where the host has left room for a split.
 __device__ __forceinline__ GroupedSplit grouped_split(const GroupedArgs& g, int total, int nt) {
-  const int left = total & 255;
-  GroupedSplit s{total, 1, nt};
-  if (g.partial == nullptr || left == 0 || left > 128) return s;
-  int k = 256 / left;
-  if (k > 8) k = 8;
-  s.per = (nt + k - 1) / k;
-  s.splits = (nt + s.per - 1) / s.per;
-  if ((nt - s.per) * 3 < 120 || s.per < 4) return GroupedSplit{total, 1, nt};
-  s.whole = total - left;
-  return s;
+  return g.partial == nullptr ? GroupedSplit{total, 1, nt} : grouped_split_round(total, nt);
 }
 
 template <typename T, bool F8, int BL>
