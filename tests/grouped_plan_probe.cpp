@@ -17,6 +17,10 @@ int main() {
       const GroupedPlan p = grouped_plan(x, c, d, false);
       const GroupedTileInfo t = grouped_tile(p.tile);
       std::printf("%d %d %d\n", t.bm, t.bn, p.join ? 1 : 0);
+    } else if (std::strcmp(kind, "few") == 0) {  // the same product for few rows: slices of K
+      ExpertsDesc x;
+      x.n = a; x.experts = b; x.f8 = e != 0; x.has_ends = f != 0;
+      std::printf("%d\n", grouped_plan(x, c, d, true).splits);
     } else if (std::strcmp(kind, "split") == 0) {  // 256 x 256 tiles, K tiles: tiles that stay whole, runs a tile and K tiles a run of the others
       const GroupedSplit s = grouped_split_round((int)a, (int)b);
       std::printf("%d %d %d\n", s.whole, s.splits, s.per);

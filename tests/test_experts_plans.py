@@ -103,3 +103,42 @@ def test_only_calls_that_may_split_bring_room_for_sums():
     assert ask(2100, 4112, 2320) < small(2100, 4112, 2320)
     whole, split = ask(16384, 11008, 4096), ask(16384, 11008, 4160)    # four rounds of tiles, and four with a quarter of a round
     assert room <= split - whole < room + (1 << 20)
+
+
+def row_tiles(counts, n, fp8):
+    """256-row tiles of the experts' rows and of those behind them; an e4m3 expert's first tile begins on a multiple of four."""
+    lo = tiles = 0
+    for c in list(counts) + [n - int(sum(counts))]:
+        hi = lo + int(c)
+        if hi > lo:
+            tiles += up(hi - (lo & ~3 if fp8 else lo), 256)
+        lo = hi
+    return tiles
+
+
+def test_the_split_cases_split(probe):
+    """What test_gpu_experts_split.py runs: the large kernel, with room for sums, and by the kernels' rule a last round that is dealt out."""
+    split_cases = pytest.importorskip("test_gpu_experts_split")
+    begun = {"Y": set(), "dX": set()}
+    for n, experts, i, o, r, kind, side, weights in split_cases.CASES:
+        for weight in weights:
+            fp8 = int(weight == "fp8")
+            K, N = (i, o) if side == "Y" else (o, i)
+            assert probe("product", [(n, experts, N, K, fp8, 1)])[0] == [256, 256, 1], (n, i, o, side, weight)
+            tiles = row_tiles(split_cases.counts(n, experts, kind), n, fp8) * up(N, 256)
+            whole, runs, per = probe("split", [(tiles, k_tiles(K, fp8))])[0]
+            assert runs > 1 and whole < tiles, (n, i, o, side, weight, tiles)
+            if fp8:
+                begun[side].update((k * per, min((k + 1) * per, k_tiles(K, fp8))) for k in range(runs))
+    for runs in begun.values():                       # both registers of W's scales, and the change between them inside a run
+        assert any(a > 64 for a, b in runs) and any(a < 64 < b for a, b in runs)
+
+
+def test_the_long_cases_run_on_the_smaller_tiles(probe):
+    for n, experts, i, o, r, kind, side, tile in pytest.importorskip("test_gpu_experts_split").LONG:
+        K, N = (i, o) if side == "Y" else (o, i)
+        assert k_tiles(K, 1) > 64
+        if tile:
+            assert probe("product", [(n, experts, N, K, 1, 1)])[0][0] == tile, (n, K, N)
+        else:
+            assert probe("few", [(n, experts, N, K, 1, 1)])[0][0] == 1, (n, K, N)

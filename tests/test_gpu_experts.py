@@ -145,7 +145,7 @@ def test_fp16(n, experts, i, o, r, kind, fp8):
 
 
 LARGE = [
-    # enough 256 x 256 tiles in both directions, several a compute unit: ragged rows and columns, K that ends inside a tile, long K
+    # enough 256 x 256 tiles forward, and backward in some: ragged rows and columns, K that ends inside a tile, long K
     (2100, 1, 2320, 4112, 24, "even"),
     (2600, 3, 2576, 3856, 40, "uneven"),
     (3000, 5, 2320, 2832, 136, "rest"),
@@ -160,7 +160,8 @@ def test_large_tiles(n, experts, i, o, r, kind, fp8):
     check(Case("f16" if experts == 3 else "bf16", fp8, n, experts, i, o, r, kind, bias=(n % 1000 != 0)))
 
 
-# tiles beyond whole rounds whose K tiles are dealt out to several workgroups, in either direction: (n, experts, i, o, r, rows per expert)
+# many tiles and a long K: the last round's K tiles are dealt out in the forward of the first case (16-bit weights) and of the last; test_gpu_experts_split.py has
+# more of those, in either direction: (n, experts, i, o, r, rows per expert)
 SPLIT = [(2048, 1, 4112, 9008, 24, "even"), (2500, 3, 9008, 3856, 72, "rest"), (2500, 3, 3856, 9008, 136, "uneven"), (9000, 1, 8080, 2064, 0, "even")]
 
 
