@@ -305,7 +305,7 @@ size_t runlora_dora_workspace_bytes(int fwd, int bwd, int64_t n, int64_t i, int6
  * runlora_workspace_bytes_w with w_dtype = RL_FP8_B128.  runlora_select takes RL_FP8_B128 as its dtype.
  *
  * runlora_fp8_quantize rounds a dense matrix (RL_F32 / RL_F16 / RL_BF16, [rows, cols]) to the same values in blocks of 128 x 128:
- * dst->data and dst->scales (RL_FP8_B128, same rows and cols, cols a multiple of 16) are written.
+ * dst->data and dst->scales (RL_FP8_B128, same rows and cols, cols a multiple of 16) are written.  Rows and cols up to 2097152.
  */
 int runlora_fp8_quantize(const rl_tensor_t* src, rl_tensor_t* dst, const rl_opts_t* opts);
 

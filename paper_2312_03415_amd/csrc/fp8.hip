@@ -1,5 +1,5 @@
 // Quantisers of the 8-bit products (see fp8.hpp).  Both are bound by memory, 2 bytes read and 1 written per 16-bit element: 8192 x 11008 bf16 in
-// blocks of 128 x 128 53 us (5.1 TB/s), its rows 70 us (3.9 TB/s; a layer with an adapter rounds them in its rank products instead).
+// blocks of 128 x 128 53 us (5.1 TB/s), its rows 58 us (4.7 TB/s; a layer with an adapter rounds them in its rank products instead).
 #include "fp8.hpp"
 
 #include "gemm.hpp"

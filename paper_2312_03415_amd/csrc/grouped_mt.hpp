@@ -127,7 +127,7 @@ __device__ __forceinline__ int grouped_swz(int q) {
 // ROWS: A, which a rank-r product reads once (X in T = s X A, dY in Z = s dY B^T), is rounded to e4m3 for the large product on the way: a
 // thread takes the 16-byte chunks of the tile that it loaded, keeps those of every other K tile, and rounds both halves of a block
 // of 128 columns together, the eight lanes of a row agreeing on its largest magnitude.  The pass over A that rounding would take is saved:
-// dY of 8192 x 11008 r 32 71 us in place of 54 + 56 in two, of 16384 x 11008 r 128 178 in place of 126 + 186.
+// dY of 8192 x 11008 r 32 69 us in place of 58 + 35 in two, of 16384 x 11008 r 128 163 in place of 134 + 102.
 template <typename T, bool F8, int AL, int BL, int BM, int BN, int WM, int NS, bool ROWS = false>
 __device__ __forceinline__ void grouped_mt_body(const GroupedArgs& g, const int bx, const int by) {
   static_assert(!ROWS || (!F8 && AL == 0), "a 16-bit A by rows");

@@ -535,7 +535,8 @@ class RunLoRAFp8Linear(nn.Module):
 class RunLoRAExperts(nn.Module):
     """One adapted linear layer per expert, on rows sorted by expert: frozen weight [experts, d_in, d_out] (a tensor or an Fp8Weight stack) and
     bias [experts, d_out], trainable A [experts, d_in, r] and B [experts, r, d_out]; layer(x [n, d_in], ends), ends (int32, on the
-    device) = where each expert's rows end, e.g. torch.bincount(expert_of_row, minlength=experts).cumsum(0, dtype=torch.int32)."""
+    device) = where each expert's rows end, e.g. torch.bincount(expert_of_row, minlength=experts).cumsum(0, dtype=torch.int32).
+    The adapters have the weight's type, over an 8-bit weight `dtype` (bfloat16 if not given)."""
 
     def __init__(self, weight, r, alpha=None, bias=None, dtype=None):
         super().__init__()
