@@ -198,6 +198,11 @@ def dtype_code(torch_dtype):
     return _dtype_codes[torch_dtype]
 
 
+def _current_device():
+    import torch
+    return torch._C._cuda_getDevice()
+
+
 _current_raw_stream = None
 
 
@@ -269,8 +274,9 @@ class Fp8Weight:
         rows, cols = w.shape[-2:]
         q = torch.empty(w.shape, dtype=torch.uint8, device=w.device)
         s = torch.empty(tuple(w.shape[:-2]) + ((rows + 127) // 128, (cols + 127) // 128), dtype=torch.uint8, device=w.device)
-        for src, dst, sc in zip(w, q, s) if w.dim() == 3 else ((w, q, s),):
-            runlora_fp8_quantize(src, dst, sc, stream)
+        with torch.cuda.device_of(w):
+            for src, dst, sc in zip(w, q, s) if w.dim() == 3 else ((w, q, s),):
+                runlora_fp8_quantize(src, dst, sc, stream)
         return Fp8Weight(q, s, rows, cols)
 
 
@@ -307,7 +313,7 @@ def stack_desc(t):
 
 
 def _one_gpu(first, *others):
-    """Refuses operands (None, tensors, Fp8Weights) that are not all in one GPU's memory: a kernel would read an address of the host's."""
+    """Refuses operands (None, tensors, Fp8Weights) that are not all in the current GPU's memory: a kernel would read addresses that are not its device's."""
     device = first.get_device()
     if device < 0:
         raise ValueError(f"operands must be on a GPU, not on {first.device}")
@@ -316,6 +322,8 @@ def _one_gpu(first, *others):
             t = t.data  # (its scales are where they are)
         if t is not None and t.get_device() != device:
             raise ValueError(f"operands must be on one GPU: {t.device}, not {first.device}")
+    if device != _current_device():
+        raise ValueError(f"operands are on {first.device}, which is not the current device")
 
 
 def _ends(ends, experts):

@@ -17,6 +17,7 @@ for the calls that have to see a Python-level function (tracing, functorch trans
     y = experts(x_sorted, ends)                                      # rows sorted by expert, ends[e] = where expert e's rows end
 """
 import ctypes
+import functools
 import math
 
 import torch
@@ -50,6 +51,15 @@ def _native():
         _autograd.init(tuple(address(f) for f in entries), rl._check)
         _native_module = _autograd
     return _native_module
+
+
+def _on_inputs_gpu(forward):
+    """A Python node's forward, run on its input's GPU: what it launches goes to the current device's stream.  (Backwards are run on theirs by autograd.)"""
+    @functools.wraps(forward)
+    def run(ctx, x, *args):
+        with torch.cuda.device_of(x):
+            return forward(ctx, x, *args)
+    return staticmethod(run)
 
 
 def _rows(x, width):
@@ -93,7 +103,7 @@ class RunLoRAFunction(torch.autograd.Function):
                 return y
         return super().apply(*args)
 
-    @staticmethod
+    @_on_inputs_gpu
     def forward(ctx, x, W, A, B, bias, scale, pair, keep_merged, dropout=None, keep_t=False):
         fwd, bwd = pair
         i, o = W.shape
@@ -209,7 +219,7 @@ class RunVeRAFunction(torch.autograd.Function):
                 return y
         return super().apply(*args)
 
-    @staticmethod
+    @_on_inputs_gpu
     def forward(ctx, x, W, A, B, d, b, bias, scale, pair):
         fwd, bwd = pair
         i, o = W.shape
@@ -299,7 +309,7 @@ class RunDoRAFunction(torch.autograd.Function):
                 return y
         return super().apply(*args)
 
-    @staticmethod
+    @_on_inputs_gpu
     def forward(ctx, x, W, A, B, m, bias, scale, bwd):
         i, o = W.shape
         r = A.shape[1]
@@ -400,7 +410,7 @@ class RunLoRAExpertsFunction(torch.autograd.Function):
                     return y
         return super().apply(x, ends, W, A, B, bias, scale)
 
-    @staticmethod
+    @_on_inputs_gpu
     def forward(ctx, x, ends, W, A, B, bias, scale):
         E, i, o = W.shape
         x2 = _rows(x, i)
@@ -450,7 +460,7 @@ class RunLoRAFp8Function(torch.autograd.Function):
                 return y
         return super().apply(x, W, A, B, bias, scale)
 
-    @staticmethod
+    @_on_inputs_gpu
     def forward(ctx, x, W, A, B, bias, scale):
         x2 = _rows(x, W.rows)
         n, r, code = x2.shape[0], A.shape[1], rl.dtype_code(x.dtype)

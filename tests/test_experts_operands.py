@@ -185,3 +185,63 @@ def test_an_8_bit_weight_stays_in_8_bits_whatever_the_module_is_turned_to(expert
         torch.nn.Sequential(layer).load_state_dict({"0." + k: v for k, v in state.items()})
         assert torch.equal(layer.weight_data.view(torch.uint8), data) and torch.equal(layer.weight_scales.view(torch.uint8), scales)
         assert state["weight_data"].dtype == d.dtype
+
+
+# ---- the GPU that a call runs on ---------------------------------------------------------------------------------------
+
+def _device_of(torch, monkeypatch):
+    """The tensors whose GPU is the current one at the moment, as torch.cuda.device_of is told."""
+    on = []
+
+    class Recorder:
+        def __init__(self, t):
+            self.t = t
+
+        def __enter__(self):
+            on.append(self.t)
+
+        def __exit__(self, *_):
+            on.pop()
+    monkeypatch.setattr(torch.cuda, "device_of", Recorder)
+    return on
+
+
+@pytest.mark.parametrize("kind", ["lora", "vera", "dora", "fp8", "experts"])
+def test_python_nodes_run_on_their_inputs_gpu(kind, monkeypatch):
+    """What a forward launches goes to the current device's stream, and the native nodes leave inputs on another GPU to the Python ones: those make it current."""
+    torch = pytest.importorskip("torch")
+    from paper_2312_03415_amd import module
+    on, called = _device_of(torch, monkeypatch), []
+
+    def stub(name):
+        monkeypatch.setattr(rl, name, lambda *a, **k: called.append((name, len(on) == 1 and on[0].shape == (40, 256))))
+    for name in ("runlora_forward", "runlora_vera_forward", "runlora_dora_forward", "runlora_experts_forward"):
+        stub(name)
+    z = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16)
+    x, W, A, B = z(40, 256), z(256, 272), z(256, 16), z(16, 272)
+    t = _operands(torch, True)
+    fn, args = {"lora": (module.RunLoRAFunction, (x, W, A, B, None, 1.0, (1, 1), False)), "vera": (module.RunVeRAFunction, (x, W, A, B, z(16), z(272), None, 1.0, (1, 1))),
+                "dora": (module.RunDoRAFunction, (x, W, A, B, z(272), None, 1.0, 4)),
+                "fp8": (module.RunLoRAFp8Function, (x, rl.Fp8Weight(t["W"].data[0], t["W"].scales[0], 256, 272), A, B, None, 1.0)),
+                "experts": (module.RunLoRAExpertsFunction, (x, t["ends"], t["W"], t["A"], t["B"], None, 1.0))}[kind]
+    type("Python" + fn.__name__, (fn,), {}).apply(*args)
+    assert len(called) == 1 and called[0][1] and not on
+
+
+@pytest.mark.parametrize("call,names", [("forward", FORWARD), ("backward", BACKWARD)])
+def test_operands_on_another_gpu_than_the_current_one_are_refused(call, names, no_library, monkeypatch):
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(rl, "_current_device", lambda: 1)
+    with _fake_gpu(torch):
+        gpu = {k: _on(v, "cuda:0") for k, v in _operands(torch, True).items()}
+        with pytest.raises(ValueError, match="current"):
+            getattr(rl, "runlora_experts_" + call)(**{k: gpu[k] for k in names})
+
+
+@pytest.mark.parametrize("shape", [(256, 272), (3, 256, 272)])
+def test_a_weight_is_quantised_on_its_gpu(shape, monkeypatch):
+    torch = pytest.importorskip("torch")
+    on, called, w = _device_of(torch, monkeypatch), [], torch.zeros(shape)
+    monkeypatch.setattr(rl, "runlora_fp8_quantize", lambda *a: called.append(len(on) == 1 and on[0] is w))
+    assert rl.Fp8Weight.quantize(w).shape == shape
+    assert called == [True] * (3 if len(shape) == 3 else 1) and not on

@@ -1,6 +1,7 @@
-"""Long contractions over experts and 8-bit weights.  Output tiles of the large grouped kernel whose K tiles are dealt out to several workgroups, in either direction, with experts, rows behind the last one's, adapters
-behind the last run only, and e4m3 runs on both sides of the 64th K tile (where a wave changes the register that W's scales are in); and the smaller tiles, which read W's scales again every 64 K tiles.  What every case here
-runs on is checked on the host (test_experts_plans.py)."""
+"""Long contractions over experts and 8-bit weights.  Output tiles of the large grouped kernel whose K tiles are dealt out to several workgroups, in either
+direction, with experts, rows behind the last one's, adapters behind the last run only, and e4m3 runs on both sides of the 64th K tile (where a wave
+changes the register that W's scales are in); and the smaller tiles, which read W's scales again every 64 K tiles.  What every case here runs on is
+checked on the host (test_experts_plans.py)."""
 import numpy as np
 import pytest
 
