@@ -294,24 +294,25 @@ GroupedPlan grouped_plan(const ExpertsDesc& d, int64_t N, int64_t K, bool slices
     const GroupedTileInfo t = grouped_tile(tile);
     return grouped_row_tiles(d.n, d.experts, d.has_ends, t.bm, d.f8) * ceil_div(N, t.bn);
   };
-  auto expected = [&](int tile) {  // tiles that there will be: an expert's last row tile is half full on average (not said of experts below half a tile)
+  auto expected = [&](int tile) {  // tiles that there will be: an expert's last row tile is half full on average
     const GroupedTileInfo t = grouped_tile(tile);
     return (d.has_ends ? (d.n + (some + 1) * (t.bm / 2)) / t.bm : ceil_div(d.n, t.bm)) * ceil_div(N, t.bn);
   };
-  // A larger tile costs less a product, as long as it is filled: it is taken where the next smaller ones are more than one round, two to a compute
-  // unit (kFill).  Measured without adapters, 16-bit / 8-bit weights, us:
-  //  128 x 128 for 64 x 128, K 768 to 8192: 540 to 672 of the smaller (270 to 336 of the larger; 8 shapes, one group) 16-28 % / 7-30 % faster, e.g. Y of 2100 x 4096 ->
-  //    2320 56 / 43 in place of 75 / 56; 500 and fewer (4 shapes of 3 to 8 uneven experts) the same to 30 % slower, 2000 rows of 8 experts 4096 -> 1792
-  //    60 / 41 in place of 46 / 33.
-  //  256 x 256 for 128 x 128, K 1536 to 8192: 576 to 768 of the smaller (144 to 192 of the larger; 6 shapes) 7-18 % / up to 22 % faster, 2300 x 4096 -> 4096 93 / 61 in place
-  //    of 108 / 70, and with 4, 8 and 16 uneven experts (540 to 672) 9-30 % / 4-28 %, 2400 rows of 4 experts 4096 -> 4096 97 / 62 in place of 136 / 73; 512 and fewer
-  //    slower, 1600 rows of 8 experts 4096 -> 4096 99 / 59 in place of 91 / 54.  A K below 1024 only where they fill a round by themselves:
-  //    3000 x 768 -> 4096 (192 of the larger) 26.4 / 28.4 in place of 25.8 / 25.9; 3000 rows of 12 experts 1032 -> 2744 38 / 31, 42 / 33 in the smaller.
+  // A larger tile costs less a product, as long as it is filled: it is taken where the next smaller ones are more than one round, two to a
+  // compute unit (kFill).  Measured without adapters, 16-bit / 8-bit weights, us:
+  //  128 x 128 for 64 x 128, K 768 to 8192.  540 to 672 of the smaller (one group, 10 shapes): 14-30 % / 9-31 % saved, Y of 2100 x 4096 -> 2320
+  //    56 / 43 in place of 75 / 56.  Fewer than 512 (3 to 8 uneven experts, 6 shapes): 7 % / 3 % saved to 31 % / 24 % lost, dX of 2000 rows of 8
+  //    experts 4096 -> 1792 60 / 41 in place of 46 / 33.
+  //  256 x 256 for 128 x 128, K 1024 to 8192.  576 to 768 of the smaller (144 to 192 of the larger; one group, 6 shapes): 5-19 % / up to 22 %
+  //    saved, 2300 x 4096 -> 4096 93 / 61 in place of 108 / 70; 540 to 672 of 4 to 16 uneven experts: 9-32 % / 1-29 %, 2400 rows of 4 experts
+  //    4096 -> 4096 97 / 62 in place of 136 / 73.  Up to 512 of them: 2-34 % lost, 1600 rows of 8 experts 4096 -> 4096 99 / 59 in place of 91 / 54.
+  //    A K below 1024 only where they fill a round by themselves: 3000 x 768 -> 4096 (192) 28.7 / 29.6 in place of 28.6 / 27.6.
   //  64 x 128 from about 160: 300 x 4096 -> 4096 (160 tiles) 33 / 24 against 34 / 25 in 32 x 128 tiles, 200 x 2048 -> 2048 (64) 18 / 15
   //    against 15.5 / 13.
-  // With 16-bit weights and a long K, fewer than half a round of 256 x 256 tiles whose K is split over the compute units are faster than one round of smaller ones:
-  // 1237 x 5456 -> 2064 (45 tiles, 86 K tiles) 51 against 64, 3000 rows of 8 experts 8192 -> 1024 (60, 128) 79 against 108, 2560 x 8192 -> 2816 (110, 128) 111
-  // against 115; not with 64 K tiles, 2048 x 4096 -> 2048 51 against 43, or with 80, 2048 x 5120 -> 3584 80 against 75; with 8-bit weights 73 against 46 and 70 against 65.
+  // With 16-bit weights and a long K, up to half a round of 256 x 256 tiles whose K is split over the compute units are faster than one round of
+  // smaller ones: 1237 x 5456 -> 2064 (45 tiles, 86 K tiles) 51 against 64, 3000 rows of 8 experts 8192 -> 1024 (60, 128) 79 against 108, 2560 x
+  // 8192 -> 2816 (110, 128) 111 against 115; not with 64 K tiles, 2048 x 4096 -> 2048 51 against 43, or with 80, 2048 x 5120 -> 3584 80 against
+  // 75; with 8-bit weights 73 against 46 and 70 against 65.
   const int64_t nk = ceil_div(K, d.f8 ? 128 : 64);
   p.tile = GT_32x128;
   // In slices of K (few rows) 64 x 128 tiles pay from 32 K tiles: 64 rows 4096 -> 11008 29 us against 33, 11008 -> 4096 33 against 35, but
