@@ -57,7 +57,8 @@ typedef enum {
   RL_F16 = 1,
   RL_BF16 = 2,
   RL_INT4_G64 = 3, /* frozen W only: symmetric int4, one fp16 scale per 64 rows (d_in) per column */
-  RL_FP8_B128 = 4  /* frozen W only: e4m3 values, one power-of-two scale per 128 x 128 block */
+  RL_FP8_B128 = 4, /* frozen W only: e4m3 values, one power-of-two scale per 128 x 128 block */
+  RL_FP8_R128 = 5  /* rows already rounded (runlora_rmsnorm_forward, runlora_fp8_forward): e4m3 values, one power-of-two scale per 128 columns of a row */
 } rl_dtype_t;
 
 typedef enum {
@@ -119,10 +120,13 @@ typedef enum {
  *   rows, cols, ld   in elements; ld = distance between consecutive rows
  *   dtype  rl_dtype_t
  *          For RL_FP8_B128: e4m3 bytes (the type with 448 as its largest value and no infinities), ld in bytes and a multiple of 16
+ *          For RL_FP8_R128: e4m3 bytes, ld = cols rounded up to a multiple of 128, zeros behind cols
  *   scales RL_INT4_G64: device pointer to fp16 scales [ceil(rows/64), cols], row-major, dense
  *          RL_FP8_B128: device pointer to scale bytes [ceil(rows/128), ceil(cols/128)], row-major, dense; byte b stands for 2^(b - 127)
  *          (255: NaN); value (k,j) = e4m3 (k,j) * scale (k/128, j/128)
- *   group  RL_INT4_G64: must be 64; RL_FP8_B128: must be 128
+ *          RL_FP8_R128: device pointer to scale bytes [ceil(cols/128)][rows rounded up to a multiple of 16], dense: the byte of row k and column j
+ *          stands at (j/128, k)
+ *   group  RL_INT4_G64: must be 64; RL_FP8_B128 and RL_FP8_R128: must be 128
  */
 typedef struct {
   void* data;
@@ -346,6 +350,87 @@ int runlora_experts_backward(const rl_tensor_t* dY, const rl_tensor_t* X, const 
                              const rl_opts_t* opts);
 /* the most that any call of these sizes takes (backward = 0: forward); r = 0: no adapter.  0 for what the calls refuse. */
 size_t runlora_experts_workspace_bytes(int backward, int64_t n, int64_t experts, int64_t i, int64_t o, int64_t r, int dtype, int w_dtype);
+
+/*
+ * Routing of n tokens to experts, in front of runlora_experts_*.  From logits l [n, E] (RL_F32 / RL_F16 / RL_BF16, any ld >= E):
+ *     s = softmax(l) over the row, or sigmoid(l);     c = s + bias
+ *     groups > 1: the E experts are `groups` runs of E / groups; a run counts with the sum of its group_top (1 or 2) largest c, and only the
+ *         groups_kept runs that count most take part (equal ones: the first)
+ *     the `top` largest c are chosen, in falling order, equal ones by index: expert [n, top]
+ *     weight_j = scale * s_j, with `renormalise` scale * s_j / sum of the chosen s: weight [n, top]
+ * The choice is that of the logits themselves where nothing is added to the scores, and of c in 64 bits otherwise.  A logit or a bias of -infinity
+ * takes its expert out of the choice (a row of nothing else goes nowhere); where fewer than `top` are left, the rest of a row is expert -1, weight 0.
+ * A row that holds a NaN (softmax: or a +infinity) gives NaN for weights and some choice in range; with sigmoid scores and no renormalise for the NaN's
+ * expert only, which comes first.
+ * The rows sorted by expert, those of an expert in the order of t * top + j, are described for the calls that read them:
+ *     ends [E]         where expert e's rows end (runlora_experts_*)
+ *     place [n, top]   row of token t's copy j; -1: none
+ *     source [n top]   t * top + j of the copy that stands on a row; -1 behind the last expert's rows
+ * runlora_route_backward: dlogits [n, E] (the type of the logits, overwritten) from the choice (`expert`, as the forward left it) and dweight.  The
+ * choice itself and the bias have no gradient.
+ *   rl_route_t   zero the struct first: groups 0 means 1, groups_kept 0 all of them, group_top 0 means 1, scale 0 means 1
+ *   expert, weight, place, source, ends, dweight   device pointers, dense, 4-byte aligned; all required
+ *   opts         forward: workspace of runlora_route_workspace_bytes() where that is not 0
+ * E in [1, 1024], top in [1, min(E, 64)], groups in [1, 64] and a divisor of E, n in [1, 8388607].  Counts and places are sums of whole numbers: the
+ * same call gives the same bits.
+ */
+enum { RL_SCORE_SOFTMAX = 0, RL_SCORE_SIGMOID = 1 };
+typedef struct {
+  int32_t experts, top, score, renormalise, groups, groups_kept, group_top;
+  float scale;
+  const float* bias; /* device pointer to E floats, or NULL */
+} rl_route_t;
+int runlora_route_forward(const rl_tensor_t* logits, const rl_route_t* route, int32_t* expert, float* weight, int32_t* place, int32_t* source,
+                          int32_t* ends, const rl_opts_t* opts);
+int runlora_route_backward(const rl_tensor_t* logits, const rl_route_t* route, const int32_t* expert, const float* dweight, rl_tensor_t* dlogits,
+                           const rl_opts_t* opts);
+/* 0 also for what the calls refuse */
+size_t runlora_route_workspace_bytes(int64_t n, int64_t experts, int64_t top);
+
+/*
+ * Rows to the experts and back, around runlora_experts_* (place and source as runlora_route_forward leaves them, top copies a token):
+ *     gather            rows[place[t, j]] = X_t                                       rows [n top, d]
+ *     gather backward   dX_t = sum_j drows[place[t, j]]
+ *     combine           Y_t = add_t + sum_j weight[t, j] rows[place[t, j]]            add may be NULL
+ *     combine backward  drows[place[t, j]] = weight[t, j] dY_t,   dweight[t, j] = sum over columns of dY_t rows[place[t, j]]
+ * A copy without a place (anything outside [0, n top)) adds nothing and has a dweight of 0; rows without a copy (source negative) are written as
+ * zeros.  fp32 sums in the order of j (of the columns in a fixed order), rounded once.  drows or dweight may be NULL (skipped); without dweight rows may
+ * be NULL.  The gradient of `add` is dY itself.
+ * RL_F32 / RL_F16 / RL_BF16; n in [1, 8388607], top in [1, 64], d a multiple of 8 (16-bit types) or 4; weight and dweight [n, top] floats, dense.
+ */
+int runlora_gather_forward(const rl_tensor_t* X, const int32_t* place, const int32_t* source, int top, rl_tensor_t* rows, const rl_opts_t* opts);
+int runlora_gather_backward(const rl_tensor_t* drows, const int32_t* place, int top, rl_tensor_t* dX, const rl_opts_t* opts);
+int runlora_combine_forward(const rl_tensor_t* rows, const int32_t* place, const float* weight, int top, const rl_tensor_t* add, rl_tensor_t* Y,
+                            const rl_opts_t* opts);
+int runlora_combine_backward(const rl_tensor_t* dY, const rl_tensor_t* rows, const int32_t* place, const int32_t* source, const float* weight, int top,
+                             rl_tensor_t* drows, float* dweight, const rl_opts_t* opts);
+
+/*
+ * Root-mean-square norm with the residual's addition:
+ *     h = X + R (R NULL: h = X),     Y = h / sqrt(mean of h^2 + eps) * gain
+ * h is rounded to the storage type before it is normed: it is the residual stream that the next layers add to, and what the backward reads.
+ *   gain    device pointer to d elements of the type, or NULL (1)
+ *   H       where h goes, or NULL; may be X or R itself (same data and ld)
+ *   rstd    n floats, 1 / sqrt(mean h^2 + eps), or NULL; required for a backward
+ *   Q       RL_FP8_R128 [n, d] or NULL: Y (as rounded to its type) in e4m3, as an RL_FP8_B128 layer rounds its rows; 16-bit types
+ * runlora_rmsnorm_backward: with N = gain dY, dX = rstd (N - h rstd^2 mean(N h)) + dH, the gradient of X and of R alike; dgain = sum over rows of
+ * dY h rstd.  H is the forward's h (X where there was no R); dH, what reaches h from elsewhere, may be NULL; dX or dgain may be NULL (skipped).
+ * workspace: runlora_rmsnorm_workspace_bytes(), for dgain only.
+ * RL_F32 / RL_F16 / RL_BF16; n in [1, 2^30], d in [1, 32768], a multiple of 8 (16-bit types) or 4.  Sums are fp32 in a fixed order.
+ */
+int runlora_rmsnorm_forward(const rl_tensor_t* X, const rl_tensor_t* R, const void* gain, float eps, rl_tensor_t* Y, rl_tensor_t* H, float* rstd,
+                            rl_tensor_t* Q, const rl_opts_t* opts);
+int runlora_rmsnorm_backward(const rl_tensor_t* dY, const rl_tensor_t* dH, const rl_tensor_t* H, const void* gain, const float* rstd, rl_tensor_t* dX,
+                             void* dgain, const rl_opts_t* opts);
+size_t runlora_rmsnorm_workspace_bytes(int64_t n, int64_t d, int dtype);
+
+/*
+ * runlora_forward(RL_FWD1, ...) over an RL_FP8_B128 W with X's rows already rounded: Q (RL_FP8_R128, X's rows and columns, as runlora_rmsnorm_forward
+ * writes them) takes the place of Q(X) in the large product, and X enters X A alone.  Where Q is Q(X) the results are those of runlora_forward, bit
+ * for bit.  Same saved record, workspace and options.
+ */
+int runlora_fp8_forward(const rl_tensor_t* X, const rl_tensor_t* Q, const rl_tensor_t* W, const rl_tensor_t* A, const rl_tensor_t* B, rl_tensor_t* Y,
+                        rl_saved_t* saved, const rl_opts_t* opts);
 
 /*
  * Choose the (forward, backward) pair of computation graphs for one layer shape, by estimated time

@@ -17,7 +17,7 @@ import os
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "librunlora.so")
 
-RL_F32, RL_F16, RL_BF16, RL_INT4_G64, RL_FP8_B128 = 0, 1, 2, 3, 4
+RL_F32, RL_F16, RL_BF16, RL_INT4_G64, RL_FP8_B128, RL_FP8_R128 = 0, 1, 2, 3, 4, 5
 FWD_DEFAULT, FWD1, FWD2, FWD3 = 0, 1, 2, 3
 BWD_DEFAULT, BWD1, BWD2, BWD3, BWD4, BWD5, BWD6, BWD7, BWD8 = 0, 1, 2, 3, 4, 5, 6, 7, 8
 FWD_VARIANTS = (FWD_DEFAULT, FWD1, FWD2, FWD3)
@@ -38,7 +38,11 @@ EXPORTS = (
     "runlora_vera_forward", "runlora_vera_backward", "runlora_vera_workspace_bytes",
     "runlora_dora_forward", "runlora_dora_backward", "runlora_dora_workspace_bytes",
     "runlora_fp8_quantize", "runlora_experts_forward", "runlora_experts_backward", "runlora_experts_workspace_bytes",
+    "runlora_route_forward", "runlora_route_backward", "runlora_route_workspace_bytes", "runlora_gather_forward", "runlora_gather_backward",
+    "runlora_combine_forward", "runlora_combine_backward", "runlora_rmsnorm_forward", "runlora_rmsnorm_backward", "runlora_rmsnorm_workspace_bytes",
+    "runlora_fp8_forward",
 )
+SCORES = ("softmax", "sigmoid")  # RL_SCORE_SOFTMAX, RL_SCORE_SIGMOID
 
 
 class rl_tensor_t(ctypes.Structure):
@@ -65,6 +69,12 @@ class rl_opts_t(ctypes.Structure):
     _fields_ = [("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
                 ("scale", ctypes.c_float), ("bias", ctypes.c_void_p), ("dropout_p", ctypes.c_float),
                 ("dropout_seed", ctypes.c_uint32)]
+
+
+class rl_route_t(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_int32), ("top", ctypes.c_int32), ("score", ctypes.c_int32), ("renormalise", ctypes.c_int32),
+                ("groups", ctypes.c_int32), ("groups_kept", ctypes.c_int32), ("group_top", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("bias", ctypes.c_void_p)]
 
 
 class rl_gemm_t(ctypes.Structure):
@@ -138,6 +148,29 @@ def lib():
     L.runlora_experts_backward.restype = ci
     L.runlora_experts_workspace_bytes.argtypes = [ci, i64, i64, i64, i64, i64, ci, ci]
     L.runlora_experts_workspace_bytes.restype = ctypes.c_size_t
+    rp = ctypes.POINTER(rl_route_t)
+    L.runlora_route_forward.argtypes = [tp, rp, vp, vp, vp, vp, vp, op]
+    L.runlora_route_forward.restype = ci
+    L.runlora_route_backward.argtypes = [tp, rp, vp, vp, tp, op]
+    L.runlora_route_backward.restype = ci
+    L.runlora_route_workspace_bytes.argtypes = [i64, i64, i64]
+    L.runlora_route_workspace_bytes.restype = ctypes.c_size_t
+    L.runlora_gather_forward.argtypes = [tp, vp, vp, ci, tp, op]
+    L.runlora_gather_forward.restype = ci
+    L.runlora_gather_backward.argtypes = [tp, vp, ci, tp, op]
+    L.runlora_gather_backward.restype = ci
+    L.runlora_combine_forward.argtypes = [tp, vp, vp, ci, tp, tp, op]
+    L.runlora_combine_forward.restype = ci
+    L.runlora_combine_backward.argtypes = [tp, tp, vp, vp, vp, ci, tp, vp, op]
+    L.runlora_combine_backward.restype = ci
+    L.runlora_rmsnorm_forward.argtypes = [tp, tp, vp, ctypes.c_float, tp, tp, vp, tp, op]
+    L.runlora_rmsnorm_forward.restype = ci
+    L.runlora_rmsnorm_backward.argtypes = [tp, tp, tp, vp, vp, tp, vp, op]
+    L.runlora_rmsnorm_backward.restype = ci
+    L.runlora_rmsnorm_workspace_bytes.argtypes = [i64, i64, ci]
+    L.runlora_rmsnorm_workspace_bytes.restype = ctypes.c_size_t
+    L.runlora_fp8_forward.argtypes = [tp, tp, tp, tp, tp, tp, sp, op]
+    L.runlora_fp8_forward.restype = ci
     L.runlora_select.argtypes = [i64, i64, i64, i64, ci, ip, ip]
     L.runlora_select.restype = ci
     L.runlora_select_by.argtypes = [ci, i64, i64, i64, i64, ci, ip, ip]
@@ -280,10 +313,85 @@ class Fp8Weight:
         return Fp8Weight(q, s, rows, cols)
 
 
-def tensor_desc(t):
-    """rl_tensor_t view of a 2-D torch tensor, an Int4Weight or an Fp8Weight (None -> NULL pointer argument)."""
+class Fp8Rows:
+    """Rows [rows, cols] in e4m3 with one power-of-two scale per 128 columns of a row (RL_FP8_R128), as the 8-bit layers round theirs: `data`
+    holds the bytes, uint8 [rows, cols rounded up to 128], `scales` the scale bytes, uint8 [ceil(cols/128), rows rounded up to 16]."""
+
+    def __init__(self, data, scales, rows, cols):
+        blocks = (cols + 127) // 128
+        for t, shape, name in ((data, (rows, blocks * 128), "data"), (scales, (blocks, (rows + 15) // 16 * 16), "scales")):
+            if tuple(t.shape) != shape or t.element_size() != 1 or not t.is_contiguous():
+                raise ValueError(f"{name} must be dense bytes {shape}")
+        if scales.device != data.device:
+            raise ValueError("data and scales must be on one device")
+        self.data, self.scales, self.rows, self.cols = data, scales, rows, cols
+
+    @property
+    def shape(self):
+        return (self.rows, self.cols)
+
+    @staticmethod
+    def empty(rows, cols, device="cuda"):
+        """Room for such rows."""
+        import torch
+        blocks = (cols + 127) // 128
+        make = lambda *shape: torch.empty(shape, dtype=torch.uint8, device=device)
+        return Fp8Rows(make(rows, blocks * 128), make(blocks, (rows + 15) // 16 * 16), rows, cols)
+
+    def values(self, dtype=None):
+        """The values that the bytes stand for (float32 if no dtype is given)."""
+        import torch
+        scale = torch.exp2(self.scales[:, :self.rows].t().float() - 127.0).to(dtype or torch.float32)
+        q = self.data.view(torch.float8_e4m3fn).to(scale.dtype).view(self.rows, -1, 128)
+        return (q * scale[:, :, None]).view(self.rows, -1)[:, :self.cols]
+
+
+class Route:
+    """How tokens are routed to experts (rl_route_t of runlora.h): `top` of `experts`, by "softmax" or "sigmoid" scores; renormalise: a token's weights
+    sum to `scale`; groups > 1: only the `groups_kept` runs of experts / groups take part whose `group_top` best scores sum to most."""
+
+    def __init__(self, experts, top, score="softmax", renormalise=True, groups=1, groups_kept=None, group_top=1, scale=1.0):
+        if score not in SCORES:
+            raise ValueError(f"score must be one of {SCORES}")
+        if not scale:
+            raise ValueError("scale must not be zero")
+        self.experts, self.top, self.score, self.renormalise = experts, top, score, bool(renormalise)
+        self.groups, self.groups_kept, self.group_top, self.scale = groups, groups if groups_kept is None else groups_kept, group_top, float(scale)
+        for name in ("experts", "top", "groups", "groups_kept", "group_top"):
+            if getattr(self, name) < 1:
+                raise ValueError(f"{name} must be at least 1")
+
+    def desc(self, bias=None):
+        """rl_route_t, with the balance bias (None or float32 [experts])."""
+        import torch
+        return rl_route_t(self.experts, self.top, SCORES.index(self.score), int(self.renormalise), self.groups, self.groups_kept, self.group_top, self.scale,
+                          _vector(bias, self.experts, torch.float32, "bias"))
+
+
+def _vector(t, count, dtype, name):
+    """Device pointer of a dense vector of `count` elements (None -> NULL)."""
     if t is None:
         return None
+    if t.dim() != 1 or t.numel() != count or t.dtype != dtype or (count > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a dense {dtype} vector of {count} elements")
+    return t.data_ptr()
+
+
+def _table(t, shape, dtype, name):
+    """Device pointer of a dense tensor of a known shape and type (None -> NULL)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a dense {dtype} tensor {tuple(shape)}")
+    return t.data_ptr()
+
+
+def tensor_desc(t):
+    """rl_tensor_t view of a 2-D torch tensor, an Int4Weight, an Fp8Weight or Fp8Rows (None -> NULL pointer argument)."""
+    if t is None:
+        return None
+    if isinstance(t, Fp8Rows):
+        return rl_tensor_t(t.data.data_ptr(), t.rows, t.cols, t.data.shape[1], RL_FP8_R128, t.scales.data_ptr(), 128)
     if isinstance(t, Fp8Weight):
         if t.experts is not None:
             raise ValueError("expected a single matrix, not a stack")
@@ -318,7 +426,7 @@ def _one_gpu(first, *others):
     if device < 0:
         raise ValueError(f"operands must be on a GPU, not on {first.device}")
     for t in others:
-        if isinstance(t, Fp8Weight):
+        if isinstance(t, (Fp8Weight, Fp8Rows)):
             t = t.data  # (its scales are where they are)
         if t is not None and t.get_device() != device:
             raise ValueError(f"operands must be on one GPU: {t.device}, not {first.device}")
@@ -509,6 +617,139 @@ def runlora_experts_backward(dY, X, ends, W, A, B, dX, dA, dB, T=None, workspace
 
 def runlora_experts_workspace_bytes(backward, n, experts, i, o, r, dtype, w_dtype=None):
     return int(lib().runlora_experts_workspace_bytes(int(bool(backward)), n, experts, i, o, r, dtype, dtype if w_dtype is None else w_dtype))
+
+
+def runlora_fp8_forward(X, Q, W, A, B, Y, saved, workspace=None, stream=None, scale=None, bias=None):
+    """runlora_forward(FWD1, ...) over an Fp8Weight with X's rows already rounded (Q: Fp8Rows, as runlora_rmsnorm_forward writes them)."""
+    if bias is not None and (bias.dtype != X.dtype or bias.numel() != Y.shape[1]):
+        raise ValueError("bias must have d_out elements of the activation dtype")
+    if not isinstance(Q, Fp8Rows) or not isinstance(W, Fp8Weight):
+        raise ValueError("Q must be Fp8Rows and W an Fp8Weight")
+    _one_gpu(X, Q, W, A, B, Y, workspace, bias)
+    dx, dq, dw, da, db, dy = (tensor_desc(t) for t in (X, Q, W, A, B, Y))
+    o = _opts(workspace, stream, scale, bias)
+    _check(lib().runlora_fp8_forward(_ref(dx), _ref(dq), _ref(dw), _ref(da), _ref(db), _ref(dy), ctypes.byref(saved), ctypes.byref(o)))
+    return Y
+
+
+def _logits_desc(t):
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("expected 2-D logits with contiguous rows")
+    rows, cols = t.shape
+    # (a single row or column may carry any stride)
+    return rl_tensor_t(t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else max(cols, t.stride(0)), dtype_code(t.dtype), None, 0)
+
+
+def runlora_route_forward(logits, route, weight, expert, place, source, ends, bias=None, workspace=None, stream=None):
+    """Routing of tokens by logits [n, experts] (see runlora.h): writes weight (float32) and expert (int32) [n, top], and the order of the rows sorted
+    by expert, place [n, top], source [n top] and ends [experts] (int32).  route: Route; bias: None or float32 [experts], added to the scores for the
+    choice alone.  workspace: runlora_route_workspace_bytes bytes."""
+    import torch
+    n, top = logits.shape[0], route.top
+    _one_gpu(logits, weight, expert, place, source, ends, bias, workspace)
+    dl, plan, o = _logits_desc(logits), route.desc(bias), _opts(workspace, stream)
+    i32 = torch.int32
+    _check(lib().runlora_route_forward(ctypes.byref(dl), ctypes.byref(plan), _table(expert, (n, top), i32, "expert"),
+                                       _table(weight, (n, top), torch.float32, "weight"), _table(place, (n, top), i32, "place"),
+                                       _table(source, (n * top,), i32, "source"), _table(ends, (route.experts,), i32, "ends"), ctypes.byref(o)))
+    return weight, expert, place, source, ends
+
+
+def runlora_route_backward(logits, route, expert, dweight, dlogits, bias=None, stream=None):
+    """Gradient of the logits from dweight (float32 [n, top]) and the choice that the forward left in `expert`; bias as in the forward."""
+    import torch
+    n, top = logits.shape[0], route.top
+    _one_gpu(logits, expert, dweight, dlogits, bias)
+    dl, gl, plan, o = _logits_desc(logits), _logits_desc(dlogits), route.desc(bias), _opts(None, stream)
+    _check(lib().runlora_route_backward(ctypes.byref(dl), ctypes.byref(plan), _table(expert, (n, top), torch.int32, "expert"),
+                                        _table(dweight, (n, top), torch.float32, "dweight"), ctypes.byref(gl), ctypes.byref(o)))
+    return dlogits
+
+
+def runlora_route_workspace_bytes(n, experts, top):
+    return int(lib().runlora_route_workspace_bytes(n, experts, top))
+
+
+def _copies(place, n):
+    if place.dim() != 2 or place.shape[0] != n:
+        raise ValueError("place must be [n, top]")
+    return place.shape[1]
+
+
+def runlora_gather_forward(X, place, source, rows, stream=None):
+    """rows[place[t, j]] = X[t] for the rows [n top, d] sorted by expert (zeros where source is negative); place and source as runlora_route_forward
+    writes them."""
+    import torch
+    top = _copies(place, X.shape[0])
+    _one_gpu(X, place, source, rows)
+    dx, dr, o = tensor_desc(X), tensor_desc(rows), _opts(None, stream)
+    _check(lib().runlora_gather_forward(_ref(dx), _table(place, place.shape, torch.int32, "place"), _table(source, (X.shape[0] * top,), torch.int32, "source"),
+                                        top, _ref(dr), ctypes.byref(o)))
+    return rows
+
+
+def runlora_gather_backward(drows, place, dX, stream=None):
+    """dX[t] = sum over j of drows[place[t, j]]."""
+    import torch
+    top = _copies(place, dX.shape[0])
+    _one_gpu(drows, place, dX)
+    dr, dx, o = tensor_desc(drows), tensor_desc(dX), _opts(None, stream)
+    _check(lib().runlora_gather_backward(_ref(dr), _table(place, place.shape, torch.int32, "place"), top, _ref(dx), ctypes.byref(o)))
+    return dX
+
+
+def runlora_combine_forward(rows, place, weight, Y, add=None, stream=None):
+    """Y[t] = add[t] + sum over j of weight[t, j] rows[place[t, j]] (weight float32 [n, top]; add None: nothing)."""
+    import torch
+    top = _copies(place, Y.shape[0])
+    _one_gpu(rows, place, weight, Y, add)
+    dr, da, dy, o = tensor_desc(rows), tensor_desc(add), tensor_desc(Y), _opts(None, stream)
+    _check(lib().runlora_combine_forward(_ref(dr), _table(place, place.shape, torch.int32, "place"), _table(weight, place.shape, torch.float32, "weight"),
+                                         top, _ref(da), _ref(dy), ctypes.byref(o)))
+    return Y
+
+
+def runlora_combine_backward(dY, rows, place, source, weight, drows, dweight, stream=None):
+    """drows[place[t, j]] = weight[t, j] dY[t] and dweight[t, j] = <dY[t], rows[place[t, j]]>; either may be None (skipped)."""
+    import torch
+    n = dY.shape[0]
+    top = _copies(place, n)
+    _one_gpu(dY, rows, place, source, weight, drows, dweight)
+    ddy, dr, gr, o = tensor_desc(dY), tensor_desc(rows), tensor_desc(drows), _opts(None, stream)
+    _check(lib().runlora_combine_backward(_ref(ddy), _ref(dr), _table(place, place.shape, torch.int32, "place"),
+                                          _table(source, (n * top,), torch.int32, "source"), _table(weight, place.shape, torch.float32, "weight"), top,
+                                          _ref(gr), _table(dweight, place.shape, torch.float32, "dweight"), ctypes.byref(o)))
+    return drows, dweight
+
+
+def runlora_rmsnorm_forward(X, gain, Y, eps=1e-6, residual=None, H=None, rstd=None, rows=None, stream=None):
+    """Y = h / sqrt(mean h^2 + eps) * gain over rows of h = X + residual (None: X), rounded to X's type before it is normed.  gain: [d] or None (1);
+    H: where h goes (may be X or residual), rstd: float32 [n] for a backward, rows: Fp8Rows that receive Y in 8 bits; each may be None."""
+    import torch
+    n, d = X.shape
+    _one_gpu(X, residual, gain, Y, H, rstd, rows)
+    dx, dr, dy, dh, dq = (tensor_desc(t) for t in (X, residual, Y, H, rows))
+    o = _opts(None, stream)
+    _check(lib().runlora_rmsnorm_forward(_ref(dx), _ref(dr), _vector(gain, d, X.dtype, "gain"), eps, _ref(dy), _ref(dh), _vector(rstd, n, torch.float32, "rstd"),
+                                         _ref(dq), ctypes.byref(o)))
+    return Y
+
+
+def runlora_rmsnorm_backward(dY, H, gain, rstd, dX, dgain=None, dH=None, workspace=None, stream=None):
+    """Gradient of X (and of the residual) and of the gain from dY and, if h was used elsewhere, dH; dX or dgain may be None (skipped).  workspace:
+    runlora_rmsnorm_workspace_bytes bytes, for dgain."""
+    import torch
+    n, d = dY.shape
+    _one_gpu(dY, H, gain, rstd, dX, dgain, dH, workspace)
+    ddy, ddh, dh, dx = (tensor_desc(t) for t in (dY, dH, H, dX))
+    o = _opts(workspace, stream)
+    _check(lib().runlora_rmsnorm_backward(_ref(ddy), _ref(ddh), _ref(dh), _vector(gain, d, dY.dtype, "gain"), _vector(rstd, n, torch.float32, "rstd"), _ref(dx),
+                                          _vector(dgain, d, dY.dtype, "dgain"), ctypes.byref(o)))
+    return dX, dgain
+
+
+def runlora_rmsnorm_workspace_bytes(n, d, dtype):
+    return int(lib().runlora_rmsnorm_workspace_bytes(n, d, dtype))
 
 
 def runlora_select(n_tokens, d_in, d_out, r, dtype, criterion=None):

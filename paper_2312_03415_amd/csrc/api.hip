@@ -9,6 +9,9 @@
 #include "dora.hpp"
 #include "fp8.hpp"
 #include "grouped.hpp"
+#include "norm.hpp"
+#include "route.hpp"
+#include "rows.hpp"
 #include "vera.hpp"
 
 using namespace rl;
@@ -386,8 +389,19 @@ void add_inputs(Ranges* in, const int32_t* ends, const rl_stack_t* W, const rl_s
   if (ends) in->add(range_of(ends, 1, 0, W->experts, 4));
 }
 
+// rows in e4m3 with a scale per 128 columns (RL_FP8_R128)
+int check_rounded(const rl_tensor_t* Q, int64_t rows, int64_t cols) {
+  if (!Q || !Q->data || !Q->scales) return RL_ERR_NULL;
+  if (Q->dtype != RL_FP8_R128) return RL_ERR_DTYPE;
+  if (Q->group != 128) return RL_ERR_UNSUPPORTED;
+  if (Q->rows != rows || Q->cols != cols || Q->ld != fp8_row_bytes(cols)) return RL_ERR_SHAPE;
+  return (reinterpret_cast<uintptr_t>(Q->data) & 15) != 0 || (reinterpret_cast<uintptr_t>(Q->scales) & 15) != 0 ? RL_ERR_ALIGN : RL_OK;
+}
+Range rounded_range(const rl_tensor_t* Q) { return range_of(Q->data, 1, 0, Q->rows * Q->ld, 1); }
+Range rounded_scales(const rl_tensor_t* Q) { return range_of(Q->scales, 1, 0, Q->ld / 128 * fp8_scale_ld(Q->rows), 1); }
+
 int experts_forward_impl(const rl_tensor_t* X, const int32_t* ends, const rl_stack_t* W, const rl_stack_t* A, const rl_stack_t* B, rl_tensor_t* Y,
-                         rl_tensor_t* T, const rl_opts_t* opts, bool use_static) {
+                         rl_tensor_t* T, const rl_opts_t* opts, bool use_static, const rl_tensor_t* Q = nullptr) {
   if (!X || !W || !Y) return RL_ERR_NULL;
   int64_t r = 0;
   int rc = check_inputs(X, W->rows, ends, W, A, B, &r);
@@ -397,6 +411,7 @@ int experts_forward_impl(const rl_tensor_t* X, const int32_t* ends, const rl_sta
   if (T && !A) return RL_ERR_SHAPE;
   if (T && (rc = check_tensor(T, n, r, X->dtype)) != RL_OK) return rc;
   if (T && T->ld > kMaxLd) return RL_ERR_UNSUPPORTED;  // (the large product reads it)
+  if (Q && (rc = check_rounded(Q, n, X->cols)) != RL_OK) return rc;
   if (opts && opts->dropout_p != 0.f) return RL_ERR_UNSUPPORTED;
   const void* bias = opts ? opts->bias : nullptr;
   if ((reinterpret_cast<uintptr_t>(bias) & 15) != 0) return RL_ERR_ALIGN;
@@ -404,6 +419,7 @@ int experts_forward_impl(const rl_tensor_t* X, const int32_t* ends, const rl_sta
   add_inputs(&in, ends, W, A, B);
   in.add(range_of(X->data, n, X->ld, X->cols, 2));
   if (bias) in.add(range_of(bias, 1, 0, W->experts * o, 2));
+  if (Q) { in.add(rounded_range(Q)); in.add(rounded_scales(Q)); }
   const Range ry = range_of(Y->data, n, Y->ld, o, 2);
   if (in.hit(ry)) return RL_ERR_ALIAS;
   if (T) {
@@ -417,6 +433,7 @@ int experts_forward_impl(const rl_tensor_t* X, const int32_t* ends, const rl_sta
   d.X = X->data; d.ldx = X->ld;
   d.Y = Y->data; d.ldy = Y->ld;
   if (T) { d.T = T->data; d.ldt = T->ld; }
+  if (Q) { d.q = static_cast<uint8_t*>(Q->data); d.qs = static_cast<uint8_t*>(Q->scales); }
   d.bias = bias;
   d.scale = opts && opts->scale != 0.f ? opts->scale : 1.f;
   const size_t need = experts_workspace(d, false);
@@ -481,13 +498,13 @@ int experts_backward_impl(const rl_tensor_t* dY, const rl_tensor_t* X, const int
 
 // the layer calls on an RL_FP8_B128 weight: a stack of one
 int fp8_forward(int variant, const rl_tensor_t* X, const rl_tensor_t* W, const rl_tensor_t* A, const rl_tensor_t* B, rl_tensor_t* Y, rl_saved_t* saved,
-                const rl_opts_t* opts, bool use_static) {
+                const rl_opts_t* opts, bool use_static, const rl_tensor_t* Q = nullptr) {
   if (variant != RL_FWD1 && variant != RL_FWD3) return RL_ERR_UNSUPPORTED;
   if (W->group != 128) return RL_ERR_UNSUPPORTED;
   const rl_stack_t w = stack_of(W), a = stack_of(A), b = stack_of(B);
   if (A->cols < 1) return RL_ERR_SHAPE;
   rl_tensor_t T{saved->T, X->rows, A->cols, saved->ldt, X->dtype, nullptr, 0};
-  const int rc = experts_forward_impl(X, nullptr, &w, &a, &b, Y, saved->T ? &T : nullptr, opts, use_static);
+  const int rc = experts_forward_impl(X, nullptr, &w, &a, &b, Y, saved->T ? &T : nullptr, opts, use_static, Q);
   if (rc != RL_OK) return rc;
   saved->fwd_variant = variant;
   saved->dtype = X->dtype;
@@ -552,6 +569,314 @@ extern "C" int runlora_fp8_quantize(const rl_tensor_t* src, rl_tensor_t* dst, co
   const hipError_t e = fp8_blocks_run(dt, src->data, src->ld, src->rows, src->cols, dst->data, dst->ld, static_cast<uint8_t*>(dst->scales),
                                       opts ? static_cast<hipStream_t>(opts->stream) : nullptr);
   return e == hipSuccess ? RL_OK : set_hip_error(e, "fp8 quantize");
+}
+
+// ---- what stands between the layers of a block with routed experts ---------------------------------------
+
+namespace {
+
+int check_ints(const void* p) { return !p ? RL_ERR_NULL : ((reinterpret_cast<uintptr_t>(p) & 3) != 0 ? RL_ERR_ALIGN : RL_OK); }
+hipStream_t stream_of(const rl_opts_t* opts) { return opts ? static_cast<hipStream_t>(opts->stream) : nullptr; }
+
+// logits and their gradient: rows of any alignment that their type has
+int check_logits(const rl_tensor_t* t, int64_t n, int64_t experts, int dtype) {
+  if (!t || !t->data) return RL_ERR_NULL;
+  if (t->dtype != dtype || internal_dtype(dtype) < 0) return RL_ERR_DTYPE;
+  if (t->rows != n || t->cols != experts || t->ld < t->cols) return RL_ERR_SHAPE;
+  return reinterpret_cast<uintptr_t>(t->data) % dtype_size(internal_dtype(dtype)) != 0 ? RL_ERR_ALIGN : RL_OK;
+}
+
+// the plan of a routing call, as the kernels take it
+int check_route(const rl_tensor_t* logits, const rl_route_t* r, RouteDesc* d) {
+  if (!logits || !r) return RL_ERR_NULL;
+  int rc = check_logits(logits, logits->rows, r->experts, logits->dtype);
+  if (rc != RL_OK) return rc;
+  if (logits->rows < 1 || r->experts < 1 || r->top < 1 || r->top > r->experts) return RL_ERR_SHAPE;
+  if (r->score != RL_SCORE_SOFTMAX && r->score != RL_SCORE_SIGMOID) return RL_ERR_VARIANT;
+  const int groups = r->groups == 0 ? 1 : r->groups, kept = r->groups_kept == 0 ? groups : r->groups_kept, group_top = r->group_top == 0 ? 1 : r->group_top;
+  if (groups < 1 || r->experts % groups != 0 || kept < 1 || kept > groups || group_top < 1) return RL_ERR_SHAPE;
+  if (r->experts > kRouteMaxExperts || r->top > kRouteMaxTop || groups > 64 || group_top > 2 || logits->rows >= kRouteMaxTokens) return RL_ERR_UNSUPPORTED;
+  if (r->bias && (rc = check_ints(r->bias)) != RL_OK) return rc;
+  d->dtype = internal_dtype(logits->dtype);
+  d->n = logits->rows;
+  d->experts = r->experts;
+  d->top = r->top;
+  d->sigmoid = r->score == RL_SCORE_SIGMOID;
+  d->renorm = r->renormalise != 0;
+  d->groups = kept == groups ? 1 : groups;  // (all of them kept: no limit)
+  d->kept = kept;
+  d->group_top = group_top;
+  d->scale = r->scale != 0.f ? r->scale : 1.f;
+  d->bias = r->bias;
+  d->logits = logits->data;
+  d->ld = logits->ld;
+  return RL_OK;
+}
+
+// rows of tokens and of their copies: [n, d] and [n top, d]
+int check_copies(const rl_tensor_t* tokens, const rl_tensor_t* copies, const int32_t* place, int top) {
+  if (!tokens || !place) return RL_ERR_NULL;
+  if (internal_dtype(tokens->dtype) < 0) return RL_ERR_DTYPE;
+  int rc = check_dims(tokens->rows, tokens->cols, 8, 8, tokens->dtype);
+  if (rc != RL_OK) return rc;
+  if (top < 1) return RL_ERR_SHAPE;
+  if (top > kRouteMaxTop || tokens->rows >= kRouteMaxTokens) return RL_ERR_UNSUPPORTED;
+  if ((rc = check_tensor(tokens, tokens->rows, tokens->cols, tokens->dtype)) != RL_OK) return rc;
+  if (copies && (rc = check_tensor(copies, tokens->rows * top, tokens->cols, tokens->dtype)) != RL_OK) return rc;
+  return check_ints(place);
+}
+Range dense_range(const rl_tensor_t* t) { return range_of(t->data, t->rows, t->ld, t->cols, dtype_size(internal_dtype(t->dtype))); }
+Range list_range(const void* p, int64_t count) { return range_of(p, 1, 0, count, 4); }
+RowsDesc rows_desc(const rl_tensor_t* tokens, const int32_t* place, int top) {
+  RowsDesc d;
+  d.dtype = internal_dtype(tokens->dtype);
+  d.n = tokens->rows; d.d = tokens->cols;
+  d.top = top;
+  d.place = place;
+  return d;
+}
+
+}  // namespace
+
+extern "C" int runlora_route_forward(const rl_tensor_t* logits, const rl_route_t* route, int32_t* expert, float* weight, int32_t* place, int32_t* source,
+                                     int32_t* ends, const rl_opts_t* opts) {
+  RouteDesc d;
+  int rc = check_route(logits, route, &d);
+  if (rc != RL_OK) return rc;
+  void* const outs[5] = {expert, weight, place, source, ends};
+  const int64_t copies = d.n * d.top;
+  Ranges used;
+  used.add(dense_range(logits));
+  if (d.bias) used.add(list_range(d.bias, d.experts));
+  for (void* p : outs) {
+    if ((rc = check_ints(p)) != RL_OK) return rc;
+    const Range x = list_range(p, p == ends ? d.experts : copies);
+    if (used.hit(x)) return RL_ERR_ALIAS;
+    used.add(x);
+  }
+  if ((rc = check_space(route_workspace(d.n, d.experts), opts)) != RL_OK) return rc;
+  d.expert = expert; d.weight = weight; d.place = place; d.source = source; d.ends = ends;
+  const hipError_t e = route_forward(d, opts ? opts->workspace : nullptr, stream_of(opts));
+  return e == hipSuccess ? RL_OK : set_hip_error(e, "route forward");
+}
+
+extern "C" int runlora_route_backward(const rl_tensor_t* logits, const rl_route_t* route, const int32_t* expert, const float* dweight, rl_tensor_t* dlogits,
+                                      const rl_opts_t* opts) {
+  RouteDesc d;
+  int rc = check_route(logits, route, &d);
+  if (rc != RL_OK) return rc;
+  if ((rc = check_ints(expert)) != RL_OK || (rc = check_ints(dweight)) != RL_OK) return rc;
+  if ((rc = check_logits(dlogits, d.n, d.experts, logits->dtype)) != RL_OK) return rc;
+  Ranges in;
+  in.add(dense_range(logits));
+  in.add(list_range(expert, d.n * d.top));
+  in.add(list_range(dweight, d.n * d.top));
+  if (in.hit(dense_range(dlogits))) return RL_ERR_ALIAS;
+  d.expert = const_cast<int32_t*>(expert);  // (only read)
+  d.dweight = dweight;
+  d.dlogits = dlogits->data;
+  d.lddl = dlogits->ld;
+  const hipError_t e = route_backward(d, stream_of(opts));
+  return e == hipSuccess ? RL_OK : set_hip_error(e, "route backward");
+}
+
+extern "C" size_t runlora_route_workspace_bytes(int64_t n, int64_t experts, int64_t top) {
+  if (n < 1 || n >= kRouteMaxTokens || experts < 1 || experts > kRouteMaxExperts || top < 1 || top > experts || top > kRouteMaxTop) return 0;
+  return route_workspace(n, experts);
+}
+
+extern "C" int runlora_gather_forward(const rl_tensor_t* X, const int32_t* place, const int32_t* source, int top, rl_tensor_t* rows, const rl_opts_t* opts) {
+  if (!rows) return RL_ERR_NULL;
+  int rc = check_copies(X, rows, place, top);
+  if (rc != RL_OK || (rc = check_ints(source)) != RL_OK) return rc;
+  Ranges in;
+  in.add(dense_range(X));
+  in.add(list_range(place, rows->rows));
+  in.add(list_range(source, rows->rows));
+  if (in.hit(dense_range(rows))) return RL_ERR_ALIAS;
+  RowsDesc d = rows_desc(X, place, top);
+  d.source = source;
+  d.in = X->data; d.ldin = X->ld;
+  d.out = rows->data; d.ldout = rows->ld;
+  const hipError_t e = rows_spread(d, stream_of(opts));
+  return e == hipSuccess ? RL_OK : set_hip_error(e, "gather forward");
+}
+
+extern "C" int runlora_gather_backward(const rl_tensor_t* drows, const int32_t* place, int top, rl_tensor_t* dX, const rl_opts_t* opts) {
+  if (!drows) return RL_ERR_NULL;
+  const int rc = check_copies(dX, drows, place, top);
+  if (rc != RL_OK) return rc;
+  Ranges in;
+  in.add(dense_range(drows));
+  in.add(list_range(place, drows->rows));
+  if (in.hit(dense_range(dX))) return RL_ERR_ALIAS;
+  RowsDesc d = rows_desc(dX, place, top);
+  d.in = drows->data; d.ldin = drows->ld;
+  d.out = dX->data; d.ldout = dX->ld;
+  const hipError_t e = rows_join(d, stream_of(opts));
+  return e == hipSuccess ? RL_OK : set_hip_error(e, "gather backward");
+}
+
+extern "C" int runlora_combine_forward(const rl_tensor_t* rows, const int32_t* place, const float* weight, int top, const rl_tensor_t* add, rl_tensor_t* Y,
+                                       const rl_opts_t* opts) {
+  if (!rows) return RL_ERR_NULL;
+  int rc = check_copies(Y, rows, place, top);
+  if (rc != RL_OK || (rc = check_ints(weight)) != RL_OK) return rc;
+  if (add && (rc = check_tensor(add, Y->rows, Y->cols, Y->dtype)) != RL_OK) return rc;
+  Ranges in;
+  in.add(dense_range(rows));
+  in.add(list_range(place, rows->rows));
+  in.add(list_range(weight, rows->rows));
+  if (add) in.add(dense_range(add));
+  if (in.hit(dense_range(Y))) return RL_ERR_ALIAS;
+  RowsDesc d = rows_desc(Y, place, top);
+  d.weight = weight;
+  d.in = rows->data; d.ldin = rows->ld;
+  if (add) { d.add = add->data; d.ldadd = add->ld; }
+  d.out = Y->data; d.ldout = Y->ld;
+  const hipError_t e = rows_join(d, stream_of(opts));
+  return e == hipSuccess ? RL_OK : set_hip_error(e, "combine forward");
+}
+
+extern "C" int runlora_combine_backward(const rl_tensor_t* dY, const rl_tensor_t* rows, const int32_t* place, const int32_t* source, const float* weight,
+                                        int top, rl_tensor_t* drows, float* dweight, const rl_opts_t* opts) {
+  int rc = check_copies(dY, drows, place, top);
+  if (rc != RL_OK) return rc;
+  if (dweight && !rows) return RL_ERR_NULL;
+  if (rows && (rc = check_tensor(rows, dY->rows * top, dY->cols, dY->dtype)) != RL_OK) return rc;
+  if ((rc = check_ints(source)) != RL_OK || (rc = check_ints(weight)) != RL_OK || (dweight && (rc = check_ints(dweight)) != RL_OK)) return rc;
+  const int64_t copies = dY->rows * top;
+  Ranges in;
+  in.add(dense_range(dY));
+  if (rows) in.add(dense_range(rows));
+  in.add(list_range(place, copies));
+  in.add(list_range(source, copies));
+  in.add(list_range(weight, copies));
+  if (drows) { if (in.hit(dense_range(drows))) return RL_ERR_ALIAS; in.add(dense_range(drows)); }
+  if (dweight && in.hit(list_range(dweight, copies))) return RL_ERR_ALIAS;
+  if (!drows && !dweight) return RL_OK;
+  RowsDesc d = rows_desc(dY, place, top);
+  d.source = source;
+  d.weight = weight;
+  d.in = dY->data; d.ldin = dY->ld;
+  if (dweight) { d.rows = rows->data; d.ldrows = rows->ld; d.dweight = dweight; }
+  if (drows) { d.out = drows->data; d.ldout = drows->ld; }
+  const hipError_t e = rows_spread(d, stream_of(opts));
+  return e == hipSuccess ? RL_OK : set_hip_error(e, "combine backward");
+}
+
+namespace {
+int check_norm(const rl_tensor_t* t, const void* gain) {
+  if (!t) return RL_ERR_NULL;
+  if (internal_dtype(t->dtype) < 0) return RL_ERR_DTYPE;
+  int rc = check_dims(t->rows, t->cols, 8, 8, t->dtype);
+  if (rc != RL_OK) return rc;
+  if (t->cols > kNormMaxWidth) return RL_ERR_UNSUPPORTED;
+  if ((reinterpret_cast<uintptr_t>(gain) & 15) != 0) return RL_ERR_ALIGN;
+  return check_tensor(t, t->rows, t->cols, t->dtype);
+}
+}  // namespace
+
+extern "C" int runlora_rmsnorm_forward(const rl_tensor_t* X, const rl_tensor_t* R, const void* gain, float eps, rl_tensor_t* Y, rl_tensor_t* H, float* rstd,
+                                       rl_tensor_t* Q, const rl_opts_t* opts) {
+  int rc = check_norm(X, gain);
+  if (rc != RL_OK) return rc;
+  const int64_t n = X->rows, width = X->cols;
+  if (!(eps >= 0.f)) return RL_ERR_SHAPE;
+  if (R && (rc = check_tensor(R, n, width, X->dtype)) != RL_OK) return rc;
+  if ((rc = check_tensor(Y, n, width, X->dtype)) != RL_OK) return rc;
+  if (H && (rc = check_tensor(H, n, width, X->dtype)) != RL_OK) return rc;
+  if (rstd && (rc = check_ints(rstd)) != RL_OK) return rc;
+  if (Q && (rc = check_rounded(Q, n, width)) != RL_OK) return rc;
+  if (Q && X->dtype == RL_F32) return RL_ERR_UNSUPPORTED;
+  // h may take the place of X or of R: a thread reads all of its pieces of a row before it writes one
+  auto same = [&](const rl_tensor_t* t) { return H && t && H->data == t->data && H->ld == t->ld; };
+  Ranges used, others;
+  used.add(dense_range(X));
+  if (!same(X)) others.add(dense_range(X));
+  if (R) {
+    used.add(dense_range(R));
+    if (!same(R)) others.add(dense_range(R));
+  }
+  if (gain) {
+    used.add(range_of(gain, 1, 0, width, dtype_size(internal_dtype(X->dtype))));
+    others.add(range_of(gain, 1, 0, width, dtype_size(internal_dtype(X->dtype))));
+  }
+  if (H) {
+    if (others.hit(dense_range(H))) return RL_ERR_ALIAS;
+    used.add(dense_range(H));
+  }
+  const Range outs[4] = {dense_range(Y), rstd ? list_range(rstd, n) : Range{nullptr, nullptr}, Q ? rounded_range(Q) : Range{nullptr, nullptr},
+                         Q ? rounded_scales(Q) : Range{nullptr, nullptr}};
+  for (const Range& x : outs) {
+    if (!x.lo) continue;
+    if (used.hit(x)) return RL_ERR_ALIAS;
+    used.add(x);
+  }
+  NormDesc d;
+  d.dtype = internal_dtype(X->dtype);
+  d.n = n; d.d = width;
+  d.eps = eps;
+  d.X = X->data; d.ldx = X->ld;
+  if (R) { d.R = R->data; d.ldr = R->ld; }
+  d.gain = gain;
+  d.Y = Y->data; d.ldy = Y->ld;
+  if (H) { d.H = H->data; d.ldh = H->ld; }
+  d.rstd = rstd;
+  if (Q) {
+    d.q = static_cast<uint8_t*>(Q->data); d.ldq = Q->ld;
+    d.qs = static_cast<uint8_t*>(Q->scales); d.ldqs = fp8_scale_ld(n);
+  }
+  const hipError_t e = norm_forward(d, stream_of(opts));
+  return e == hipSuccess ? RL_OK : set_hip_error(e, "rmsnorm forward");
+}
+
+extern "C" int runlora_rmsnorm_backward(const rl_tensor_t* dY, const rl_tensor_t* dH, const rl_tensor_t* H, const void* gain, const float* rstd,
+                                        rl_tensor_t* dX, void* dgain, const rl_opts_t* opts) {
+  int rc = check_norm(dY, gain);
+  if (rc != RL_OK) return rc;
+  const int64_t n = dY->rows, width = dY->cols;
+  const size_t esz = dtype_size(internal_dtype(dY->dtype));
+  if (dH && (rc = check_tensor(dH, n, width, dY->dtype)) != RL_OK) return rc;
+  if ((rc = check_tensor(H, n, width, dY->dtype)) != RL_OK) return rc;
+  if ((rc = check_ints(rstd)) != RL_OK) return rc;
+  if (dX && (rc = check_tensor(dX, n, width, dY->dtype)) != RL_OK) return rc;
+  if ((reinterpret_cast<uintptr_t>(dgain) & 15) != 0) return RL_ERR_ALIGN;
+  Ranges in;
+  in.add(dense_range(dY));
+  if (dH) in.add(dense_range(dH));
+  in.add(dense_range(H));
+  if (gain) in.add(range_of(gain, 1, 0, width, esz));
+  in.add(list_range(rstd, n));
+  if (dX) { if (in.hit(dense_range(dX))) return RL_ERR_ALIAS; in.add(dense_range(dX)); }
+  if (dgain && in.hit(range_of(dgain, 1, 0, width, esz))) return RL_ERR_ALIAS;
+  if (!dX && !dgain) return RL_OK;
+  NormDesc d;
+  d.dtype = internal_dtype(dY->dtype);
+  d.n = n; d.d = width;
+  d.X = H->data; d.ldx = H->ld;
+  d.gain = gain;
+  d.rstd = const_cast<float*>(rstd);  // (only read)
+  d.dY = dY->data; d.lddy = dY->ld;
+  if (dH) { d.dH = dH->data; d.lddh = dH->ld; }
+  if (dX) { d.dX = dX->data; d.lddx = dX->ld; }
+  d.dgain = dgain;
+  if ((rc = check_space(norm_backward_workspace(d.dtype, n, width, dgain != nullptr), opts)) != RL_OK) return rc;
+  const hipError_t e = norm_backward(d, opts ? opts->workspace : nullptr, stream_of(opts));
+  return e == hipSuccess ? RL_OK : set_hip_error(e, "rmsnorm backward");
+}
+
+extern "C" size_t runlora_rmsnorm_workspace_bytes(int64_t n, int64_t d, int dtype) {
+  const int dt = internal_dtype(dtype);
+  if (dt < 0 || check_dims(n, d, 8, 8, dtype) != RL_OK || d > kNormMaxWidth) return 0;
+  return norm_backward_workspace(dt, n, d, true);
+}
+
+extern "C" int runlora_fp8_forward(const rl_tensor_t* X, const rl_tensor_t* Q, const rl_tensor_t* W, const rl_tensor_t* A, const rl_tensor_t* B,
+                                   rl_tensor_t* Y, rl_saved_t* saved, const rl_opts_t* opts) {
+  if (!X || !Q || !W || !A || !B || !Y || !saved) return RL_ERR_NULL;
+  if (W->dtype != RL_FP8_B128) return RL_ERR_DTYPE;
+  return fp8_forward(RL_FWD1, X, W, A, B, Y, saved, opts, false, Q);
 }
 
 namespace {

@@ -549,7 +549,9 @@ hipError_t main_run(const ExpertsDesc& d, bool backward, const Space& w, const v
 size_t experts_workspace(const ExpertsDesc& d, bool backward) { return space(d, backward, nullptr).bytes; }
 
 hipError_t experts_forward(const ExpertsDesc& d, void* workspace, hipStream_t stream) {
-  const Space w = space(d, false, workspace);
+  Space w = space(d, false, workspace);
+  const bool rounded = d.f8 && d.q != nullptr;  // (their place in the workspace stays unused)
+  if (rounded) { w.q = d.q; w.s = d.qs; }
   hipError_t e;
   if (few(d)) {
     FewArgs f{};
@@ -561,7 +563,7 @@ hipError_t experts_forward(const ExpertsDesc& d, void* workspace, hipStream_t st
     f.n = (int)d.n; f.K = (int)d.i; f.N = (int)d.o; f.R = (int)d.r;
     f.slices = w.slices; f.splits = grouped_plan(d, d.o, d.i, true).splits;
     f.scale = d.scale;
-    if (d.f8) {
+    if (d.f8 && !rounded) {
       f.q = w.q; f.qs = w.s; f.ldq = w.ldq; f.ldqs = w.lds;
       f.qx = (int)ceil_div(d.n, 4);
       f.qy = (int)ceil_div(w.ldq, 512);
@@ -574,9 +576,9 @@ hipError_t experts_forward(const ExpertsDesc& d, void* workspace, hipStream_t st
   const int64_t ldt = d.T ? d.ldt : d.r;
   if (d.r > 0) {
     const Turn turn{d.B, w.turned, d.ldb, d.sb, (int)d.r, (int)d.o, (int)((d.r < kTurnRows ? ceil_div(d.o, kThreads) * (d.r / 8) : ceil_div(d.o, 64) * ceil_div(d.r, 64)) * d.experts)};
-    if ((e = rank_run(d, w, d.X, d.ldx, d.i, false, d.f8, T, ldt, turn, stream)) != hipSuccess) return e;
+    if ((e = rank_run(d, w, d.X, d.ldx, d.i, false, d.f8 && !rounded, T, ldt, turn, stream)) != hipSuccess) return e;
   }
-  return main_run(d, false, w, T, ldt, w.turned, d.r, d.o * d.r, d.Y, d.ldy, false, d.r > 0, stream);
+  return main_run(d, false, w, T, ldt, w.turned, d.r, d.o * d.r, d.Y, d.ldy, false, d.r > 0 || rounded, stream);
 }
 
 hipError_t experts_backward(const ExpertsDesc& d, void* workspace, hipStream_t stream) {

@@ -108,6 +108,7 @@ struct ExpertsDesc {
   void *Y = nullptr, *T = nullptr, *dX = nullptr, *dA = nullptr, *dB = nullptr;
   int64_t ldy = 0, ldt = 0, lddx = 0, ldda = 0, sda = 0, lddb = 0, sdb = 0;
   bool has_T = false;  // backward: T holds s X A already
+  uint8_t *q = nullptr, *qs = nullptr;  // forward over an e4m3 W: X rounded already (fp8_row_bytes, fp8_scale_ld), or nullptr
   float scale = 1.f;
 };
 // what a large product of K into N columns runs on: a function of sizes alone, shared by the workspace query and the call.  slices: K in `splits`

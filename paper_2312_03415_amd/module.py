@@ -15,6 +15,9 @@ for the calls that have to see a Python-level function (tracing, functorch trans
     layer8 = RunLoRAFp8Linear.from_linear(nn_linear, r=16, alpha=32) # the frozen W in 8 bits
     experts = RunLoRAExperts(weight_stack, r=16, alpha=32)           # one adapted layer per expert
     y = experts(x_sorted, ends)                                      # rows sorted by expert, ends[e] = where expert e's rows end
+    norm = RunRMSNorm(d); h, x = norm(y, x)                          # the norm of the residual stream x + y, and the stream
+    weight, _, place, source, ends = RunRouter(8, 2)(h @ router)     # every token to its two best of eight experts
+    y = RunCombineFunction.apply(experts(RunGatherFunction.apply(h, place, source), ends), place, source, weight, x)
 """
 import ctypes
 import functools
@@ -450,18 +453,18 @@ class RunLoRAExpertsFunction(torch.autograd.Function):
 
 class RunLoRAFp8Function(torch.autograd.Function):
     """y = Q(x) W + bias + scale (x A) B over an Fp8Weight (runlora.h); gradients for x, A and B, the large product of dx on Q(dy).
-    scale XA (n*r elements) is kept for the backward."""
+    scale XA (n*r elements) is kept for the backward.  rows: Q(x) where it is there already (an Fp8Rows, e.g. RunRMSNorm's)."""
 
     @classmethod
-    def apply(cls, x, W, A, B, bias, scale):
-        if cls is RunLoRAFp8Function and isinstance(W, rl.Fp8Weight):
+    def apply(cls, x, W, A, B, bias, scale, rows=None):
+        if cls is RunLoRAFp8Function and isinstance(W, rl.Fp8Weight) and rows is None:
             y = _native().experts(x, A, B, W.data, W.scales, None, bias, scale, W.cols)
             if y is not None:
                 return y
-        return super().apply(x, W, A, B, bias, scale)
+        return super().apply(x, W, A, B, bias, scale, rows)
 
     @_on_inputs_gpu
-    def forward(ctx, x, W, A, B, bias, scale):
+    def forward(ctx, x, W, A, B, bias, scale, rows=None):
         x2 = _rows(x, W.rows)
         n, r, code = x2.shape[0], A.shape[1], rl.dtype_code(x.dtype)
         y = torch.empty((n, W.cols), dtype=x.dtype, device=x.device)
@@ -469,7 +472,10 @@ class RunLoRAFp8Function(torch.autograd.Function):
         ctx.saved, ctx.w_shape, ctx.x_shape = rl.new_saved(T), W.shape, x.shape
         if n > 0:
             ws = _workspace(x.device, rl.runlora_workspace_bytes(rl.FWD1, -1, n, W.rows, W.cols, r, code, rl.RL_FP8_B128))
-            rl.runlora_forward(rl.FWD1, x2, W, A, B, y, ctx.saved, workspace=ws, scale=scale, bias=bias)
+            if rows is None:
+                rl.runlora_forward(rl.FWD1, x2, W, A, B, y, ctx.saved, workspace=ws, scale=scale, bias=bias)
+            else:
+                rl.runlora_fp8_forward(x2, rows, W, A, B, y, ctx.saved, workspace=ws, scale=scale, bias=bias)
         ctx.save_for_backward(x2, A, B, T, W.data, W.scales)
         return y.view(*x.shape[:-1], W.cols)
 
@@ -494,7 +500,7 @@ class RunLoRAFp8Function(torch.autograd.Function):
             code = rl.dtype_code(dy.dtype)
             ws = _workspace(dy.device, rl.runlora_workspace_bytes(-1, rl.BWD1, n, i, o, r, code, rl.RL_FP8_B128))
             rl.runlora_backward(rl.BWD1, dy2, saved, W, A, B, dx, dA, dB, workspace=ws)
-        return dx.view(ctx.x_shape) if need_x else None, None, dA, dB, None, None
+        return dx.view(ctx.x_shape) if need_x else None, None, dA, dB, None, None, None
 
 
 def _bytes_of_state(module, state, prefix, *_):
@@ -535,8 +541,9 @@ class RunLoRAFp8Linear(nn.Module):
     def weight(self):
         return rl.Fp8Weight(self.weight_data, self.weight_scales, self.d_in, self.d_out)
 
-    def forward(self, x):
-        return RunLoRAFp8Function.apply(x, self.weight, self.lora_A, self.lora_B, self.bias, self.scale)
+    def forward(self, x, rows=None):
+        """rows: x's rows in 8 bits, where the operator in front has left them (RunRMSNorm)."""
+        return RunLoRAFp8Function.apply(x, self.weight, self.lora_A, self.lora_B, self.bias, self.scale, rows)
 
     def extra_repr(self):
         return f"d_in={self.d_in}, d_out={self.d_out}, r={self.r}, scale={self.scale:g}, bias={self.bias is not None}"
@@ -569,6 +576,187 @@ class RunLoRAExperts(nn.Module):
 
     def extra_repr(self):
         return f"experts={self.experts}, d_in={self.d_in}, d_out={self.d_out}, r={self.r}, scale={self.scale:g}, bias={self.bias is not None}"
+
+
+class RunRMSNormFunction(torch.autograd.Function):
+    """y = h / sqrt(mean h^2 + eps) * gain over the last dimension (runlora_rmsnorm_forward / _backward); without a residual h = x and y is returned, with
+    one h = x + residual and (y, h) are.  rows=True appends y's rows in 8 bits: the bytes and scales of an Fp8Rows.  Gradients for x, residual and gain."""
+
+    @classmethod
+    def apply(cls, x, gain, eps, residual=None, rows=False):
+        return super().apply(x, gain, eps, residual, rows)
+
+    @_on_inputs_gpu
+    def forward(ctx, x, gain, eps, residual=None, rows=False):
+        d = x.shape[-1]
+        x2 = _rows(x, d)
+        n = x2.shape[0]
+        if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype):
+            raise ValueError("the residual must have x's shape and type")
+        r2 = None if residual is None else _rows(residual, d)
+        y = torch.empty((n, d), dtype=x.dtype, device=x.device)
+        h = x2 if residual is None else torch.empty_like(y)
+        rstd = torch.empty((n,), dtype=torch.float32, device=x.device)
+        q = rl.Fp8Rows.empty(n, d, x.device) if rows else None
+        if n > 0:
+            rl.runlora_rmsnorm_forward(x2, gain, y, eps, r2, None if residual is None else h, rstd, q)
+        ctx.x_shape, ctx.residual = x.shape, residual is not None
+        ctx.save_for_backward(h, gain, rstd)
+        ctx.set_materialize_grads(False)
+        out = (y.view(x.shape),) + (() if residual is None else (h.view(x.shape),))
+        if rows:
+            ctx.mark_non_differentiable(q.data, q.scales)
+            out += (q.data, q.scales)
+        return out if len(out) > 1 else out[0]
+
+    @staticmethod
+    def backward(ctx, dy, dh=None, *_):
+        h, gain, rstd = ctx.saved_tensors
+        if not ctx.residual:
+            dh = None
+        if dy is None:
+            return (dh if ctx.needs_input_grad[0] else None), None, None, (dh if ctx.needs_input_grad[3] else None), None
+        d = h.shape[-1]
+        h2, dy2 = _rows(h, d), _rows(dy, d)
+        n = h2.shape[0]
+        need_x, need_gain = ctx.needs_input_grad[0] or ctx.needs_input_grad[3], ctx.needs_input_grad[1]
+        make = torch.empty if n > 0 else torch.zeros
+        dx = torch.empty((n, d), dtype=h2.dtype, device=h2.device) if need_x else None
+        dgain = make((d,), dtype=h2.dtype, device=h2.device) if need_gain else None
+        if n > 0 and (need_x or need_gain):
+            ws = _workspace(dy.device, rl.runlora_rmsnorm_workspace_bytes(n, d, rl.dtype_code(h2.dtype))) if need_gain else None
+            rl.runlora_rmsnorm_backward(dy2, h2, gain, rstd, dx, dgain, None if dh is None else _rows(dh, d), ws)
+        dx = dx.view(ctx.x_shape) if need_x else None
+        return (dx if ctx.needs_input_grad[0] else None), dgain, None, (dx if ctx.needs_input_grad[3] else None), None
+
+
+class RunRMSNorm(nn.Module):
+    """Root-mean-square norm of the last dimension with a gain [d]: norm(x) = y, norm(x, residual) = (y, x + residual).  rows=True appends y's rows in 8 bits
+    (binding.Fp8Rows), which a RunLoRAFp8Linear takes next to y."""
+
+    def __init__(self, d, eps=1e-6, dtype=torch.bfloat16, device="cuda", trainable=False):
+        super().__init__()
+        self.d, self.eps = d, float(eps)
+        self.weight = nn.Parameter(torch.ones(d, dtype=dtype, device=device), requires_grad=trainable)
+
+    def forward(self, x, residual=None, rows=False):
+        out = RunRMSNormFunction.apply(x, self.weight, self.eps, residual, rows)
+        if not rows:
+            return out
+        *tensors, data, scales = out
+        return (*tensors, rl.Fp8Rows(data, scales, x.numel() // self.d, self.d))
+
+    def extra_repr(self):
+        return f"{self.d}, eps={self.eps:g}"
+
+
+class RunRouteFunction(torch.autograd.Function):
+    """(weight, expert, place, source, ends) of logits [n, experts] (runlora_route_forward / _backward); gradient of the weights for the logits."""
+
+    @classmethod
+    def apply(cls, logits, route, bias=None):
+        return super().apply(logits, route, bias)
+
+    @_on_inputs_gpu
+    def forward(ctx, logits, route, bias=None):
+        l2 = logits if logits.dim() == 2 and (logits.shape[1] < 2 or logits.stride(1) == 1) and logits.stride(0) >= logits.shape[1] else logits.contiguous()
+        n, top = l2.shape[0], route.top
+        make = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=l2.device)
+        weight, expert, place = make((n, top), torch.float32), make((n, top), torch.int32), make((n, top), torch.int32)
+        source, ends = make((n * top,), torch.int32), make((route.experts,), torch.int32)
+        if n > 0:
+            ws = _workspace(l2.device, rl.runlora_route_workspace_bytes(n, route.experts, top))
+            rl.runlora_route_forward(l2, route, weight, expert, place, source, ends, bias, ws)
+        else:
+            ends.zero_()
+        ctx.route = route
+        ctx.save_for_backward(l2, expert, bias)
+        ctx.mark_non_differentiable(expert, place, source, ends)
+        return weight, expert, place, source, ends
+
+    @staticmethod
+    def backward(ctx, dweight, *_):
+        logits, expert, bias = ctx.saved_tensors
+        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        if logits.shape[0] > 0:
+            rl.runlora_route_backward(logits, ctx.route, expert, dweight.contiguous(), dlogits, bias)
+        return dlogits, None, None
+
+
+class RunRouter(nn.Module):
+    """Routing of tokens by logits [n, experts] to `top` experts each: router(logits) = (weight, expert, place, source, ends), what RunGatherFunction,
+    RunLoRAExperts and RunCombineFunction read.  balance=True: a bias [experts] (float32, a buffer that starts at 0) is added to the scores for the choice
+    alone.  Options as binding.Route."""
+
+    def __init__(self, experts, top, score="softmax", renormalise=True, groups=1, groups_kept=None, group_top=1, scale=1.0, balance=False, device="cuda"):
+        super().__init__()
+        self.route = rl.Route(experts, top, score, renormalise, groups, groups_kept, group_top, scale)
+        self.register_buffer("bias", torch.zeros(experts, dtype=torch.float32, device=device) if balance else None)
+
+    def forward(self, logits):
+        return RunRouteFunction.apply(logits, self.route, None if self.bias is None else self.bias.float())
+
+    def extra_repr(self):
+        r = self.route
+        return f"experts={r.experts}, top={r.top}, score={r.score}, renormalise={r.renormalise}, groups={r.groups}, scale={r.scale:g}"
+
+
+class RunGatherFunction(torch.autograd.Function):
+    """rows [n top, d] sorted by expert from x [n, d] (runlora_gather_forward / _backward); place and source as RunRouteFunction gives them."""
+
+    @_on_inputs_gpu
+    def forward(ctx, x, place, source):
+        x2 = _rows(x, x.shape[-1])
+        n, d = x2.shape
+        rows = torch.empty((n * place.shape[1], d), dtype=x.dtype, device=x.device)
+        if n > 0:
+            rl.runlora_gather_forward(x2, place, source, rows)
+        ctx.x_shape = x.shape
+        ctx.save_for_backward(place)
+        return rows
+
+    @staticmethod
+    def backward(ctx, drows):
+        place, = ctx.saved_tensors
+        d = ctx.x_shape[-1]
+        dx = torch.empty((place.shape[0], d), dtype=drows.dtype, device=drows.device)
+        if place.shape[0] > 0:
+            rl.runlora_gather_backward(_rows(drows, d), place, dx)
+        return dx.view(ctx.x_shape), None, None
+
+
+class RunCombineFunction(torch.autograd.Function):
+    """y_t = add_t + sum over j of weight[t, j] rows[place[t, j]] (runlora_combine_forward / _backward); gradients for rows, weight and add."""
+
+    @classmethod
+    def apply(cls, rows, place, source, weight, add=None):
+        return super().apply(rows, place, source, weight, add)
+
+    @_on_inputs_gpu
+    def forward(ctx, rows, place, source, weight, add=None):
+        r2 = _rows(rows, rows.shape[-1])
+        n, d = place.shape[0], r2.shape[1]
+        if add is not None and (add.shape[-1] != d or add.dtype != rows.dtype or add.numel() != n * d):
+            raise ValueError("add must have one row a token, of the rows' type")
+        y = torch.empty((n, d), dtype=rows.dtype, device=rows.device)
+        weight = weight.contiguous()
+        if n > 0:
+            rl.runlora_combine_forward(r2, place, weight, y, None if add is None else _rows(add, d))
+        ctx.add_shape = None if add is None else add.shape
+        ctx.save_for_backward(r2, place, source, weight)
+        return y if add is None else y.view(add.shape)
+
+    @staticmethod
+    def backward(ctx, dy):
+        rows, place, source, weight = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        d = rows.shape[1]
+        dy2 = _rows(dy, d)
+        drows = torch.empty((place.numel(), d), dtype=rows.dtype, device=rows.device) if need[0] else None
+        dweight = torch.empty_like(weight) if need[3] else None
+        if place.shape[0] > 0 and (need[0] or need[3]):
+            rl.runlora_combine_backward(dy2, _rows(rows, d), place, source, weight, drows, dweight)
+        return drows, None, None, dweight, (dy if need[4] else None)
 
 
 def wrap_linears(model, r, alpha=None, targets=None, pair=None, keep_merged=False, dropout=0.0, adapter="lora"):
