@@ -4,11 +4,12 @@ time of a training step, and time of a step that answers one token per sequence.
     python -m paper_2312_03415_amd.experts_timing --model opt1.3b --experts 8 --top 2 --batch 4 --seq 2048 --rank 32
 
 Attention's projections are RunLoRAFp8Linear (kind fp8) or RunLoRALinear (kind 16bit); the MLP's are RunLoRAExperts over a stack of
-8-bit or 16-bit weights.  Every token goes to its `top` best experts: its row is repeated, the rows are sorted by expert, the experts'
-products run on the sorted rows with the counts left on the device, and a token's rows are added up with the router's weights.
+8-bit or 16-bit weights.  Every token goes to its `top` best experts (RunRouter): its row is copied to the rows sorted by expert, the experts'
+products run on them with the counts left on the device, and a token's rows are added to the residual stream with the router's weights.
+Where the model has root-mean-square norms they are RunRMSNorm, with the residual's addition and, in front of 8-bit projections, the rows in 8 bits.
 
 Both kinds hold the same synthetic weights (N(0, 1/d_in); the 8-bit ones rounded); inputs and the upstream gradient are N(0, 1); attention,
-normalisation, the router and the activation are torch's own operators.  Prints one JSON line.
+layer norms, the router's product and the activation are torch's own operators.  Prints one JSON line.
 """
 import argparse
 import json
@@ -19,30 +20,25 @@ import torch.nn.functional as F
 from torch import nn
 
 from . import binding as rl
-from .block_timing import MODELS, RMSNorm, time_block
-from .module import RunLoRAExperts, RunLoRAFp8Linear, RunLoRALinear
+from .block_timing import MODELS, time_block
+from .module import RunCombineFunction, RunGatherFunction, RunLoRAExperts, RunLoRAFp8Linear, RunLoRALinear, RunRMSNorm, RunRouter
 
 
 class RoutedMLP(nn.Module):
-    """x [n, d] -> sum over a token's experts of weight * expert MLP(x)."""
+    """x [n, d] -> sum over a token's experts of weight * expert MLP(x), added to `add` if that is given."""
 
     def __init__(self, router, top, gate, up, down):
         super().__init__()
         self.register_buffer("router", router)  # [d, experts]
+        self.route = RunRouter(router.shape[1], top, device=router.device)
         self.top, self.gate, self.up, self.down = top, gate, up, down
 
-    def forward(self, x):
-        n, experts = x.shape[0], self.router.shape[1]
-        weight, expert = (x.float() @ self.router).topk(self.top, dim=1)
-        weight = weight.softmax(1)
-        sorted_expert, order = expert.flatten().sort(stable=True)  # row j of the sorted ones is token order[j] // top
-        ends = torch.searchsorted(sorted_expert, torch.arange(experts, device=x.device), right=True).to(torch.int32)
-        rows = x[order // self.top]
+    def forward(self, x, add=None):
+        weight, _, place, source, ends = self.route(x.float() @ self.router)
+        rows = RunGatherFunction.apply(x, place, source)
         up = self.up(rows, ends)
         hidden = F.relu(up) if self.gate is None else F.silu(self.gate(rows, ends)) * up
-        y = self.down(hidden, ends)
-        back = torch.empty_like(order).scatter_(0, order, torch.arange(n * self.top, device=x.device))
-        return (y[back].view(n, self.top, -1).float() * weight[..., None]).sum(1).to(x.dtype)
+        return RunCombineFunction.apply(self.down(hidden, ends), place, source, weight, add)
 
 
 class RoutedBlock(nn.Module):
@@ -53,7 +49,7 @@ class RoutedBlock(nn.Module):
         super().__init__()
         d, ffn = cfg["d"], cfg["ffn"]
         self.heads = cfg["heads"]
-        norm = (lambda: RMSNorm(d, dtype, device)) if cfg["rms"] else (lambda: nn.LayerNorm(d, dtype=dtype, device=device))
+        norm = (lambda: RunRMSNorm(d, dtype=dtype, device=device)) if cfg["rms"] else (lambda: nn.LayerNorm(d, dtype=dtype, device=device))
         self.norm1, self.norm2 = norm(), norm()
         for p in list(self.norm1.parameters()) + list(self.norm2.parameters()):
             p.requires_grad_(False)
@@ -62,14 +58,25 @@ class RoutedBlock(nn.Module):
 
     def forward(self, x, cache=None):
         b, s, d = x.shape
-        h = self.norm1(x)
+        rms = isinstance(self.norm1, RunRMSNorm)
+        given = ()
+        if rms and isinstance(self.q_proj, RunLoRAFp8Linear):
+            h, rows = self.norm1(x, rows=True)
+            given = (rows,)  # rounded once for the three projections
+        else:
+            h = self.norm1(x)
         split = lambda t: t.view(b, s, self.heads, d // self.heads).transpose(1, 2)
-        q, k, v = split(self.q_proj(h)), split(self.k_proj(h)), split(self.v_proj(h))
+        q, k, v = (split(proj(h, *given)) for proj in (self.q_proj, self.k_proj, self.v_proj))
         if cache is not None:
             k, v = torch.cat((cache[0], k), 2), torch.cat((cache[1], v), 2)
         a = F.scaled_dot_product_attention(q, k, v, is_causal=cache is None)
-        x = x + self.o_proj(a.transpose(1, 2).reshape(b, s, d))
-        return x + self.mlp(self.norm2(x).view(b * s, d)).view(b, s, d)
+        a = self.o_proj(a.transpose(1, 2).reshape(b, s, d))
+        if rms:
+            h, x = self.norm2(a, x)
+        else:
+            x = x + a
+            h = self.norm2(x)
+        return self.mlp(h.view(b * s, d), x).view(b, s, d)
 
 
 def build_block(cfg, kind, experts, top, r, alpha, dtype, device, seed):
