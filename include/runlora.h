@@ -433,6 +433,12 @@ int runlora_fp8_forward(const rl_tensor_t* X, const rl_tensor_t* Q, const rl_ten
                         rl_saved_t* saved, const rl_opts_t* opts);
 
 /*
+ * The values that rounded rows stand for: out [rows, cols] (RL_F32 / RL_F16 / RL_BF16, cols a multiple of 8) = Q (RL_FP8_R128), rounded to out's type
+ * (exact in RL_F32 and RL_BF16 within their range).  Rows up to 2^30, cols up to 2097152.
+ */
+int runlora_fp8_values(const rl_tensor_t* Q, rl_tensor_t* out, const rl_opts_t* opts);
+
+/*
  * Choose the (forward, backward) pair of computation graphs for one layer shape, by estimated time
  * or by operation count (the selection step named in the abstract).  Pure host function,
  * thread-safe, no HIP call.  Uses the time model unless the environment variable

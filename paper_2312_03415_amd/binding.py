@@ -40,7 +40,7 @@ EXPORTS = (
     "runlora_fp8_quantize", "runlora_experts_forward", "runlora_experts_backward", "runlora_experts_workspace_bytes",
     "runlora_route_forward", "runlora_route_backward", "runlora_route_workspace_bytes", "runlora_gather_forward", "runlora_gather_backward",
     "runlora_combine_forward", "runlora_combine_backward", "runlora_rmsnorm_forward", "runlora_rmsnorm_backward", "runlora_rmsnorm_workspace_bytes",
-    "runlora_fp8_forward",
+    "runlora_fp8_forward", "runlora_fp8_values",
 )
 SCORES = ("softmax", "sigmoid")  # RL_SCORE_SOFTMAX, RL_SCORE_SIGMOID
 
@@ -171,6 +171,8 @@ def lib():
     L.runlora_rmsnorm_workspace_bytes.restype = ctypes.c_size_t
     L.runlora_fp8_forward.argtypes = [tp, tp, tp, tp, tp, tp, sp, op]
     L.runlora_fp8_forward.restype = ci
+    L.runlora_fp8_values.argtypes = [tp, tp, op]
+    L.runlora_fp8_values.restype = ci
     L.runlora_select.argtypes = [i64, i64, i64, i64, ci, ip, ip]
     L.runlora_select.restype = ci
     L.runlora_select_by.argtypes = [ci, i64, i64, i64, i64, ci, ip, ip]
@@ -339,11 +341,11 @@ class Fp8Rows:
         return Fp8Rows(make(rows, blocks * 128), make(blocks, (rows + 15) // 16 * 16), rows, cols)
 
     def values(self, dtype=None):
-        """The values that the bytes stand for (float32 if no dtype is given)."""
+        """The values that the bytes stand for, rounded to dtype (None: float32, exact)."""
         import torch
-        scale = torch.exp2(self.scales[:, :self.rows].t().float() - 127.0).to(dtype or torch.float32)
-        q = self.data.view(torch.float8_e4m3fn).to(scale.dtype).view(self.rows, -1, 128)
-        return (q * scale[:, :, None]).view(self.rows, -1)[:, :self.cols]
+        out = torch.empty((self.rows, self.cols), dtype=dtype or torch.float32, device=self.data.device)
+        with torch.cuda.device_of(out):
+            return runlora_fp8_values(self, out) if self.rows else out
 
 
 class Route:
@@ -361,11 +363,15 @@ class Route:
             if getattr(self, name) < 1:
                 raise ValueError(f"{name} must be at least 1")
 
+    @property
+    def how(self):
+        """The whole numbers of rl_route_t in their order."""
+        return (self.experts, self.top, SCORES.index(self.score), int(self.renormalise), self.groups, self.groups_kept, self.group_top)
+
     def desc(self, bias=None):
         """rl_route_t, with the balance bias (None or float32 [experts])."""
         import torch
-        return rl_route_t(self.experts, self.top, SCORES.index(self.score), int(self.renormalise), self.groups, self.groups_kept, self.group_top, self.scale,
-                          _vector(bias, self.experts, torch.float32, "bias"))
+        return rl_route_t(*self.how, self.scale, _vector(bias, self.experts, torch.float32, "bias"))
 
 
 def _vector(t, count, dtype, name):
@@ -630,6 +636,14 @@ def runlora_fp8_forward(X, Q, W, A, B, Y, saved, workspace=None, stream=None, sc
     o = _opts(workspace, stream, scale, bias)
     _check(lib().runlora_fp8_forward(_ref(dx), _ref(dq), _ref(dw), _ref(da), _ref(db), _ref(dy), ctypes.byref(saved), ctypes.byref(o)))
     return Y
+
+
+def runlora_fp8_values(Q, out, stream=None):
+    """out [rows, cols] = the values that Q (Fp8Rows) stands for, rounded to out's type."""
+    _one_gpu(out, Q)
+    dq, do, o = tensor_desc(Q), tensor_desc(out), _opts(None, stream)
+    _check(lib().runlora_fp8_values(_ref(dq), _ref(do), ctypes.byref(o)))
+    return out
 
 
 def _logits_desc(t):

@@ -879,6 +879,22 @@ extern "C" int runlora_fp8_forward(const rl_tensor_t* X, const rl_tensor_t* Q, c
   return fp8_forward(RL_FWD1, X, W, A, B, Y, saved, opts, false, Q);
 }
 
+extern "C" int runlora_fp8_values(const rl_tensor_t* Q, rl_tensor_t* out, const rl_opts_t* opts) {
+  if (!Q || !out) return RL_ERR_NULL;
+  const int dt = internal_dtype(out->dtype);
+  if (dt < 0) return RL_ERR_DTYPE;
+  int rc = check_dims(out->rows, out->cols, 8, 8, out->dtype);
+  if (rc != RL_OK) return rc;
+  if (out->cols > kMaxLd) return RL_ERR_UNSUPPORTED;
+  if (out->cols % 8 != 0) return RL_ERR_ALIGN;
+  if ((rc = check_tensor(out, out->rows, out->cols, out->dtype)) != RL_OK || (rc = check_rounded(Q, out->rows, out->cols)) != RL_OK) return rc;
+  const Range x = dense_range(out);
+  if (overlap(x, rounded_range(Q)) || overlap(x, rounded_scales(Q))) return RL_ERR_ALIAS;
+  const hipError_t e = fp8_values_run(dt, Q->data, Q->ld, static_cast<const uint8_t*>(Q->scales), fp8_scale_ld(Q->rows), out->rows, out->cols, out->data, out->ld,
+                                      stream_of(opts));
+  return e == hipSuccess ? RL_OK : set_hip_error(e, "fp8 values");
+}
+
 namespace {
 // use_static: the scratch is this device's copy of the library's fixed array instead of opts->workspace
 int forward_impl(int variant, const rl_tensor_t* X, const rl_tensor_t* W, const rl_tensor_t* A, const rl_tensor_t* B,

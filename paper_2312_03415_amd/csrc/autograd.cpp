@@ -11,7 +11,9 @@
 // ExpertsNode is the same for RunLoRAExpertsFunction and RunLoRAFp8Function (999 rows of 12 experts 1032 -> 2744 r 8, forward +
 // backward: 168 us a pass with the Python node, 86 of them the GPU's).
 //
-// lora(...), vera(...), dora(...) and experts(...) return None where their node does not apply, and the caller then takes the Python node: tensor subclasses, torch
+// NormNode, RouteNode, GatherNode and CombineNode are RunRMSNormFunction, RunRouteFunction, RunGatherFunction and RunCombineFunction.
+//
+// lora(...), vera(...), dora(...), experts(...), norm(...), route(...), gather(...) and combine(...) return None where their node does not apply, and the caller then takes the Python node: tensor subclasses, torch
 // function / dispatch modes, functorch transforms and tracing (all of which have to see a Python-level function), devices
 // other than the current GPU, and operands that only the Python path's checks describe properly.  Forward-mode gradients are
 // refused by either node, saved-tensor hooks apply to both (the same tensors are saved in the same order).
@@ -47,6 +49,17 @@ decltype(&runlora_dora_workspace_bytes) p_dora_workspace_bytes = nullptr;
 decltype(&runlora_experts_forward) p_experts_forward = nullptr;
 decltype(&runlora_experts_backward) p_experts_backward = nullptr;
 decltype(&runlora_experts_workspace_bytes) p_experts_workspace_bytes = nullptr;
+decltype(&runlora_fp8_forward) p_fp8_forward = nullptr;
+decltype(&runlora_rmsnorm_forward) p_rmsnorm_forward = nullptr;
+decltype(&runlora_rmsnorm_backward) p_rmsnorm_backward = nullptr;
+decltype(&runlora_rmsnorm_workspace_bytes) p_rmsnorm_workspace_bytes = nullptr;
+decltype(&runlora_route_forward) p_route_forward = nullptr;
+decltype(&runlora_route_backward) p_route_backward = nullptr;
+decltype(&runlora_route_workspace_bytes) p_route_workspace_bytes = nullptr;
+decltype(&runlora_gather_forward) p_gather_forward = nullptr;
+decltype(&runlora_gather_backward) p_gather_backward = nullptr;
+decltype(&runlora_combine_forward) p_combine_forward = nullptr;
+decltype(&runlora_combine_backward) p_combine_backward = nullptr;
 PyObject* g_check = nullptr;
 
 void check(int rc) {
@@ -369,7 +382,7 @@ const int32_t* ends_of(const at::Tensor& ends, int64_t experts, const at::Tensor
 struct ExpertsNode : public torch::autograd::Function<ExpertsNode> {
   static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& A, const at::Tensor& B, const at::Tensor& W,
                             const std::optional<at::Tensor>& scales, const std::optional<at::Tensor>& ends, const std::optional<at::Tensor>& bias,
-                            double scale, int64_t o) {
+                            double scale, int64_t o, const std::optional<at::Tensor>& q, const std::optional<at::Tensor>& q_scales) {
     const int code = dtype_code(x.scalar_type());
     const at::Tensor s = scales.has_value() ? *scales : at::Tensor(), e = ends.has_value() ? *ends : at::Tensor();
     const rl_stack_t dw = stack_desc(W, x, code, o, s), da = stack_desc(A, x, code), db = stack_desc(B, x, code);
@@ -381,7 +394,16 @@ struct ExpertsNode : public torch::autograd::Function<ExpertsNode> {
     const rl_opts_t opts = options(x, ws, bias, scale);
     const rl_tensor_t dx = desc(x2, code);
     rl_tensor_t dy = desc(y, code), dt = desc(T, code);
-    check(p_experts_forward(&dx, ends_of(e, dw.experts, x), &dw, &da, &db, &dy, &dt, &opts));
+    if (q.has_value()) {  // (one matrix)
+      const rl_tensor_t tq{q->data_ptr(), n, dw.rows, q->size(1), RL_FP8_R128, q_scales->data_ptr(), 128};
+      const rl_tensor_t tw{dw.data, dw.rows, dw.cols, dw.ld, dw.dtype, dw.scales, dw.group}, ta = desc(A, code), tb = desc(B, code);
+      rl_saved_t saved{};
+      saved.T = T.data_ptr();
+      saved.ldt = r;
+      check(p_fp8_forward(&dx, &tq, &tw, &ta, &tb, &dy, &saved, &opts));
+    } else {
+      check(p_experts_forward(&dx, ends_of(e, dw.experts, x), &dw, &da, &db, &dy, &dt, &opts));
+    }
     ctx->save_for_backward({x2, e, A, B, T, W, s});  // (the Python nodes' order; what a call lacks is skipped by both)
     ctx->saved_data["scale"] = scale;
     ctx->saved_data["o"] = o;
@@ -415,9 +437,246 @@ struct ExpertsNode : public torch::autograd::Function<ExpertsNode> {
                              dB.defined() ? &tb : nullptr, &opts));
     if (dx.defined()) dx = dx.view(ctx->saved_data["x_shape"].toIntVector());
     at::Tensor none;
-    return {dx, dA, dB, none, none, none, none, none, none};
+    return {dx, dA, dB, none, none, none, none, none, none, none, none};
   }
 };
+
+// y, h where there is a residual, and y's rows in 8 bits (bytes and scales) where they are asked for
+struct NormNode : public torch::autograd::Function<NormNode> {
+  static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const std::optional<at::Tensor>& gain,
+                                                const std::optional<at::Tensor>& residual, double eps, bool bytes) {
+    const int code = dtype_code(x.scalar_type());
+    const int64_t d = x.size(-1);
+    const at::Tensor x2 = rows(x, d), r2 = residual.has_value() ? rows(*residual, d) : at::Tensor();
+    const int64_t n = x2.size(0);
+    const at::Tensor y = at::empty({n, d}, x.options()), h = residual.has_value() ? at::empty({n, d}, x.options()) : x2;
+    const at::Tensor rstd = at::empty({n}, x.options().dtype(at::kFloat));
+    at::Tensor q, qs;
+    rl_tensor_t tq{};
+    if (bytes) {
+      const int64_t blocks = (d + 127) / 128;
+      q = at::empty({n, blocks * 128}, x.options().dtype(at::kByte));
+      qs = at::empty({blocks, (n + 15) / 16 * 16}, x.options().dtype(at::kByte));
+      tq = rl_tensor_t{q.data_ptr(), n, d, blocks * 128, RL_FP8_R128, qs.data_ptr(), 128};
+    }
+    const rl_tensor_t tx = desc(x2, code), tr = residual.has_value() ? desc(r2, code) : rl_tensor_t{};
+    rl_tensor_t ty = desc(y, code), th = desc(h, code);
+    rl_opts_t opts{};
+    opts.stream = c10::hip::getCurrentHIPStream(x.device().index()).stream();
+    check(p_rmsnorm_forward(&tx, residual.has_value() ? &tr : nullptr, gain.has_value() ? gain->data_ptr() : nullptr, (float)eps, &ty,
+                            residual.has_value() ? &th : nullptr, rstd.data_ptr<float>(), bytes ? &tq : nullptr, &opts));
+    ctx->save_for_backward({h, gain.has_value() ? *gain : at::Tensor(), rstd});
+    ctx->saved_data["x_shape"] = x.sizes().vec();
+    ctx->saved_data["residual"] = residual.has_value();
+    ctx->saved_data["gain"] = gain.has_value();
+    ctx->set_materialize_grads(false);
+    torch::autograd::variable_list out{y.view(x.sizes())};
+    if (residual.has_value()) out.push_back(h.view(x.sizes()));
+    if (bytes) {
+      ctx->mark_non_differentiable({q, qs});
+      out.push_back(q);
+      out.push_back(qs);
+    }
+    return out;
+  }
+
+  static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+    const auto vars = ctx->get_saved_variables();
+    const bool residual = ctx->saved_data["residual"].toBool(), gain = ctx->saved_data["gain"].toBool();
+    // (edges are those of the tensors that there are)
+    const bool need_x = ctx->needs_input_grad(0), need_gain = gain && ctx->needs_input_grad(1), need_r = residual && ctx->needs_input_grad(gain ? 2 : 1);
+    const at::Tensor none, dh = residual && grads.size() > 1 ? grads[1] : none;
+    if (!grads[0].defined()) return {need_x ? dh : none, none, need_r ? dh : none, none, none};
+    TORCH_CHECK_VALUE(vars[0].is_cuda(), "the saved input came back on ", vars[0].device());
+    const int64_t d = vars[0].size(-1);
+    const at::Tensor h2 = rows(vars[0], d);
+    const c10::OptionalDeviceGuard guard(h2.device());
+    const at::Tensor dy2 = rows(grads[0], d), dh2 = dh.defined() ? rows(dh, d) : none;
+    const int64_t n = h2.size(0);
+    const int code = dtype_code(h2.scalar_type());
+    const float* const rstd = static_cast<const float*>(saved_vec(vars[2], n, at::kFloat, h2, "rstd"));
+    const void* const w = gain ? saved_vec(vars[1], d, dy2.scalar_type(), h2, "gain") : nullptr;
+    at::Tensor dx, dw;
+    rl_tensor_t tx{};
+    if (need_x || need_r) { dx = at::empty({n, d}, h2.options()); tx = desc(dx, code); }
+    if (need_gain) dw = at::empty({d}, h2.options());
+    const at::Tensor ws = need_gain ? scratch(p_rmsnorm_workspace_bytes(n, d, code), h2) : none;
+    rl_opts_t opts{};
+    opts.stream = c10::hip::getCurrentHIPStream(h2.device().index()).stream();
+    if (need_gain) {
+      opts.workspace = ws.data_ptr();
+      opts.workspace_bytes = (size_t)ws.numel();
+    }
+    const rl_tensor_t ty = desc(dy2, dtype_code(dy2.scalar_type())), tg = dh.defined() ? desc(dh2, dtype_code(dh2.scalar_type())) : rl_tensor_t{}, th = desc(h2, code);
+    check(p_rmsnorm_backward(&ty, dh.defined() ? &tg : nullptr, &th, w, rstd, dx.defined() ? &tx : nullptr, need_gain ? dw.data_ptr() : nullptr, &opts));
+    if (dx.defined()) dx = dx.view(ctx->saved_data["x_shape"].toIntVector());
+    return {need_x ? dx : none, dw, need_r ? dx : none, none, none};
+  }
+};
+
+// rows of logits as the library takes them: any distance between them, which a single row may have wrong
+rl_tensor_t logits_desc(const at::Tensor& t) {
+  TORCH_CHECK_VALUE(t.is_cuda() && t.dim() == 2 && (t.size(1) < 2 || t.stride(1) == 1), "expected 2-D logits with contiguous rows");
+  const int64_t ld = t.size(0) > 1 ? t.stride(0) : std::max(t.size(1), t.stride(0));
+  return rl_tensor_t{t.data_ptr(), t.size(0), t.size(1), ld, dtype_code(t.scalar_type()), nullptr, 0};
+}
+template <typename V>
+V* saved_table(const at::Tensor& t, at::IntArrayRef sizes, at::ScalarType type, const at::Tensor& x, const char* name) {
+  TORCH_CHECK_VALUE(t.device() == x.device() && t.sizes() == sizes && t.scalar_type() == type && t.is_contiguous(), name, " must be a dense tensor of ", sizes);
+  return t.data_ptr<V>();
+}
+
+struct RouteNode : public torch::autograd::Function<RouteNode> {
+  static rl_route_t plan(const std::vector<int64_t>& how, double scale, const at::Tensor& bias) {
+    return rl_route_t{(int32_t)how[0], (int32_t)how[1], (int32_t)how[2], (int32_t)how[3], (int32_t)how[4], (int32_t)how[5], (int32_t)how[6], (float)scale,
+                      bias.defined() ? bias.data_ptr<float>() : nullptr};
+  }
+  static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& logits, const std::optional<at::Tensor>& bias,
+                                                std::vector<int64_t> how, double scale) {
+    const rl_tensor_t tl = logits_desc(logits);
+    const int64_t n = tl.rows, top = how[1];
+    const at::TensorOptions ints = logits.options().dtype(at::kInt);
+    const at::Tensor weight = at::empty({n, top}, logits.options().dtype(at::kFloat)), expert = at::empty({n, top}, ints), place = at::empty({n, top}, ints),
+                     source = at::empty({n * top}, ints), ends = at::empty({how[0]}, ints);
+    const at::Tensor ws = scratch(p_route_workspace_bytes(n, how[0], top), logits);
+    rl_opts_t opts{};
+    opts.stream = c10::hip::getCurrentHIPStream(logits.device().index()).stream();
+    opts.workspace = ws.data_ptr();
+    opts.workspace_bytes = (size_t)ws.numel();
+    const rl_route_t route = plan(how, scale, bias.has_value() ? *bias : at::Tensor());
+    check(p_route_forward(&tl, &route, expert.data_ptr<int32_t>(), weight.data_ptr<float>(), place.data_ptr<int32_t>(), source.data_ptr<int32_t>(),
+                          ends.data_ptr<int32_t>(), &opts));
+    ctx->save_for_backward({logits, expert, bias.has_value() ? *bias : at::Tensor()});
+    ctx->saved_data["how"] = how;
+    ctx->saved_data["scale"] = scale;
+    ctx->mark_non_differentiable({expert, place, source, ends});
+    return {weight, expert, place, source, ends};
+  }
+
+  static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+    const auto vars = ctx->get_saved_variables();
+    const at::Tensor &logits = vars[0], &bias = vars[2];
+    const std::vector<int64_t> how = ctx->saved_data["how"].toIntVector();
+    const rl_tensor_t tl = logits_desc(logits);
+    const c10::OptionalDeviceGuard guard(logits.device());
+    const int32_t* const expert = saved_table<int32_t>(vars[1], {tl.rows, how[1]}, at::kInt, logits, "expert");
+    if (bias.defined()) saved_table<float>(bias, {how[0]}, at::kFloat, logits, "bias");
+    const at::Tensor dw = grads[0].contiguous(), dl = at::empty({tl.rows, tl.cols}, logits.options());
+    rl_tensor_t td = logits_desc(dl);
+    rl_opts_t opts{};
+    opts.stream = c10::hip::getCurrentHIPStream(logits.device().index()).stream();
+    const rl_route_t route = plan(how, ctx->saved_data["scale"].toDouble(), bias);
+    check(p_route_backward(&tl, &route, expert, saved_table<float>(dw, {tl.rows, how[1]}, at::kFloat, logits, "dweight"), &td, &opts));
+    at::Tensor none;
+    return {dl, none, none, none};
+  }
+};
+
+struct GatherNode : public torch::autograd::Function<GatherNode> {
+  static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& place, const at::Tensor& source) {
+    const int code = dtype_code(x.scalar_type());
+    const at::Tensor x2 = rows(x, x.size(-1));
+    const at::Tensor out = at::empty({place.numel(), x2.size(1)}, x.options());
+    const rl_tensor_t tx = desc(x2, code);
+    rl_tensor_t tr = desc(out, code);
+    rl_opts_t opts{};
+    opts.stream = c10::hip::getCurrentHIPStream(x.device().index()).stream();
+    check(p_gather_forward(&tx, place.data_ptr<int32_t>(), source.data_ptr<int32_t>(), (int)place.size(1), &tr, &opts));
+    ctx->save_for_backward({place});
+    ctx->saved_data["x_shape"] = x.sizes().vec();
+    return out;
+  }
+
+  static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+    const auto vars = ctx->get_saved_variables();
+    const at::Tensor& place = vars[0];
+    const c10::OptionalDeviceGuard guard(grads[0].device());
+    const at::Tensor dr = rows(grads[0], grads[0].size(-1));
+    const int code = dtype_code(dr.scalar_type());
+    TORCH_CHECK_VALUE(place.dim() == 2 && place.numel() == dr.size(0), "place came back as another table");
+    const at::Tensor dx = at::empty({place.size(0), dr.size(1)}, dr.options());
+    const rl_tensor_t tr = desc(dr, code);
+    rl_tensor_t tx = desc(dx, code);
+    rl_opts_t opts{};
+    opts.stream = c10::hip::getCurrentHIPStream(dr.device().index()).stream();
+    check(p_gather_backward(&tr, saved_table<int32_t>(place, place.sizes(), at::kInt, dr, "place"), (int)place.size(1), &tx, &opts));
+    at::Tensor none;
+    return {dx.view(ctx->saved_data["x_shape"].toIntVector()), none, none};
+  }
+};
+
+struct CombineNode : public torch::autograd::Function<CombineNode> {
+  static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& back, const at::Tensor& weight, const at::Tensor& place, const at::Tensor& source,
+                            const std::optional<at::Tensor>& add) {
+    const int code = dtype_code(back.scalar_type());
+    const int64_t n = place.size(0), d = back.size(-1);
+    const at::Tensor r2 = rows(back, d), w = weight.contiguous(), a2 = add.has_value() ? rows(*add, d) : at::Tensor();
+    at::Tensor y = at::empty({n, d}, back.options());
+    const rl_tensor_t tr = desc(r2, code), ta = add.has_value() ? desc(a2, code) : rl_tensor_t{};
+    rl_tensor_t ty = desc(y, code);
+    rl_opts_t opts{};
+    opts.stream = c10::hip::getCurrentHIPStream(back.device().index()).stream();
+    check(p_combine_forward(&tr, place.data_ptr<int32_t>(), w.data_ptr<float>(), (int)place.size(1), add.has_value() ? &ta : nullptr, &ty, &opts));
+    ctx->save_for_backward({r2, place, source, w});
+    ctx->saved_data["add"] = add.has_value();
+    return add.has_value() ? y.view(add->sizes()) : y;
+  }
+
+  static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+    const auto vars = ctx->get_saved_variables();
+    const at::Tensor &place = vars[1], &w = vars[3];
+    TORCH_CHECK_VALUE(vars[0].is_cuda() && vars[0].dim() == 2, "the saved rows came back as ", vars[0].sizes(), " on ", vars[0].device());
+    const int64_t d = vars[0].size(1);
+    const at::Tensor r2 = rows(vars[0], d);
+    const c10::OptionalDeviceGuard guard(r2.device());
+    const at::Tensor dy = rows(grads[0], d), none;
+    const int code = dtype_code(r2.scalar_type());
+    const bool need_r = ctx->needs_input_grad(0), need_w = ctx->needs_input_grad(1), need_a = ctx->saved_data["add"].toBool() && ctx->needs_input_grad(4);
+    at::Tensor dr, dw;
+    rl_tensor_t tr{};
+    if (need_r) { dr = at::empty({r2.size(0), d}, r2.options()); tr = desc(dr, code); }
+    if (need_w) dw = at::empty(w.sizes(), w.options());
+    if (need_r || need_w) {
+      const rl_tensor_t ty = desc(dy, dtype_code(dy.scalar_type())), tb = desc(r2, code);
+      rl_opts_t opts{};
+      opts.stream = c10::hip::getCurrentHIPStream(r2.device().index()).stream();
+      TORCH_CHECK_VALUE(place.dim() == 2 && place.numel() == r2.size(0), "place came back as another table");
+      check(p_combine_backward(&ty, &tb, saved_table<int32_t>(place, place.sizes(), at::kInt, r2, "place"),
+                               saved_table<int32_t>(vars[2], {place.numel()}, at::kInt, r2, "source"), saved_table<float>(w, place.sizes(), at::kFloat, r2, "weight"),
+                               (int)place.size(1), need_r ? &tr : nullptr, need_w ? dw.data_ptr<float>() : nullptr, &opts));
+    }
+    return {dr, dw, none, none, need_a ? grads[0] : none};
+  }
+};
+
+// no mode, transform or tracer that has to see a Python-level function
+bool plainly_called() {
+  return !(torch::jit::tracer::isTracing() || at::impl::torch_function_mode_enabled() || c10::impl::TorchDispatchModeTLS::any_modes_set() ||
+           c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode));
+}
+// a plain tensor with elements on the current GPU
+const at::Tensor* plain_tensor(PyObject* o) {
+  if (!THPVariable_CheckExact(o)) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda() || t.layout() != at::kStrided || t.numel() == 0 || t.device().index() != c10::hip::current_device() || t.is_conj() || t.is_neg() || t._is_zerotensor())
+    return nullptr;
+  return &t;
+}
+bool plain_ints(const at::Tensor* t, int64_t dim) { return t != nullptr && t->scalar_type() == at::kInt && t->dim() == dim && t->is_contiguous(); }
+
+PyObject* tuple_of(const torch::autograd::variable_list& list) {
+  PyObject* out = PyTuple_New((Py_ssize_t)list.size());
+  if (out == nullptr) throw python_error();
+  for (size_t k = 0; k < list.size(); ++k) {
+    PyObject* t = THPVariable_Wrap(list[k]);
+    if (t == nullptr) {
+      Py_DECREF(out);
+      throw python_error();
+    }
+    PyTuple_SET_ITEM(out, (Py_ssize_t)k, t);
+  }
+  return out;
+}
 
 bool plain_2d(const at::Tensor& t, const at::Tensor& x) {
   return t.dim() == 2 && t.stride(1) == 1 && t.scalar_type() == x.scalar_type() && t.device() == x.device() && t.layout() == at::kStrided;
@@ -548,11 +807,111 @@ PyObject* py_dora(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-// experts(x, A, B, W, scales, ends, bias, scale, d_out): y, or None; scales, ends and bias may be None.  W, A and B are stacks, or with ends
-// None matrices; the library's checks have the messages for sizes that do not fit
+// norm(x, gain, eps, residual, bytes): (y, [h,] [bytes, scales]), or None; gain and residual may be None
+PyObject* py_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 5 || p_rmsnorm_forward == nullptr || !PyFloat_CheckExact(args[2]) || !PyBool_Check(args[4]) || !plainly_called()) Py_RETURN_NONE;
+  const at::Tensor* const x = plain_tensor(args[0]);
+  if (x == nullptr || x->dim() < 1 || dtype_code(x->scalar_type()) < 0) Py_RETURN_NONE;
+  std::optional<at::Tensor> gain, residual;
+  if (args[1] != Py_None) {
+    const at::Tensor* const t = plain_tensor(args[1]);
+    if (t == nullptr || t->dim() != 1 || t->numel() != x->size(-1) || t->stride(0) != 1 || t->scalar_type() != x->scalar_type()) Py_RETURN_NONE;
+    gain = *t;
+  }
+  if (args[3] != Py_None) {
+    const at::Tensor* const t = plain_tensor(args[3]);
+    if (t == nullptr || t->sizes() != x->sizes() || t->scalar_type() != x->scalar_type()) Py_RETURN_NONE;
+    residual = *t;
+  }
+  torch::autograd::variable_list out;
+  {
+    pybind11::gil_scoped_release release;
+    out = NormNode::apply(*x, gain, residual, PyFloat_AS_DOUBLE(args[2]), args[4] == Py_True);
+  }
+  return tuple_of(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// route(logits, bias, (experts, top, score, renormalise, groups, groups_kept, group_top), scale): (weight, expert, place, source, ends), or None
+PyObject* py_route(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 4 || p_route_forward == nullptr || !PyTuple_CheckExact(args[2]) || PyTuple_GET_SIZE(args[2]) != 7 || !PyFloat_CheckExact(args[3]) || !plainly_called())
+    Py_RETURN_NONE;
+  std::vector<int64_t> how(7);
+  for (int k = 0; k < 7; ++k) {
+    PyObject* const v = PyTuple_GET_ITEM(args[2], k);
+    if (!PyLong_CheckExact(v)) Py_RETURN_NONE;
+    how[k] = PyLong_AsLongLong(v);
+    if (PyErr_Occurred()) {
+      PyErr_Clear();
+      Py_RETURN_NONE;
+    }
+    if (how[k] < 0 || how[k] > 1 << 30) Py_RETURN_NONE;
+  }
+  const at::Tensor* const l = plain_tensor(args[0]);
+  if (l == nullptr || l->dim() != 2 || dtype_code(l->scalar_type()) < 0 || (l->size(1) > 1 && l->stride(1) != 1) || (l->size(0) > 1 && l->stride(0) < l->size(1)) ||
+      l->size(1) != how[0] || how[1] > how[0] || how[1] < 1)
+    Py_RETURN_NONE;
+  std::optional<at::Tensor> bias;
+  if (args[1] != Py_None) {
+    const at::Tensor* const t = plain_tensor(args[1]);
+    if (t == nullptr || t->dim() != 1 || t->numel() != how[0] || t->stride(0) != 1 || t->scalar_type() != at::kFloat) Py_RETURN_NONE;
+    bias = *t;
+  }
+  torch::autograd::variable_list out;
+  {
+    pybind11::gil_scoped_release release;
+    out = RouteNode::apply(*l, bias, how, PyFloat_AS_DOUBLE(args[3]));
+  }
+  return tuple_of(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// gather(x, place, source): rows, or None
+PyObject* py_gather(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 3 || p_gather_forward == nullptr || !plainly_called()) Py_RETURN_NONE;
+  const at::Tensor *const x = plain_tensor(args[0]), *const place = plain_tensor(args[1]), *const source = plain_tensor(args[2]);
+  if (x == nullptr || x->dim() < 1 || dtype_code(x->scalar_type()) < 0 || !plain_ints(place, 2) || !plain_ints(source, 1)) Py_RETURN_NONE;
+  if (place->size(0) != x->numel() / x->size(-1) || source->numel() != place->numel()) Py_RETURN_NONE;
+  at::Tensor out;
+  {
+    pybind11::gil_scoped_release release;
+    out = GatherNode::apply(*x, *place, *source);
+  }
+  return THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// combine(rows, place, source, weight, add): y, or None; add may be None
+PyObject* py_combine(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 5 || p_combine_forward == nullptr || !plainly_called()) Py_RETURN_NONE;
+  const at::Tensor *const back = plain_tensor(args[0]), *const place = plain_tensor(args[1]), *const source = plain_tensor(args[2]), *const weight = plain_tensor(args[3]);
+  if (back == nullptr || back->dim() != 2 || dtype_code(back->scalar_type()) < 0 || !plain_ints(place, 2) || !plain_ints(source, 1)) Py_RETURN_NONE;
+  if (weight == nullptr || weight->scalar_type() != at::kFloat || weight->sizes() != place->sizes() || source->numel() != place->numel() || back->size(0) != place->numel())
+    Py_RETURN_NONE;
+  std::optional<at::Tensor> add;
+  if (args[4] != Py_None) {
+    const at::Tensor* const t = plain_tensor(args[4]);
+    if (t == nullptr || t->dim() < 1 || t->size(-1) != back->size(1) || t->numel() != place->size(0) * back->size(1) || t->scalar_type() != back->scalar_type()) Py_RETURN_NONE;
+    add = *t;
+  }
+  at::Tensor out;
+  {
+    pybind11::gil_scoped_release release;
+    out = CombineNode::apply(*back, *weight, *place, *source, add);
+  }
+  return THPVariable_Wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// experts(x, A, B, W, scales, ends, bias, scale, d_out[, rows, row_scales]): y, or None; scales, ends, bias and the last two may be None.  W, A and B are
+// stacks, or with ends None matrices; rows: x's rows in 8 bits, for an 8-bit matrix; the library's checks have the messages for sizes that do not fit
 PyObject* py_experts(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
-  if (nargs != 9 || p_experts_forward == nullptr || !PyFloat_CheckExact(args[7]) || !PyLong_CheckExact(args[8])) Py_RETURN_NONE;
+  if ((nargs != 9 && nargs != 11) || p_experts_forward == nullptr || !PyFloat_CheckExact(args[7]) || !PyLong_CheckExact(args[8])) Py_RETURN_NONE;
   const int64_t o = PyLong_AsLongLong(args[8]);
   if (PyErr_Occurred()) {
     PyErr_Clear();
@@ -583,32 +942,48 @@ PyObject* py_experts(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (bias.has_value() && (bias->scalar_type() != x.scalar_type() || !bias->is_contiguous() || bias->dim() != dim - 1 || bias->size(-1) != o ||
                             (dim == 3 && bias->size(0) != W.size(0))))
     Py_RETURN_NONE;
+  std::optional<at::Tensor> q, q_scales;
+  if (nargs == 11 && args[9] != Py_None) {
+    const at::Tensor *const t = plain_tensor(args[9]), *const u = plain_tensor(args[10]);
+    const int64_t n = x.numel() / x.size(-1), blocks = (x.size(-1) + 127) / 128;
+    if (t == nullptr || u == nullptr || ends.has_value() || !scales.has_value() || t->element_size() != 1 || u->element_size() != 1) Py_RETURN_NONE;
+    if (t->sizes() != at::IntArrayRef({n, blocks * 128}) || u->sizes() != at::IntArrayRef({blocks, (n + 15) / 16 * 16}) || !t->is_contiguous() || !u->is_contiguous()) Py_RETURN_NONE;
+    q = *t;
+    q_scales = *u;
+  }
   at::Tensor y;
   {
     pybind11::gil_scoped_release release;
-    y = ExpertsNode::apply(x, A, B, W, scales, ends, bias, PyFloat_AS_DOUBLE(args[7]), o);
+    y = ExpertsNode::apply(x, A, B, W, scales, ends, bias, PyFloat_AS_DOUBLE(args[7]), o, q, q_scales);
   }
   return THPVariable_Wrap(y);
   END_HANDLE_TH_ERRORS
 }
 
-// init((forward, backward, workspace_bytes addresses of LoRA, of VeRA, of DoRA, of the experts: twelve in all), check)
+// init(addresses of the library's entry points in the order below, check)
 PyObject* py_init(PyObject*, PyObject* args) {
-  unsigned long long a[12];
-  PyObject* chk;
-  if (!PyArg_ParseTuple(args, "(KKKKKKKKKKKK)O", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &a[9], &a[10], &a[11], &chk)) return nullptr;
-  p_forward = reinterpret_cast<decltype(p_forward)>(a[0]);
-  p_backward = reinterpret_cast<decltype(p_backward)>(a[1]);
-  p_workspace_bytes = reinterpret_cast<decltype(p_workspace_bytes)>(a[2]);
-  p_vera_forward = reinterpret_cast<decltype(p_vera_forward)>(a[3]);
-  p_vera_backward = reinterpret_cast<decltype(p_vera_backward)>(a[4]);
-  p_vera_workspace_bytes = reinterpret_cast<decltype(p_vera_workspace_bytes)>(a[5]);
-  p_dora_forward = reinterpret_cast<decltype(p_dora_forward)>(a[6]);
-  p_dora_backward = reinterpret_cast<decltype(p_dora_backward)>(a[7]);
-  p_dora_workspace_bytes = reinterpret_cast<decltype(p_dora_workspace_bytes)>(a[8]);
-  p_experts_forward = reinterpret_cast<decltype(p_experts_forward)>(a[9]);
-  p_experts_backward = reinterpret_cast<decltype(p_experts_backward)>(a[10]);
-  p_experts_workspace_bytes = reinterpret_cast<decltype(p_experts_workspace_bytes)>(a[11]);
+  PyObject *list, *chk;
+  if (!PyArg_ParseTuple(args, "O!O", &PyTuple_Type, &list, &chk)) return nullptr;
+  unsigned long long a[23];
+  constexpr Py_ssize_t count = sizeof(a) / sizeof(a[0]);
+  if (PyTuple_GET_SIZE(list) != count) {
+    PyErr_SetString(PyExc_TypeError, "another number of entry points was expected");
+    return nullptr;
+  }
+  for (Py_ssize_t k = 0; k < count; ++k) {
+    a[k] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(list, k));
+    if (PyErr_Occurred()) return nullptr;
+  }
+  int k = 0;
+  auto take = [&](auto& p) { p = reinterpret_cast<std::remove_reference_t<decltype(p)>>(a[k++]); };
+  take(p_forward); take(p_backward); take(p_workspace_bytes);
+  take(p_vera_forward); take(p_vera_backward); take(p_vera_workspace_bytes);
+  take(p_dora_forward); take(p_dora_backward); take(p_dora_workspace_bytes);
+  take(p_experts_forward); take(p_experts_backward); take(p_experts_workspace_bytes);
+  take(p_fp8_forward);
+  take(p_rmsnorm_forward); take(p_rmsnorm_backward); take(p_rmsnorm_workspace_bytes);
+  take(p_route_forward); take(p_route_backward); take(p_route_workspace_bytes);
+  take(p_gather_forward); take(p_gather_backward); take(p_combine_forward); take(p_combine_backward);
   Py_INCREF(chk);
   Py_XDECREF(g_check);
   g_check = chk;
@@ -619,6 +994,10 @@ PyMethodDef methods[] = {{"lora", reinterpret_cast<PyCFunction>(reinterpret_cast
                          {"vera", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_vera)), METH_FASTCALL, "VeRA layer as a native autograd node, or None"},
                          {"dora", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_dora)), METH_FASTCALL, "DoRA layer as a native autograd node, or None"},
                          {"experts", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_experts)), METH_FASTCALL, "layer over expert stacks or an 8-bit weight as a native autograd node, or None"},
+                         {"norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_norm)), METH_FASTCALL, "root-mean-square norm as a native autograd node, or None"},
+                         {"route", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_route)), METH_FASTCALL, "routing to experts as a native autograd node, or None"},
+                         {"gather", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_gather)), METH_FASTCALL, "rows to the experts as a native autograd node, or None"},
+                         {"combine", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_combine)), METH_FASTCALL, "the experts' rows back as a native autograd node, or None"},
                          {"init", py_init, METH_VARARGS, "hand over librunlora's entry points"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_autograd", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -58,6 +58,37 @@ __global__ __launch_bounds__(kThreads) void fp8_blocks_kernel(const T* __restric
   if (threadIdx.x == 0) s[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = (uint8_t)byte;
 }
 
+// a thread takes eight columns of a row
+template <typename T>
+__global__ __launch_bounds__(kThreads) void fp8_values_kernel(const uint8_t* __restrict__ q, int64_t ldq, const uint8_t* __restrict__ s, int64_t lds, int64_t n,
+                                                              int K, T* __restrict__ out, int64_t ldo) {
+  const int pieces = K / 8;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n * pieces; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t row = i / pieces;
+    const int col = (int)(i - row * pieces) * 8;
+    const i32x2 b = *reinterpret_cast<const i32x2*>(q + row * ldq + col);
+    const int byte = s[(int64_t)(col >> 7) * lds + row];
+    T o[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(b[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(b[h], true);
+      const float v[4] = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[4 * h + k] = from_f32<T>(byte == 255 ? __builtin_nanf("") : ldexpf(v[k], byte - 127));
+    }
+    typedef __attribute__((__vector_size__(4 * sizeof(int)))) int v4;
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) reinterpret_cast<v4*>(out + row * ldo + col)[k] = reinterpret_cast<const v4*>(o)[k];
+  }
+}
+template <typename T>
+hipError_t values_run(const void* q, int64_t ldq, const uint8_t* s, int64_t lds, int64_t n, int64_t K, void* out, int64_t ldo, hipStream_t stream) {
+  int64_t groups = (n * (K / 8) + kThreads - 1) / kThreads;
+  if (groups > (1 << 20)) groups = 1 << 20;
+  launch_timed(fp8_values_kernel<T>, dim3((unsigned)groups), dim3(kThreads), 0, stream, static_cast<const uint8_t*>(q), ldq, s, lds, n, (int)K, static_cast<T*>(out), ldo);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t rows_run(const void* X, int64_t ldx, int64_t n, int64_t K, void* q, int64_t ldq, uint8_t* s, int64_t lds, hipStream_t stream) {
   const unsigned gy = (unsigned)((ldq + 511) / 512);
@@ -81,6 +112,11 @@ hipError_t blocks_run(const void* W, int64_t ldw, int64_t rows, int64_t cols, vo
 
 hipError_t fp8_rows_run(int dtype, const void* X, int64_t ldx, int64_t n, int64_t K, void* q, int64_t ldq, uint8_t* s, int64_t lds, hipStream_t stream) {
   return dtype == DT_BF16 ? rows_run<__bf16>(X, ldx, n, K, q, ldq, s, lds, stream) : rows_run<_Float16>(X, ldx, n, K, q, ldq, s, lds, stream);
+}
+
+hipError_t fp8_values_run(int dtype, const void* q, int64_t ldq, const uint8_t* s, int64_t lds, int64_t n, int64_t K, void* out, int64_t ldo, hipStream_t stream) {
+  if (dtype == DT_F32) return values_run<float>(q, ldq, s, lds, n, K, out, ldo, stream);
+  return dtype == DT_BF16 ? values_run<__bf16>(q, ldq, s, lds, n, K, out, ldo, stream) : values_run<_Float16>(q, ldq, s, lds, n, K, out, ldo, stream);
 }
 
 hipError_t fp8_blocks_run(int dtype, const void* W, int64_t ldw, int64_t rows, int64_t cols, void* q, int64_t ldq, uint8_t* s, hipStream_t stream) {

@@ -91,6 +91,8 @@ __device__ __forceinline__ void fp8_rows_tile(const T* __restrict__ X, int64_t l
 hipError_t fp8_rows_run(int dtype, const void* X, int64_t ldx, int64_t n, int64_t K, void* q, int64_t ldq, uint8_t* s, int64_t lds, hipStream_t stream);
 // W [rows, cols] in blocks of 128 x 128: q [rows][ldq], s [ceil(rows / 128)][ceil(cols / 128)]
 hipError_t fp8_blocks_run(int dtype, const void* W, int64_t ldw, int64_t rows, int64_t cols, void* q, int64_t ldq, uint8_t* s, hipStream_t stream);
+// out [n, K] (f32 / f16 / bf16) = the values that rounded rows q [n][ldq], s [ldq / 128][lds] stand for
+hipError_t fp8_values_run(int dtype, const void* q, int64_t ldq, const uint8_t* s, int64_t lds, int64_t n, int64_t K, void* out, int64_t ldo, hipStream_t stream);
 
 inline int64_t fp8_row_bytes(int64_t K) { return (K + 127) / 128 * 128; }
 inline int64_t fp8_scale_ld(int64_t n) { return (n + 15) / 16 * 16; }

@@ -50,7 +50,10 @@ def _native():
         address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
         entries = (lib.runlora_forward, lib.runlora_backward, lib.runlora_call_workspace_bytes, lib.runlora_vera_forward, lib.runlora_vera_backward,
                    lib.runlora_vera_workspace_bytes, lib.runlora_dora_forward, lib.runlora_dora_backward, lib.runlora_dora_workspace_bytes,
-                   lib.runlora_experts_forward, lib.runlora_experts_backward, lib.runlora_experts_workspace_bytes)
+                   lib.runlora_experts_forward, lib.runlora_experts_backward, lib.runlora_experts_workspace_bytes, lib.runlora_fp8_forward,
+                   lib.runlora_rmsnorm_forward, lib.runlora_rmsnorm_backward, lib.runlora_rmsnorm_workspace_bytes,
+                   lib.runlora_route_forward, lib.runlora_route_backward, lib.runlora_route_workspace_bytes,
+                   lib.runlora_gather_forward, lib.runlora_gather_backward, lib.runlora_combine_forward, lib.runlora_combine_backward)
         _autograd.init(tuple(address(f) for f in entries), rl._check)
         _native_module = _autograd
     return _native_module
@@ -457,8 +460,8 @@ class RunLoRAFp8Function(torch.autograd.Function):
 
     @classmethod
     def apply(cls, x, W, A, B, bias, scale, rows=None):
-        if cls is RunLoRAFp8Function and isinstance(W, rl.Fp8Weight) and rows is None:
-            y = _native().experts(x, A, B, W.data, W.scales, None, bias, scale, W.cols)
+        if cls is RunLoRAFp8Function and isinstance(W, rl.Fp8Weight):
+            y = _native().experts(x, A, B, W.data, W.scales, None, bias, scale, W.cols, *(() if rows is None else (rows.data, rows.scales)))
             if y is not None:
                 return y
         return super().apply(x, W, A, B, bias, scale, rows)
@@ -584,6 +587,10 @@ class RunRMSNormFunction(torch.autograd.Function):
 
     @classmethod
     def apply(cls, x, gain, eps, residual=None, rows=False):
+        if cls is RunRMSNormFunction:
+            out = _native().norm(x, gain, eps, residual, rows)
+            if out is not None:
+                return out if len(out) > 1 else out[0]
         return super().apply(x, gain, eps, residual, rows)
 
     @_on_inputs_gpu
@@ -655,6 +662,10 @@ class RunRouteFunction(torch.autograd.Function):
 
     @classmethod
     def apply(cls, logits, route, bias=None):
+        if cls is RunRouteFunction:
+            out = _native().route(logits, bias, route.how, route.scale)
+            if out is not None:
+                return out
         return super().apply(logits, route, bias)
 
     @_on_inputs_gpu
@@ -704,6 +715,14 @@ class RunRouter(nn.Module):
 class RunGatherFunction(torch.autograd.Function):
     """rows [n top, d] sorted by expert from x [n, d] (runlora_gather_forward / _backward); place and source as RunRouteFunction gives them."""
 
+    @classmethod
+    def apply(cls, x, place, source):
+        if cls is RunGatherFunction:
+            rows = _native().gather(x, place, source)
+            if rows is not None:
+                return rows
+        return super().apply(x, place, source)
+
     @_on_inputs_gpu
     def forward(ctx, x, place, source):
         x2 = _rows(x, x.shape[-1])
@@ -730,6 +749,10 @@ class RunCombineFunction(torch.autograd.Function):
 
     @classmethod
     def apply(cls, rows, place, source, weight, add=None):
+        if cls is RunCombineFunction:
+            y = _native().combine(rows, place, source, weight, add)
+            if y is not None:
+                return y
         return super().apply(rows, place, source, weight, add)
 
     @_on_inputs_gpu

@@ -169,6 +169,21 @@ def test_norm_rows_beyond_31_bits():
     assert np.abs(to_f64(want) - z).max() < 2 ** -7 * np.abs(z).max()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_values_of_8bit_rows(dtype):
+    """All 256 bytes at scale bytes from both ends, each rounded once to the type."""
+    rl = _rl()
+    n, d = 20, 264
+    q = rl.Fp8Rows.empty(n, d)
+    q.data.copy_(torch.arange(q.data.numel(), device="cuda").view_as(q.data) * 7 % 256)
+    byte = np.resize([0, 1, 5, 100, 112, 120, 127, 130, 140, 230, 246, 255], (3, n))
+    q.scales[:, :n] = torch.from_numpy(byte.astype(np.uint8)).cuda()
+    got = q.values(torch_dtype(dtype)).cpu()
+    v = experts_oracle.e4m3_value(q.data[:, :d].cpu().numpy()) * np.where(byte == 255, np.nan, np.ldexp(1.0, byte.astype(np.int64) - 127))[np.arange(d) // 128].T
+    want = torch.from_numpy(v).float().to(torch_dtype(dtype))   # (exact in float32: 4 bits and an exponent of at least -127 - 9)
+    assert torch.equal(torch.nan_to_num(got.float(), nan=1.5e30), torch.nan_to_num(want.float(), nan=1.5e30))
+
+
 @pytest.mark.parametrize("n", [1, 40, 300])
 def test_8bit_layer_on_given_rows(n):
     """The bits of the layer that rounds its rows itself."""
@@ -724,6 +739,101 @@ def test_captured_training_pass():
         want = step(x.detach().clone().requires_grad_(True))
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
+
+
+def test_python_nodes_give_the_native_ones_bits():
+    """A torch function mode sends the calls to the Python nodes."""
+    from torch.overrides import TorchFunctionMode
+    from paper_2312_03415_amd import module as m
+
+    class Watching(TorchFunctionMode):
+        def __torch_function__(self, func, types, args=(), kwargs=None):
+            return func(*args, **(kwargs or {}))
+
+    rl = _rl()
+    n, d, E, top = 70, 144, 12, 3
+    g = gen(6)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    bf = torch.bfloat16
+    x, r, gain, l = randn(n, d).to(bf), randn(n, d).to(bf), randn(d).to(bf), randn(n, E)
+    W, A, B = rl.Fp8Weight.quantize(randn(d, 160).to(bf)), randn(d, 8).to(bf), randn(8, 160).to(bf)
+    bias = 0.1 * randn(E)
+    dy, dh = randn(n, d).to(bf), randn(n, d).to(bf)
+    plan = rl.Route(E, top, "sigmoid", groups=4, groups_kept=2, group_top=2)
+
+    def run():
+        leaves = [t.clone().requires_grad_(True) for t in (x, r, gain, l, A)]
+        y, h, data, scales = m.RunRMSNormFunction.apply(leaves[0], leaves[2], 1e-5, leaves[1], True)
+        z, = (m.RunRMSNormFunction.apply(h, None, 1e-5),)
+        weight, expert, place, source, ends = m.RunRouteFunction.apply(leaves[3], plan, bias)
+        rows = m.RunGatherFunction.apply(z, place, source)
+        out = m.RunCombineFunction.apply(rows, place, source, weight, h)
+        q = m.RunLoRAFp8Function.apply(y, W, leaves[4], B, None, 2.0, rl.Fp8Rows(data, scales, n, d))
+        grads = torch.autograd.grad((out, q), leaves, (dy, torch.ones_like(q)))
+        return [y, h, data, scales[:, :n], z, weight, expert, place, source, ends, rows, out, q, *grads]
+
+    native = run()
+    with Watching():
+        python = run()
+    names = [t.grad_fn.name() for t in (native[0], native[5], native[10], native[11])], [t.grad_fn.name() for t in (python[0], python[5], python[10], python[11])]
+    assert all("Node" in a and "Function" in b for a, b in zip(*names)), names
+    for k, (a, b) in enumerate(zip(native, python)):
+        assert torch.equal(a, b), k
+
+
+def test_saved_tensor_hooks_and_second_use():
+    """What is saved may come back laid out anew or from the host's memory and back; a second backward through a kept graph gives the same bits."""
+    from paper_2312_03415_amd import module as m
+    n, d, E, top = 40, 136, 8, 2
+    g = gen(16)
+    x0, l0 = torch.randn(n, d, generator=g, device="cuda").bfloat16(), torch.randn(n, E, generator=g, device="cuda")
+    dy = torch.randn(n, d, generator=g, device="cuda").bfloat16()
+    norm, route = m.RunRMSNorm(d, trainable=True), m.RunRouter(E, top)
+
+    def run():
+        x, l = x0.clone().requires_grad_(True), l0.clone().requires_grad_(True)
+        y, h = norm(x, x0)
+        weight, _, place, source, _ = route(l)
+        out = m.RunCombineFunction.apply(m.RunGatherFunction.apply(y, place, source), place, source, weight, h)
+        first = torch.autograd.grad(out, (x, l, norm.weight), dy, retain_graph=True)
+        return first, torch.autograd.grad(out, (x, l, norm.weight), dy)
+
+    want, again = run()
+    assert all(torch.equal(a, b) for a, b in zip(want, again))
+    with torch.autograd.graph.save_on_cpu():
+        assert all(torch.equal(a, b) for a, b in zip(run()[0], want))
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t.cpu()), pytest.raises(Exception):
+        run()
+
+
+def test_modules_refuse():
+    from paper_2312_03415_amd import module as m
+    rl = _rl()
+    bf = torch.bfloat16
+    t = lambda *s, dtype=bf: torch.zeros(s, dtype=dtype, device="cuda")
+    norm, route = m.RunRMSNorm(64), m.RunRouter(8, 2)
+    for bad in (t(3, 72), t(3, 64, dtype=torch.float16), t(3, 64).cpu()):
+        with pytest.raises((ValueError, rl.RunLoRAError)):
+            norm(bad)
+    for residual in (t(4, 64), t(3, 64, dtype=torch.float32), t(3, 64).cpu()):
+        with pytest.raises((ValueError, rl.RunLoRAError)):
+            norm(t(3, 64), residual)
+    for bad in (t(3, 9), t(3, 2, 8), t(3, 8).cpu()):
+        with pytest.raises((ValueError, rl.RunLoRAError)):
+            route(bad)
+    with pytest.raises(rl.RunLoRAError):
+        m.RunRouteFunction.apply(t(3, 8), rl.Route(8, 9), None)
+    with pytest.raises((KeyError, ValueError, rl.RunLoRAError)):
+        route(t(3, 8, dtype=torch.int32))
+    weight, _, place, source, _ = route(t(5, 8))
+    for bad in ((t(4, 64), place, source), (t(5, 64), place.long(), source), (t(5, 64), place, source[:-1]), (t(5, 60), place, source)):
+        with pytest.raises((ValueError, rl.RunLoRAError)):
+            m.RunGatherFunction.apply(*bad)
+    rows = t(10, 64)
+    for bad in ((rows[:9], place, source, weight, None), (rows, place, source, weight.double(), None), (rows, place, source, weight, t(4, 64)),
+                (rows, place, source, weight[:, :1], None), (rows, place[:, :1].contiguous(), source, weight, None)):
+        with pytest.raises((ValueError, rl.RunLoRAError)):
+            m.RunCombineFunction.apply(*bad)
 
 
 def test_empty_batches():

@@ -2,7 +2,6 @@
 import ctypes
 import itertools
 
-import numpy as np
 import pytest
 
 from paper_2312_03415_amd import binding as rl
@@ -324,11 +323,17 @@ def test_front_end_refuses():
         rl.Fp8Rows(t(3, 100, dtype=torch.uint8), t(1, 16, dtype=torch.uint8), 3, 100)
     with pytest.raises(ValueError, match="scales"):
         rl.Fp8Rows(t(3, 128, dtype=torch.uint8), t(1, 3, dtype=torch.uint8), 3, 100)
-    q = rl.Fp8Rows.empty(3, 100, "cpu")
-    q.data.zero_()
-    q.scales.fill_(127)
-    q.data[1, 5] = 0x38   # 1.0
-    q.scales[0, 1] = 130
-    v = np.zeros((3, 100))
-    v[1, 5] = 8.0
-    assert np.array_equal(q.values().numpy(), v)
+    with pytest.raises(ValueError, match="on a GPU"):
+        rl.Fp8Rows.empty(3, 104, "cpu").values()
+
+
+def test_8bit_values_are_checked():
+    call = lambda q, out: rl.lib().runlora_fp8_values(ref(q), ref(out), None)
+    assert call(None, tensor(N, D)) == NULL and call(rounded(N, D), None) == NULL
+    assert call(tensor(N, D), tensor(N, D)) in (NULL, DTYPE) and call(rounded(N, D), tensor(N, D, 42)) == DTYPE
+    assert call(rounded(N, D), tensor(N + 1, D)) == SHAPE and call(rounded(N, D), tensor(N, D + 8)) == SHAPE
+    assert call(rounded(N, 260), tensor(N, 260, rl.RL_F32)) == ALIGN
+    for name in ("data", "scales"):
+        q, out = rounded(N, D), tensor(N, D)
+        setattr(q, name, out.data + 16)
+        assert call(q, out) == rl.RL_ERR_ALIAS
