@@ -654,7 +654,7 @@ extern "C" int runlora_route_forward(const rl_tensor_t* logits, const rl_route_t
     if (used.hit(x)) return RL_ERR_ALIAS;
     used.add(x);
   }
-  if ((rc = check_space(route_workspace(d.n, d.experts), opts)) != RL_OK) return rc;
+  if ((rc = check_space(route_workspace(d.n, d.experts, d.top), opts)) != RL_OK) return rc;
   d.expert = expert; d.weight = weight; d.place = place; d.source = source; d.ends = ends;
   const hipError_t e = route_forward(d, opts ? opts->workspace : nullptr, stream_of(opts));
   return e == hipSuccess ? RL_OK : set_hip_error(e, "route forward");
@@ -682,7 +682,7 @@ extern "C" int runlora_route_backward(const rl_tensor_t* logits, const rl_route_
 
 extern "C" size_t runlora_route_workspace_bytes(int64_t n, int64_t experts, int64_t top) {
   if (n < 1 || n >= kRouteMaxTokens || experts < 1 || experts > kRouteMaxExperts || top < 1 || top > experts || top > kRouteMaxTop) return 0;
-  return route_workspace(n, experts);
+  return route_workspace(n, experts, top);
 }
 
 extern "C" int runlora_gather_forward(const rl_tensor_t* X, const int32_t* place, const int32_t* source, int top, rl_tensor_t* rows, const rl_opts_t* opts) {

@@ -549,6 +549,7 @@ struct RouteNode : public torch::autograd::Function<RouteNode> {
     ctx->save_for_backward({logits, expert, bias.has_value() ? *bias : at::Tensor()});
     ctx->saved_data["how"] = how;
     ctx->saved_data["scale"] = scale;
+    ctx->set_materialize_grads(false);  // (zeros for the four tables would be four launches)
     ctx->mark_non_differentiable({expert, place, source, ends});
     return {weight, expert, place, source, ends};
   }
@@ -557,6 +558,8 @@ struct RouteNode : public torch::autograd::Function<RouteNode> {
     const auto vars = ctx->get_saved_variables();
     const at::Tensor &logits = vars[0], &bias = vars[2];
     const std::vector<int64_t> how = ctx->saved_data["how"].toIntVector();
+    at::Tensor none;
+    if (!grads[0].defined()) return {none, none, none, none};
     const rl_tensor_t tl = logits_desc(logits);
     const c10::OptionalDeviceGuard guard(logits.device());
     const int32_t* const expert = saved_table<int32_t>(vars[1], {tl.rows, how[1]}, at::kInt, logits, "expert");
@@ -567,7 +570,6 @@ struct RouteNode : public torch::autograd::Function<RouteNode> {
     opts.stream = c10::hip::getCurrentHIPStream(logits.device().index()).stream();
     const rl_route_t route = plan(how, ctx->saved_data["scale"].toDouble(), bias);
     check(p_route_backward(&tl, &route, expert, saved_table<float>(dw, {tl.rows, how[1]}, at::kFloat, logits, "dweight"), &td, &opts));
-    at::Tensor none;
     return {dl, none, none, none};
   }
 };

@@ -14,30 +14,38 @@ template <int CTRL>
 __device__ __forceinline__ uint32_t dpp32(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
 }
-// one step: the group's other half as this lane sees it
+// one step: the group's other half as this lane sees it (1 to 8 lanes)
 template <int STEP>
-__device__ __forceinline__ uint32_t across32(uint32_t x, bool upper) {
+__device__ __forceinline__ uint32_t across32(uint32_t x) {
   if constexpr (STEP == 1) return dpp32<0xB1>(x);        // quad_perm [1, 0, 3, 2]
   else if constexpr (STEP == 2) return dpp32<0x4E>(x);   // quad_perm [2, 3, 0, 1]
   else if constexpr (STEP == 4) return dpp32<0x141>(x);  // row_half_mirror
-  else if constexpr (STEP == 8) return dpp32<0x140>(x);  // row_mirror
-  else if constexpr (STEP == 16) {
-    const auto s = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    return upper ? s[0] : s[1];
-  } else {
-    const auto s = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    return upper ? s[0] : s[1];
-  }
+  else return dpp32<0x140>(x);                           // row_mirror
 }
 template <int STEP, typename V>
 __device__ __forceinline__ V across(V v) {
-  const bool upper = (threadIdx.x & STEP) != 0;
   if constexpr (sizeof(V) == 4) {
-    return __builtin_bit_cast(V, across32<STEP>(__builtin_bit_cast(uint32_t, v), upper));
+    return __builtin_bit_cast(V, across32<STEP>(__builtin_bit_cast(uint32_t, v)));
   } else {
     const uint64_t u = __builtin_bit_cast(uint64_t, v);
-    const uint64_t lo = across32<STEP>((uint32_t)u, upper), hi = across32<STEP>((uint32_t)(u >> 32), upper);
+    const uint64_t lo = across32<STEP>((uint32_t)u), hi = across32<STEP>((uint32_t)(u >> 32));
     return __builtin_bit_cast(V, lo | hi << 32);
+  }
+}
+// steps of 16 and 32 lanes: both halves' values on every lane, in the same order
+template <int STEP, typename V, typename Op>
+__device__ __forceinline__ V join_halves(V v, Op op) {
+  auto swap = [](uint32_t x) {
+    if constexpr (STEP == 16) return __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    else return __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  };
+  if constexpr (sizeof(V) == 4) {
+    const auto s = swap(__builtin_bit_cast(uint32_t, v));
+    return op(__builtin_bit_cast(V, (uint32_t)s[0]), __builtin_bit_cast(V, (uint32_t)s[1]));
+  } else {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const auto lo = swap((uint32_t)u), hi = swap((uint32_t)(u >> 32));
+    return op(__builtin_bit_cast(V, (uint64_t)lo[0] | (uint64_t)hi[0] << 32), __builtin_bit_cast(V, (uint64_t)lo[1] | (uint64_t)hi[1] << 32));
   }
 }
 struct OpAdd { template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a + b; } };
@@ -48,8 +56,8 @@ __device__ __forceinline__ V lanes_reduce(V v, Op op) {
   if constexpr (L > 2) v = op(v, across<2>(v));
   if constexpr (L > 4) v = op(v, across<4>(v));
   if constexpr (L > 8) v = op(v, across<8>(v));
-  if constexpr (L > 16) v = op(v, across<16>(v));
-  if constexpr (L > 32) v = op(v, across<32>(v));
+  if constexpr (L > 16) v = join_halves<16>(v, op);
+  if constexpr (L > 32) v = join_halves<32>(v, op);
   return v;
 }
 template <int L, typename V> __device__ __forceinline__ V lanes_sum(V v) { return lanes_reduce<L>(v, OpAdd()); }

@@ -132,26 +132,43 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
   for (int k = 0; k < (G ? V : 1); ++k)
 #pragma unroll
     for (int e = 0; e < E; ++e) dg[k][e] = 0.f;
-  for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < g.n; r0 += (int64_t)gridDim.x * ROWS) {
-    const int64_t row = r0 + threadIdx.x / P;
-    const bool there = row < g.n;
-    Piece<T> h[V], y[V], b[V];
-    const float rstd = there ? g.rstd[row] : 0.f;
+  // A row's pieces, the next row's on their way while this one's are used; of the widest rows, which with dg would not fit the registers, each when it
+  // is needed (their second reading comes from L2).
+  constexpr bool AHEAD = P <= 512;
+  auto piece = [&](const void* t, int64_t ld, int64_t row, int k) {
+    const int c = k * P + own;
+    return t != nullptr && row < g.n && c < pieces ? Piece<T>::load(static_cast<const T*>(t) + row * ld + (int64_t)c * E) : Piece<T>::zero();
+  };
+  constexpr int N = AHEAD ? V : 1;
+  auto fetch = [&](int64_t row, Piece<T> (&h)[N], Piece<T> (&y)[N], Piece<T> (&b)[N], float& rstd) {
+    rstd = row < g.n ? g.rstd[row] : 0.f;
+    if constexpr (AHEAD) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) {
-      const int c = k * P + own;
-      const bool ok = there && c < pieces;
-      h[k] = ok ? Piece<T>::load(static_cast<const T*>(g.X) + row * g.ldx + (int64_t)c * E) : Piece<T>::zero();
-      y[k] = ok ? Piece<T>::load(static_cast<const T*>(g.dY) + row * g.lddy + (int64_t)c * E) : Piece<T>::zero();
-      b[k] = ok && g.dH != nullptr ? Piece<T>::load(static_cast<const T*>(g.dH) + row * g.lddh + (int64_t)c * E) : Piece<T>::zero();
+      for (int k = 0; k < V; ++k) {
+        h[k] = piece(g.X, g.ldx, row, k);
+        y[k] = piece(g.dY, g.lddy, row, k);
+        b[k] = piece(g.dH, g.lddh, row, k);
+      }
     }
+  };
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  Piece<T> h[N], y[N], b[N], h2[N], y2[N], b2[N];
+  float rstd, rstd2 = 0.f;
+  int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / P;
+  fetch(row, h, y, b, rstd);
+  for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < g.n; r0 += step, row += step) {
+    const bool there = row < g.n;
+    if (r0 + step < g.n) fetch(row + step, h2, y2, b2, rstd2);
+    auto get_h = [&](int k, float (&f)[E]) { if constexpr (AHEAD) h[k].get(f); else piece(g.X, g.ldx, row, k).get(f); };
+    auto get_y = [&](int k, float (&f)[E]) { if constexpr (AHEAD) y[k].get(f); else piece(g.dY, g.lddy, row, k).get(f); };
+    auto get_b = [&](int k, float (&f)[E]) { if constexpr (AHEAD) b[k].get(f); else piece(g.dH, g.lddh, row, k).get(f); };
     float dot = 0.f;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       const int c = k * P + own;
       float a[E], u[E], w[E];
-      h[k].get(a);
-      y[k].get(u);
+      get_h(k, a);
+      get_y(k, u);
       (gain != nullptr && c < pieces ? Piece<T>::load(gain + (int64_t)c * E) : Piece<T>::zero()).get(w);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -159,6 +176,7 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
         if constexpr (G) dg[k][e] += u[e] * xhat;
         dot += (gain != nullptr ? u[e] * w[e] : u[e]) * xhat;
       }
+      if constexpr (!AHEAD) __builtin_amdgcn_sched_barrier(0);  // (one piece after the other: the loads of all would not fit)
     }
     if (g.dX != nullptr) {
       const float mean = row_sum<P>(dot, part) * scale;
@@ -167,9 +185,9 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
         const int c = k * P + own;
         if (!there || c >= pieces) continue;
         float a[E], u[E], z[E], w[E];
-        h[k].get(a);
-        y[k].get(u);
-        b[k].get(z);
+        get_h(k, a);
+        get_y(k, u);
+        get_b(k, z);
         (gain != nullptr ? Piece<T>::load(gain + (int64_t)c * E) : Piece<T>::zero()).get(w);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -178,6 +196,13 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
         }
         Piece<T>::of(z).store(static_cast<T*>(g.dX) + row * g.lddx + (int64_t)c * E);
       }
+    }
+    rstd = rstd2;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      h[k] = h2[k];
+      y[k] = y2[k];
+      b[k] = b2[k];
     }
   }
   if constexpr (G) {
@@ -204,30 +229,28 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
   }
 }
 
-// dg = the sum of the partial rows: 32 columns a workgroup, eight threads a column, which take the rows k, k + 8, .. in order
+// dg = the sum of the partial rows: 32 columns a workgroup, 32 threads a column, which take the rows k, k + 32, .. in order
 template <typename T>
-__global__ __launch_bounds__(256) void norm_gain_kernel(const float* __restrict__ partial, int rows, int d, T* __restrict__ out) {
-  __shared__ float part[256];
+__global__ __launch_bounds__(1024) void norm_gain_kernel(const float* __restrict__ partial, int rows, int d, T* __restrict__ out) {
+  __shared__ float part[32][33];
   const int c = threadIdx.x & 31, k = threadIdx.x >> 5, col = blockIdx.x * 32 + c;
   float s = 0.f;
   if (col < d) {
 #pragma unroll 8
-    for (int r = k; r < rows; r += 8) s += partial[(int64_t)r * d + col];
+    for (int r = k; r < rows; r += 32) s += partial[(int64_t)r * d + col];
   }
-  part[threadIdx.x] = s;
+  part[k][c] = s;
   __syncthreads();
-  if (k == 0 && col < d) {
-#pragma unroll
-    for (int j = 1; j < 8; ++j) s += part[32 * j + c];
-    out[col] = (T)s;
-  }
+  // (threads 32 c .. 32 c + 31 hold column c now)
+  s = lanes_sum<32>(part[c][k]);
+  if (c == 0 && (int)blockIdx.x * 32 + k < d) out[blockIdx.x * 32 + k] = (T)s;
 }
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // calls f(P, V) as compile-time values: the smallest that holds a row of `pieces`
 template <int P_, int V_> struct Hold { static constexpr int P = P_, V = V_; };
-template <typename F>
+template <typename T, typename F>
 hipError_t by_width(int64_t pieces, F&& f) {
   if (pieces <= 16) return f(Hold<16, 1>());
   if (pieces <= 32) return f(Hold<32, 1>());
@@ -237,9 +260,11 @@ hipError_t by_width(int64_t pieces, F&& f) {
   if (pieces <= 512) return f(Hold<256, 2>());
   if (pieces <= 768) return f(Hold<256, 3>());
   if (pieces <= 1024) return f(Hold<256, 4>());
-  if (pieces <= 2048) return f(Hold<256, 8>());
-  if (pieces <= 4096) return f(Hold<1024, 4>());
-  return f(Hold<1024, 8>());
+  if (pieces <= 2048) return f(Hold<512, 4>());
+  if constexpr (sizeof(T) == 4) {
+    if (pieces > 4096) return f(Hold<1024, 8>());
+  }
+  return f(Hold<1024, 4>());
 }
 int64_t rows_at_once(int64_t pieces) { return pieces <= 16 ? 16 : (pieces <= 32 ? 8 : (pieces <= 128 ? 4 : 1)); }
 
@@ -254,7 +279,7 @@ int64_t backward_groups(int64_t n, int64_t pieces) {
 template <typename T>
 hipError_t forward_t(const NormDesc& d, hipStream_t s) {
   const int64_t pieces = d.d / Piece<T>::N;
-  return by_width(pieces, [&](auto hold) {
+  return by_width<T>(pieces, [&](auto hold) {
     constexpr int P = decltype(hold)::P, V = decltype(hold)::V;
     int64_t groups = ceil_div(d.n, Shape<P>::kRows);
     if (groups > kForwardGroups) groups = kForwardGroups;
@@ -273,7 +298,7 @@ hipError_t forward_t(const NormDesc& d, hipStream_t s) {
 template <typename T>
 hipError_t backward_t(const NormDesc& d, float* partial, hipStream_t s) {
   const int64_t pieces = d.d / Piece<T>::N, groups = backward_groups(d.n, pieces);
-  hipError_t e = by_width(pieces, [&](auto hold) {
+  hipError_t e = by_width<T>(pieces, [&](auto hold) {
     constexpr int P = decltype(hold)::P, V = decltype(hold)::V;
     const dim3 grid((unsigned)groups), block(Shape<P>::kThreads);
     if (d.dgain != nullptr) {
@@ -284,7 +309,7 @@ hipError_t backward_t(const NormDesc& d, float* partial, hipStream_t s) {
     return hipGetLastError();
   });
   if (e != hipSuccess || d.dgain == nullptr) return e;
-  launch_timed(norm_gain_kernel<T>, dim3((unsigned)ceil_div(d.d, 32)), dim3(256), 0, s, static_cast<const float*>(partial), (int)groups, (int)d.d,
+  launch_timed(norm_gain_kernel<T>, dim3((unsigned)ceil_div(d.d, 32)), dim3(1024), 0, s, static_cast<const float*>(partial), (int)groups, (int)d.d,
                static_cast<T*>(d.dgain));
   return hipGetLastError();
 }

@@ -23,7 +23,7 @@ struct RouteDesc {
 constexpr int kRouteMaxExperts = 1024, kRouteMaxTop = 64;
 constexpr int64_t kRouteMaxTokens = 1 << 23;
 
-size_t route_workspace(int64_t n, int64_t experts);
+size_t route_workspace(int64_t n, int64_t experts, int64_t top);
 hipError_t route_forward(const RouteDesc& d, void* workspace, hipStream_t s);
 hipError_t route_backward(const RouteDesc& d, hipStream_t s);
 

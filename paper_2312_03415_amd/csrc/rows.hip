@@ -59,21 +59,31 @@ __global__ __launch_bounds__(kThreads) void spread_kernel(RowsDesc g) {
     for (int64_t c = (int64_t)own * E; c < g.d; c += P * E) {
       if (!in_range) break;
       float x[E];
-      Piece<T>::load(in + c).get(x);
+      Piece<T> r[B];
+      const Piece<T> xs = Piece<T>::load(in + c);
+      if (rows != nullptr) {  // (all of them on their way before the first is used)
 #pragma unroll
-      for (int j = 0; j < B; ++j) {
-        if (p[j] < 0) continue;
-        if (rows != nullptr) {
-          float r[E];
-          Piece<T>::load(rows + p[j] * g.ldrows + c).get(r);
+        for (int j = 0; j < B; ++j) r[j] = p[j] >= 0 ? Piece<T>::load(rows + p[j] * g.ldrows + c) : Piece<T>::zero();
+      }
+      xs.get(x);
+      if (out != nullptr) {
 #pragma unroll
-          for (int k = 0; k < E; ++k) dot[j] += x[k] * r[k];
-        }
-        if (out != nullptr) {
+        for (int j = 0; j < B; ++j) {
+          if (p[j] < 0) continue;
           float o[E];
 #pragma unroll
           for (int k = 0; k < E; ++k) o[k] = w[j] * x[k];
           Piece<T>::of(o).store(out + p[j] * g.ldout + c);
+        }
+      }
+      if (rows != nullptr) {
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+          float f[E];
+          r[j].get(f);
+          // (a copy without a place: its own zeros, whatever dY holds)
+#pragma unroll
+          for (int k = 0; k < E; ++k) dot[j] += p[j] >= 0 ? x[k] * f[k] : 0.f;
         }
       }
     }
@@ -109,7 +119,7 @@ __global__ __launch_bounds__(kThreads) void spread_kernel(RowsDesc g) {
 
 template <typename T, int P>
 __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowsDesc g) {
-  constexpr int E = Piece<T>::N;
+  constexpr int E = Piece<T>::N, B = 8;
   const int64_t t = (int64_t)blockIdx.x * (kThreads / P) + threadIdx.x / P;
   if (t >= g.n) return;
   const int64_t m = g.n * g.top;
@@ -124,15 +134,24 @@ __global__ __launch_bounds__(kThreads) void join_rows_kernel(RowsDesc g) {
 #pragma unroll
       for (int k = 0; k < E; ++k) acc[k] = 0.f;
     }
-#pragma unroll 4
-    for (int j = 0; j < g.top; ++j) {
-      const int64_t p = place[j];
-      if (p < 0 || p >= m) continue;
-      const float w = weight != nullptr ? weight[j] : 1.f;
-      float r[E];
-      Piece<T>::load(in + p * g.ldin + c).get(r);
+    for (int j0 = 0; j0 < g.top; j0 += B) {
+      Piece<T> r[B];
+      float w[B];
+      bool ok[B];
 #pragma unroll
-      for (int k = 0; k < E; ++k) acc[k] += w * r[k];
+      for (int j = 0; j < B; ++j) {  // (all of them on their way before the first is used)
+        const int64_t p = j0 + j < g.top ? place[j0 + j] : -1;
+        ok[j] = p >= 0 && p < m;
+        w[j] = ok[j] && weight != nullptr ? weight[j0 + j] : 1.f;
+        r[j] = ok[j] ? Piece<T>::load(in + p * g.ldin + c) : Piece<T>::zero();
+      }
+#pragma unroll
+      for (int j = 0; j < B; ++j) {
+        float f[E];
+        r[j].get(f);
+#pragma unroll
+        for (int k = 0; k < E; ++k) acc[k] = ok[j] ? acc[k] + w[j] * f[k] : acc[k];
+      }
     }
     Piece<T>::of(acc).store(static_cast<T*>(g.out) + t * g.ldout + c);
   }

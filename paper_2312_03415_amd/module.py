@@ -683,10 +683,13 @@ class RunRouteFunction(torch.autograd.Function):
         ctx.route = route
         ctx.save_for_backward(l2, expert, bias)
         ctx.mark_non_differentiable(expert, place, source, ends)
+        ctx.set_materialize_grads(False)
         return weight, expert, place, source, ends
 
     @staticmethod
     def backward(ctx, dweight, *_):
+        if dweight is None:
+            return None, None, None
         logits, expert, bias = ctx.saved_tensors
         dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
         if logits.shape[0] > 0:
