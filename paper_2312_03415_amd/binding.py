@@ -344,8 +344,12 @@ class Fp8Rows:
         """The values that the bytes stand for, rounded to dtype (None: float32, exact)."""
         import torch
         out = torch.empty((self.rows, self.cols), dtype=dtype or torch.float32, device=self.data.device)
+        if not self.rows:
+            return out
+        if out.get_device() < 0 or out.get_device() == _current_device():  # (host memory: refused)
+            return runlora_fp8_values(self, out)
         with torch.cuda.device_of(out):
-            return runlora_fp8_values(self, out) if self.rows else out
+            return runlora_fp8_values(self, out)
 
 
 class Route:
@@ -363,10 +367,8 @@ class Route:
             if getattr(self, name) < 1:
                 raise ValueError(f"{name} must be at least 1")
 
-    @property
-    def how(self):
-        """The whole numbers of rl_route_t in their order."""
-        return (self.experts, self.top, SCORES.index(self.score), int(self.renormalise), self.groups, self.groups_kept, self.group_top)
+        # the whole numbers of rl_route_t in their order
+        self.how = (self.experts, self.top, SCORES.index(self.score), int(self.renormalise), self.groups, self.groups_kept, self.group_top)
 
     def desc(self, bias=None):
         """rl_route_t, with the balance bias (None or float32 [experts])."""
@@ -625,6 +627,18 @@ def runlora_experts_workspace_bytes(backward, n, experts, i, o, r, dtype, w_dtyp
     return int(lib().runlora_experts_workspace_bytes(int(bool(backward)), n, experts, i, o, r, dtype, dtype if w_dtype is None else w_dtype))
 
 
+_native_calls = None
+
+
+def _native():
+    """The native module's calls into kept buffers (csrc/autograd.cpp): the marshalling of small calls, without Python's share of it."""
+    global _native_calls
+    if _native_calls is None:
+        from . import module
+        _native_calls = module._native()
+    return _native_calls
+
+
 def runlora_fp8_forward(X, Q, W, A, B, Y, saved, workspace=None, stream=None, scale=None, bias=None):
     """runlora_forward(FWD1, ...) over an Fp8Weight with X's rows already rounded (Q: Fp8Rows, as runlora_rmsnorm_forward writes them)."""
     if bias is not None and (bias.dtype != X.dtype or bias.numel() != Y.shape[1]):
@@ -640,6 +654,8 @@ def runlora_fp8_forward(X, Q, W, A, B, Y, saved, workspace=None, stream=None, sc
 
 def runlora_fp8_values(Q, out, stream=None):
     """out [rows, cols] = the values that Q (Fp8Rows) stands for, rounded to out's type."""
+    if stream is None and Q.cols == out.shape[-1] and _native().values_into(Q.data, Q.scales, out):
+        return out
     _one_gpu(out, Q)
     dq, do, o = tensor_desc(Q), tensor_desc(out), _opts(None, stream)
     _check(lib().runlora_fp8_values(_ref(dq), _ref(do), ctypes.byref(o)))
@@ -658,6 +674,8 @@ def runlora_route_forward(logits, route, weight, expert, place, source, ends, bi
     """Routing of tokens by logits [n, experts] (see runlora.h): writes weight (float32) and expert (int32) [n, top], and the order of the rows sorted
     by expert, place [n, top], source [n top] and ends [experts] (int32).  route: Route; bias: None or float32 [experts], added to the scores for the
     choice alone.  workspace: runlora_route_workspace_bytes bytes."""
+    if stream is None and _native().route_into(logits, route.how, route.scale, bias, weight, expert, place, source, ends, workspace):
+        return weight, expert, place, source, ends
     import torch
     n, top = logits.shape[0], route.top
     _one_gpu(logits, weight, expert, place, source, ends, bias, workspace)
@@ -693,6 +711,8 @@ def _copies(place, n):
 def runlora_gather_forward(X, place, source, rows, stream=None):
     """rows[place[t, j]] = X[t] for the rows [n top, d] sorted by expert (zeros where source is negative); place and source as runlora_route_forward
     writes them."""
+    if stream is None and _native().gather_into(X, place, source, rows):
+        return rows
     import torch
     top = _copies(place, X.shape[0])
     _one_gpu(X, place, source, rows)
@@ -714,6 +734,8 @@ def runlora_gather_backward(drows, place, dX, stream=None):
 
 def runlora_combine_forward(rows, place, weight, Y, add=None, stream=None):
     """Y[t] = add[t] + sum over j of weight[t, j] rows[place[t, j]] (weight float32 [n, top]; add None: nothing)."""
+    if stream is None and _native().combine_into(rows, place, weight, Y, add):
+        return Y
     import torch
     top = _copies(place, Y.shape[0])
     _one_gpu(rows, place, weight, Y, add)
@@ -739,6 +761,8 @@ def runlora_combine_backward(dY, rows, place, source, weight, drows, dweight, st
 def runlora_rmsnorm_forward(X, gain, Y, eps=1e-6, residual=None, H=None, rstd=None, rows=None, stream=None):
     """Y = h / sqrt(mean h^2 + eps) * gain over rows of h = X + residual (None: X), rounded to X's type before it is normed.  gain: [d] or None (1);
     H: where h goes (may be X or residual), rstd: float32 [n] for a backward, rows: Fp8Rows that receive Y in 8 bits; each may be None."""
+    if stream is None and _native().norm_into(X, gain, Y, eps, residual, H, rstd, *((None, None) if rows is None else (rows.data, rows.scales))):
+        return Y
     import torch
     n, d = X.shape
     _one_gpu(X, residual, gain, Y, H, rstd, rows)

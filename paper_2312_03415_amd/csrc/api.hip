@@ -620,7 +620,7 @@ int check_copies(const rl_tensor_t* tokens, const rl_tensor_t* copies, const int
   int rc = check_dims(tokens->rows, tokens->cols, 8, 8, tokens->dtype);
   if (rc != RL_OK) return rc;
   if (top < 1) return RL_ERR_SHAPE;
-  if (top > kRouteMaxTop || tokens->rows >= kRouteMaxTokens) return RL_ERR_UNSUPPORTED;
+  if (top > kRouteMaxTop || tokens->rows >= kRouteMaxTokens || !rows_fit(internal_dtype(tokens->dtype), tokens->rows, tokens->cols)) return RL_ERR_UNSUPPORTED;
   if ((rc = check_tensor(tokens, tokens->rows, tokens->cols, tokens->dtype)) != RL_OK) return rc;
   if (copies && (rc = check_tensor(copies, tokens->rows * top, tokens->cols, tokens->dtype)) != RL_OK) return rc;
   return check_ints(place);

@@ -50,6 +50,7 @@ decltype(&runlora_experts_forward) p_experts_forward = nullptr;
 decltype(&runlora_experts_backward) p_experts_backward = nullptr;
 decltype(&runlora_experts_workspace_bytes) p_experts_workspace_bytes = nullptr;
 decltype(&runlora_fp8_forward) p_fp8_forward = nullptr;
+decltype(&runlora_fp8_values) p_fp8_values = nullptr;
 decltype(&runlora_rmsnorm_forward) p_rmsnorm_forward = nullptr;
 decltype(&runlora_rmsnorm_backward) p_rmsnorm_backward = nullptr;
 decltype(&runlora_rmsnorm_workspace_bytes) p_rmsnorm_workspace_bytes = nullptr;
@@ -835,22 +836,28 @@ PyObject* py_norm(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+// the whole numbers of a plan; false where they are not seven of them
+bool plan_of(PyObject* o, std::vector<int64_t>* how) {
+  if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 7) return false;
+  for (int k = 0; k < 7; ++k) {
+    PyObject* const v = PyTuple_GET_ITEM(o, k);
+    if (!PyLong_CheckExact(v)) return false;
+    (*how)[k] = PyLong_AsLongLong(v);
+    if (PyErr_Occurred()) {
+      PyErr_Clear();
+      return false;
+    }
+    if ((*how)[k] < 0 || (*how)[k] > 1 << 30) return false;
+  }
+  return true;
+}
+
 // route(logits, bias, (experts, top, score, renormalise, groups, groups_kept, group_top), scale): (weight, expert, place, source, ends), or None
 PyObject* py_route(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
-  if (nargs != 4 || p_route_forward == nullptr || !PyTuple_CheckExact(args[2]) || PyTuple_GET_SIZE(args[2]) != 7 || !PyFloat_CheckExact(args[3]) || !plainly_called())
-    Py_RETURN_NONE;
+  if (nargs != 4 || p_route_forward == nullptr || !PyFloat_CheckExact(args[3]) || !plainly_called()) Py_RETURN_NONE;
   std::vector<int64_t> how(7);
-  for (int k = 0; k < 7; ++k) {
-    PyObject* const v = PyTuple_GET_ITEM(args[2], k);
-    if (!PyLong_CheckExact(v)) Py_RETURN_NONE;
-    how[k] = PyLong_AsLongLong(v);
-    if (PyErr_Occurred()) {
-      PyErr_Clear();
-      Py_RETURN_NONE;
-    }
-    if (how[k] < 0 || how[k] > 1 << 30) Py_RETURN_NONE;
-  }
+  if (!plan_of(args[2], &how)) Py_RETURN_NONE;
   const at::Tensor* const l = plain_tensor(args[0]);
   if (l == nullptr || l->dim() != 2 || dtype_code(l->scalar_type()) < 0 || (l->size(1) > 1 && l->stride(1) != 1) || (l->size(0) > 1 && l->stride(0) < l->size(1)) ||
       l->size(1) != how[0] || how[1] > how[0] || how[1] < 1)
@@ -966,7 +973,7 @@ PyObject* py_experts(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 PyObject* py_init(PyObject*, PyObject* args) {
   PyObject *list, *chk;
   if (!PyArg_ParseTuple(args, "O!O", &PyTuple_Type, &list, &chk)) return nullptr;
-  unsigned long long a[23];
+  unsigned long long a[24];
   constexpr Py_ssize_t count = sizeof(a) / sizeof(a[0]);
   if (PyTuple_GET_SIZE(list) != count) {
     PyErr_SetString(PyExc_TypeError, "another number of entry points was expected");
@@ -982,7 +989,7 @@ PyObject* py_init(PyObject*, PyObject* args) {
   take(p_vera_forward); take(p_vera_backward); take(p_vera_workspace_bytes);
   take(p_dora_forward); take(p_dora_backward); take(p_dora_workspace_bytes);
   take(p_experts_forward); take(p_experts_backward); take(p_experts_workspace_bytes);
-  take(p_fp8_forward);
+  take(p_fp8_forward); take(p_fp8_values);
   take(p_rmsnorm_forward); take(p_rmsnorm_backward); take(p_rmsnorm_workspace_bytes);
   take(p_route_forward); take(p_route_backward); take(p_route_workspace_bytes);
   take(p_gather_forward); take(p_gather_backward); take(p_combine_forward); take(p_combine_backward);
@@ -990,6 +997,139 @@ PyObject* py_init(PyObject*, PyObject* args) {
   Py_XDECREF(g_check);
   g_check = chk;
   Py_RETURN_NONE;
+}
+
+// ---- binding.py's calls into buffers that the caller keeps ----------------------------------------------
+//
+// The same call as through ctypes, with the operands' descriptors made here: 3 us of host time where Python's marshalling and checks take 6 to 8 (the
+// kernels of a small call take 3 to 4).  Each returns True, or None where anything is not as the call wants it: binding.py's own path has the messages.
+
+// rows of a matrix; None where `optional`
+struct RowsArg {
+  rl_tensor_t t{};
+  bool there = false, ok = false;
+  RowsArg(PyObject* o, bool optional = false) {
+    if (o == Py_None) {
+      ok = optional;
+      return;
+    }
+    const at::Tensor* const x = plain_tensor(o);
+    if (x == nullptr || x->dim() != 2 || x->stride(1) != 1) return;
+    const int code = dtype_code(x->scalar_type());
+    if (code < 0) return;
+    t = desc(*x, code);
+    there = ok = true;
+  }
+  const rl_tensor_t* in() const { return there ? &t : nullptr; }
+  rl_tensor_t* out() { return there ? &t : nullptr; }
+};
+// a dense tensor of `count` elements of a type; None where `optional`
+struct ListArg {
+  void* p = nullptr;
+  int64_t last = 0;  // its last dimension
+  bool ok = false;
+  ListArg(PyObject* o, at::ScalarType type, int64_t dim, int64_t count, bool optional = false) {
+    if (o == Py_None) {
+      ok = optional;
+      return;
+    }
+    const at::Tensor* const x = plain_tensor(o);
+    if (x == nullptr || x->scalar_type() != type || x->dim() != dim || (count >= 0 && x->numel() != count) || !x->is_contiguous()) return;
+    p = x->data_ptr();
+    last = x->size(-1);
+    ok = true;
+  }
+};
+at::ScalarType scalar_type(int code) { return code == RL_F32 ? at::kFloat : (code == RL_F16 ? at::kHalf : at::kBFloat16); }
+rl_opts_t current_options() {
+  rl_opts_t o{};
+  o.stream = c10::hip::getCurrentHIPStream(c10::hip::current_device()).stream();
+  return o;
+}
+
+// norm_into(X, gain, Y, eps, residual, H, rstd, bytes, scales)
+PyObject* py_norm_into(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 9 || p_rmsnorm_forward == nullptr || !PyFloat_CheckExact(args[3])) Py_RETURN_NONE;
+  RowsArg x(args[0]), y(args[2]), r(args[4], true), h(args[5], true);
+  if (!x.ok || !y.ok || !r.ok || !h.ok) Py_RETURN_NONE;
+  const int64_t n = x.t.rows, d = x.t.cols, blocks = (d + 127) / 128;
+  const ListArg gain(args[1], scalar_type(x.t.dtype), 1, d, true), rstd(args[6], at::kFloat, 1, n, true), q(args[7], at::kByte, 2, n * blocks * 128, true),
+      qs(args[8], at::kByte, 2, blocks * ((n + 15) / 16 * 16), true);
+  if (!gain.ok || !rstd.ok || !q.ok || !qs.ok || (q.p == nullptr) != (qs.p == nullptr) || (q.p != nullptr && q.last != blocks * 128)) Py_RETURN_NONE;
+  rl_tensor_t tq{q.p, n, d, blocks * 128, RL_FP8_R128, qs.p, 128};
+  const rl_opts_t opts = current_options();
+  check(p_rmsnorm_forward(x.in(), r.in(), gain.p, (float)PyFloat_AS_DOUBLE(args[3]), y.out(), h.out(), static_cast<float*>(rstd.p), q.p != nullptr ? &tq : nullptr, &opts));
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+// route_into(logits, plan, scale, bias, weight, expert, place, source, ends, workspace)
+PyObject* py_route_into(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  std::vector<int64_t> how(7);
+  if (nargs != 10 || p_route_forward == nullptr || !plan_of(args[1], &how) || !PyFloat_CheckExact(args[2])) Py_RETURN_NONE;
+  const at::Tensor* const l = plain_tensor(args[0]);
+  if (l == nullptr || l->dim() != 2 || dtype_code(l->scalar_type()) < 0 || (l->size(1) > 1 && l->stride(1) != 1)) Py_RETURN_NONE;
+  const rl_tensor_t tl = logits_desc(*l);
+  const int64_t n = tl.rows, copies = n * how[1];
+  const ListArg bias(args[3], at::kFloat, 1, how[0], true), weight(args[4], at::kFloat, 2, copies), expert(args[5], at::kInt, 2, copies),
+      place(args[6], at::kInt, 2, copies), source(args[7], at::kInt, 1, copies), ends(args[8], at::kInt, 1, how[0]), ws(args[9], at::kByte, 1, -1, true);
+  if (!bias.ok || !weight.ok || !expert.ok || !place.ok || !source.ok || !ends.ok || !ws.ok) Py_RETURN_NONE;
+  if (weight.last != how[1] || expert.last != how[1] || place.last != how[1]) Py_RETURN_NONE;
+  rl_opts_t opts = current_options();
+  opts.workspace = ws.p;
+  opts.workspace_bytes = (size_t)ws.last;
+  const rl_route_t route{(int32_t)how[0], (int32_t)how[1], (int32_t)how[2], (int32_t)how[3], (int32_t)how[4], (int32_t)how[5], (int32_t)how[6],
+                         (float)PyFloat_AS_DOUBLE(args[2]), static_cast<const float*>(bias.p)};
+  check(p_route_forward(&tl, &route, static_cast<int32_t*>(expert.p), static_cast<float*>(weight.p), static_cast<int32_t*>(place.p),
+                        static_cast<int32_t*>(source.p), static_cast<int32_t*>(ends.p), &opts));
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+// gather_into(X, place, source, rows)
+PyObject* py_gather_into(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 4 || p_gather_forward == nullptr) Py_RETURN_NONE;
+  RowsArg x(args[0]), rows(args[3]);
+  if (!x.ok || !rows.ok) Py_RETURN_NONE;
+  const ListArg place(args[1], at::kInt, 2, rows.t.rows), source(args[2], at::kInt, 1, rows.t.rows);
+  if (!place.ok || !source.ok || place.last * x.t.rows != rows.t.rows) Py_RETURN_NONE;
+  const rl_opts_t opts = current_options();
+  check(p_gather_forward(x.in(), static_cast<const int32_t*>(place.p), static_cast<const int32_t*>(source.p), (int)place.last, rows.out(), &opts));
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+// combine_into(rows, place, weight, Y, add)
+PyObject* py_combine_into(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 5 || p_combine_forward == nullptr) Py_RETURN_NONE;
+  RowsArg rows(args[0]), y(args[3]), add(args[4], true);
+  if (!rows.ok || !y.ok || !add.ok) Py_RETURN_NONE;
+  const ListArg place(args[1], at::kInt, 2, rows.t.rows), weight(args[2], at::kFloat, 2, rows.t.rows);
+  if (!place.ok || !weight.ok || place.last != weight.last || place.last * y.t.rows != rows.t.rows) Py_RETURN_NONE;
+  const rl_opts_t opts = current_options();
+  check(p_combine_forward(rows.in(), static_cast<const int32_t*>(place.p), static_cast<const float*>(weight.p), (int)place.last, add.in(), y.out(), &opts));
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
+// values_into(bytes, scales, out)
+PyObject* py_values_into(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 3 || p_fp8_values == nullptr) Py_RETURN_NONE;
+  RowsArg out(args[2]);
+  if (!out.ok) Py_RETURN_NONE;
+  const int64_t n = out.t.rows, blocks = (out.t.cols + 127) / 128;
+  const ListArg q(args[0], at::kByte, 2, n * blocks * 128), s(args[1], at::kByte, 2, blocks * ((n + 15) / 16 * 16));
+  if (!q.ok || !s.ok || q.last != blocks * 128) Py_RETURN_NONE;
+  const rl_tensor_t tq{q.p, n, out.t.cols, blocks * 128, RL_FP8_R128, s.p, 128};
+  const rl_opts_t opts = current_options();
+  check(p_fp8_values(&tq, out.out(), &opts));
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
 }
 
 PyMethodDef methods[] = {{"lora", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_lora)), METH_FASTCALL, "LoRA layer as a native autograd node, or None"},
@@ -1000,6 +1140,11 @@ PyMethodDef methods[] = {{"lora", reinterpret_cast<PyCFunction>(reinterpret_cast
                          {"route", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_route)), METH_FASTCALL, "routing to experts as a native autograd node, or None"},
                          {"gather", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_gather)), METH_FASTCALL, "rows to the experts as a native autograd node, or None"},
                          {"combine", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_combine)), METH_FASTCALL, "the experts' rows back as a native autograd node, or None"},
+                         {"norm_into", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_norm_into)), METH_FASTCALL, "runlora_rmsnorm_forward, or None"},
+                         {"route_into", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_route_into)), METH_FASTCALL, "runlora_route_forward, or None"},
+                         {"gather_into", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_gather_into)), METH_FASTCALL, "runlora_gather_forward, or None"},
+                         {"combine_into", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_combine_into)), METH_FASTCALL, "runlora_combine_forward, or None"},
+                         {"values_into", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(py_values_into)), METH_FASTCALL, "runlora_fp8_values, or None"},
                          {"init", py_init, METH_VARARGS, "hand over librunlora's entry points"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_autograd", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -9,6 +9,12 @@
 
 namespace rl {
 
+// An output of this size or more is stored past the caches: with what is read beside it, it would not stay in the 256 MB in front of the memory
+// until the next kernel reads it, and would be written back while that one runs.  Forward and backward, us, past them / through them: rows of 8192 x 4096
+// to two experts (128 MB) 70 / 81, back from eight of 8192 x 2048 (256 MB) 162 / 173, norms of 16384 x 5120 (160 MB) 255 / 266; below, the backward finds
+// what the forward wrote: 8192 x 4096 (64 MB) 102 / 97, 16384 x 2048 106 / 99.
+constexpr int64_t kStreamBytes = 128LL << 20;
+
 #if defined(__HIPCC__)
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp32(uint32_t x) {
@@ -72,6 +78,16 @@ struct Piece {
   __device__ __forceinline__ static Piece zero() { return Piece{V4{0, 0, 0, 0}}; }
   __device__ __forceinline__ static Piece load(const T* p) { return Piece{*reinterpret_cast<const V4*>(p)}; }
   __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<V4*>(p) = v; }
+  // past the caches, where `stream` (kStreamBytes).  The empty statements keep the compiler from making one ordinary store of the two.
+  __device__ __forceinline__ void store(T* p, bool stream) const {
+    if (stream) {
+      asm volatile("");
+      __builtin_nontemporal_store(v, reinterpret_cast<V4*>(p));
+      asm volatile("");
+    } else {
+      store(p);
+    }
+  }
   __device__ __forceinline__ void get(float (&f)[N]) const {
     T t[N];
     *reinterpret_cast<V4*>(t) = v;

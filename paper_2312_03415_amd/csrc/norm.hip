@@ -51,8 +51,8 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_forward_kernel(NormDe
     for (int k = 0; k < V; ++k) {
       const int c = k * P + own;
       const bool ok = there && c < pieces;
-      h[k] = ok ? Piece<T>::load(static_cast<const T*>(g.X) + row * g.ldx + (int64_t)c * E) : Piece<T>::zero();
-      w[k] = ok && g.R != nullptr ? Piece<T>::load(static_cast<const T*>(g.R) + row * g.ldr + (int64_t)c * E) : Piece<T>::zero();
+      h[k] = ok ? Piece<T>::load(static_cast<const T*>(g.X) + row * g.ldx + (uint32_t)(c * E)) : Piece<T>::zero();
+      w[k] = ok && g.R != nullptr ? Piece<T>::load(static_cast<const T*>(g.R) + row * g.ldr + (uint32_t)(c * E)) : Piece<T>::zero();
     }
     float sq = 0.f;
 #pragma unroll
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_forward_kernel(NormDe
 #pragma unroll
       for (int e = 0; e < E; ++e) sq += a[e] * a[e];
       const int c = k * P + own;
-      if (g.H != nullptr && there && c < pieces) h[k].store(static_cast<T*>(g.H) + row * g.ldh + (int64_t)c * E);
+      if (g.H != nullptr && there && c < pieces) h[k].store(static_cast<T*>(g.H) + row * g.ldh + (uint32_t)(c * E), g.stream);
     }
     const float rstd = rsqrtf(row_sum<P>(sq, part) * scale + g.eps);
     if (g.rstd != nullptr && there && own == 0) g.rstd[row] = rstd;
@@ -84,12 +84,12 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_forward_kernel(NormDe
       for (int e = 0; e < E; ++e) a[e] *= rstd;
       if (gain != nullptr) {
         float b[E];
-        (ok ? Piece<T>::load(gain + (int64_t)c * E) : Piece<T>::zero()).get(b);
+        (ok ? Piece<T>::load(gain + (uint32_t)(c * E)) : Piece<T>::zero()).get(b);
 #pragma unroll
         for (int e = 0; e < E; ++e) a[e] *= b[e];
       }
       const Piece<T> y = Piece<T>::of(a);
-      if (ok) y.store(static_cast<T*>(g.Y) + row * g.ldy + (int64_t)c * E);
+      if (ok) y.store(static_cast<T*>(g.Y) + row * g.ldy + (uint32_t)(c * E), g.stream);
       if constexpr (Q) {
         // 16 lanes hold a block of 128 columns (E = 8): the rows that the 8-bit layers would make of y
         y.get(a);
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
   constexpr int E = Piece<T>::N, ROWS = Shape<P>::kRows;
   __shared__ float part[16];
   __shared__ float cols[G && ROWS > 1 ? ROWS : 1][G && ROWS > 1 ? P * V * E : 1];
-  const int own = threadIdx.x % P;
+  int own = threadIdx.x % P;
   const int pieces = (int)(g.d / E);
   const float scale = 1.f / (float)g.d;
   const T* const gain = static_cast<const T*>(g.gain);
@@ -134,10 +134,10 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
     for (int e = 0; e < E; ++e) dg[k][e] = 0.f;
   // A row's pieces, the next row's on their way while this one's are used; of the widest rows, which with dg would not fit the registers, each when it
   // is needed (their second reading comes from L2).
-  constexpr bool AHEAD = P <= 512;
+  constexpr bool AHEAD = V <= 4;
   auto piece = [&](const void* t, int64_t ld, int64_t row, int k) {
     const int c = k * P + own;
-    return t != nullptr && row < g.n && c < pieces ? Piece<T>::load(static_cast<const T*>(t) + row * ld + (int64_t)c * E) : Piece<T>::zero();
+    return t != nullptr && row < g.n && c < pieces ? Piece<T>::load(static_cast<const T*>(t) + row * ld + (uint32_t)(c * E)) : Piece<T>::zero();
   };
   constexpr int N = AHEAD ? V : 1;
   auto fetch = [&](int64_t row, Piece<T> (&h)[N], Piece<T> (&y)[N], Piece<T> (&b)[N], float& rstd) {
@@ -158,6 +158,7 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
   fetch(row, h, y, b, rstd);
   for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < g.n; r0 += step, row += step) {
     const bool there = row < g.n;
+    if constexpr (!AHEAD) asm volatile("" : "+v"(own));  // (or every piece's addresses are worked out ahead of the rows, and fill the registers)
     if (r0 + step < g.n) fetch(row + step, h2, y2, b2, rstd2);
     auto get_h = [&](int k, float (&f)[E]) { if constexpr (AHEAD) h[k].get(f); else piece(g.X, g.ldx, row, k).get(f); };
     auto get_y = [&](int k, float (&f)[E]) { if constexpr (AHEAD) y[k].get(f); else piece(g.dY, g.lddy, row, k).get(f); };
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
       float a[E], u[E], w[E];
       get_h(k, a);
       get_y(k, u);
-      (gain != nullptr && c < pieces ? Piece<T>::load(gain + (int64_t)c * E) : Piece<T>::zero()).get(w);
+      (gain != nullptr && c < pieces ? Piece<T>::load(gain + (uint32_t)(c * E)) : Piece<T>::zero()).get(w);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float xhat = a[e] * rstd;
@@ -188,13 +189,14 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
         get_h(k, a);
         get_y(k, u);
         get_b(k, z);
-        (gain != nullptr ? Piece<T>::load(gain + (int64_t)c * E) : Piece<T>::zero()).get(w);
+        (gain != nullptr ? Piece<T>::load(gain + (uint32_t)(c * E)) : Piece<T>::zero()).get(w);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const float v = rstd * ((gain != nullptr ? u[e] * w[e] : u[e]) - a[e] * rstd * mean);
           z[e] = g.dH != nullptr ? v + z[e] : v;
         }
-        Piece<T>::of(z).store(static_cast<T*>(g.dX) + row * g.lddx + (int64_t)c * E);
+        Piece<T>::of(z).store(static_cast<T*>(g.dX) + row * g.lddx + (uint32_t)(c * E), g.stream);
+        if constexpr (!AHEAD) __builtin_amdgcn_sched_barrier(0);
       }
     }
     rstd = rstd2;
@@ -262,18 +264,18 @@ hipError_t by_width(int64_t pieces, F&& f) {
   if (pieces <= 1024) return f(Hold<256, 4>());
   if (pieces <= 2048) return f(Hold<512, 4>());
   if constexpr (sizeof(T) == 4) {
-    if (pieces > 4096) return f(Hold<1024, 8>());
+    if (pieces > 4096) return f(Hold<512, 16>());
   }
-  return f(Hold<1024, 4>());
+  return f(Hold<512, 8>());
 }
 int64_t rows_at_once(int64_t pieces) { return pieces <= 16 ? 16 : (pieces <= 32 ? 8 : (pieces <= 128 ? 4 : 1)); }
 
 constexpr int64_t kForwardGroups = 1 << 16;  // workgroups; beyond that they walk over rows
-constexpr int64_t kBackwardGroups = 1024;
-
+// The backward's: as many as are at work at once, four to a compute unit, two where the pieces held ahead fill the registers (16384 x 5120: 251 us a
+// pass with 512, 255 with 1024, 279 with 768).
 int64_t backward_groups(int64_t n, int64_t pieces) {
-  const int64_t g = ceil_div(n, rows_at_once(pieces));
-  return g < kBackwardGroups ? g : kBackwardGroups;
+  const int64_t g = ceil_div(n, rows_at_once(pieces)), most = pieces > 512 ? 512 : 1024;
+  return g < most ? g : most;
 }
 
 template <typename T>
@@ -314,16 +316,22 @@ hipError_t backward_t(const NormDesc& d, float* partial, hipStream_t s) {
   return hipGetLastError();
 }
 
+bool streams(const NormDesc& d) { return d.n * d.d * (d.dtype == DT_F32 ? 4 : 2) >= kStreamBytes; }
+
 }  // namespace
 
-hipError_t norm_forward(const NormDesc& d, hipStream_t s) {
+hipError_t norm_forward(const NormDesc& desc, hipStream_t s) {
+  NormDesc d = desc;
+  d.stream = streams(d);
   if (d.dtype == DT_F32) return forward_t<float>(d, s);
   return d.dtype == DT_BF16 ? forward_t<__bf16>(d, s) : forward_t<_Float16>(d, s);
 }
 size_t norm_backward_workspace(int dtype, int64_t n, int64_t d, bool dgain) {
   return dgain ? (size_t)(backward_groups(n, d / (dtype == DT_F32 ? 4 : 8)) * d) * 4 : 0;
 }
-hipError_t norm_backward(const NormDesc& d, void* workspace, hipStream_t s) {
+hipError_t norm_backward(const NormDesc& desc, void* workspace, hipStream_t s) {
+  NormDesc d = desc;
+  d.stream = streams(d);
   float* const partial = static_cast<float*>(workspace);
   if (d.dtype == DT_F32) return backward_t<float>(d, partial, s);
   return d.dtype == DT_BF16 ? backward_t<__bf16>(d, partial, s) : backward_t<_Float16>(d, partial, s);

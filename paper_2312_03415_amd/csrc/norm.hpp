@@ -21,6 +21,7 @@ struct NormDesc {
   int64_t lddy = 0, lddh = 0;
   void *dX = nullptr, *dgain = nullptr;
   int64_t lddx = 0;
+  bool stream = false;  // (set by the launches)
 };
 constexpr int64_t kNormMaxWidth = 32768;  // a row is held in registers
 

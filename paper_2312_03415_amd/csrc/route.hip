@@ -705,7 +705,8 @@ static_assert(kRouteMaxTokens / kGroups + 1024 < 65536, "counts are 16 bits");
 
 // Lanes a token: as few as hold the choice and one more, from 16 on, with up to 16 experts each.
 struct RoutePlan {
-  int lanes, per, waves, each, groups;  // per: experts a lane
+  int lanes, per, waves, each, groups;  // per: experts a lane;  waves, each, groups: of a workgroup, its tokens, workgroups
+  unsigned room;                        // bytes a wave has in LDS
 };
 RoutePlan route_plan(int64_t n, int64_t experts, int64_t top, int64_t groups) {
   RoutePlan p;
@@ -715,8 +716,16 @@ RoutePlan route_plan(int64_t n, int64_t experts, int64_t top, int64_t groups) {
   p.per = 1;
   while (p.per * p.lanes < experts) p.per *= 2;
   const int64_t side = 64 / p.lanes;
-  // LDS: up to 10 KB a wave (route_room)
-  const int most = p.per * p.lanes > 512 ? 4 : (p.per > 8 ? 8 : 16);
+  // one after the other: its rows' keys (all rows' in 32 bits, or one's in 64), its choices, its counts
+  int64_t room = experts * 4 > 256 ? experts * 4 : 256;
+  if (groups > 1) {
+    const int64_t all = (experts + 3 * p.lanes) * 4 * side, one = (experts + 3 * 64) * 8;
+    room = all > room ? all : room;
+    room = one > room ? one : room;
+  }
+  p.room = (unsigned)(ceil_div(room, 16) * 16);
+  int most = p.per > 8 ? 8 : 16;  // (the kernel's launch bounds)
+  while (most * p.room > (48u << 10)) most /= 2;
   if (n <= 4 * most * side) {
     p.waves = (int)ceil_div(n, side);
     if (p.waves > most) p.waves = most;
@@ -731,15 +740,6 @@ RoutePlan route_plan(int64_t n, int64_t experts, int64_t top, int64_t groups) {
   p.each = (int)(ceil_div(ceil_div(n, kGroups), at_once) * at_once);
   p.groups = (int)ceil_div(n, p.each);
   return p;
-}
-// bytes a wave has in LDS, one after the other, for its rows' keys (all rows' in 32 bits, or one's in 64), for its choices, or for its counts
-unsigned route_room(const RoutePlan& p, int64_t experts, int64_t groups) {
-  int64_t room = experts * 4 > 256 ? experts * 4 : 256;
-  if (groups > 1) {
-    const int64_t all = (experts + 3 * p.lanes) * 4 * (64 / p.lanes), one = (experts + 3 * 64) * 8;
-    room = all > one ? all : one;
-  }
-  return (unsigned)(ceil_div(room, 16) * 16);
 }
 
 template <int L_, int K_> struct Split { static constexpr int L = L_, K = K_; };
@@ -768,16 +768,15 @@ template <typename T>
 hipError_t forward_t(const RouteDesc& d, void* workspace, hipStream_t s) {
   const RoutePlan p = route_plan(d.n, d.experts, d.top, d.groups);
   const bool wide = route_wide(d);
-  const unsigned room = route_room(p, d.experts, d.groups);
-  const unsigned lds = (unsigned)ceil_div(d.experts * 4, 16) * 16 + (wide ? (p.lanes * p.per > 64 ? p.lanes * p.per : 64) * 4 : 0) + room * p.waves;
+  const unsigned lds = (unsigned)ceil_div(d.experts * 4, 16) * 16 + (wide ? (p.lanes * p.per > 64 ? p.lanes * p.per : 64) * 4 : 0) + p.room * p.waves;
   hipError_t e = by_lanes(p.lanes, p.per, [&](auto split) {
     constexpr int L = decltype(split)::L, K = decltype(split)::K;
     const dim3 grid((unsigned)p.groups), block((unsigned)(p.waves * 64));
     const int fast = fast_rows(d.logits, d.ld, d.experts, K, sizeof(T));
     if (wide) {
-      launch_timed(route_choose_kernel<T, L, K, true>, grid, block, lds, s, d, p.each, fast, (int)room, workspace, (int)(p.groups == 1));
+      launch_timed(route_choose_kernel<T, L, K, true>, grid, block, lds, s, d, p.each, fast, (int)p.room, workspace, (int)(p.groups == 1));
     } else {
-      launch_timed(route_choose_kernel<T, L, K, false>, grid, block, lds, s, d, p.each, fast, (int)room, workspace, (int)(p.groups == 1));
+      launch_timed(route_choose_kernel<T, L, K, false>, grid, block, lds, s, d, p.each, fast, (int)p.room, workspace, (int)(p.groups == 1));
     }
     return hipGetLastError();
   });

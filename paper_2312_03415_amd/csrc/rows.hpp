@@ -21,7 +21,14 @@ struct RowsDesc {
   void* out = nullptr;         // spread: nullptr = not wanted
   int64_t ldout = 0;
   float* dweight = nullptr;
+  bool stream = false;  // (set by the launches)
 };
+// a call's 64 x 16 bytes of rows are counted in 32 bits
+inline bool rows_fit(int dtype, int64_t n, int64_t d) {
+  const int64_t wide = dtype == 0 ? 256 : 512;  // DT_F32
+  return (d + wide - 1) / wide <= ((1LL << 32) - 1) / n;
+}
+
 // out[place[t, j]] = weight[t, j] in[t] (no weight: the rows as they are), zeros on rows without a copy; dweight[t, j] = <in[t], rows[place[t, j]]>
 hipError_t rows_spread(const RowsDesc& d, hipStream_t s);
 // out[t] = add[t] + sum over j of weight[t, j] in[place[t, j]]

@@ -50,7 +50,7 @@ def _native():
         address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
         entries = (lib.runlora_forward, lib.runlora_backward, lib.runlora_call_workspace_bytes, lib.runlora_vera_forward, lib.runlora_vera_backward,
                    lib.runlora_vera_workspace_bytes, lib.runlora_dora_forward, lib.runlora_dora_backward, lib.runlora_dora_workspace_bytes,
-                   lib.runlora_experts_forward, lib.runlora_experts_backward, lib.runlora_experts_workspace_bytes, lib.runlora_fp8_forward,
+                   lib.runlora_experts_forward, lib.runlora_experts_backward, lib.runlora_experts_workspace_bytes, lib.runlora_fp8_forward, lib.runlora_fp8_values,
                    lib.runlora_rmsnorm_forward, lib.runlora_rmsnorm_backward, lib.runlora_rmsnorm_workspace_bytes,
                    lib.runlora_route_forward, lib.runlora_route_backward, lib.runlora_route_workspace_bytes,
                    lib.runlora_gather_forward, lib.runlora_gather_backward, lib.runlora_combine_forward, lib.runlora_combine_backward)

@@ -246,7 +246,8 @@ def test_route_sizes(n, E, top):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("E,top,groups,kept,group_top", [(8, 2, 2, 1, 1), (24, 4, 8, 3, 2), (64, 6, 8, 3, 2), (120, 6, 8, 3, 1), (256, 8, 8, 4, 2), (63, 4, 21, 5, 2),
-                                                         (64, 3, 64, 9, 1), (640, 8, 64, 2, 2), (1024, 20, 4, 1, 2)])
+                                                         (64, 3, 64, 9, 1), (640, 8, 64, 2, 2), (1024, 20, 4, 1, 2), (512, 8, 64, 12, 2), (512, 33, 16, 9, 1), (256, 16, 32, 5, 2),
+                                                         (96, 5, 12, 4, 2), (40, 6, 40, 17, 1), (1023, 9, 33, 6, 2), (4, 1, 4, 2, 1)])
 @pytest.mark.parametrize("biased", [False, True])
 def test_route_groups(dtype, E, top, groups, kept, group_top, biased):
     bias = torch.randn(E, generator=gen(E), device="cuda") * 0.1 if biased else None
@@ -604,6 +605,7 @@ def test_norm_module():
     (wx, wg), (bx, bg) = ref.norm_backward(to_f64(dy), hd, to_f64(w), 1e-6, to_f64(dh), "bf16")
     for leaf in leaves:
         close("dx", leaf.grad.view(30, d), wx, bx)
+    assert leaves[0].grad.data_ptr() != leaves[1].grad.data_ptr()   # (one gradient for both, but not one memory)
     close("dgain", norm.weight.grad, wg, bg)
     # either output alone, neither input wanted, no rows
     x1 = x.clone().requires_grad_(True)
