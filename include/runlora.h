@@ -393,6 +393,7 @@ size_t runlora_route_workspace_bytes(int64_t n, int64_t experts, int64_t top);
  *     gather backward   dX_t = sum_j drows[place[t, j]]
  *     combine           Y_t = add_t + sum_j weight[t, j] rows[place[t, j]]            add may be NULL
  *     combine backward  drows[place[t, j]] = weight[t, j] dY_t,   dweight[t, j] = sum over columns of dY_t rows[place[t, j]]
+ * Places are different rows: of two copies on one row the gather and drows hold either.
  * A copy without a place (anything outside [0, n top)) adds nothing and has a dweight of 0; rows without a copy (source negative) are written as
  * zeros.  fp32 sums in the order of j (of the columns in a fixed order), rounded once.  drows or dweight may be NULL (skipped); without dweight rows may
  * be NULL.  The gradient of `add` is dY itself.

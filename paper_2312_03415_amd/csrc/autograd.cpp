@@ -442,13 +442,20 @@ struct ExpertsNode : public torch::autograd::Function<ExpertsNode> {
   }
 };
 
+// rows(), without a view where t is such a matrix already
+at::Tensor matrix(const at::Tensor& t, int64_t cols) {
+  if (t.dim() == 2 && t.size(1) == cols && t.stride(1) == 1 && t.stride(0) % 8 == 0 && t.stride(0) >= cols && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0) return t;
+  return rows(t, cols);
+}
+at::Tensor in_shape(const at::Tensor& t, at::IntArrayRef sizes) { return t.sizes() == sizes ? t : t.view(sizes); }
+
 // y, h where there is a residual, and y's rows in 8 bits (bytes and scales) where they are asked for
 struct NormNode : public torch::autograd::Function<NormNode> {
   static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const std::optional<at::Tensor>& gain,
                                                 const std::optional<at::Tensor>& residual, double eps, bool bytes) {
     const int code = dtype_code(x.scalar_type());
     const int64_t d = x.size(-1);
-    const at::Tensor x2 = rows(x, d), r2 = residual.has_value() ? rows(*residual, d) : at::Tensor();
+    const at::Tensor x2 = matrix(x, d), r2 = residual.has_value() ? matrix(*residual, d) : at::Tensor();
     const int64_t n = x2.size(0);
     const at::Tensor y = at::empty({n, d}, x.options()), h = residual.has_value() ? at::empty({n, d}, x.options()) : x2;
     const at::Tensor rstd = at::empty({n}, x.options().dtype(at::kFloat));
@@ -471,8 +478,8 @@ struct NormNode : public torch::autograd::Function<NormNode> {
     ctx->saved_data["residual"] = residual.has_value();
     ctx->saved_data["gain"] = gain.has_value();
     ctx->set_materialize_grads(false);
-    torch::autograd::variable_list out{y.view(x.sizes())};
-    if (residual.has_value()) out.push_back(h.view(x.sizes()));
+    torch::autograd::variable_list out{in_shape(y, x.sizes())};
+    if (residual.has_value()) out.push_back(in_shape(h, x.sizes()));
     if (bytes) {
       ctx->mark_non_differentiable({q, qs});
       out.push_back(q);
@@ -490,9 +497,9 @@ struct NormNode : public torch::autograd::Function<NormNode> {
     if (!grads[0].defined()) return {need_x ? dh : none, none, need_r ? dh : none, none, none};
     TORCH_CHECK_VALUE(vars[0].is_cuda(), "the saved input came back on ", vars[0].device());
     const int64_t d = vars[0].size(-1);
-    const at::Tensor h2 = rows(vars[0], d);
+    const at::Tensor h2 = matrix(vars[0], d);
     const c10::OptionalDeviceGuard guard(h2.device());
-    const at::Tensor dy2 = rows(grads[0], d), dh2 = dh.defined() ? rows(dh, d) : none;
+    const at::Tensor dy2 = matrix(grads[0], d), dh2 = dh.defined() ? matrix(dh, d) : none;
     const int64_t n = h2.size(0);
     const int code = dtype_code(h2.scalar_type());
     const float* const rstd = static_cast<const float*>(saved_vec(vars[2], n, at::kFloat, h2, "rstd"));
@@ -510,7 +517,7 @@ struct NormNode : public torch::autograd::Function<NormNode> {
     }
     const rl_tensor_t ty = desc(dy2, dtype_code(dy2.scalar_type())), tg = dh.defined() ? desc(dh2, dtype_code(dh2.scalar_type())) : rl_tensor_t{}, th = desc(h2, code);
     check(p_rmsnorm_backward(&ty, dh.defined() ? &tg : nullptr, &th, w, rstd, dx.defined() ? &tx : nullptr, need_gain ? dw.data_ptr() : nullptr, &opts));
-    if (dx.defined()) dx = dx.view(ctx->saved_data["x_shape"].toIntVector());
+    if (dx.defined()) dx = in_shape(dx, ctx->saved_data["x_shape"].toIntVector());
     return {need_x ? dx : none, dw, need_r ? dx : none, none, none};
   }
 };
@@ -578,7 +585,7 @@ struct RouteNode : public torch::autograd::Function<RouteNode> {
 struct GatherNode : public torch::autograd::Function<GatherNode> {
   static at::Tensor forward(torch::autograd::AutogradContext* ctx, const at::Tensor& x, const at::Tensor& place, const at::Tensor& source) {
     const int code = dtype_code(x.scalar_type());
-    const at::Tensor x2 = rows(x, x.size(-1));
+    const at::Tensor x2 = matrix(x, x.size(-1));
     const at::Tensor out = at::empty({place.numel(), x2.size(1)}, x.options());
     const rl_tensor_t tx = desc(x2, code);
     rl_tensor_t tr = desc(out, code);
@@ -594,7 +601,7 @@ struct GatherNode : public torch::autograd::Function<GatherNode> {
     const auto vars = ctx->get_saved_variables();
     const at::Tensor& place = vars[0];
     const c10::OptionalDeviceGuard guard(grads[0].device());
-    const at::Tensor dr = rows(grads[0], grads[0].size(-1));
+    const at::Tensor dr = matrix(grads[0], grads[0].size(-1));
     const int code = dtype_code(dr.scalar_type());
     TORCH_CHECK_VALUE(place.dim() == 2 && place.numel() == dr.size(0), "place came back as another table");
     const at::Tensor dx = at::empty({place.size(0), dr.size(1)}, dr.options());
@@ -604,7 +611,7 @@ struct GatherNode : public torch::autograd::Function<GatherNode> {
     opts.stream = c10::hip::getCurrentHIPStream(dr.device().index()).stream();
     check(p_gather_backward(&tr, saved_table<int32_t>(place, place.sizes(), at::kInt, dr, "place"), (int)place.size(1), &tx, &opts));
     at::Tensor none;
-    return {dx.view(ctx->saved_data["x_shape"].toIntVector()), none, none};
+    return {in_shape(dx, ctx->saved_data["x_shape"].toIntVector()), none, none};
   }
 };
 
@@ -613,7 +620,7 @@ struct CombineNode : public torch::autograd::Function<CombineNode> {
                             const std::optional<at::Tensor>& add) {
     const int code = dtype_code(back.scalar_type());
     const int64_t n = place.size(0), d = back.size(-1);
-    const at::Tensor r2 = rows(back, d), w = weight.contiguous(), a2 = add.has_value() ? rows(*add, d) : at::Tensor();
+    const at::Tensor r2 = matrix(back, d), w = weight.contiguous(), a2 = add.has_value() ? matrix(*add, d) : at::Tensor();
     at::Tensor y = at::empty({n, d}, back.options());
     const rl_tensor_t tr = desc(r2, code), ta = add.has_value() ? desc(a2, code) : rl_tensor_t{};
     rl_tensor_t ty = desc(y, code);
@@ -622,7 +629,7 @@ struct CombineNode : public torch::autograd::Function<CombineNode> {
     check(p_combine_forward(&tr, place.data_ptr<int32_t>(), w.data_ptr<float>(), (int)place.size(1), add.has_value() ? &ta : nullptr, &ty, &opts));
     ctx->save_for_backward({r2, place, source, w});
     ctx->saved_data["add"] = add.has_value();
-    return add.has_value() ? y.view(add->sizes()) : y;
+    return add.has_value() ? in_shape(y, add->sizes()) : y;
   }
 
   static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
@@ -630,9 +637,9 @@ struct CombineNode : public torch::autograd::Function<CombineNode> {
     const at::Tensor &place = vars[1], &w = vars[3];
     TORCH_CHECK_VALUE(vars[0].is_cuda() && vars[0].dim() == 2, "the saved rows came back as ", vars[0].sizes(), " on ", vars[0].device());
     const int64_t d = vars[0].size(1);
-    const at::Tensor r2 = rows(vars[0], d);
+    const at::Tensor r2 = matrix(vars[0], d);
     const c10::OptionalDeviceGuard guard(r2.device());
-    const at::Tensor dy = rows(grads[0], d), none;
+    const at::Tensor dy = matrix(grads[0], d), none;
     const int code = dtype_code(r2.scalar_type());
     const bool need_r = ctx->needs_input_grad(0), need_w = ctx->needs_input_grad(1), need_a = ctx->saved_data["add"].toBool() && ctx->needs_input_grad(4);
     at::Tensor dr, dw;

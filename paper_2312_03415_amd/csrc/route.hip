@@ -377,7 +377,9 @@ inline __host__ __device__ int count_bytes(int each) { return each < 256 ? 1 : 2
 
 // Workgroup b takes the tokens [b each, (b + 1) each), L lanes a token with K experts each, 64 / L tokens side by side in a wave: their experts and weights,
 // and how many rows every expert gets (counts [b][experts] in the workspace).  A single workgroup places them too.
-// Bound by its instructions (16384 x 256 in 32 bits is 16 MB, 3 us): a maximum over 16 lanes serves four tokens at once, where one over 64 serves one.
+// Bound by its instructions and, with one round of waves, by their latency (16384 x 256 in 32 bits, biased sigmoid scores, 8 groups, top 8: 16 MB, 3 us;
+// 1300 vector instructions a wave of four tokens, 9 us of them; 18 us): a maximum over 16 lanes serves four tokens at once, where one over 64 serves one
+// (38 us).  The scores in 64 bits for every row took 45.
 template <typename T, int L, int K, bool WIDE>
 __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route_choose_kernel(RouteDesc g, int each, int fast, int room, void* counts, int single) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -539,10 +541,10 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
 
 // Workgroup b places the rows of the tokens [b each, (b + 1) each), those of `part` workgroups of the choice, behind those of the tokens before: it adds up
 // everybody's counts ([groups][experts] of C), W experts a thread and the groups dealt out to the threads that are left.  Reading the counts is what grows
-// with both numbers: 512 groups of 256 experts in bytes by 256 workgroups ... us, in 16 bits by 512 17.6; a thread an expert, one group after the other,
-// took 15 us for 256.
+// with both numbers: 512 groups of 256 experts in bytes, read by 256 workgroups, take 7.6 us in all, in 16 bits by 512 17.6; a thread an expert, one group
+// after the other, took 15 for 256.
 template <typename C>
-__global__ __launch_bounds__(1024) void route_place_kernel(RouteDesc g, int each, const C* counts, int groups, int part) {
+__global__ __launch_bounds__(512) void route_place_kernel(RouteDesc g, int each, const C* counts, int groups, int part) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ int total;
   int* const starts = reinterpret_cast<int*>(lds);  // [experts]
@@ -559,20 +561,20 @@ __global__ __launch_bounds__(1024) void route_place_kernel(RouteDesc g, int each
   auto add = [&](auto width) {
     constexpr int W = decltype(width)::value;
     typedef __attribute__((__vector_size__(W * sizeof(C)))) C vec;
-    const int columns = g.experts / W, parts = (int)blockDim.x > columns ? (int)blockDim.x / columns : 1;
-    for (int c = (int)threadIdx.x; c < columns * parts; c += (int)blockDim.x) {
+    const int columns = g.experts / W, slices = (int)blockDim.x > columns ? (int)blockDim.x / columns : 1;
+    for (int c = (int)threadIdx.x; c < columns * slices; c += (int)blockDim.x) {
       int sum[W], before[W];
 #pragma unroll
       for (int k = 0; k < W; ++k) sum[k] = before[k] = 0;
-      const int column = c % columns, part = c / columns;
+      const int column = c % columns, slice = c / columns;
       const C* const from = counts + column * W;
       if constexpr (W == 4 && sizeof(C) == 1) {
         // two bytes a word at a time: 256 of them do not pass 16 bits
-        for (int b0 = part; b0 < groups; b0 += 256 * parts) {
+        for (int b0 = slice; b0 < groups; b0 += 256 * slices) {
           uint32_t even = 0, odd = 0, even_b = 0, odd_b = 0;
-          const int end = b0 + 256 * parts < groups ? b0 + 256 * parts : groups;
+          const int end = b0 + 256 * slices < groups ? b0 + 256 * slices : groups;
 #pragma unroll 16
-          for (int b = b0; b < end; b += parts) {
+          for (int b = b0; b < end; b += slices) {
             const uint32_t v = *reinterpret_cast<const uint32_t*>(from + (int64_t)b * g.experts), u = b < own ? v : 0u;
             even += v & 0x00FF00FFu;
             odd += (v >> 8) & 0x00FF00FFu;
@@ -584,7 +586,7 @@ __global__ __launch_bounds__(1024) void route_place_kernel(RouteDesc g, int each
         }
       } else {
 #pragma unroll 8
-        for (int b = part; b < groups; b += parts) {
+        for (int b = slice; b < groups; b += slices) {
           const vec v = *reinterpret_cast<const vec*>(from + (int64_t)b * g.experts);
 #pragma unroll
           for (int k = 0; k < W; ++k) {
@@ -618,7 +620,7 @@ inline __host__ __device__ bool route_wide(const RouteDesc& g) { return g.bias !
 //     softmax over chosen:    dl_j = q_j (D_j - sum_k D_k q_k)               and zero elsewhere
 //     sigmoid:                dl_j = s_j (1 - s_j) D_j;   over the chosen: q_j (1 - s_j) (D_j - sum_k D_k q_k)
 // A row is put together in LDS, most of it zeros, and leaves as whole pieces (each lane's own K elements compared with every choice, and stored K apart:
-// 12 us for 16384 x 256 top 8, ... so).
+// 12 us for 16384 x 256 top 8 in 32 bits, 7.0 so, 17 MB written).
 template <typename T, int L, int K>
 __global__ __launch_bounds__(256) void route_backward_kernel(RouteDesc g, int fast, int fast_out) {
   constexpr int SIDE = 64 / L;
@@ -781,7 +783,8 @@ hipError_t forward_t(const RouteDesc& d, void* workspace, hipStream_t s) {
     return hipGetLastError();
   });
   if (e != hipSuccess || p.groups == 1) return e;
-  const int waves = d.experts > 512 ? 8 : 16, part = (p.groups + 255) / 256;
+  // (eight waves: 2000 x 120 top 6 5.7 us, sixteen 6.4, four 7.4; 16384 x 256 top 8 7.6, 8.2, 10.2)
+  const int waves = 8, part = (p.groups + 255) / 256;
   const dim3 grid((unsigned)((p.groups + part - 1) / part)), block((unsigned)(waves * 64));
   const unsigned space = (unsigned)((2 + waves) * d.experts * 4);
   if (count_bytes(p.each) == 1) {

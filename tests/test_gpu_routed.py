@@ -359,8 +359,8 @@ def test_route_nan_and_infinity(E, biased, grouped):
 def test_route_odd_addresses_and_strides():
     """Logits and their gradient at odd addresses, with rows apart; what lies between is left."""
     rl = _rl()
-    n, E = 131, 37
-    for dtype in ("bf16", "f32"):
+    n = 131
+    for dtype, E in (("bf16", 37), ("f32", 37), ("bf16", 64), ("f32", 64), ("f16", 256), ("f32", 256)):
         l = logits(n, E, dtype, 6)
         wide = nan((n + 1, 2 * E + 1), l.dtype)
         part = wide.flatten()[1:1 + n * (2 * E + 1)].view(n, 2 * E + 1)[:, :E]
@@ -836,6 +836,60 @@ def test_modules_refuse():
                 (rows, place, source, weight[:, :1], None), (rows, place[:, :1].contiguous(), source, weight, None)):
         with pytest.raises((ValueError, rl.RunLoRAError)):
             m.RunCombineFunction.apply(*bad)
+
+
+def test_streams_and_threads():
+    """Training passes at once from several threads, each on a stream of its own, give the bits of one alone."""
+    import threading
+    from paper_2312_03415_amd import module as m
+    n, d, E, top = 333, 264, 24, 4
+    norm, route = m.RunRMSNorm(d, trainable=True), m.RunRouter(E, top, "sigmoid", groups=4, groups_kept=2, group_top=2, balance=True)
+    router = torch.randn(d, E, generator=gen(2), device="cuda") / 8
+
+    def work(seed):
+        g = gen(seed)
+        x, r, dy = (torch.randn(n, d, generator=g, device="cuda").bfloat16() for _ in range(3))
+        out = []
+        for _ in range(5):
+            a, b = x.clone().requires_grad_(True), r.clone().requires_grad_(True)
+            y, h, rows = norm(a, b, rows=True)
+            weight, expert, place, source, ends = route(y.float() @ router)
+            o = m.RunCombineFunction.apply(m.RunGatherFunction.apply(y, place, source), place, source, weight, h)
+            out = [o, expert, ends, rows.values(), *torch.autograd.grad(o, (a, b, norm.weight), dy)]
+        return [t.detach() for t in out]
+
+    want = [work(s) for s in range(4)]
+    torch.cuda.synchronize()
+    got, streams = [None] * 4, [torch.cuda.Stream() for _ in range(4)]
+
+    def run(k):
+        with torch.cuda.stream(streams[k]):
+            got[k] = work(k)
+            streams[k].synchronize()
+
+    threads = [threading.Thread(target=run, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for k in range(4):
+        assert got[k] is not None and all(torch.equal(a, b) for a, b in zip(got[k], want[k])), k
+
+
+def test_router_module_options():
+    """What RunRouter is asked for reaches the routing; a model's conversion leaves the choice to the balance bias as it then is."""
+    from paper_2312_03415_amd.module import RunRouter
+    l = logits(90, 48, "f32", 12)
+    how = dict(score="sigmoid", renormalise=False, groups=6, groups_kept=2, group_top=2, scale=2.5)
+    route = RunRouter(48, 5, balance=True, **how)
+    with torch.no_grad():
+        route.bias.normal_(0, 0.1)
+    assert "bias" in route.state_dict()
+    for module in (route, route.bfloat16()):
+        want = ref.Routing(to_f64(l), 5, bias=to_f64(module.bias), **how)
+        weight, expert, place, source, ends = module(l)
+        assert np.array_equal(expert.cpu().numpy(), want.expert) and np.array_equal(place.cpu().numpy(), want.place)
+        close("weight", weight, want.weight, want.weight_bound())
 
 
 def test_empty_batches():
