@@ -137,6 +137,7 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
   // A row's pieces, the next row's on their way while this one's are used; of the widest rows, which with dg would not fit the registers, each when it
   // is needed (their second reading comes from L2).
   constexpr bool AHEAD = V <= 4;
+  constexpr int UNROLL = AHEAD ? V : 1;  // of the second reading
   auto piece = [&](const void* t, int64_t ld, int64_t row, int k) {
     const int c = k * P + own;
     return t != nullptr && row < g.n && c < pieces ? Piece<T>::load(static_cast<const T*>(t) + row * ld + (uint32_t)(c * E)) : Piece<T>::zero();
@@ -160,7 +161,6 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
   fetch(row, h, y, b, rstd);
   for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < g.n; r0 += step, row += step) {
     const bool there = row < g.n;
-    if constexpr (!AHEAD) asm volatile("" : "+v"(own));  // (or every piece's addresses are worked out ahead of the rows, and fill the registers)
     if (r0 + step < g.n) fetch(row + step, h2, y2, b2, rstd2);
     auto get_h = [&](int k, float (&f)[E]) { if constexpr (AHEAD) h[k].get(f); else piece(g.X, g.ldx, row, k).get(f); };
     auto get_y = [&](int k, float (&f)[E]) { if constexpr (AHEAD) y[k].get(f); else piece(g.dY, g.lddy, row, k).get(f); };
@@ -168,7 +168,9 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
     float dot = 0.f;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
+      if constexpr (!AHEAD) asm volatile("" : "+v"(own)::"memory");  // (one piece after the other: the addresses and loads of all would not fit)
       const int c = k * P + own;
+      if (!AHEAD && c >= pieces) continue;  // (where pieces are held, those behind the row are zero)
       float a[E], u[E], w[E];
       get_h(k, a);
       get_y(k, u);
@@ -179,11 +181,10 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
         if constexpr (G) dg[k][e] += u[e] * xhat;
         dot += (gain != nullptr ? u[e] * w[e] : u[e]) * xhat;
       }
-      if constexpr (!AHEAD) __builtin_amdgcn_sched_barrier(0);  // (one piece after the other: the loads of all would not fit)
     }
     if (g.dX != nullptr) {
       const float mean = row_sum<P>(dot, part) * scale;
-#pragma unroll
+#pragma unroll UNROLL
       for (int k = 0; k < V; ++k) {
         const int c = k * P + own;
         if (!there || c >= pieces) continue;
@@ -198,7 +199,6 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
           z[e] = g.dH != nullptr ? v + z[e] : v;
         }
         Piece<T>::of(z).store(static_cast<T*>(g.dX) + row * g.lddx + (uint32_t)(c * E), g.stream);
-        if constexpr (!AHEAD) __builtin_amdgcn_sched_barrier(0);
       }
     }
     rstd = rstd2;

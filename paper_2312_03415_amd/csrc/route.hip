@@ -12,6 +12,46 @@
 #include "lanes.hpp"
 
 namespace rl {
+
+static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+RoutePlan route_plan(int64_t n, int64_t experts, int64_t top, int64_t groups) {
+  RoutePlan p;
+  const int64_t more = top < experts ? top + 1 : top;
+  p.lanes = experts <= 8 && groups <= 8 ? 8 : 16;
+  while (p.lanes < 64 && (p.lanes < more || p.lanes < groups || experts > 16 * p.lanes)) p.lanes *= 2;
+  p.per = 1;
+  while (p.per * p.lanes < experts) p.per *= 2;
+  const int64_t side = 64 / p.lanes;
+  // one after the other: its rows' keys (all rows' in 32 bits, or one's in 64), its choices, its counts
+  int64_t room = experts * 4 > 256 ? experts * 4 : 256;
+  if (groups > 1) {
+    const int64_t all = (experts + 3 * p.lanes) * 4 * side, one = (experts + 3 * 64) * 8;
+    room = all > room ? all : room;
+    room = one > room ? one : room;
+  }
+  p.room = (unsigned)(ceil_div(room, 16) * 16);
+  int most = p.per > 8 ? 8 : 16;  // (the kernel's launch bounds)
+  while (most * p.room > (48u << 10)) most /= 2;
+  if (n <= 4 * most * side) {
+    p.waves = (int)ceil_div(n, side);
+    if (p.waves > most) p.waves = most;
+    if (p.waves < 4) p.waves = 4;
+    p.groups = 1;
+    p.each = (int)n;
+    return p;
+  }
+  p.waves = 4;
+  while (p.waves < most && ceil_div(n, p.waves * side) > kRouteGroups) p.waves *= 2;
+  const int64_t at_once = p.waves * side;
+  p.each = (int)(ceil_div(ceil_div(n, kRouteGroups), at_once) * at_once);
+  p.groups = (int)ceil_div(n, p.each);
+  return p;
+}
+unsigned route_lds(const RoutePlan& p, int64_t experts, bool wide) {
+  return (unsigned)((experts * 4 + 15) / 16 * 16) + (wide ? (p.lanes * p.per > 64 ? p.lanes * p.per : 64) * 4 : 0) + p.room * (unsigned)p.waves;
+}
+
 namespace {
 
 constexpr float kNone = -INFINITY;  // the score of an expert that cannot be chosen
@@ -72,11 +112,11 @@ bool fast_rows(const void* p, int64_t ld, int64_t experts, int K, size_t esz) {
   return experts % K == 0 && reinterpret_cast<uintptr_t>(p) % b == 0 && (size_t)ld * esz % b == 0;
 }
 
-// exp by the exponential of 2: off by a unit and by u |x| through its argument
+// exp by the exponential of 2: off by a unit (2 u) and, through its argument, by 1.5 u |x|
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 
-// row maximum (not counting NaN; 0 where nothing is left) and sum of exp(l - max) of a row's logits, l = -inf where there is none.  (A term is off by
-// u |l - max| of itself, of which exp keeps little: 12 u of the sum over 1024 equal terms, less otherwise.)
+// row maximum (not counting NaN; 0 where nothing is left) and sum of exp(l - max) of a row's logits, l = -inf where there is none.  (The terms are off by
+// 2 u and 2.5 u |l - max| of themselves: weighted by themselves, that is at most (2.5 ln E + 2) u of the sum.)
 template <int L, int K>
 __device__ __forceinline__ void softmax_stats(const float (&l)[K], float* top, float* sum) {
   float m = kNone;
@@ -286,7 +326,6 @@ __device__ __forceinline__ void scores64(const RouteDesc& g, const float (&l)[K]
   for (int k = 0; k < K; ++k) key[k] = l[k] == kNone ? (double)kNone : ranked(key[k] + (double)bias[k]);  // (behind the last expert: -inf)
 }
 
-
 // adds where an expert's rows start, by their counts, to starts; all of them in *total, where an expert's end in `ends` (or nullptr).  All threads.
 __device__ __forceinline__ void scan_counts(const int* counts, int* starts, int experts, int* total, int32_t* ends) {
   if (threadIdx.x < 64) {
@@ -432,9 +471,10 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
           odd += s;
         }
         close = odd != odd;  // (a NaN, or infinite biases: 64 bits sort them out)
-        // How far two c may be off together.  sigmoid: exp is off by a unit and u |l|, of which s (1 - s) keeps under 1.3 u, the sum and the
-        // reciprocal by 4 u s: 2^-21 at most each.  softmax: exp by 2 u and u |l - max|, of which s keeps 0.4 u max s, the sum by 22 u and its terms'
-        // 12 u, two products 3 u: under 2^-18 max s each, max s = 1 / sum.  The sum with the bias: u |c|; the key's upper 28 bits: 16 u |c|.
+        // How far two c may be off together, u = 2^-24.  sigmoid: exp is off by 2 u and, through its argument, 1.5 u |l|, of which s (1 - s) keeps under u;
+        // 1 + e and the reciprocal by 3 u s: under 2^-21 each.  softmax: exp by 2 u and 2.5 u |l - max|, of which s keeps under u max s; the sum by 21 u and
+        // by its terms' (2.5 ln 1024 + 2) u; the quotient and the product by 2 u: under 2^-18 max s each, max s = 1 / sum.  With the bias: u |c| each; the
+        // keys' lower four bits: 30 u |c|.
         const float high = g.sigmoid ? 1.f : inverse;
         off = (g.sigmoid ? 0x1p-20f : 0x1p-17f * high) + 0x1p-18f * (high + most);
       } else {
@@ -465,7 +505,8 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
         if (!apart && !(sub + 2 < more && logit == next_l && mine_b == next_b)) close = true;
       }
       if (more > L) close = true;
-      // rows that 32 bits do not decide: the whole wave takes one after the other, so that its 64-bit keys are few a lane
+      // Rows that 32 bits do not decide: the whole wave takes one after the other, so that its 64-bit keys are few a lane.  (All rows of 16384 x 256 of one
+      // value, zero bias: both launches take 42 us, of random ones 27.)
       if (sub >= g.top) expert = -1;
       const uint64_t undecided = __ballot(close && there);
       if (undecided != 0) {
@@ -698,52 +739,6 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteDesc g, int fa
   }
 }
 
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// ---- plans --------------------------------------------------------------------------------------------
-
-constexpr int64_t kGroups = 512;  // workgroups of a large call; counts of at most 65535 rows an expert in each of them (kRouteMaxTokens)
-static_assert(kRouteMaxTokens / kGroups + 1024 < 65536, "counts are 16 bits");
-
-// Lanes a token: as few as hold the choice and one more, from 16 on, with up to 16 experts each.
-struct RoutePlan {
-  int lanes, per, waves, each, groups;  // per: experts a lane;  waves, each, groups: of a workgroup, its tokens, workgroups
-  unsigned room;                        // bytes a wave has in LDS
-};
-RoutePlan route_plan(int64_t n, int64_t experts, int64_t top, int64_t groups) {
-  RoutePlan p;
-  const int64_t more = top < experts ? top + 1 : top;
-  p.lanes = experts <= 8 && groups <= 8 ? 8 : 16;
-  while (p.lanes < 64 && (p.lanes < more || p.lanes < groups || experts > 16 * p.lanes)) p.lanes *= 2;
-  p.per = 1;
-  while (p.per * p.lanes < experts) p.per *= 2;
-  const int64_t side = 64 / p.lanes;
-  // one after the other: its rows' keys (all rows' in 32 bits, or one's in 64), its choices, its counts
-  int64_t room = experts * 4 > 256 ? experts * 4 : 256;
-  if (groups > 1) {
-    const int64_t all = (experts + 3 * p.lanes) * 4 * side, one = (experts + 3 * 64) * 8;
-    room = all > room ? all : room;
-    room = one > room ? one : room;
-  }
-  p.room = (unsigned)(ceil_div(room, 16) * 16);
-  int most = p.per > 8 ? 8 : 16;  // (the kernel's launch bounds)
-  while (most * p.room > (48u << 10)) most /= 2;
-  if (n <= 4 * most * side) {
-    p.waves = (int)ceil_div(n, side);
-    if (p.waves > most) p.waves = most;
-    if (p.waves < 4) p.waves = 4;
-    p.groups = 1;
-    p.each = (int)n;
-    return p;
-  }
-  p.waves = 4;
-  while (p.waves < most && ceil_div(n, p.waves * side) > kGroups) p.waves *= 2;
-  const int64_t at_once = p.waves * side;
-  p.each = (int)(ceil_div(ceil_div(n, kGroups), at_once) * at_once);
-  p.groups = (int)ceil_div(n, p.each);
-  return p;
-}
-
 template <int L_, int K_> struct Split { static constexpr int L = L_, K = K_; };
 template <typename F>
 hipError_t by_lanes(int lanes, int per, F&& f) {
@@ -770,7 +765,7 @@ template <typename T>
 hipError_t forward_t(const RouteDesc& d, void* workspace, hipStream_t s) {
   const RoutePlan p = route_plan(d.n, d.experts, d.top, d.groups);
   const bool wide = route_wide(d);
-  const unsigned lds = (unsigned)ceil_div(d.experts * 4, 16) * 16 + (wide ? (p.lanes * p.per > 64 ? p.lanes * p.per : 64) * 4 : 0) + p.room * p.waves;
+  const unsigned lds = route_lds(p, d.experts, wide);
   hipError_t e = by_lanes(p.lanes, p.per, [&](auto split) {
     constexpr int L = decltype(split)::L, K = decltype(split)::K;
     const dim3 grid((unsigned)p.groups), block((unsigned)(p.waves * 64));
@@ -810,7 +805,7 @@ hipError_t backward_t(const RouteDesc& d, hipStream_t s) {
 size_t route_workspace(int64_t n, int64_t experts, int64_t top) {
   // (the counts of the most workgroups there can be: what serves many tokens serves fewer)
   for (int64_t groups : {1, 16, 32, 64})  // (what the groups change of the plan)
-    if (route_plan(n, experts, top, groups).groups > 1) return (size_t)kGroups * (size_t)experts * 2;
+    if (route_plan(n, experts, top, groups).groups > 1) return (size_t)kRouteGroups * (size_t)experts * 2;
   return 0;
 }
 hipError_t route_forward(const RouteDesc& d, void* workspace, hipStream_t s) {
