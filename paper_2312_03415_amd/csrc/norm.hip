@@ -122,6 +122,7 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_forward_kernel(NormDe
 // without the next row on its way 283.)
 template <typename T, int P, int V, bool G>
 __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormDesc g, float* partial) {
+#pragma clang fp contract(off)  // (dx is the same bits with and without dg)
   constexpr int E = Piece<T>::N, ROWS = Shape<P>::kRows;
   __shared__ float part[16];
   __shared__ float cols[G && ROWS > 1 ? ROWS : 1][G && ROWS > 1 ? P * V * E : 1];
@@ -134,16 +135,15 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
   for (int k = 0; k < (G ? V : 1); ++k)
 #pragma unroll
     for (int e = 0; e < E; ++e) dg[k][e] = 0.f;
-  // A row's pieces, the next row's on their way while this one's are used; of the widest rows, which with dg would not fit the registers, each when it
-  // is needed (their second reading comes from L2).
-  constexpr bool AHEAD = V <= 4;
-  constexpr int UNROLL = AHEAD ? V : 1;  // of the second reading
+  // A row's pieces, the next row's on their way while this one's are used; of the widest rows, where both would not fit the registers with dg, this one's
+  // alone, in twice the threads (4096 x 32768, a pass over bf16 / f32: 190 / 344 us; by 512 threads that read a row twice 225 / 425).
+  constexpr bool AHEAD = V <= 4 && P <= 512;
+  static_assert(AHEAD || ROWS == 1);
   auto piece = [&](const void* t, int64_t ld, int64_t row, int k) {
     const int c = k * P + own;
     return t != nullptr && row < g.n && c < pieces ? Piece<T>::load(static_cast<const T*>(t) + row * ld + (uint32_t)(c * E)) : Piece<T>::zero();
   };
-  constexpr int N = AHEAD ? V : 1;
-  auto fetch = [&](int64_t row, Piece<T> (&h)[N], Piece<T> (&y)[N], Piece<T> (&b)[N], float& rstd) {
+  auto fetch = [&](int64_t row, Piece<T> (&h)[V], Piece<T> (&y)[V], Piece<T> (&b)[V], float& rstd) {
     rstd = row < g.n ? g.rstd[row] : 0.f;
     if constexpr (AHEAD) {
 #pragma unroll
@@ -155,55 +155,61 @@ __global__ __launch_bounds__(Shape<P>::kThreads) void norm_backward_kernel(NormD
     }
   };
   const int64_t step = (int64_t)gridDim.x * ROWS;
-  Piece<T> h[N], y[N], b[N], h2[N], y2[N], b2[N];
+  Piece<T> h[V], y[V], b[V], h2[V], y2[V], b2[V];
   float rstd, rstd2 = 0.f;
   int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / P;
   fetch(row, h, y, b, rstd);
   for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < g.n; r0 += step, row += step) {
     const bool there = row < g.n;
     if (r0 + step < g.n) fetch(row + step, h2, y2, b2, rstd2);
-    auto get_h = [&](int k, float (&f)[E]) { if constexpr (AHEAD) h[k].get(f); else piece(g.X, g.ldx, row, k).get(f); };
-    auto get_y = [&](int k, float (&f)[E]) { if constexpr (AHEAD) y[k].get(f); else piece(g.dY, g.lddy, row, k).get(f); };
+    if constexpr (!AHEAD) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const int c = k * P + own < pieces ? k * P + own : 0;  // (behind the row its first piece, unused: as many zeros would take registers too)
+        h[k] = Piece<T>::load(static_cast<const T*>(g.X) + row * g.ldx + (uint32_t)(c * E));
+        y[k] = Piece<T>::load(static_cast<const T*>(g.dY) + row * g.lddy + (uint32_t)(c * E));
+      }
+    }
     auto get_b = [&](int k, float (&f)[E]) { if constexpr (AHEAD) b[k].get(f); else piece(g.dH, g.lddh, row, k).get(f); };
     float dot = 0.f;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      if constexpr (!AHEAD) asm volatile("" : "+v"(own)::"memory");  // (one piece after the other: the addresses and loads of all would not fit)
+      if constexpr (!AHEAD) asm volatile("" : "+v"(own)::"memory");  // (one piece after the other: addresses and gains of all would not fit)
       const int c = k * P + own;
-      if (!AHEAD && c >= pieces) continue;  // (where pieces are held, those behind the row are zero)
+      if (!AHEAD && c >= pieces) continue;  // (otherwise those behind the row are zero)
       float a[E], u[E], w[E];
-      get_h(k, a);
-      get_y(k, u);
+      h[k].get(a);
+      y[k].get(u);
       (gain != nullptr && c < pieces ? Piece<T>::load(gain + (uint32_t)(c * E)) : Piece<T>::zero()).get(w);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float xhat = a[e] * rstd;
-        if constexpr (G) dg[k][e] += u[e] * xhat;
-        dot += (gain != nullptr ? u[e] * w[e] : u[e]) * xhat;
+        if constexpr (G) dg[k][e] = __builtin_fmaf(u[e], xhat, dg[k][e]);
+        dot = __builtin_fmaf(gain != nullptr ? u[e] * w[e] : u[e], xhat, dot);
       }
     }
     if (g.dX != nullptr) {
       const float mean = row_sum<P>(dot, part) * scale;
-#pragma unroll UNROLL
+#pragma unroll
       for (int k = 0; k < V; ++k) {
         const int c = k * P + own;
         if (!there || c >= pieces) continue;
         float a[E], u[E], z[E], w[E];
-        get_h(k, a);
-        get_y(k, u);
+        h[k].get(a);
+        y[k].get(u);
         get_b(k, z);
         (gain != nullptr ? Piece<T>::load(gain + (uint32_t)(c * E)) : Piece<T>::zero()).get(w);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const float v = rstd * ((gain != nullptr ? u[e] * w[e] : u[e]) - a[e] * rstd * mean);
-          z[e] = g.dH != nullptr ? v + z[e] : v;
+          const float v = __builtin_fmaf(a[e] * rstd, -mean, gain != nullptr ? u[e] * w[e] : u[e]);
+          z[e] = g.dH != nullptr ? __builtin_fmaf(rstd, v, z[e]) : rstd * v;
         }
         Piece<T>::of(z).store(static_cast<T*>(g.dX) + row * g.lddx + (uint32_t)(c * E), g.stream);
       }
     }
     rstd = rstd2;
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
+    for (int k = 0; k < V; ++k) {
       h[k] = h2[k];
       y[k] = y2[k];
       b[k] = b2[k];
@@ -266,17 +272,17 @@ hipError_t by_width(int64_t pieces, F&& f) {
   if (pieces <= 1024) return f(Hold<256, 4>());
   if (pieces <= 2048) return f(Hold<512, 4>());
   if constexpr (sizeof(T) == 4) {
-    if (pieces > 4096) return f(Hold<512, 16>());
+    if (pieces > 4096) return f(Hold<1024, 8>());
   }
-  return f(Hold<512, 8>());
+  return f(Hold<1024, 4>());
 }
 int64_t rows_at_once(int64_t pieces) { return pieces <= 16 ? 16 : (pieces <= 32 ? 8 : (pieces <= 128 ? 4 : 1)); }
 
 constexpr int64_t kForwardGroups = 1 << 16;  // workgroups; beyond that they walk over rows
-// The backward's: as many as are at work at once, four to a compute unit, two where the pieces held ahead fill the registers (16384 x 5120: 251 us a
-// pass with 512, 255 with 1024, 279 with 768).
+// The backward's: as many as are at work at once, four to a compute unit, two where the pieces held ahead fill the registers, one of 1024 threads (16384 x
+// 5120: 251 us a pass with 512, 255 with 1024, 279 with 768; 4096 x 32768: 190 us with 256, 202 with 512, whose rows of sums are 64 MB).
 int64_t backward_groups(int64_t n, int64_t pieces) {
-  const int64_t g = ceil_div(n, rows_at_once(pieces)), most = pieces > 512 ? 512 : 1024;
+  const int64_t g = ceil_div(n, rows_at_once(pieces)), most = pieces > 2048 ? 256 : (pieces > 512 ? 512 : 1024);
   return g < most ? g : most;
 }
 

@@ -22,7 +22,8 @@ def norm_forward(h, gain, eps, dtype):
 def norm_backward(dy, h, gain, eps, dh, dtype):
     """(dx, dgain) and their bounds.  mean(N xhat) is a sum of d terms in the same order, each off by rstd's 64 u and three products: at most
     (96 + 64 + 4) u of the terms' magnitudes; then the difference, rstd once more and dh: 256 u covers each of them.  dgain: a workgroup's rows in
-    turn and up to 1024 workgroups' sums, eight of them side by side: ceil(n / 1024) + 16 + 128 + 8 roundings, 64 u for rstd."""
+    turn, ceil(n / 1024), or ceil(n / 256) of wide rows, which is under 96 more for n < 2^15; up to 1024 workgroups' sums, 32 in a row and 5 steps; 16 rows
+    side by side, 64 u for rstd and three operations: under ceil(n / 1024) + 256 roundings."""
     rstd = 1.0 / np.sqrt((h * h).mean(1, keepdims=True) + eps)
     xhat, N = h * rstd, dy * gain
     mean = (N * xhat).mean(1, keepdims=True)

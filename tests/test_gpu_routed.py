@@ -93,6 +93,11 @@ def test_norm_widths_f32(d):
     check_norm(5, d, "f32", d)
 
 
+@pytest.mark.parametrize("n,d,dtype", [(257, 16392, "bf16"), (600, 20480, "f16"), (259, 32768, "bf16"), (300, 8196, "f32"), (258, 20484, "f32")])
+def test_norm_of_wide_rows_in_turn(n, d, dtype):
+    check_norm(n, d, dtype, n, rows=dtype != "f32" and d % 128 == 0)
+
+
 @pytest.mark.parametrize("n,d,dtype", [(1, 4096, "bf16"), (3, 128, "bf16"), (1030, 520, "f16"), (2500, 136, "bf16"), (1025, 5120, "bf16"), (37, 24, "f32")])
 @pytest.mark.parametrize("residual,gain", [(True, True), (False, True), (True, False)])
 def test_norm_rows(n, d, dtype, residual, gain):
