@@ -359,14 +359,13 @@ class Route:
     def __init__(self, experts, top, score="softmax", renormalise=True, groups=1, groups_kept=None, group_top=1, scale=1.0):
         if score not in SCORES:
             raise ValueError(f"score must be one of {SCORES}")
-        if not scale:
-            raise ValueError("scale must not be zero")
+        if not 0 < abs(ctypes.c_float(scale).value) < float("inf"):
+            raise ValueError("scale must be finite and not zero, in 32 bits")
         self.experts, self.top, self.score, self.renormalise = experts, top, score, bool(renormalise)
         self.groups, self.groups_kept, self.group_top, self.scale = groups, groups if groups_kept is None else groups_kept, group_top, float(scale)
         for name in ("experts", "top", "groups", "groups_kept", "group_top"):
-            if getattr(self, name) < 1:
-                raise ValueError(f"{name} must be at least 1")
-
+            if not 1 <= getattr(self, name) < 1 << 31:
+                raise ValueError(f"{name} must be at least 1, in 32 bits")
         # the whole numbers of rl_route_t in their order
         self.how = (self.experts, self.top, SCORES.index(self.score), int(self.renormalise), self.groups, self.groups_kept, self.group_top)
 

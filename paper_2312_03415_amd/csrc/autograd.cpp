@@ -28,6 +28,7 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/csrc/utils/pybind.h>
@@ -447,7 +448,17 @@ at::Tensor matrix(const at::Tensor& t, int64_t cols) {
   if (t.dim() == 2 && t.size(1) == cols && t.stride(1) == 1 && t.stride(0) % 8 == 0 && t.stride(0) >= cols && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0) return t;
   return rows(t, cols);
 }
-at::Tensor in_shape(const at::Tensor& t, at::IntArrayRef sizes) { return t.sizes() == sizes ? t : t.view(sizes); }
+// a dense tensor of any shape whose last dimension is `cols`, as a matrix
+rl_tensor_t dense_desc(const at::Tensor& t, int64_t n, int64_t cols, int code) { return rl_tensor_t{t.data_ptr(), n, cols, cols, code, nullptr, 0}; }
+
+// What a backward returns: where a graph of it is asked for, tensors whose own backward refuses (the library has no second derivatives).
+torch::autograd::variable_list once(torch::autograd::variable_list list) {
+  if (!at::GradMode::is_enabled()) return list;
+  for (at::Tensor& t : list)
+    if (t.defined()) t = t.detach().requires_grad_(true);
+  const int64_t count = (int64_t)list.size();
+  return (*std::make_shared<torch::autograd::DelayedError>("this gradient has no derivative: the operator can be differentiated once", count))(std::move(list));
+}
 
 // y, h where there is a residual, and y's rows in 8 bits (bytes and scales) where they are asked for
 struct NormNode : public torch::autograd::Function<NormNode> {
@@ -457,7 +468,7 @@ struct NormNode : public torch::autograd::Function<NormNode> {
     const int64_t d = x.size(-1);
     const at::Tensor x2 = matrix(x, d), r2 = residual.has_value() ? matrix(*residual, d) : at::Tensor();
     const int64_t n = x2.size(0);
-    const at::Tensor y = at::empty({n, d}, x.options()), h = residual.has_value() ? at::empty({n, d}, x.options()) : x2;
+    const at::Tensor y = at::empty(x.sizes(), x.options()), h = residual.has_value() ? at::empty(x.sizes(), x.options()) : x2;
     const at::Tensor rstd = at::empty({n}, x.options().dtype(at::kFloat));
     at::Tensor q, qs;
     rl_tensor_t tq{};
@@ -468,7 +479,7 @@ struct NormNode : public torch::autograd::Function<NormNode> {
       tq = rl_tensor_t{q.data_ptr(), n, d, blocks * 128, RL_FP8_R128, qs.data_ptr(), 128};
     }
     const rl_tensor_t tx = desc(x2, code), tr = residual.has_value() ? desc(r2, code) : rl_tensor_t{};
-    rl_tensor_t ty = desc(y, code), th = desc(h, code);
+    rl_tensor_t ty = dense_desc(y, n, d, code), th = dense_desc(h, n, d, code);  // (th: of a residual's h alone)
     rl_opts_t opts{};
     opts.stream = c10::hip::getCurrentHIPStream(x.device().index()).stream();
     check(p_rmsnorm_forward(&tx, residual.has_value() ? &tr : nullptr, gain.has_value() ? gain->data_ptr() : nullptr, (float)eps, &ty,
@@ -478,8 +489,8 @@ struct NormNode : public torch::autograd::Function<NormNode> {
     ctx->saved_data["residual"] = residual.has_value();
     ctx->saved_data["gain"] = gain.has_value();
     ctx->set_materialize_grads(false);
-    torch::autograd::variable_list out{in_shape(y, x.sizes())};
-    if (residual.has_value()) out.push_back(in_shape(h, x.sizes()));
+    torch::autograd::variable_list out{y};
+    if (residual.has_value()) out.push_back(h);
     if (bytes) {
       ctx->mark_non_differentiable({q, qs});
       out.push_back(q);
@@ -494,7 +505,7 @@ struct NormNode : public torch::autograd::Function<NormNode> {
     // (edges are those of the tensors that there are)
     const bool need_x = ctx->needs_input_grad(0), need_gain = gain && ctx->needs_input_grad(1), need_r = residual && ctx->needs_input_grad(gain ? 2 : 1);
     const at::Tensor none, dh = residual && grads.size() > 1 ? grads[1] : none;
-    if (!grads[0].defined()) return {need_x ? dh : none, none, need_r ? dh : none, none, none};
+    if (!grads[0].defined()) return {need_x ? dh : none, none, need_r ? dh : none, none, none};  // (as it came, graph and all)
     TORCH_CHECK_VALUE(vars[0].is_cuda(), "the saved input came back on ", vars[0].device());
     const int64_t d = vars[0].size(-1);
     const at::Tensor h2 = matrix(vars[0], d);
@@ -506,7 +517,7 @@ struct NormNode : public torch::autograd::Function<NormNode> {
     const void* const w = gain ? saved_vec(vars[1], d, dy2.scalar_type(), h2, "gain") : nullptr;
     at::Tensor dx, dw;
     rl_tensor_t tx{};
-    if (need_x || need_r) { dx = at::empty({n, d}, h2.options()); tx = desc(dx, code); }
+    if (need_x || need_r) { dx = at::empty(ctx->saved_data["x_shape"].toIntVector(), h2.options()); tx = dense_desc(dx, n, d, code); }
     if (need_gain) dw = at::empty({d}, h2.options());
     const at::Tensor ws = need_gain ? scratch(p_rmsnorm_workspace_bytes(n, d, code), h2) : none;
     rl_opts_t opts{};
@@ -517,8 +528,7 @@ struct NormNode : public torch::autograd::Function<NormNode> {
     }
     const rl_tensor_t ty = desc(dy2, dtype_code(dy2.scalar_type())), tg = dh.defined() ? desc(dh2, dtype_code(dh2.scalar_type())) : rl_tensor_t{}, th = desc(h2, code);
     check(p_rmsnorm_backward(&ty, dh.defined() ? &tg : nullptr, &th, w, rstd, dx.defined() ? &tx : nullptr, need_gain ? dw.data_ptr() : nullptr, &opts));
-    if (dx.defined()) dx = in_shape(dx, ctx->saved_data["x_shape"].toIntVector());
-    return {need_x ? dx : none, dw, need_r ? dx : none, none, none};
+    return once({need_x ? dx : none, dw, need_r ? dx : none, none, none});
   }
 };
 
@@ -578,7 +588,7 @@ struct RouteNode : public torch::autograd::Function<RouteNode> {
     opts.stream = c10::hip::getCurrentHIPStream(logits.device().index()).stream();
     const rl_route_t route = plan(how, ctx->saved_data["scale"].toDouble(), bias);
     check(p_route_backward(&tl, &route, expert, saved_table<float>(dw, {tl.rows, how[1]}, at::kFloat, logits, "dweight"), &td, &opts));
-    return {dl, none, none, none};
+    return once({dl, none, none, none});
   }
 };
 
@@ -604,14 +614,14 @@ struct GatherNode : public torch::autograd::Function<GatherNode> {
     const at::Tensor dr = matrix(grads[0], grads[0].size(-1));
     const int code = dtype_code(dr.scalar_type());
     TORCH_CHECK_VALUE(place.dim() == 2 && place.numel() == dr.size(0), "place came back as another table");
-    const at::Tensor dx = at::empty({place.size(0), dr.size(1)}, dr.options());
+    const at::Tensor dx = at::empty(ctx->saved_data["x_shape"].toIntVector(), dr.options());
     const rl_tensor_t tr = desc(dr, code);
-    rl_tensor_t tx = desc(dx, code);
+    rl_tensor_t tx = dense_desc(dx, place.size(0), dr.size(1), code);
     rl_opts_t opts{};
     opts.stream = c10::hip::getCurrentHIPStream(dr.device().index()).stream();
     check(p_gather_backward(&tr, saved_table<int32_t>(place, place.sizes(), at::kInt, dr, "place"), (int)place.size(1), &tx, &opts));
     at::Tensor none;
-    return {in_shape(dx, ctx->saved_data["x_shape"].toIntVector()), none, none};
+    return once({dx, none, none});
   }
 };
 
@@ -621,15 +631,15 @@ struct CombineNode : public torch::autograd::Function<CombineNode> {
     const int code = dtype_code(back.scalar_type());
     const int64_t n = place.size(0), d = back.size(-1);
     const at::Tensor r2 = matrix(back, d), w = weight.contiguous(), a2 = add.has_value() ? matrix(*add, d) : at::Tensor();
-    at::Tensor y = at::empty({n, d}, back.options());
+    const at::Tensor y = at::empty(add.has_value() ? add->sizes() : at::IntArrayRef({n, d}), back.options());
     const rl_tensor_t tr = desc(r2, code), ta = add.has_value() ? desc(a2, code) : rl_tensor_t{};
-    rl_tensor_t ty = desc(y, code);
+    rl_tensor_t ty = dense_desc(y, n, d, code);
     rl_opts_t opts{};
     opts.stream = c10::hip::getCurrentHIPStream(back.device().index()).stream();
     check(p_combine_forward(&tr, place.data_ptr<int32_t>(), w.data_ptr<float>(), (int)place.size(1), add.has_value() ? &ta : nullptr, &ty, &opts));
     ctx->save_for_backward({r2, place, source, w});
     ctx->saved_data["add"] = add.has_value();
-    return add.has_value() ? in_shape(y, add->sizes()) : y;
+    return y;
   }
 
   static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
@@ -655,7 +665,9 @@ struct CombineNode : public torch::autograd::Function<CombineNode> {
                                saved_table<int32_t>(vars[2], {place.numel()}, at::kInt, r2, "source"), saved_table<float>(w, place.sizes(), at::kFloat, r2, "weight"),
                                (int)place.size(1), need_r ? &tr : nullptr, need_w ? dw.data_ptr<float>() : nullptr, &opts));
     }
-    return {dr, dw, none, none, need_a ? grads[0] : none};
+    auto out = once({dr, dw, none, none, none});
+    if (need_a) out[4] = grads[0];
+    return out;
   }
 };
 

@@ -25,6 +25,7 @@ import math
 
 import torch
 from torch import nn
+from torch.autograd.function import once_differentiable
 
 from . import binding as rl
 
@@ -601,22 +602,23 @@ class RunRMSNormFunction(torch.autograd.Function):
         if residual is not None and (residual.shape != x.shape or residual.dtype != x.dtype):
             raise ValueError("the residual must have x's shape and type")
         r2 = None if residual is None else _rows(residual, d)
-        y = torch.empty((n, d), dtype=x.dtype, device=x.device)
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         h = x2 if residual is None else torch.empty_like(y)
         rstd = torch.empty((n,), dtype=torch.float32, device=x.device)
         q = rl.Fp8Rows.empty(n, d, x.device) if rows else None
         if n > 0:
-            rl.runlora_rmsnorm_forward(x2, gain, y, eps, r2, None if residual is None else h, rstd, q)
+            rl.runlora_rmsnorm_forward(x2, gain, y.view(n, d), eps, r2, None if residual is None else h.view(n, d), rstd, q)
         ctx.x_shape, ctx.residual = x.shape, residual is not None
         ctx.save_for_backward(h, gain, rstd)
         ctx.set_materialize_grads(False)
-        out = (y.view(x.shape),) + (() if residual is None else (h.view(x.shape),))
+        out = (y,) if residual is None else (y, h)
         if rows:
             ctx.mark_non_differentiable(q.data, q.scales)
             out += (q.data, q.scales)
         return out if len(out) > 1 else out[0]
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dh=None, *_):
         h, gain, rstd = ctx.saved_tensors
         if not ctx.residual:
@@ -687,6 +689,7 @@ class RunRouteFunction(torch.autograd.Function):
         return weight, expert, place, source, ends
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dweight, *_):
         if dweight is None:
             return None, None, None
@@ -738,6 +741,7 @@ class RunGatherFunction(torch.autograd.Function):
         return rows
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, drows):
         place, = ctx.saved_tensors
         d = ctx.x_shape[-1]
@@ -764,15 +768,15 @@ class RunCombineFunction(torch.autograd.Function):
         n, d = place.shape[0], r2.shape[1]
         if add is not None and (add.shape[-1] != d or add.dtype != rows.dtype or add.numel() != n * d):
             raise ValueError("add must have one row a token, of the rows' type")
-        y = torch.empty((n, d), dtype=rows.dtype, device=rows.device)
+        y = torch.empty((n, d) if add is None else add.shape, dtype=rows.dtype, device=rows.device)
         weight = weight.contiguous()
         if n > 0:
-            rl.runlora_combine_forward(r2, place, weight, y, None if add is None else _rows(add, d))
-        ctx.add_shape = None if add is None else add.shape
+            rl.runlora_combine_forward(r2, place, weight, y.view(n, d), None if add is None else _rows(add, d))
         ctx.save_for_backward(r2, place, source, weight)
-        return y if add is None else y.view(add.shape)
+        return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         rows, place, source, weight = ctx.saved_tensors
         need = ctx.needs_input_grad

@@ -1,5 +1,6 @@
 """What stands between the layers of a block with routed experts, on the GPU against the float64 reference of routed_oracle.py: routing, rows to the
 experts and back, root-mean-square norms with the residual and 8-bit rows, and all of them together."""
+import contextlib
 import math
 
 import numpy as np
@@ -11,6 +12,7 @@ from helpers import to_f64, torch_dtype
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
+from torch.overrides import TorchFunctionMode  # noqa: E402
 
 
 def _rl():
@@ -748,15 +750,60 @@ def test_captured_training_pass():
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
 
 
-def test_python_nodes_give_the_native_ones_bits():
-    """A torch function mode sends the calls to the Python nodes."""
-    from torch.overrides import TorchFunctionMode
+class Watching(TorchFunctionMode):
+    """A torch function mode: it sends calls to the Python nodes."""
+
+    def __torch_function__(self, func, types, args=(), kwargs=None):
+        return func(*args, **(kwargs or {}))
+
+
+def every_node(n=14, d=72, E=6, top=2):
+    """(outputs, leaves) of one call of each node, 3-D where it may be."""
     from paper_2312_03415_amd import module as m
+    g = gen(12)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    bf = torch.bfloat16
+    x, r, gain, l = [t.requires_grad_(True) for t in (randn(2, n // 2, d).to(bf), randn(2, n // 2, d).to(bf), randn(d).to(bf), randn(n, E))]
+    y, h = m.RunRMSNormFunction.apply(x, gain, 1e-5, r)
+    weight, expert, place, source, ends = m.RunRouteFunction.apply(l, _rl().Route(E, top))
+    rows = m.RunGatherFunction.apply(y.detach().view(n, d).requires_grad_(True), place, source)
+    out = m.RunCombineFunction.apply(rows.detach().requires_grad_(True), place, source, weight.detach().requires_grad_(True), h.detach())
+    return y, h, weight, rows, out
 
-    class Watching(TorchFunctionMode):
-        def __torch_function__(self, func, types, args=(), kwargs=None):
-            return func(*args, **(kwargs or {}))
 
+@pytest.mark.parametrize("python", [False, True])
+def test_second_derivatives_are_refused(python):
+    with Watching() if python else contextlib.nullcontext():
+        y, h, weight, rows, out = every_node()
+        for t in (y, weight, rows, out):
+            leaf = next(f[0].variable for f in t.grad_fn.next_functions if hasattr(f[0], "variable"))
+            first, = torch.autograd.grad(t.float().pow(2).sum(), leaf, retain_graph=True)
+            again, = torch.autograd.grad(t.float().pow(2).sum(), leaf, create_graph=True)
+            assert torch.equal(first, again.detach())
+            with pytest.raises(RuntimeError, match="once|twice"):
+                again.float().sum().backward()
+
+
+@pytest.mark.parametrize("python", [False, True])
+def test_outputs_may_be_changed_in_place(python):
+    """Where no gradient reads them: y and the combined rows; h is read, which autograd notices."""
+    with Watching() if python else contextlib.nullcontext():
+        y, h, weight, rows, out = every_node()
+        for t in (y, out):
+            assert not t._is_view()
+            leaf = next(f[0].variable for f in t.grad_fn.next_functions if hasattr(f[0], "variable"))
+            want, = torch.autograd.grad(t, leaf, 2 * torch.ones_like(t), retain_graph=True)
+            t.mul_(2)
+            got, = torch.autograd.grad(t, leaf, torch.ones_like(t))
+            assert torch.equal(got, want)
+        y, h, *_ = every_node()
+        h.add_(1)
+        with pytest.raises(RuntimeError, match="inplace"):
+            y.sum().backward()
+
+
+def test_python_nodes_give_the_native_ones_bits():
+    from paper_2312_03415_amd import module as m
     rl = _rl()
     n, d, E, top = 70, 144, 12, 3
     g = gen(6)

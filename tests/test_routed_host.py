@@ -311,11 +311,12 @@ def test_front_end_refuses():
         rl.runlora_combine_backward(t(4, 16), t(8, 16), t(4, 2, dtype=i32), t(8, dtype=i32), t(4, 2, dtype=f32), t(8, 16), t(4, 2, dtype=f32))
     with pytest.raises(ValueError, match="place"):
         rl.runlora_combine_forward(t(8, 16), t(5, 2, dtype=i32), t(4, 2, dtype=f32), t(4, 16))
-    for bad in (dict(score="relu"), dict(scale=0.0), dict(groups=0), dict(groups_kept=0), dict(group_top=0)):
+    for bad in (dict(score="relu"), dict(scale=0.0), dict(scale=1e-50), dict(scale=float("inf")), dict(scale=float("nan")), dict(groups=0), dict(groups_kept=0), dict(group_top=0)):
         with pytest.raises(ValueError):
             rl.Route(8, 2, **bad)
-    with pytest.raises(ValueError):
-        rl.Route(8, 0)
+    for experts, top in ((8, 0), ((1 << 32) + 8, 2), (8, (1 << 32) + 2)):
+        with pytest.raises(ValueError):
+            rl.Route(experts, top)
     for bias in (t(8), t(7, dtype=f32), t(16, dtype=f32)[::2]):
         with pytest.raises(ValueError, match="bias"):
             rl.Route(8, 2).desc(bias)
