@@ -352,7 +352,7 @@ int runlora_experts_backward(const rl_tensor_t* dY, const rl_tensor_t* X, const 
 size_t runlora_experts_workspace_bytes(int backward, int64_t n, int64_t experts, int64_t i, int64_t o, int64_t r, int dtype, int w_dtype);
 
 /*
- * Routing of n tokens to experts, in front of runlora_experts_*.  From logits l [n, E] (RL_F32 / RL_F16 / RL_BF16, any ld >= E):
+ * Routing of n tokens to experts, in front of runlora_experts_*.  From logits l [n, E] (RL_F32 / RL_F16 / RL_BF16, any ld in [E, 2^31]):
  *     s = softmax(l) over the row, or sigmoid(l);     c = s + bias
  *     groups > 1: the E experts are `groups` runs of E / groups; a run counts with the sum of its group_top (1 or 2) largest c, and only the
  *         groups_kept runs that count most take part (equal ones: the first)
@@ -397,7 +397,7 @@ size_t runlora_route_workspace_bytes(int64_t n, int64_t experts, int64_t top);
  * A copy without a place (anything outside [0, n top)) adds nothing and has a dweight of 0; rows without a copy (source negative) are written as
  * zeros.  fp32 sums in the order of j (of the columns in a fixed order), rounded once.  drows or dweight may be NULL (skipped); without dweight rows may
  * be NULL.  The gradient of `add` is dY itself.
- * RL_F32 / RL_F16 / RL_BF16; n in [1, 8388607], top in [1, 64], d a multiple of 8 (16-bit types) or 4, n * d below 2^40; weight and dweight [n, top] floats, dense.
+ * RL_F32 / RL_F16 / RL_BF16; n in [1, 8388607], top in [1, 64], d a multiple of 8 (16-bit types) or 4, n * d at most 2^39; weight and dweight [n, top] floats, dense.
  */
 int runlora_gather_forward(const rl_tensor_t* X, const int32_t* place, const int32_t* source, int top, rl_tensor_t* rows, const rl_opts_t* opts);
 int runlora_gather_backward(const rl_tensor_t* drows, const int32_t* place, int top, rl_tensor_t* dX, const rl_opts_t* opts);

@@ -583,6 +583,7 @@ int check_logits(const rl_tensor_t* t, int64_t n, int64_t experts, int dtype) {
   if (!t || !t->data) return RL_ERR_NULL;
   if (t->dtype != dtype || internal_dtype(dtype) < 0) return RL_ERR_DTYPE;
   if (t->rows != n || t->cols != experts || t->ld < t->cols) return RL_ERR_SHAPE;
+  if (n > 1 && t->ld > int64_t(1) << 31) return RL_ERR_UNSUPPORTED;  // (addresses of any n of them fit 64 bits)
   return reinterpret_cast<uintptr_t>(t->data) % dtype_size(internal_dtype(dtype)) != 0 ? RL_ERR_ALIGN : RL_OK;
 }
 

@@ -87,7 +87,7 @@ NULL, SHAPE, DTYPE, VARIANT, ALIGN, UNSUPPORTED = rl.RL_ERR_NULL, rl.RL_ERR_SHAP
 @pytest.mark.parametrize("path,value,code", [
     ("logits", None, NULL), ("route", None, NULL), ("logits.data", None, NULL), ("expert", None, NULL),
     ("logits.dtype", rl.RL_FP8_B128, DTYPE), ("logits.dtype", 42, DTYPE), ("logits.rows", 0, SHAPE), ("logits.cols", E + 1, SHAPE), ("logits.ld", E - 1, SHAPE),
-    ("logits.data", 0x100000002, ALIGN), ("logits.rows", 1 << 23, UNSUPPORTED),
+    ("logits.data", 0x100000002, ALIGN), ("logits.rows", 1 << 23, UNSUPPORTED), ("logits.ld", (1 << 31) + 1, UNSUPPORTED),
     ("route.top", 0, SHAPE), ("route.top", E + 1, SHAPE), ("route.score", 2, VARIANT), ("route.score", -1, VARIANT), ("route.groups", 5, SHAPE),
     ("route.groups", -1, SHAPE), ("route.groups_kept", 5, SHAPE), ("route.groups_kept", -1, SHAPE), ("route.group_top", 3, UNSUPPORTED),
     ("route.group_top", -1, SHAPE), ("route.experts", 0, SHAPE), ("route.bias", 0x100000001, ALIGN), ("expert", 0x100000001, ALIGN)])
