@@ -115,18 +115,40 @@ bool fast_rows(const void* p, int64_t ld, int64_t experts, int K, size_t esz) {
 // exp by the exponential of 2: off by a unit (2 u) and, through its argument, by 1.5 u |x|
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 
-// row maximum (not counting NaN; 0 where nothing is left) and sum of exp(l - max) of a row's logits, l = -inf where there is none.  (The terms are off by
-// 2 u and 2.5 u |l - max| of themselves: weighted by themselves, that is at most (2.5 ln E + 2) u of the sum.)
+// exp in 64 bits to 2^-31 of itself, which is what a weight of 32 bits needs: x = n ln 2 + r, |r| <= 0.3466, and the series of exp(r) to r^8 (the rest is
+// below r^9 / 9! = 2^-32.2).  0 far below, infinity far above.
+__device__ __forceinline__ double exp64(double x) {
+  x = x < -2000.0 ? -2000.0 : (x > 2000.0 ? 2000.0 : x);
+  const double n = __builtin_rint(x * 1.4426950408889634074), r = __builtin_fma(n, -0.69314718055994530942, x);
+  double p = 1.0 / 40320;
+  p = __builtin_fma(p, r, 1.0 / 5040);
+  p = __builtin_fma(p, r, 1.0 / 720);
+  p = __builtin_fma(p, r, 1.0 / 120);
+  p = __builtin_fma(p, r, 1.0 / 24);
+  p = __builtin_fma(p, r, 1.0 / 6);
+  p = __builtin_fma(p, r, 0.5);
+  p = __builtin_fma(p, r, 1.0);
+  p = __builtin_fma(p, r, 1.0);
+  return ldexp(p, (int)n);
+}
+
+// row maximum (not counting NaN; 0 where nothing is left) and sum of exp(l - max) of a row's logits, l = -inf where there is none.  (A term is off by
+// under 3 u of itself, with what its argument loses put back to first order, and by u |l - max| for the difference's own rounding: weighted by themselves
+// the terms are off by at most (ln E + 3) u of the sum.  In 64 bits the additions add nothing to that.)
 template <int L, int K>
-__device__ __forceinline__ void softmax_stats(const float (&l)[K], float* top, float* sum) {
+__device__ __forceinline__ void softmax_stats(const float (&l)[K], float* top, double* sum) {
   float m = kNone;
 #pragma unroll
   for (int k = 0; k < K; ++k) m = l[k] > m ? l[k] : m;
   m = lanes_max<L>(m);
   const float base = m == kNone ? 0.f : m;
-  float s = 0.f;
+  double s = 0.0;
 #pragma unroll
-  for (int k = 0; k < K; ++k) s += fast_exp(l[k] - base);
+  for (int k = 0; k < K; ++k) {
+    constexpr float log2e = 1.44269504088896341f;
+    const float x = l[k] - base, a = x * log2e, e = __builtin_amdgcn_exp2f(a);
+    s += (double)(e != 0.f ? __builtin_fmaf(e, 0.693147181f * __builtin_fmaf(x, log2e, -a), e) : e);  // (x = -inf has no rest)
+  }
   *top = base;
   *sum = lanes_sum<L>(s);
 }
@@ -417,7 +439,7 @@ inline __host__ __device__ int count_bytes(int each) { return each < 256 ? 1 : 2
 // Workgroup b takes the tokens [b each, (b + 1) each), L lanes a token with K experts each, 64 / L tokens side by side in a wave: their experts and weights,
 // and how many rows every expert gets (counts [b][experts] in the workspace).  A single workgroup places them too.
 // Bound by its instructions and, with one round of waves, by their latency (16384 x 256 in 32 bits, biased sigmoid scores, 8 groups, top 8: 16 MB, 3 us;
-// 1300 vector instructions a wave of four tokens, 9 us of them; 18 us): a maximum over 16 lanes serves four tokens at once, where one over 64 serves one
+// 1400 vector instructions a wave of four tokens, 10 us of them; 19 us): a maximum over 16 lanes serves four tokens at once, where one over 64 serves one
 // (38 us).  The scores in 64 bits for every row took 45.
 template <typename T, int L, int K, bool WIDE>
 __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route_choose_kernel(RouteDesc g, int each, int fast, int room, void* counts, int single) {
@@ -452,12 +474,13 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
     const T* const row = static_cast<const T*>(g.logits) + (there ? t : first) * g.ld;
     float l[K];
     load_row<T, K>(row, sub, g.experts, there, fast != 0, l);
-    float base = 0.f, sum = 1.f;
+    float base = 0.f;
+    double sum = 1.0;
     if (!g.sigmoid && (!g.renorm || WIDE)) softmax_stats<L, K>(l, &base, &sum);
     constexpr bool UNIQUE = !WIDE && sizeof(T) == 2;
     // one more than asked for, where there is one and a lane for it: the last of the choice has a neighbour too
     const int more = UNIQUE || g.top == g.experts ? g.top : g.top + 1;
-    const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+    const float inverse = sum == 0.0 ? 0.f : 1.f / (float)sum;
     float off = 0.f;
     bool close = false;
     uint32_t key[K], mine_key;
@@ -472,8 +495,8 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
         }
         close = odd != odd;  // (a NaN, or infinite biases: 64 bits sort them out)
         // How far two c may be off together, u = 2^-24.  sigmoid: exp is off by 2 u and, through its argument, 1.5 u |l|, of which s (1 - s) keeps under u;
-        // 1 + e and the reciprocal by 3 u s: under 2^-21 each.  softmax: exp by 2 u and 2.5 u |l - max|, of which s keeps under u max s; the sum by 21 u and
-        // by its terms' (2.5 ln 1024 + 2) u; the quotient and the product by 2 u: under 2^-18 max s each, max s = 1 / sum.  With the bias: u |c| each; the
+        // 1 + e and the reciprocal by 3 u s: under 2^-21 each.  softmax: exp by 2 u and 2.5 u |l - max|, of which s keeps under u max s; the sum by
+        // (ln 1024 + 3) u and its rounding; the quotient and the product by 2 u: under 2^-18 max s each, max s = 1 / sum.  With the bias: u |c| each; the
         // keys' lower four bits: 30 u |c|.
         const float high = g.sigmoid ? 1.f : inverse;
         off = (g.sigmoid ? 0x1p-20f : 0x1p-17f * high) + 0x1p-18f * (high + most);
@@ -530,26 +553,27 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
         logit = expert >= 0 ? (float)row[expert] : 0.f;
       }
     }
-    // weights: lane j holds choice j
+    // Weights: lane j holds choice j.  In 64 bits, rounded once: 3 10^-8 of their norm, where a chain of 32-bit operations left 8 10^-8 and took 1 us of
+    // 35 less (16384 x 256, with its gradient).
     const bool chosen = sub < g.top && expert >= 0;
-    float w = 0.f;
+    double w = 0.0;
     if (g.renorm) {
       // scores over the largest of the chosen ones: their sum is at least 1 (sigmoid: 1/2), however small they are
       const float a = g.sigmoid ? (logit < 0.f ? logit : (logit != logit ? logit : 0.f)) : logit;
       const float m = lanes_max<L>(chosen ? ranked(a) : kNone);
       if (chosen) {
-        w = expf(a - m);
-        if (g.sigmoid) w = w / (1.f + expf(-fabsf(logit)));
+        w = exp64((double)a - (double)m);
+        if (g.sigmoid) w = w / (1.0 + exp64(-fabs((double)logit)));
       }
-      const float s = lanes_sum<L>(w);
+      const double s = lanes_sum<L>(w);
       if (chosen) w = w / s;
       if (!g.sigmoid && sum != sum) w = sum;  // a NaN in the row
     } else if (chosen) {
-      w = g.sigmoid ? 1.f / (1.f + expf(-logit)) : expf(logit - base) / sum;
+      w = g.sigmoid ? 1.0 / (1.0 + exp64(-(double)logit)) : exp64((double)logit - (double)base) / sum;
     }
     if (there && sub < g.top) {
       g.expert[t * g.top + sub] = expert;
-      g.weight[t * g.top + sub] = chosen ? g.scale * w : 0.f;
+      g.weight[t * g.top + sub] = chosen ? (float)((double)g.scale * w) : 0.f;
       if (expert >= 0) atomicAdd(&count[expert], 1);
     }
   }
@@ -661,7 +685,7 @@ inline __host__ __device__ bool route_wide(const RouteDesc& g) { return g.bias !
 //     softmax over chosen:    dl_j = q_j (D_j - sum_k D_k q_k)               and zero elsewhere
 //     sigmoid:                dl_j = s_j (1 - s_j) D_j;   over the chosen: q_j (1 - s_j) (D_j - sum_k D_k q_k)
 // A row is put together in LDS, most of it zeros, and leaves as whole pieces (each lane's own K elements compared with every choice, and stored K apart:
-// 12 us for 16384 x 256 top 8 in 32 bits, 7.0 so, 17 MB written).
+// 12 us for 16384 x 256 top 8 in 32 bits, 7.6 so, 17 MB written).
 template <typename T, int L, int K>
 __global__ __launch_bounds__(256) void route_backward_kernel(RouteDesc g, int fast, int fast_out) {
   constexpr int SIDE = 64 / L;
@@ -682,7 +706,8 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteDesc g, int fa
     }
   }
   const bool chosen = expert >= 0;
-  float out[K], base = 0.f, sum = 1.f, v = 0.f;
+  float out[K], base = 0.f, v = 0.f;
+  double sum = 1.0;
 #pragma unroll
   for (int k = 0; k < K; ++k) out[k] = 0.f;
   if (!g.sigmoid && (!g.renorm || route_wide(g))) {  // (with a bias a NaN need not be among the chosen: as in the forward)
@@ -690,30 +715,32 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteDesc g, int fa
     load_row<T, K>(row, sub, g.experts, there, fast != 0, l);
     softmax_stats<L, K>(l, &base, &sum);
     if (!g.renorm) {
-      const float p = expf(logit - base) / sum, mean = lanes_sum<L>(chosen ? d * p : 0.f);
-      v = p * (d - mean);
+      const double p = exp64((double)logit - (double)base) / sum, mean = lanes_sum<L>(chosen ? (double)d * p : 0.0);
+      v = (float)(p * ((double)d - mean));
+      const float off_chosen = sum == 0.0 ? 0.f : -(float)(mean / sum);
 #pragma unroll
-      for (int k = 0; k < K; ++k) out[k] = sum == 0.f ? 0.f : -expf(l[k] - base) / sum * mean;
+      for (int k = 0; k < K; ++k) out[k] = sum == 0.0 ? 0.f : expf(l[k] - base) * off_chosen;
     }
   }
-  if (g.renorm || g.sigmoid) {
-    const float s = g.sigmoid ? 1.f / (1.f + expf(-logit)) : 1.f, left = g.sigmoid ? 1.f / (1.f + expf(logit)) : 1.f;
+  if (g.renorm || g.sigmoid) {  // (the chosen alone: in 64 bits, as the weights)
+    const double far = g.sigmoid ? exp64(-fabs((double)logit)) : 0.0;
+    double x = 0.0;
     if (g.renorm) {
       const float a = g.sigmoid ? (logit < 0.f ? logit : (logit != logit ? logit : 0.f)) : logit;
       const float m = lanes_max<L>(chosen ? ranked(a) : kNone);
-      float q = 0.f;
-      if (chosen) {
-        q = expf(a - m);
-        if (g.sigmoid) q = q / (1.f + expf(-fabsf(logit)));
-      }
-      const float all = lanes_sum<L>(q);
+      double q = 0.0;
+      if (chosen) q = exp64((double)a - (double)m) / (1.0 + far);
+      const double all = lanes_sum<L>(q);
       if (chosen) q = q / all;
-      const float mean = lanes_sum<L>(chosen ? d * q : 0.f);
-      if (chosen) v = q * left * (d - mean);
-      if (sum != sum) v = sum;
+      const double mean = lanes_sum<L>(chosen ? (double)d * q : 0.0);
+      if (chosen) x = q * ((double)d - mean);
+      if (sum != sum) x = sum;
     } else if (chosen) {
-      v = s * left * d;
+      x = (logit < 0.f ? far : 1.0) / (1.0 + far) * (double)d;
     }
+    // 1 - s
+    if (g.sigmoid && chosen) x = x * ((logit < 0.f ? 1.0 : far) / (1.0 + far));
+    v = (float)x;
   }
 #pragma unroll
   for (int k = 0; k < K; ++k) mine[sub * K + k] = out[k];
