@@ -251,6 +251,18 @@ def test_route_sizes(n, E, top):
             check_route(logits(n, E, "f32", n + E), top, "f32", score=score, renormalise=renormalise, scale=2.5)
 
 
+@pytest.mark.parametrize("n,E,top", [(300, 8, 2), (300, 60, 7), (90, 256, 8), (40, 1024, 33)])
+@pytest.mark.parametrize("score,renormalise", [("softmax", True), ("sigmoid", True), ("sigmoid", False), ("softmax", False)])
+def test_route_weights_are_rounded_once(n, E, top, score, renormalise):
+    """exp to 2^-31 of itself, at most three of them to a weight and the rest in 64 bits: u (2^-24) and 2^-28 for all else.  Softmax over the whole row: its
+    sum has terms of 3 u and u |l - max| of themselves, (ln E + 3) u of the sum."""
+    l = logits(n, E, "f32", E + top, 6.0)
+    want = ref.Routing(to_f64(l), top, score=score, renormalise=renormalise, scale=0.75)
+    weight = route_call(l, top, None, score=score, renormalise=renormalise, scale=0.75)[1][0]
+    off = ref.U + 2.0 ** -28 + (0.0 if renormalise or score == "sigmoid" else (math.log(E) + 3) * ref.U)
+    close("weight", weight, want.weight, off * np.abs(want.weight) + 2.0 ** -149)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("E,top,groups,kept,group_top", [(8, 2, 2, 1, 1), (24, 4, 8, 3, 2), (64, 6, 8, 3, 2), (120, 6, 8, 3, 1), (256, 8, 8, 4, 2), (63, 4, 21, 5, 2),
                                                          (64, 3, 64, 9, 1), (640, 8, 64, 2, 2), (1024, 20, 4, 1, 2), (512, 8, 64, 12, 2), (512, 33, 16, 9, 1), (256, 16, 32, 5, 2),
