@@ -1,9 +1,9 @@
 // Routing of tokens to experts (route.hpp): scores, choice and weights of a token's experts, and the order of the rows sorted by expert.
 //
-// The choice is decided on the logits themselves where nothing is added to the scores (they have the same order), otherwise on c = s + bias as 64 bits
-// have it: in 32 bits the two closest of a row's candidates would change places once in some 10^5 rows.  c is formed in 32 bits first, with a bound of
-// its error, and only the rows in which two neighbours of the choice (or of the groups at its border) are closer than that go through the 64-bit
-// exponentials.
+// The choice is decided on the logits themselves where nothing is added to the scores (they have the same order, and scores that round to the same number
+// would lose it), otherwise on c = s + bias as 64 bits have it: in 32 bits the two closest of a row's candidates would change places once in some 10^5
+// rows.  Groups are ranked by sums of c either way.  c is formed in 32 bits first, with a bound of its error, and only the rows in which two neighbours of
+// the choice (or of the groups at its border) are closer than that go through the 64-bit exponentials.
 #include "route.hpp"
 
 #include <type_traits>
@@ -487,6 +487,7 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
     double sum = 1.0;
     if (!g.sigmoid && (!g.renorm || WIDE)) softmax_stats<L, K>(l, &base, &sum);
     constexpr bool UNIQUE = !WIDE && sizeof(T) == 2;
+    const bool added = WIDE && g.bias != nullptr;  // chosen by c, otherwise by the logits of the groups that are left
     // one more than asked for, where there is one and a lane for it: the last of the choice has a neighbour too
     const int more = UNIQUE || g.top == g.experts ? g.top : g.top + 1;
     const float inverse = sum == 0.0 ? 0.f : 1.f / (float)sum;
@@ -517,6 +518,15 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
         const float border = keep_groups<L, K>(g, at, c, reinterpret_cast<float*>(keys) + (lane / L) * (g.groups * at.pitch), sub);
         if (WIDE && !(border > 2.f * off)) close = true;  // (sums of two)
       }
+      if constexpr (WIDE) {
+        if (!added) {  // (read again: held beside c, 16 of them do not fit the registers)
+          float again[K];
+          asm volatile("" ::: "memory");
+          load_row<T, K>(row, sub, g.experts, there, fast != 0, again);
+#pragma unroll
+          for (int k = 0; k < K; ++k) c[k] = c[k] == kNone ? kNone : ranked(again[k]);
+        }
+      }
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         if constexpr (UNIQUE) key[k] = row_key<T>(c[k], sub * K + k);
@@ -526,13 +536,13 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
     int expert = choose<L, K, UNIQUE>(more <= L ? more : L, key, sub, lane, list, &mine_key);
     float logit = expert >= 0 ? (float)row[expert] : 0.f;
     if constexpr (!UNIQUE) {
-      const float mine_b = WIDE && expert >= 0 ? bias[expert] : 0.f;
-      const float v = WIDE ? ranked((g.sigmoid ? __builtin_amdgcn_rcpf(1.f + fast_exp(-logit)) : fast_exp(logit - base) * inverse) + mine_b) : 0.f;
+      const float mine_b = added && expert >= 0 ? bias[expert] : 0.f;
+      const float v = added ? ranked((g.sigmoid ? __builtin_amdgcn_rcpf(1.f + fast_exp(-logit)) : fast_exp(logit - base) * inverse) + mine_b) : 0.f;
       const int from = (lane & ~(L - 1)) | (sub + 1 < L ? sub + 1 : sub);
       const float next = __shfl(v, from), next_l = __shfl(logit, from), next_b = __shfl(mine_b, from);
       const uint32_t next_key = (uint32_t)__shfl((int)mine_key, from);
       if (sub + 1 < more && sub + 1 < L && expert >= 0 && next_key > kLeast) {
-        const bool apart = WIDE ? v - next > off : mine_key >> 4 != next_key >> 4;
+        const bool apart = added ? v - next > off : mine_key >> 4 != next_key >> 4;
         // (equal logits with equal biases are equal in any precision; behind the last pair others may stand that are not)
         if (!apart && !(sub + 2 < more && logit == next_l && mine_b == next_b)) close = true;
       }
@@ -556,6 +566,12 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
             for (int k = 0; k < FEW; ++k) key64[k] = (double)ranked(l64[k]);
           }
           if (g.groups > 1) keep_groups<64, FEW>(g, at64, key64, reinterpret_cast<double*>(keys), lane);
+          if constexpr (WIDE) {
+            if (!added) {
+#pragma unroll
+              for (int k = 0; k < FEW; ++k) key64[k] = key64[k] == (double)kNone ? (double)kNone : (double)ranked(l64[k]);
+            }
+          }
           const int found = __shfl(choose64<64, FEW>(g.top, key64, lane, lane), sub);
           if (lane / L == r) expert = sub < g.top ? found : -1;
         }

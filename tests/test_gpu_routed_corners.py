@@ -1,0 +1,50 @@
+"""Corners of what stands between the layers of a block with routed experts, on the GPU against the float64 reference of routed_oracle.py."""
+import math
+
+import numpy as np
+import pytest
+
+import routed_oracle as ref
+from helpers import to_f64, torch_dtype
+from test_gpu_routed import check_route, gen
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+# ---- groups that count with their two best, nothing added to the scores ----------------------------------------------
+
+def alike(kind, n, E, dtype, seed):
+    """Logits whose 64-bit scores are the same number although they differ."""
+    rand = torch.rand(n, E, generator=gen(seed), device="cuda")
+    if kind == "large":         # sigmoid(38 and more) is 1
+        l = 38 + 20 * rand
+    elif kind == "small":       # exp(1e-17) is 1
+        l = (rand - 0.5) * 1e-17
+    elif kind == "neighbours":  # one step of 32 bits apart: their sigmoids differ by less than 2^-53
+        l = 30 + torch.floor(8 * rand) * 2.0 ** -19
+    else:                       # softmax: exp(-747) is below the smallest 64-bit number
+        l = 60 * rand
+        l[:, 0] = 60 + 760
+    return l.to(torch_dtype(dtype))
+
+
+@pytest.mark.parametrize("E,top,groups,kept", [(8, 1, 2, 1), (8, 2, 4, 2), (24, 4, 8, 3), (64, 6, 8, 3), (120, 6, 8, 3), (256, 8, 8, 4), (512, 33, 16, 9), (640, 64, 64, 20),
+                                               (1024, 20, 4, 2), (1023, 9, 33, 6)])
+@pytest.mark.parametrize("kind,dtype", [("large", "f32"), ("large", "bf16"), ("small", "f32"), ("neighbours", "f32"), ("far", "f32"), ("far", "f16")])
+def test_groups_by_their_two_best_choose_by_the_logits(E, top, groups, kept, kind, dtype):
+    """Nothing is added to the scores: the groups are ranked by them, the choice is that of the logits, also of those whose scores are the same number."""
+    l = alike(kind, 70, E, dtype, E + top)
+    score = "softmax" if kind == "far" else "sigmoid"
+    scores = ref.Routing(to_f64(l), top, score=score).s
+    assert len(np.unique(scores[:, 1:])) == 1 and len(torch.unique(l[:, 1:])) > 4
+    l[11, ::3] = -math.inf
+    l[12] = -math.inf
+    for renormalise in (True, False):
+        check_route(l, top, dtype, score=score, renormalise=renormalise, groups=groups, groups_kept=kept, group_top=2, scale=2.5)
+
+
+def test_groups_by_their_two_best_of_one_row():
+    l = torch.tensor([[40.0, 41, -5, -5, 0, 1, 2, 3], [0, 1, 2, 3, 40, 41, 42, 40]], device="cuda")
+    want = check_route(l, 1, "f32", score="sigmoid", groups=2, groups_kept=1, group_top=2)
+    assert want.expert.tolist() == [[1], [6]]
