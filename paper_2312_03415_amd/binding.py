@@ -354,20 +354,28 @@ class Fp8Rows:
 
 class Route:
     """How tokens are routed to experts (rl_route_t of runlora.h): `top` of `experts`, by "softmax" or "sigmoid" scores; renormalise: a token's weights
-    sum to `scale`; groups > 1: only the `groups_kept` runs of experts / groups take part whose `group_top` best scores sum to most."""
+    sum to `scale`; groups > 1: only the `groups_kept` runs of experts / groups take part whose `group_top` best scores sum to most.  A plan is not changed
+    once it is made: tables are sized, and a backward is run, by the one that the forward had."""
 
     def __init__(self, experts, top, score="softmax", renormalise=True, groups=1, groups_kept=None, group_top=1, scale=1.0):
         if score not in SCORES:
             raise ValueError(f"score must be one of {SCORES}")
         if not 0 < abs(ctypes.c_float(scale).value) < float("inf"):
             raise ValueError("scale must be finite and not zero, in 32 bits")
-        self.experts, self.top, self.score, self.renormalise = experts, top, score, bool(renormalise)
-        self.groups, self.groups_kept, self.group_top, self.scale = groups, groups if groups_kept is None else groups_kept, group_top, float(scale)
+        plan = dict(experts=experts, top=top, score=score, renormalise=bool(renormalise), groups=groups,
+                    groups_kept=groups if groups_kept is None else groups_kept, group_top=group_top, scale=float(scale))
         for name in ("experts", "top", "groups", "groups_kept", "group_top"):
-            if not 1 <= getattr(self, name) < 1 << 31:
+            if not 1 <= plan[name] < 1 << 31:
                 raise ValueError(f"{name} must be at least 1, in 32 bits")
         # the whole numbers of rl_route_t in their order
-        self.how = (self.experts, self.top, SCORES.index(self.score), int(self.renormalise), self.groups, self.groups_kept, self.group_top)
+        plan["how"] = (experts, top, SCORES.index(score), int(plan["renormalise"]), groups, plan["groups_kept"], group_top)
+        self.__dict__.update(plan)
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"a Route is not changed once it is made ({name}): make another")
+
+    def __delattr__(self, name):
+        self.__setattr__(name, None)
 
     def desc(self, bias=None):
         """rl_route_t, with the balance bias (None or float32 [experts])."""
