@@ -613,8 +613,9 @@ struct GatherNode : public torch::autograd::Function<GatherNode> {
     const c10::OptionalDeviceGuard guard(grads[0].device());
     const at::Tensor dr = matrix(grads[0], grads[0].size(-1));
     const int code = dtype_code(dr.scalar_type());
-    TORCH_CHECK_VALUE(place.dim() == 2 && place.numel() == dr.size(0), "place came back as another table");
     const at::Tensor dx = at::empty(ctx->saved_data["x_shape"].toIntVector(), dr.options());
+    // (dx has the forward's rows: a table of as many entries may have others)
+    TORCH_CHECK_VALUE(place.dim() == 2 && place.numel() == dr.size(0) && place.size(0) * dr.size(1) == dx.numel(), "place came back as another table");
     const rl_tensor_t tr = desc(dr, code);
     rl_tensor_t tx = dense_desc(dx, place.size(0), dr.size(1), code);
     rl_opts_t opts{};
