@@ -768,7 +768,9 @@ def runlora_combine_backward(dY, rows, place, source, weight, drows, dweight, st
 def runlora_rmsnorm_forward(X, gain, Y, eps=1e-6, residual=None, H=None, rstd=None, rows=None, stream=None):
     """Y = h / sqrt(mean h^2 + eps) * gain over rows of h = X + residual (None: X), rounded to X's type before it is normed.  gain: [d] or None (1);
     H: where h goes (may be X or residual), rstd: float32 [n] for a backward, rows: Fp8Rows that receive Y in 8 bits; each may be None."""
-    if stream is None and _native().norm_into(X, gain, Y, eps, residual, H, rstd, *((None, None) if rows is None else (rows.data, rows.scales))):
+    # (bytes of other columns may lie in as many blocks: the library has the message)
+    if stream is None and (rows is None or rows.cols == X.shape[-1]) and _native().norm_into(
+            X, gain, Y, eps, residual, H, rstd, *((None, None) if rows is None else (rows.data, rows.scales))):
         return Y
     import torch
     n, d = X.shape

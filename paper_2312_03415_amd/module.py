@@ -461,7 +461,7 @@ class RunLoRAFp8Function(torch.autograd.Function):
 
     @classmethod
     def apply(cls, x, W, A, B, bias, scale, rows=None):
-        if cls is RunLoRAFp8Function and isinstance(W, rl.Fp8Weight):
+        if cls is RunLoRAFp8Function and isinstance(W, rl.Fp8Weight) and (rows is None or rows.cols == W.rows):
             y = _native().experts(x, A, B, W.data, W.scales, None, bias, scale, W.cols, *(() if rows is None else (rows.data, rows.scales)))
             if y is not None:
                 return y

@@ -7,7 +7,7 @@ import pytest
 
 import routed_oracle as ref
 from helpers import to_f64, torch_dtype
-from test_gpu_routed import Watching, check_route, gen, placed
+from test_gpu_routed import Watching, _rl, check_route, gen, placed
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -65,3 +65,19 @@ def test_a_saved_table_of_another_shape_is_refused(python, shape):
             rows = m.RunGatherFunction.apply(x, place, source)
         with pytest.raises((ValueError, RuntimeError)):
             rows.sum().backward()
+
+
+def test_8bit_rows_of_another_width_are_refused():
+    """Rows of 120 columns lie in as many bytes as rows of 128, and are others."""
+    from paper_2312_03415_amd import module as m
+    rl = _rl()
+    g = gen(3)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()
+    x, W, A, B = randn(40, 128), rl.Fp8Weight.quantize(randn(128, 64)), randn(128, 8), randn(8, 64)
+    y, rows = torch.empty_like(x), rl.Fp8Rows.empty(40, 128)
+    rl.runlora_rmsnorm_forward(x, None, y, rows=rows)
+    with pytest.raises(rl.RunLoRAError):
+        rl.runlora_rmsnorm_forward(x, None, y, rows=rl.Fp8Rows(rows.data, rows.scales, 40, 120))
+    with pytest.raises(rl.RunLoRAError):
+        m.RunLoRAFp8Function.apply(y, W, A, B, None, 1.0, rl.Fp8Rows(rows.data, rows.scales, 40, 120))
+    assert torch.isfinite(m.RunLoRAFp8Function.apply(y, W, A, B, None, 1.0, rows)).all()
