@@ -721,12 +721,13 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteDesc g, int fa
   const T* const row = static_cast<const T*>(g.logits) + (there ? t : 0) * g.ld;
   float* const mine = &rows[wave][(lane / L) * (L * K)];
   int expert = -1;
-  float d = 0.f, logit = 0.f;
+  float logit = 0.f;
+  double d = 0.0;  // D: the product's 48 bits
   if (there && sub < g.top) {
     expert = g.expert[t * g.top + sub];
     if (expert >= g.experts) expert = -1;
     if (expert >= 0) {
-      d = g.scale * g.dweight[t * g.top + sub];
+      d = (double)g.scale * (double)g.dweight[t * g.top + sub];
       logit = (float)row[expert];
     }
   }
@@ -740,8 +741,8 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteDesc g, int fa
     load_row<T, K>(row, sub, g.experts, there, fast != 0, l);
     softmax_stats<L, K>(l, &base, &sum);
     if (!g.renorm) {
-      const double p = exp64((double)logit - (double)base) / sum, mean = lanes_sum<L>(chosen ? (double)d * p : 0.0);
-      v = (float)(p * ((double)d - mean));
+      const double p = exp64((double)logit - (double)base) / sum, mean = lanes_sum<L>(chosen ? d * p : 0.0);
+      v = (float)(p * (d - mean));
       const float off_chosen = sum == 0.0 ? 0.f : -(float)(mean / sum);
 #pragma unroll
       for (int k = 0; k < K; ++k) out[k] = sum == 0.0 ? 0.f : expf(l[k] - base) * off_chosen;
@@ -757,11 +758,11 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteDesc g, int fa
       if (chosen) q = exp64((double)a - (double)m) / (1.0 + far);
       const double all = lanes_sum<L>(q);
       if (chosen) q = q / all;
-      const double mean = lanes_sum<L>(chosen ? (double)d * q : 0.0);
-      if (chosen) x = q * ((double)d - mean);
+      const double mean = lanes_sum<L>(chosen ? d * q : 0.0);
+      if (chosen) x = q * (d - mean);
       if (sum != sum) x = sum;
     } else if (chosen) {
-      x = (logit < 0.f ? far : 1.0) / (1.0 + far) * (double)d;
+      x = (logit < 0.f ? far : 1.0) / (1.0 + far) * d;
     }
     // 1 - s
     if (g.sigmoid && chosen) x = x * ((logit < 0.f ? 1.0 : far) / (1.0 + far));

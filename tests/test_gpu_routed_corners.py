@@ -7,7 +7,7 @@ import pytest
 
 import routed_oracle as ref
 from helpers import to_f64, torch_dtype
-from test_gpu_routed import Watching, _rl, check_route, gen, placed
+from test_gpu_routed import Watching, _rl, check_route, close, gen, logits, nan, placed, route_call
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -49,6 +49,29 @@ def test_groups_by_their_two_best_of_one_row():
     l = torch.tensor([[40.0, 41, -5, -5, 0, 1, 2, 3], [0, 1, 2, 3, 40, 41, 42, 40]], device="cuda")
     want = check_route(l, 1, "f32", score="sigmoid", groups=2, groups_kept=1, group_top=2)
     assert want.expert.tolist() == [[1], [6]]
+
+
+# ---- one rounding ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n,E,top", [(300, 8, 2), (300, 60, 7), (90, 256, 8), (40, 1024, 33)])
+@pytest.mark.parametrize("score,renormalise", [("softmax", True), ("sigmoid", True), ("sigmoid", False)])
+def test_route_gradients_are_rounded_once(n, E, top, score, renormalise):
+    """D = scale dw holds 48 bits, exp is off by 2^-31 of itself, at most three of them to a factor: the chosen experts' gradients are off by the rounding of
+    the result, u (2^-24), and by 2^-28 of what q |D| and q sum |D q| come to before they cancel."""
+    rl = _rl()
+    l = logits(n, E, "f32", E + top, 6.0)
+    how = dict(score=score, renormalise=renormalise, scale=2.7)
+    want = ref.Routing(to_f64(l), top, **dict(how, scale=float(np.float32(2.7))))
+    plan, (weight, expert, *_) = route_call(l, top, **how)
+    dw, dl = torch.randn(n, top, generator=gen(E), device="cuda"), nan((n, E), torch.float32)
+    rl.runlora_route_backward(l, plan, expert, dw, dl)
+    D = want.scale * to_f64(dw)
+    mean = (np.abs(D) * want.q).sum(1, keepdims=True) if renormalise else 0.0
+    left = want.left if score == "sigmoid" else 1.0
+    magnitude = np.zeros((n, E))
+    np.put_along_axis(magnitude, want.expert, want.q * left * (np.abs(D) + mean), 1)
+    exact = want.backward(to_f64(dw), "f32")[0]
+    close("dlogits", dl, exact, ref.U * np.abs(exact) + 2.0 ** -28 * magnitude + 2.0 ** -149)
 
 
 # ---- operands that do not belong together ----------------------------------------------------------------------------
