@@ -80,6 +80,10 @@ __device__ __forceinline__ int here(int v) {
   asm volatile("" : "+s"(v));
   return v;
 }
+__device__ __forceinline__ int lane_here(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
 
 // Lane `sub` of the L that share a row holds the experts sub K .. sub K + K - 1, so that the lowest lane has the lowest index.  `fast`: whole rows of
 // pieces of 16 bytes, or of K elements, at aligned addresses.
@@ -102,9 +106,9 @@ __device__ __forceinline__ void load_row(const T* row, int sub, int experts, boo
       return;
     }
   }
-  const int count = here(experts);
+  const int count = here(experts), first = lane_here(sub * K);
 #pragma unroll
-  for (int k = 0; k < K; ++k) l[k] = there && sub * K + k < count ? (float)row[sub * K + k] : kNone;
+  for (int k = 0; k < K; ++k) l[k] = there && first + k < count ? (float)row[first + k] : kNone;
 }
 // (decided on the host: experts a multiple of K, and rows that start where the pieces do)
 bool fast_rows(const void* p, int64_t ld, int64_t experts, int K, size_t esz) {
@@ -117,8 +121,7 @@ __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp
 
 // exp in 64 bits to 2^-31 of itself, which is what a weight of 32 bits needs: x = n ln 2 + r, |r| <= 0.3466, and the series of exp(r) to r^8 (the rest is
 // below r^9 / 9! = 2^-32.2).  0 far below, infinity far above.
-__device__ __forceinline__ double exp64(double x) {
-  x = x < -2000.0 ? -2000.0 : (x > 2000.0 ? 2000.0 : x);
+__device__ __forceinline__ double exp64_near(double x) {  // (x within 2000 of 0)
   const double n = __builtin_rint(x * 1.4426950408889634074), r = __builtin_fma(n, -0.69314718055994530942, x);
   double p = 1.0 / 40320;
   p = __builtin_fma(p, r, 1.0 / 5040);
@@ -131,26 +134,38 @@ __device__ __forceinline__ double exp64(double x) {
   p = __builtin_fma(p, r, 1.0);
   return ldexp(p, (int)n);
 }
+__device__ __forceinline__ double exp64(double x) { return exp64_near(x < -2000.0 ? -2000.0 : (x > 2000.0 ? 2000.0 : x)); }
+// exp(l - base) of l <= base
+__device__ __forceinline__ double row_term(float l, float base) { return exp64_near(l - base < -1900.f ? -1900.0 : (double)l - (double)base); }
 
-// row maximum (not counting NaN; 0 where nothing is left) and sum of exp(l - max) of a row's logits, l = -inf where there is none.  (A term is off by
-// under 3 u of itself, with what its argument loses put back to first order, and by u |l - max| for the difference's own rounding: weighted by themselves
-// the terms are off by at most (ln E + 3) u of the sum.  In 64 bits the additions add nothing to that.)
+// row maximum (not counting NaN; 0 where nothing is left) of a row's logits, l = -inf where there is none
 template <int L, int K>
-__device__ __forceinline__ void softmax_stats(const float (&l)[K], float* top, double* sum) {
+__device__ __forceinline__ float row_base(const float (&l)[K]) {
   float m = kNone;
 #pragma unroll
   for (int k = 0; k < K; ++k) m = l[k] > m ? l[k] : m;
   m = lanes_max<L>(m);
-  const float base = m == kNone ? 0.f : m;
+  return m == kNone ? 0.f : m;
+}
+// Sum of exp(l - base).  `exact`: the weights are quotients by it, its terms have 2^-31 (us, with them / with those of 32 bits: 1999 x 120 f16 12.2 / 12.0,
+// 16384 x 256 f32 20.5 / 19.4; the error of a weight 2.5 / 3.3 10^-8).  Otherwise it serves the ranks of c alone: a term is off by under 3 u of itself, with
+// what its argument's product loses put back to first order, and by 1.23 u |l - base| for the difference's rounding and that of log2 e: weighted by
+// themselves the terms are off by at most (1.23 ln E + 3) u of the sum.  In 64 bits the additions add nothing to either.
+template <int L, int K>
+__device__ __forceinline__ double row_sum(const float (&l)[K], float base, bool exact) {
   double s = 0.0;
+  if (exact) {
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    constexpr float log2e = 1.44269504088896341f;
-    const float x = l[k] - base, a = x * log2e, e = __builtin_amdgcn_exp2f(a);
-    s += (double)(e != 0.f ? __builtin_fmaf(e, 0.693147181f * __builtin_fmaf(x, log2e, -a), e) : e);  // (x = -inf has no rest)
+    for (int k = 0; k < K; ++k) s += row_term(l[k], base);
+  } else {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      constexpr float log2e = 1.44269504088896341f;
+      const float x = l[k] - base, a = x * log2e, e = __builtin_amdgcn_exp2f(a);
+      s += (double)(e != 0.f ? __builtin_fmaf(e, 0.693147181f * __builtin_fmaf(x, log2e, -a), e) : e);  // (x = -inf has no rest)
+    }
   }
-  *top = base;
-  *sum = lanes_sum<L>(s);
+  return lanes_sum<L>(s);
 }
 
 // Which groups are kept, by the sum of their best `group_top` (1 or 2) keys: the keys outside them become -inf.  Where q = 1, 2, .. 16 lanes hold a group
@@ -185,10 +200,10 @@ __device__ __forceinline__ V keep_groups(const RouteDesc& g, const Groups& at, V
 #pragma unroll
     for (int k = 0; k < K; ++k) look(key[k]);
   } else {
-    const int inverse = here(at.inverse), experts = here(g.experts);
+    const int inverse = here(at.inverse), experts = here(g.experts), first = lane_here(sub * K);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int e = sub * K + k;
+      const int e = first + k;
       if (e < experts) scratch[e + at.of(e, inverse) * (at.pitch - at.size)] = key[k];
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -227,10 +242,10 @@ __device__ __forceinline__ V keep_groups(const RouteDesc& g, const Groups& at, V
 #pragma unroll
     for (int k = 0; k < K; ++k) key[k] = out ? (V)kNone : key[k];
   } else {
-    const int inverse = here(at.inverse);
+    const int inverse = here(at.inverse), first = lane_here(sub * K);
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (((kept >> (at.of(sub * K + k, inverse) * q & 63)) & 1) == 0) key[k] = (V)kNone;  // (behind the last expert: -inf already)
+      if (((kept >> (at.of(first + k, inverse) * q & 63)) & 1) == 0) key[k] = (V)kNone;  // (behind the last expert: -inf already)
   }
   return first_out == (V)kNone ? (V)INFINITY : last_in - first_out;
 }
@@ -485,7 +500,10 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
     load_row<T, K>(row, sub, g.experts, there, fast != 0, l);
     float base = 0.f;
     double sum = 1.0;
-    if (!g.sigmoid && (!g.renorm || WIDE)) softmax_stats<L, K>(l, &base, &sum);
+    if (!g.sigmoid && (!g.renorm || WIDE)) {
+      base = row_base<L, K>(l);
+      sum = row_sum<L, K>(l, base, !g.renorm);
+    }
     constexpr bool UNIQUE = !WIDE && sizeof(T) == 2;
     const bool added = WIDE && g.bias != nullptr;  // chosen by c, otherwise by the logits of the groups that are left
     // one more than asked for, where there is one and a lane for it: the last of the choice has a neighbour too
@@ -506,7 +524,7 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
         close = odd != odd;  // (a NaN, or infinite biases: 64 bits sort them out)
         // How far two c may be off together, u = 2^-24.  sigmoid: exp is off by 2 u and, through its argument, 1.5 u |l|, of which s (1 - s) keeps under u;
         // 1 + e and the reciprocal by 3 u s: under 2^-21 each.  softmax: exp by 2 u and 2.5 u |l - max|, of which s keeps under u max s; the sum by
-        // (ln 1024 + 3) u and its rounding; the quotient and the product by 2 u: under 2^-18 max s each, max s = 1 / sum.  With the bias: u |c| each; the
+        // (1.23 ln 1024 + 3) u and its rounding; the quotient and the product by 2 u: under 2^-18 max s each, max s = 1 / sum.  With the bias: u |c| each; the
         // keys' lower four bits: 30 u |c|.
         const float high = g.sigmoid ? 1.f : inverse;
         off = (g.sigmoid ? 0x1p-20f : 0x1p-17f * high) + 0x1p-18f * (high + most);
@@ -578,7 +596,7 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
         logit = expert >= 0 ? (float)row[expert] : 0.f;
       }
     }
-    // Weights: lane j holds choice j.  In 64 bits, rounded once: 3 10^-8 of their norm, where a chain of 32-bit operations left 8 10^-8 and took 1 us of
+    // Weights: lane j holds choice j.  In 64 bits, rounded once: 2.8 10^-8 of their norm, where a chain of 32-bit operations left 8 10^-8 and took 1 us of
     // 35 less (16384 x 256, with its gradient).
     const bool chosen = sub < g.top && expert >= 0;
     double w = 0.0;
@@ -739,13 +757,22 @@ __global__ __launch_bounds__(256) void route_backward_kernel(RouteDesc g, int fa
   if (!g.sigmoid && (!g.renorm || route_wide(g))) {  // (with a bias a NaN need not be among the chosen: as in the forward)
     float l[K];
     load_row<T, K>(row, sub, g.experts, there, fast != 0, l);
-    softmax_stats<L, K>(l, &base, &sum);
+    base = row_base<L, K>(l);
     if (!g.renorm) {
+      double e[K], s = 0.0;
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        e[k] = row_term(l[k], base);
+        s += e[k];
+      }
+      sum = lanes_sum<L>(s);
       const double p = exp64((double)logit - (double)base) / sum, mean = lanes_sum<L>(chosen ? d * p : 0.0);
       v = (float)(p * (d - mean));
-      const float off_chosen = sum == 0.0 ? 0.f : -(float)(mean / sum);
+      const double off_chosen = sum == 0.0 ? 0.0 : -mean / sum;
 #pragma unroll
-      for (int k = 0; k < K; ++k) out[k] = sum == 0.0 ? 0.f : expf(l[k] - base) * off_chosen;
+      for (int k = 0; k < K; ++k) out[k] = sum == 0.0 ? 0.f : (float)(e[k] * off_chosen);
+    } else {
+      sum = row_sum<L, K>(l, base, false);
     }
   }
   if (g.renorm || g.sigmoid) {  // (the chosen alone: in 64 bits, as the weights)

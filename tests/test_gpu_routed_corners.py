@@ -74,6 +74,31 @@ def test_route_gradients_are_rounded_once(n, E, top, score, renormalise):
     close("dlogits", dl, exact, ref.U * np.abs(exact) + 2.0 ** -28 * magnitude + 2.0 ** -149)
 
 
+@pytest.mark.parametrize("n,E,top", [(300, 8, 2), (300, 60, 7), (90, 256, 8), (40, 1024, 33)])
+def test_whole_row_softmax_is_rounded_once(n, E, top):
+    """The same where the sum is the whole row's: weights, gradients of the chosen experts and of the others, p_e sum D q.  Masked logits, and the largest and
+    lowest ones, among them."""
+    rl = _rl()
+    l = logits(n, E, "f32", E + top, 6.0)
+    l[3, 1:] = -math.inf
+    l[4, ::2] = -math.inf
+    l[5, 0] = 3e38
+    l[6] = torch.finfo(torch.float32).min
+    l[8] = -math.inf
+    how = dict(score="softmax", renormalise=False, scale=2.7)
+    want = ref.Routing(to_f64(l), top, **dict(how, scale=float(np.float32(2.7))))
+    plan, (weight, expert, *_) = route_call(l, top, **how)
+    close("weight", weight, want.weight, (ref.U + 2.0 ** -28) * np.abs(want.weight) + 2.0 ** -149)
+    dw, dl = torch.randn(n, top, generator=gen(E), device="cuda"), nan((n, E), torch.float32)
+    rl.runlora_route_backward(l, plan, expert, dw, dl)
+    D = want.scale * to_f64(dw)
+    mean = (np.abs(D) * want.q).sum(1, keepdims=True)
+    magnitude = want.s * mean
+    np.put_along_axis(magnitude, want.expert, want.q * (np.abs(D) + mean), 1)
+    exact = want.backward(to_f64(dw), "f32")[0]
+    close("dlogits", dl, exact, ref.U * np.abs(exact) + 2.0 ** -28 * magnitude + 2.0 ** -149)
+
+
 # ---- operands that do not belong together ----------------------------------------------------------------------------
 
 @pytest.mark.parametrize("python", [False, True])
