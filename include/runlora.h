@@ -367,7 +367,7 @@ size_t runlora_experts_workspace_bytes(int backward, int64_t n, int64_t experts,
  *     place [n, top]   row of token t's copy j; -1: none
  *     source [n top]   t * top + j of the copy that stands on a row; -1 behind the last expert's rows
  * runlora_route_backward: dlogits [n, E] (the type of the logits, overwritten) from the choice (`expert`, as the forward left it) and dweight.  The
- * choice itself and the bias have no gradient.
+ * choice itself and the bias have no gradient; of the bias the backward asks whether it is NULL and reads nothing.
  *   rl_route_t   zero the struct first: groups 0 means 1, groups_kept 0 all of them, group_top 0 means 1, scale 0 means 1
  *   expert, weight, place, source, ends, dweight   device pointers, dense, 4-byte aligned; all required
  *   opts         forward: workspace of runlora_route_workspace_bytes() where that is not 0

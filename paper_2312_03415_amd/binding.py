@@ -695,7 +695,8 @@ def runlora_route_forward(logits, route, weight, expert, place, source, ends, bi
 
 
 def runlora_route_backward(logits, route, expert, dweight, dlogits, bias=None, stream=None):
-    """Gradient of the logits from dweight (float32 [n, top]) and the choice that the forward left in `expert`; bias as in the forward."""
+    """Gradient of the logits from dweight (float32 [n, top]) and the choice that the forward left in `expert`; bias as in the forward (its
+    values are not read)."""
     import torch
     n, top = logits.shape[0], route.top
     _one_gpu(logits, expert, dweight, dlogits, bias)

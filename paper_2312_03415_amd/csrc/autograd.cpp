@@ -564,7 +564,9 @@ struct RouteNode : public torch::autograd::Function<RouteNode> {
     const rl_route_t route = plan(how, scale, bias.has_value() ? *bias : at::Tensor());
     check(p_route_forward(&tl, &route, expert.data_ptr<int32_t>(), weight.data_ptr<float>(), place.data_ptr<int32_t>(), source.data_ptr<int32_t>(),
                           ends.data_ptr<int32_t>(), &opts));
-    ctx->save_for_backward({logits, expert, bias.has_value() ? *bias : at::Tensor()});
+    ctx->save_for_backward({logits, expert});
+    // (the backward asks whether there is one and reads none of it: it may be updated in place before that)
+    if (bias.has_value()) ctx->saved_data["bias"] = bias->detach();
     ctx->saved_data["how"] = how;
     ctx->saved_data["scale"] = scale;
     ctx->set_materialize_grads(false);  // (zeros for the four tables would be four launches)
@@ -574,14 +576,15 @@ struct RouteNode : public torch::autograd::Function<RouteNode> {
 
   static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
     const auto vars = ctx->get_saved_variables();
-    const at::Tensor &logits = vars[0], &bias = vars[2];
+    const at::Tensor& logits = vars[0];
+    const auto kept = ctx->saved_data.find("bias");
+    const at::Tensor bias = kept != ctx->saved_data.end() ? kept->second.toTensor() : at::Tensor();
     const std::vector<int64_t> how = ctx->saved_data["how"].toIntVector();
     at::Tensor none;
     if (!grads[0].defined()) return {none, none, none, none};
     const rl_tensor_t tl = logits_desc(logits);
     const c10::OptionalDeviceGuard guard(logits.device());
     const int32_t* const expert = saved_table<int32_t>(vars[1], {tl.rows, how[1]}, at::kInt, logits, "expert");
-    if (bias.defined()) saved_table<float>(bias, {how[0]}, at::kFloat, logits, "bias");
     const at::Tensor dw = grads[0].contiguous(), dl = at::empty({tl.rows, tl.cols}, logits.options());
     rl_tensor_t td = logits_desc(dl);
     rl_opts_t opts{};

@@ -682,8 +682,8 @@ class RunRouteFunction(torch.autograd.Function):
             rl.runlora_route_forward(l2, route, weight, expert, place, source, ends, bias, ws)
         else:
             ends.zero_()
-        ctx.route = route
-        ctx.save_for_backward(l2, expert, bias)
+        ctx.route, ctx.bias = route, bias  # (the backward asks whether there is a bias and reads none of it: it may be updated in place before that)
+        ctx.save_for_backward(l2, expert)
         ctx.mark_non_differentiable(expert, place, source, ends)
         ctx.set_materialize_grads(False)
         return weight, expert, place, source, ends
@@ -693,10 +693,10 @@ class RunRouteFunction(torch.autograd.Function):
     def backward(ctx, dweight, *_):
         if dweight is None:
             return None, None, None
-        logits, expert, bias = ctx.saved_tensors
+        logits, expert = ctx.saved_tensors
         dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
         if logits.shape[0] > 0:
-            rl.runlora_route_backward(logits, ctx.route, expert, dweight.contiguous(), dlogits, bias)
+            rl.runlora_route_backward(logits, ctx.route, expert, dweight.contiguous(), dlogits, ctx.bias)
         return dlogits, None, None
 
 

@@ -99,6 +99,32 @@ def test_whole_row_softmax_is_rounded_once(n, E, top):
     close("dlogits", dl, exact, ref.U * np.abs(exact) + 2.0 ** -28 * magnitude + 2.0 ** -149)
 
 
+# ---- the balance bias ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("python", [False, True])
+@pytest.mark.parametrize("score,renormalise", [("softmax", True), ("softmax", False), ("sigmoid", True)])
+def test_bias_may_be_updated_before_the_backward(python, score, renormalise):
+    """The bias decides the choice, which the forward keeps: an update between the two leaves the gradient's bits, of a row with a NaN too."""
+    from paper_2312_03415_amd.module import RunRouter
+    route = RunRouter(24, 4, score, renormalise, balance=True)
+    l0 = logits(33, 24, "f32", 5)
+    l0[7, 3] = float("nan")
+    dw = torch.randn(33, 4, generator=gen(6), device="cuda")
+
+    def run(update):
+        l = l0.clone().requires_grad_(True)
+        weight = route(l)[0]
+        if update:
+            route.bias.add_(torch.randn(24, generator=gen(7), device="cuda"))
+        return torch.autograd.grad(weight, l, dw)[0]
+
+    with Watching() if python else contextlib.nullcontext():
+        want = run(False)
+        got = run(True)
+    assert torch.isnan(want[7]).any() and torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
+
+
 # ---- operands that do not belong together ----------------------------------------------------------------------------
 
 @pytest.mark.parametrize("python", [False, True])
