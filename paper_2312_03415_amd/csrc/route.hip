@@ -168,9 +168,17 @@ __device__ __forceinline__ double row_sum(const float (&l)[K], float base, bool 
   return lanes_sum<L>(s);
 }
 
+// How far c = s + bias in 32 bits may be off, u = 2^-24: `one` for the score, u |c| for the sum and 30 u |c| for its key's lower four bits.  (By its own
+// magnitude: an expert that a bias of -10^9 takes out says nothing about the others.)  As a number, so that infinities stay apart from the rest.
+__device__ __forceinline__ float off_by(float one, float c) {
+  const float off = __builtin_fmaf(0x1p-19f, fabsf(c), one);
+  return off < 3.4028234e38f ? off : 3.4028234e38f;
+}
+
 // Which groups are kept, by the sum of their best `group_top` (1 or 2) keys: the keys outside them become -inf.  Where q = 1, 2, .. 16 lanes hold a group
 // each looks through its own keys; otherwise a row's keys go through LDS, q lanes to a group whatever its size (groups lie an odd number of q words apart
-// there: banks).  Returns the distance between the last group kept and the next.  All lanes of the wave take part.
+// there: banks).  BOUND: returns whether what the keys are off by (one: a score, see off_by) can change nothing about it: every sum that is kept is above
+// every other by more than both are off by.  All lanes of the wave take part.
 struct Groups {
   int size, q, pitch = 0, inverse = 0;
   bool own;
@@ -187,8 +195,8 @@ struct Groups {
   // e / size: e <= 1023
   __device__ __forceinline__ static int of(int e, int inverse) { return (int)(__umul24((unsigned)e, (unsigned)inverse) >> 21); }
 };
-template <int L, int K, typename V>
-__device__ __forceinline__ V keep_groups(const RouteDesc& g, const Groups& at, V (&key)[K], V* scratch, int sub) {
+template <int L, int K, bool BOUND, typename V>
+__device__ __forceinline__ bool keep_groups(const RouteDesc& g, const Groups& at, V (&key)[K], V* scratch, int sub, float one = 0.f) {
   const int q = at.q, group = sub / q;
   V a = (V)kNone, b = (V)kNone;  // best and second best
   auto look = [&](V v) {
@@ -222,7 +230,8 @@ __device__ __forceinline__ V keep_groups(const RouteDesc& g, const Groups& at, V
   if (q > 2) { const V a2 = across<2>(a), b2 = across<2>(b); merge(a2, b2); }
   if (q > 4) { const V a2 = across<4>(a), b2 = across<4>(b); merge(a2, b2); }
   if (q > 8) { const V a2 = across<8>(a), b2 = across<8>(b); merge(a2, b2); }
-  const V rank = g.group_top > 1 && b != (V)kNone ? a + b : a;
+  const bool two = g.group_top > 1 && b != (V)kNone;
+  const V rank = two ? a + b : a;
   int before = 0;
   for (int o = 0; o < g.groups; ++o) {
     const V r = from_lane<L>(rank, o * q);
@@ -234,9 +243,15 @@ __device__ __forceinline__ V keep_groups(const RouteDesc& g, const Groups& at, V
     if constexpr (L < 64) m = (m >> (threadIdx.x & 63 & ~(L - 1))) & ((1ull << L) - 1);
     return m;
   };
-  const uint64_t kept = mine(real && before < g.kept), last = mine(real && before == g.kept - 1), next = mine(real && before == g.kept);
-  // (every place is taken once, and a limited choice leaves a group out: both are there; a group that has nothing to choose is no neighbour)
-  const V first_out = from_lane<L>(rank, __builtin_ctzll(next | 1ull << (L - 1))), last_in = from_lane<L>(rank, __builtin_ctzll(last | 1ull << (L - 1)));
+  const uint64_t kept = mine(real && before < g.kept);
+  bool sure = true;
+  if constexpr (BOUND) {
+    // (a group that has nothing to choose is no neighbour)
+    const float off = off_by(one, a) + (two ? off_by(one, b) : 0.f);
+    const bool counts = real && rank != kNone;
+    const float low = -lanes_max<L>(counts && before < g.kept ? off - rank : kNone), high = lanes_max<L>(counts && before >= g.kept ? rank + off : kNone);
+    sure = low > high;
+  }
   if (at.own) {
     const bool out = ((kept >> (group * q & 63)) & 1) == 0;
 #pragma unroll
@@ -247,7 +262,7 @@ __device__ __forceinline__ V keep_groups(const RouteDesc& g, const Groups& at, V
     for (int k = 0; k < K; ++k)
       if (((kept >> (at.of(first + k, inverse) * q & 63)) & 1) == 0) key[k] = (V)kNone;  // (behind the last expert: -inf already)
   }
-  return first_out == (V)kNone ? (V)INFINITY : last_in - first_out;
+  return sure;
 }
 
 // Keys of one word that no two experts of a lane (K <= 16) share: bits whose order as whole numbers is that of the values (no NaN, no -0), the upper 28 of
@@ -478,18 +493,10 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
   char* const keys = rest + (size_t)wave * room;
   int* const list = reinterpret_cast<int*>(keys);
   for (int k = threadIdx.x; k < g.experts; k += blockDim.x) count[k] = 0;
-  float most = 0.f;  // the largest magnitude of a finite bias
   if constexpr (WIDE) {
     for (int k = threadIdx.x; k < (L * K > 64 ? L * K : 64); k += blockDim.x) bias[k] = g.bias != nullptr && k < g.experts ? g.bias[k] : 0.f;
   }
   __syncthreads();
-  if constexpr (WIDE) {
-    for (int k = lane; k < g.experts; k += 64) {
-      const float a = fabsf(bias[k]);
-      most = a < INFINITY && a > most ? a : most;
-    }
-    most = lanes_max<64>(most);
-  }
   const Groups at(g, L, K);
   const int64_t first = (int64_t)blockIdx.x * each, last = first + each < g.n ? first + each : g.n;
   for (int64_t t0 = first + wave * SIDE; t0 < last; t0 += waves * SIDE) {
@@ -509,7 +516,7 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
     // one more than asked for, where there is one and a lane for it: the last of the choice has a neighbour too
     const int more = UNIQUE || g.top == g.experts ? g.top : g.top + 1;
     const float inverse = sum == 0.0 ? 0.f : 1.f / (float)sum;
-    float off = 0.f;
+    float one = 0.f;
     bool close = false;
     uint32_t key[K], mine_key;
     {
@@ -522,19 +529,16 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
           odd += s;
         }
         close = odd != odd;  // (a NaN, or infinite biases: 64 bits sort them out)
-        // How far two c may be off together, u = 2^-24.  sigmoid: exp is off by 2 u and, through its argument, 1.5 u |l|, of which s (1 - s) keeps under u;
-        // 1 + e and the reciprocal by 3 u s: under 2^-21 each.  softmax: exp by 2 u and 2.5 u |l - max|, of which s keeps under u max s; the sum by
-        // (1.23 ln 1024 + 3) u and its rounding; the quotient and the product by 2 u: under 2^-18 max s each, max s = 1 / sum.  With the bias: u |c| each; the
-        // keys' lower four bits: 30 u |c|.
-        const float high = g.sigmoid ? 1.f : inverse;
-        off = (g.sigmoid ? 0x1p-20f : 0x1p-17f * high) + 0x1p-18f * (high + most);
+        // How far a score may be off.  sigmoid: exp is off by 2 u and, through its argument, 1.5 u |l|, of which s (1 - s) keeps under u; 1 + e and the
+        // reciprocal by 3 u s: under 2^-21.  softmax: exp by 2 u and 2.5 u |l - max|, of which s keeps under u max s; the sum by (1.23 ln 1024 + 3) u and
+        // its rounding; the quotient and the product by 2 u: under 2^-18 max s, max s = 1 / sum.
+        one = g.sigmoid ? 0x1p-21f : 0x1p-18f * inverse;
       } else {
 #pragma unroll
         for (int k = 0; k < K; ++k) c[k] = ranked(l[k]);
       }
       if (g.groups > 1) {
-        const float border = keep_groups<L, K>(g, at, c, reinterpret_cast<float*>(keys) + (lane / L) * (g.groups * at.pitch), sub);
-        if (WIDE && !(border > 2.f * off)) close = true;  // (sums of two)
+        if (!keep_groups<L, K, WIDE>(g, at, c, reinterpret_cast<float*>(keys) + (lane / L) * (g.groups * at.pitch), sub, one)) close = true;
       }
       if constexpr (WIDE) {
         if (!added) {  // (read again: held beside c, 16 of them do not fit the registers)
@@ -560,7 +564,7 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
       const float next = __shfl(v, from), next_l = __shfl(logit, from), next_b = __shfl(mine_b, from);
       const uint32_t next_key = (uint32_t)__shfl((int)mine_key, from);
       if (sub + 1 < more && sub + 1 < L && expert >= 0 && next_key > kLeast) {
-        const bool apart = added ? v - next > off : mine_key >> 4 != next_key >> 4;
+        const bool apart = added ? v - next > off_by(one, v) + off_by(one, next) : mine_key >> 4 != next_key >> 4;
         // (equal logits with equal biases are equal in any precision; behind the last pair others may stand that are not)
         if (!apart && !(sub + 2 < more && logit == next_l && mine_b == next_b)) close = true;
       }
@@ -583,7 +587,7 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
 #pragma unroll
             for (int k = 0; k < FEW; ++k) key64[k] = (double)ranked(l64[k]);
           }
-          if (g.groups > 1) keep_groups<64, FEW>(g, at64, key64, reinterpret_cast<double*>(keys), lane);
+          if (g.groups > 1) keep_groups<64, FEW, false>(g, at64, key64, reinterpret_cast<double*>(keys), lane);
           if constexpr (WIDE) {
             if (!added) {
 #pragma unroll
