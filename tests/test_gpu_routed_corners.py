@@ -31,7 +31,7 @@ def alike(kind, n, E, dtype, seed):
 
 
 @pytest.mark.parametrize("E,top,groups,kept", [(8, 1, 2, 1), (8, 2, 4, 2), (24, 4, 8, 3), (64, 6, 8, 3), (120, 6, 8, 3), (256, 8, 8, 4), (512, 33, 16, 9), (640, 64, 64, 20),
-                                               (1024, 20, 4, 2), (1023, 9, 33, 6)])
+                                               (1024, 20, 4, 2), (1023, 9, 33, 6), (16, 4, 16, 5)])
 @pytest.mark.parametrize("kind,dtype", [("large", "f32"), ("large", "bf16"), ("small", "f32"), ("neighbours", "f32"), ("far", "f32"), ("far", "f16")])
 def test_groups_by_their_two_best_choose_by_the_logits(E, top, groups, kept, kind, dtype):
     """Nothing is added to the scores: the groups are ranked by them, the choice is that of the logits, also of those whose scores are the same number."""
@@ -197,3 +197,51 @@ def test_8bit_rows_of_another_width_are_refused():
     with pytest.raises(rl.RunLoRAError):
         m.RunLoRAFp8Function.apply(y, W, A, B, None, 1.0, rl.Fp8Rows(rows.data, rows.scales, 40, 120))
     assert torch.isfinite(m.RunLoRAFp8Function.apply(y, W, A, B, None, 1.0, rows)).all()
+
+
+# ---- plans and transforms --------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n,i,o,r", [(2307, 1104, 4112, 16), (2307, 1104, 4112, 64), (2049, 2064, 4368, 8), (300, 1040, 4112, 16), (17, 1104, 272, 8)])
+def test_8bit_layer_on_given_rows_of_a_prompt(n, i, o, r):
+    """The bits of the layer that rounds its rows itself, on 256 x 256 tiles too; scale bytes behind the last row are nobody's."""
+    rl = _rl()
+    g = gen(n + r)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=torch.bfloat16)
+    W, A, B, bias = rl.Fp8Weight.quantize(randn(i, o) * 0.03), randn(i, r) * 0.03, randn(r, o), randn(o)
+    x, w = randn(n, i), randn(i)
+    h, q = torch.empty_like(x), rl.Fp8Rows.empty(n, i)
+    q.scales.fill_(255)
+    rl.runlora_rmsnorm_forward(x, w, h, rows=q)
+    assert (q.scales[:, n:] == 255).all()
+    ws = rl.new_workspace(rl.FWD1, -1, n, i, o, r, rl.RL_BF16, w_dtype=rl.RL_FP8_B128)
+    got, want, T, T0 = (nan((n, k), torch.bfloat16) for k in (o, o, r, r))
+    rl.runlora_forward(rl.FWD1, h, W, A, B, want, rl.new_saved(T0), workspace=ws, scale=1.5, bias=bias)
+    ws.fill_(255)
+    rl.runlora_fp8_forward(h, q, W, A, B, got, rl.new_saved(T), workspace=ws, scale=1.5, bias=bias)
+    assert torch.isfinite(want).all() and torch.equal(got, want) and torch.equal(T, T0)
+
+
+def node_calls():
+    """(name, call, its differentiable input) of the four nodes."""
+    from paper_2312_03415_amd import module as m
+    place, source = (torch.from_numpy(t).cuda() for t in placed(13, 2, 4, 3))
+    x, rows, l = (torch.randn(*s, generator=gen(k), device="cuda") for k, s in enumerate(((13, 72), (26, 72), (13, 8))))
+    weight = torch.rand(13, 2, generator=gen(4), device="cuda")
+    return [("norm", lambda t: m.RunRMSNormFunction.apply(t, None, 1e-5), x), ("route", lambda t: m.RunRouteFunction.apply(t, _rl().Route(8, 2))[0], l),
+            ("gather", lambda t: m.RunGatherFunction.apply(t, place, source), x),
+            ("combine", lambda t: m.RunCombineFunction.apply(t, place, source, weight, x), rows)]
+
+
+@pytest.mark.parametrize("at", range(4))
+def test_transforms_are_refused(at):
+    """vmap, functional gradients and forward mode, in which no node has a rule: an error, never an answer without its tangent."""
+    import torch.autograd.forward_ad as fwd
+    name, call, t = node_calls()[at]
+    with pytest.raises(RuntimeError):
+        torch.func.vmap(call)(torch.stack((t, t)))
+    with pytest.raises(RuntimeError):
+        torch.func.grad(lambda v: call(v).sum())(t)
+    for leaf in (t, t.clone().requires_grad_(True)):
+        with fwd.dual_level(), pytest.raises((RuntimeError, NotImplementedError)):
+            call(fwd.make_dual(leaf, torch.ones_like(t)))
+    assert torch.isfinite(call(t)).all()
