@@ -315,7 +315,17 @@ class Fp8Weight:
         return Fp8Weight(q, s, rows, cols)
 
 
-class Fp8Rows:
+class _Fixed:
+    """Attributes that are checked against each other when the object is made, and not changed afterwards."""
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"a {type(self).__name__} is not changed once it is made ({name}): make another")
+
+    def __delattr__(self, name):
+        self.__setattr__(name, None)
+
+
+class Fp8Rows(_Fixed):
     """Rows [rows, cols] in e4m3 with one power-of-two scale per 128 columns of a row (RL_FP8_R128), as the 8-bit layers round theirs: `data`
     holds the bytes, uint8 [rows, cols rounded up to 128], `scales` the scale bytes, uint8 [ceil(cols/128), rows rounded up to 16]."""
 
@@ -326,7 +336,7 @@ class Fp8Rows:
                 raise ValueError(f"{name} must be dense bytes {shape}")
         if scales.device != data.device:
             raise ValueError("data and scales must be on one device")
-        self.data, self.scales, self.rows, self.cols = data, scales, rows, cols
+        self.__dict__.update(data=data, scales=scales, rows=rows, cols=cols)
 
     @property
     def shape(self):
@@ -352,7 +362,7 @@ class Fp8Rows:
             return runlora_fp8_values(self, out)
 
 
-class Route:
+class Route(_Fixed):
     """How tokens are routed to experts (rl_route_t of runlora.h): `top` of `experts`, by "softmax" or "sigmoid" scores; renormalise: a token's weights
     sum to `scale`; groups > 1: only the `groups_kept` runs of experts / groups take part whose `group_top` best scores sum to most.  A plan is not changed
     once it is made: tables are sized, and a backward is run, by the one that the forward had."""
@@ -370,12 +380,6 @@ class Route:
         # the whole numbers of rl_route_t in their order
         plan["how"] = (experts, top, SCORES.index(score), int(plan["renormalise"]), groups, plan["groups_kept"], group_top)
         self.__dict__.update(plan)
-
-    def __setattr__(self, name, value):
-        raise AttributeError(f"a Route is not changed once it is made ({name}): make another")
-
-    def __delattr__(self, name):
-        self.__setattr__(name, None)
 
     def desc(self, bias=None):
         """rl_route_t, with the balance bias (None or float32 [experts])."""

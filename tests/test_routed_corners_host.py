@@ -28,3 +28,18 @@ def test_a_plans_numbers_are_one():
         assert r.how == (24, 4, 1, 0, 8, 3, 2) and (r.experts, r.top, r.score, r.renormalise) == (24, 4, "sigmoid", False)
         d = r.desc()
         assert tuple(getattr(d, f) for f, _ in d._fields_[:7]) == r.how and d.scale == r.scale == 2.5 and d.bias is None
+
+
+@pytest.mark.parametrize("name,value", [("rows", 41), ("cols", 256), ("data", None), ("scales", None), ("more", 1)])
+def test_8bit_rows_are_not_changed(name, value):
+    """With `rows` set behind the bytes' back a norm of as many rows would write past them."""
+    torch = pytest.importorskip("torch")
+    q = rl.Fp8Rows.empty(40, 120, "cpu")
+    with pytest.raises(AttributeError, match="make another"):
+        setattr(q, name, value)
+    with pytest.raises(AttributeError):
+        delattr(q, name)
+    q.data.fill_(0x38)  # (the bytes themselves are room to write into)
+    for r in (q, copy.copy(q), copy.deepcopy(q)):
+        assert r.shape == (40, 120) and tuple(r.data.shape) == (40, 128) and tuple(r.scales.shape) == (1, 48)
+        assert torch.equal(r.data, q.data)
