@@ -51,6 +51,20 @@ def test_groups_by_their_two_best_of_one_row():
     assert want.expert.tolist() == [[1], [6]]
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_nan_and_infinity_of_one_row(dtype):
+    """Without a bias they count as much, with one the NaN's expert comes first; it alone has a NaN for its weight."""
+    l = logits(40, 24, dtype, 9)
+    l[:, 3], l[:, 7] = math.inf, math.nan
+    l[20:, 3], l[20:, 7] = math.nan, math.inf
+    for bias in (None, torch.zeros(24, device="cuda")):
+        _, (weight, expert, *_) = route_call(l, 2, bias, score="sigmoid", renormalise=False)
+        nan_at = torch.where(torch.arange(40, device="cuda") < 20, 7, 3).int()
+        first = nan_at if bias is not None else torch.full_like(nan_at, 3)
+        assert torch.equal(expert[:, 0], first) and torch.equal(expert[:, 1], 10 - first)
+        assert torch.equal(torch.isnan(weight), expert == nan_at[:, None]) and (weight[~torch.isnan(weight)] == 1).all()
+
+
 # ---- one rounding ----------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("n,E,top", [(300, 8, 2), (300, 60, 7), (90, 256, 8), (40, 1024, 33)])
