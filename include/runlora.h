@@ -358,10 +358,11 @@ size_t runlora_experts_workspace_bytes(int backward, int64_t n, int64_t experts,
  *         groups_kept runs that count most take part (equal ones: the first)
  *     the `top` largest c are chosen, in falling order, equal ones by index: expert [n, top]
  *     weight_j = scale * s_j, with `renormalise` scale * s_j / sum of the chosen s: weight [n, top]
- * The choice is that of the logits themselves where nothing is added to the scores, and of c in 64 bits otherwise.  A logit or a bias of -infinity
+ * The choice is that of the logits themselves where nothing is added to the scores (and of groups that count with their one best), and of c in 64 bits
+ * otherwise.  A logit or a bias of -infinity
  * takes its expert out of the choice (a row of nothing else goes nowhere); where fewer than `top` are left, the rest of a row is expert -1, weight 0.
  * A row that holds a NaN (softmax: or a +infinity) gives NaN for weights and some choice in range; with sigmoid scores and no renormalise for the NaN's
- * expert only, which comes first.
+ * expert only, which comes first (without a bias +infinity counts as much, and the lower index is taken).
  * The rows sorted by expert, those of an expert in the order of t * top + j, are described for the calls that read them:
  *     ends [E]         where expert e's rows end (runlora_experts_*)
  *     place [n, top]   row of token t's copy j; -1: none
@@ -417,7 +418,8 @@ int runlora_combine_backward(const rl_tensor_t* dY, const rl_tensor_t* rows, con
  * runlora_rmsnorm_backward: with N = gain dY, dX = rstd (N - h rstd^2 mean(N h)) + dH, the gradient of X and of R alike; dgain = sum over rows of
  * dY h rstd.  H is the forward's h (X where there was no R); dH, what reaches h from elsewhere, may be NULL; dX or dgain may be NULL (skipped).
  * workspace: runlora_rmsnorm_workspace_bytes(), for dgain only.
- * RL_F32 / RL_F16 / RL_BF16; n in [1, 2^30], d in [1, 32768], a multiple of 8 (16-bit types) or 4.  Sums are fp32 in a fixed order.
+ * RL_F32 / RL_F16 / RL_BF16; n in [1, 2^30], d in [1, 32768], a multiple of 8 (16-bit types) or 4.  Sums are fp32 in a fixed order: a row
+ * whose squares leave fp32's range (|h| from 1.8e19 on) has an rstd of 0.
  */
 int runlora_rmsnorm_forward(const rl_tensor_t* X, const rl_tensor_t* R, const void* gain, float eps, rl_tensor_t* Y, rl_tensor_t* H, float* rstd,
                             rl_tensor_t* Q, const rl_opts_t* opts);

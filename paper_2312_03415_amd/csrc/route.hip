@@ -478,7 +478,7 @@ inline __host__ __device__ int count_bytes(int each) { return each < 256 ? 1 : 2
 // Workgroup b takes the tokens [b each, (b + 1) each), L lanes a token with K experts each, 64 / L tokens side by side in a wave: their experts and weights,
 // and how many rows every expert gets (counts [b][experts] in the workspace).  A single workgroup places them too.
 // Bound by its instructions and, with one round of waves, by their latency (16384 x 256 in 32 bits, biased sigmoid scores, 8 groups, top 8: 16 MB, 3 us;
-// 1400 vector instructions a wave of four tokens, 10 us of them; 19 us): a maximum over 16 lanes serves four tokens at once, where one over 64 serves one
+// 1400 vector instructions a wave of four tokens, 10 us of them; 18 us): a maximum over 16 lanes serves four tokens at once, where one over 64 serves one
 // (38 us).  The scores in 64 bits for every row took 45.
 template <typename T, int L, int K, bool WIDE>
 __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route_choose_kernel(RouteDesc g, int each, int fast, int room, void* counts, int single) {
@@ -570,7 +570,7 @@ __global__ __launch_bounds__(K > 8 ? 512 : 1024, L * K > 256 ? 2 : 4) void route
       }
       if (more > L) close = true;
       // Rows that 32 bits do not decide: the whole wave takes one after the other, so that its 64-bit keys are few a lane.  (All rows of 16384 x 256 of one
-      // value, zero bias: both launches take 42 us, of random ones 27.)
+      // value, zero bias: both launches take 41 us, of random ones 24.)
       if (sub >= g.top) expert = -1;
       const uint64_t undecided = __ballot(close && there);
       if (undecided != 0) {
